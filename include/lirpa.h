@@ -254,6 +254,110 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
               const lirpa_bab_params* params, lirpa_bab_result* result, void* ws,
               size_t ws_bytes, hipStream_t stream);
 
+/* =============================================================================================
+ * The feed-forward block of a language model
+ *
+ * The passes of the networks whose answers are bounded: what a user runs to train such a block,
+ * to search its input box for a violating point (the gradient of the input), and to serve it.
+ * A block is a root-mean-square norm that adds the residual, then
+ *     out = (act(x Wg^T) * (x Wu^T)) Wd^T
+ * and its backward pass reads activations that the forward pass kept in 8 bits.
+ *
+ * Conventions of these calls, besides those above:
+ * - `dtype` is the type of every tensor of a call unless a parameter says otherwise.  Products
+ *   of 16-bit types run on their matrix instructions with 32-bit sums; LIRPA_F32 operands are
+ *   split into three bf16 parts each (24 bits), and the six products of the largest parts are
+ *   summed in 32 bits.  Sums, norms and their reductions are held in 32 bits.
+ * - A matrix has contiguous rows; `ld` is the distance of two rows in elements (at least the
+ *   row's length, less than 2^22).  Any alignment of the element type is taken; rows that start
+ *   on 16 bytes and whose length is a multiple of 8 elements are read in place, others are
+ *   copied once per call into the workspace.  Outputs must not overlap inputs unless a
+ *   parameter says so.
+ * - `rows` may be 0: nothing is read, sums over rows come out as 0.  Widths are 1 to 2^20,
+ *   rows up to 2^31 - 1.
+ * - Every call is deterministic: the order of its sums depends on sizes alone.
+ * ============================================================================================= */
+typedef enum { LIRPA_F32 = 0, LIRPA_BF16 = 1, LIRPA_F16 = 2 } lirpa_dtype;
+
+/* The gate's activation: relu, x / (1 + e^-x), x Phi(x) (Phi: the normal distribution function).
+ * relu's slope at 0 is 0. */
+typedef enum { LIRPA_GATE_RELU = 0, LIRPA_GATE_SILU = 1, LIRPA_GATE_GELU = 2 } lirpa_gate;
+
+/* A matrix [rows][n] held in 8 bits.  Groups of 32 columns of a row share a scale 2^e, e being
+ * the least whole number in [-120, 121] with 127 * 2^e >= the group's largest magnitude, and a
+ * value is held as the nearest whole multiple of it (ties to even); magnitudes over 127 * 2^121
+ * are held as that.  The buffer is
+ *     int8   [rows][groups * 32]   groups = ceil(n / 32); columns past n are 0
+ *     uint8  [rows][groups]        e + 127; 255 marks a group with an infinity or a NaN, all of
+ *                                  which reads back as NaN
+ * and starts on 16 bytes.  A multiple of at most 127 with a power-of-two scale is exact in bf16
+ * (and in f16 in its range), so reading it back rounds nothing. */
+size_t lirpa_q8_bytes(int64_t rows, int n); /* 0 for invalid arguments */
+int lirpa_q8_pack(int dtype, int64_t rows, int n, const void* x, int64_t ldx, void* q8,
+                  hipStream_t stream);
+int lirpa_q8_unpack(int dtype, int64_t rows, int n, const void* q8, void* x, int64_t ldx,
+                    hipStream_t stream);
+
+/* Root-mean-square norm with the residual's addition, per row:
+ *     h = x + res,  rstd = 1 / sqrt(mean(h^2) + eps),  y = w * h * rstd.
+ * res may be NULL (h = x).  Outputs, each NULL where it is not wanted: sum = h (may be the buffer
+ * of x or res), y, y8 = y in 8 bits (lirpa_q8 layout, from y before it is rounded to dtype), rstd
+ * (float [rows]).  All are computed from h in 32 bits.  w is [n].  eps >= 0, finite. */
+int lirpa_norm_forward(int dtype, int64_t rows, int n, const void* x, int64_t ldx,
+                       const void* res, int64_t ldr, const void* w, float eps, void* sum,
+                       int64_t lds, void* y, int64_t ldy, void* y8, float* rstd,
+                       hipStream_t stream);
+
+/* Its backward pass: with xhat = h * rstd and t = w * dy,
+ *     dh = rstd * (t - xhat * mean(t * xhat)) + dsum,   dw = sum over rows of dy * xhat.
+ * dsum (the gradient that reaches h past the norm) may be NULL; dh is the gradient of x and of
+ * res, and may be the buffer of dy or dsum.  dh or dw may be NULL. */
+size_t lirpa_norm_workspace_bytes(int64_t rows, int n); /* 0 for invalid arguments */
+int lirpa_norm_backward(int dtype, int64_t rows, int n, const void* dy, int64_t lddy,
+                        const void* dsum, int64_t ldds, const void* h, int64_t ldh,
+                        const void* w, const float* rstd, void* dh, int64_t lddh, void* dw,
+                        void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* A gated feed-forward block: Wg, Wu [n_hidden][n_model] and Wd [n_model][n_hidden] with row
+ * distances ldg, ldu, ldd (device pointers, read during a call's enqueued work only). */
+typedef struct {
+  int dtype, gate, n_model, n_hidden;
+  const void *Wg, *Wu, *Wd;
+  int64_t ldg, ldu, ldd;
+} lirpa_ffn;
+
+/* What a forward pass keeps of its projections g = x Wg^T and u = x Wu^T. */
+typedef enum {
+  LIRPA_KEEP_NONE = -1,
+  LIRPA_KEEP_FULL = 0, /* [rows][n_hidden] of dtype, contiguous */
+  LIRPA_KEEP_8 = 8     /* two lirpa_q8 buffers of n_hidden columns */
+} lirpa_keep;
+
+/* Workspace of a call over up to `rows` rows: backward 0 for lirpa_ffn_forward, 1 for
+ * lirpa_ffn_backward.  0 for invalid arguments. */
+size_t lirpa_ffn_workspace_bytes(const lirpa_ffn* ffn, int64_t rows, int backward);
+
+/* out = (act(x Wg^T) * (x Wu^T)) Wd^T for x [rows][n_model].  The product act(g) * u is rounded
+ * to dtype between the two matrix products (f32: to 24 bits), so in f16 it has to stay under
+ * 65520.  keep: see lirpa_keep; g, u receive the projections, NULL with LIRPA_KEEP_NONE.  With
+ * LIRPA_KEEP_8 the packed values come from the 32-bit sums. */
+int lirpa_ffn_forward(const lirpa_ffn* ffn, int64_t rows, const void* x, int64_t ldx, void* out,
+                      int64_t ldo, int keep, void* g, void* u, void* ws, size_t ws_bytes,
+                      hipStream_t stream);
+
+/* Gradients from what was kept: keep = LIRPA_KEEP_8: x, g, u are lirpa_q8 buffers (ldx is
+ * ignored); LIRPA_KEEP_FULL: x [rows][n_model] with ldx, g, u as lirpa_ffn_forward wrote them.
+ *     da = dout Wd, dg = da * u * act'(g), du = da * act(g),
+ *     dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x, dWd = dout^T (act(g) * u).
+ * dx [rows][n_model] with lddx; dWg, dWu [n_hidden][n_model] and dWd [n_model][n_hidden],
+ * contiguous.  Each may be NULL where it is not wanted (at least one is not); x may be NULL where
+ * neither dWg nor dWu is wanted.  dg, du and act(g) * u are rounded to dtype (f32: to 24 bits)
+ * before their products. */
+int lirpa_ffn_backward(const lirpa_ffn* ffn, int64_t rows, const void* dout, int64_t lddo,
+                       int keep, const void* x, int64_t ldx, const void* g, const void* u,
+                       void* dx, int64_t lddx, void* dWg, void* dWu, void* dWd, void* ws,
+                       size_t ws_bytes, hipStream_t stream);
+
 /* Kernel timing, for profiling harnesses.  Between lirpa_timing_begin() and
  * lirpa_timing_end() every kernel the calls of this thread enqueue is bracketed by a pair of
  * hipEvents recorded on the call's own stream.  lirpa_timing_end() waits for those events and

@@ -1,0 +1,129 @@
+"""The feed-forward block of a language model over ``liblirpa.so``: norm, gated block, 8 bits.
+
+Convenience owners in the manner of ``lirpa.Network``: they allocate outputs and workspaces on
+torch's current stream, where the calls run, and leave every computation to the library.
+
+    norm, ffn = Norm(w), FeedForward(Wg, Wu, Wd, "silu")
+    n = norm.forward(x, res, want8=True)              # h = x + res and its norm, also in 8 bits
+    out, kept = ffn.forward(n.y, keep=8, x8=n.y8)     # what the backward pass needs, in 8 bits
+    ...
+    grads = ffn.backward(dout, kept)                  # dx, dWg, dWu, dWd
+    dh, dw = norm.backward(grads["dx"], n.sum, n.rstd, dsum)
+"""
+from __future__ import annotations
+
+import collections
+
+import torch
+
+from . import lirpa
+
+
+class Q8:
+    """A matrix [rows, n] in 8 bits with a power-of-two scale per 32 columns of a row."""
+
+    def __init__(self, rows, n, buf=None, device="cuda"):
+        self.rows, self.n = rows, n
+        if buf is None:
+            buf = torch.empty(lirpa.lirpa_q8_bytes(rows, n), dtype=torch.uint8, device=device)
+        self.buf = buf
+
+    @staticmethod
+    def pack(x):
+        q = Q8(x.shape[0], x.shape[1], device=x.device)
+        lirpa.lirpa_q8_pack(x, q.buf)
+        return q
+
+    def values(self, dtype=torch.float32):
+        x = torch.empty((self.rows, self.n), dtype=dtype, device=self.buf.device)
+        lirpa.lirpa_q8_unpack(self.buf, x)
+        return x
+
+
+Normed = collections.namedtuple("Normed", "y sum y8 rstd")
+
+
+class Norm:
+    """y = w h / sqrt(mean(h^2) + eps) of h = x + res."""
+
+    def __init__(self, w, eps=1e-5):
+        self.w, self.eps = w, float(eps)
+
+    def forward(self, x, res=None, want8=False, want_y=True):
+        """Normed(y, sum, y8, rstd): sum is h (x itself without a residual); y8 a Q8 of y where
+        wanted, else None; rstd is float32 [rows]."""
+        rows, n = x.shape
+        y = torch.empty((rows, n), dtype=x.dtype, device=x.device) if want_y else None
+        h = torch.empty((rows, n), dtype=x.dtype, device=x.device) if res is not None else None
+        y8 = Q8(rows, n, device=x.device) if want8 else None
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+        lirpa.lirpa_norm_forward(x, res, self.w, self.eps, h, y, y8.buf if want8 else None, rstd)
+        return Normed(y, x if h is None else h, y8, rstd)
+
+    def backward(self, dy, h, rstd, dsum=None, want_dw=True):
+        """(dh, dw): dh is the gradient of x and of res, dsum that of h past the norm."""
+        rows, n = dy.shape
+        dh = torch.empty((rows, n), dtype=dy.dtype, device=dy.device)
+        dw = ws = None
+        need = 0
+        if want_dw:
+            dw = torch.empty(n, dtype=dy.dtype, device=dy.device)
+            need = lirpa.lirpa_norm_workspace_bytes(rows, n)
+            ws = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        lirpa.lirpa_norm_backward(dy, dsum, h, self.w, rstd, dh, dw, ws, need)
+        return dh, dw
+
+
+class Kept:
+    """What a forward pass kept for its backward pass: x and the projections g, u, as Q8
+    (``keep`` 8; uint8 buffers in the library's layout are taken too) or as tensors (``keep`` 0)."""
+
+    def __init__(self, keep, rows, x, g, u):
+        self.keep, self.rows = keep, rows
+        self.x, self.g, self.u = x, g, u
+
+    def raw(self):
+        return [t.buf if isinstance(t, Q8) else t for t in (self.x, self.g, self.u)]
+
+
+class FeedForward:
+    """out = (act(x Wg^T) * (x Wu^T)) Wd^T; Wg, Wu [hidden, model], Wd [model, hidden], gate one of
+    relu, silu, gelu."""
+
+    def __init__(self, Wg, Wu, Wd, gate="silu"):
+        self.weights = (Wg, Wu, Wd)
+        self.block = lirpa.lirpa_ffn_block(Wg, Wu, Wd, gate)
+
+    def _workspace(self, rows, backward):
+        need = lirpa.lirpa_ffn_workspace_bytes(self.block, rows, backward)
+        return torch.empty(need, dtype=torch.uint8, device=self.weights[0].device), need
+
+    def forward(self, x, keep=None, x8=None):
+        """out; with ``keep`` (8 or 0) (out, Kept).  ``x8``: x in 8 bits where the caller has it
+        (a norm's y8); it is packed here otherwise."""
+        rows, dev, hidden = x.shape[0], x.device, self.block.n_hidden
+        out = torch.empty((rows, self.block.n_model), dtype=x.dtype, device=dev)
+        ws, need = self._workspace(rows, 0)
+        if keep is None:
+            lirpa.lirpa_ffn_forward(self.block, x, out, lirpa.KEEP_NONE, None, None, ws, need)
+            return out
+        if keep == 8:
+            g, u = Q8(rows, hidden, device=dev), Q8(rows, hidden, device=dev)
+            kept = Kept(8, rows, Q8.pack(x) if x8 is None else x8, g, u)
+        else:
+            g, u = (torch.empty((rows, hidden), dtype=x.dtype, device=dev) for _ in range(2))
+            kept = Kept(keep, rows, x, g, u)
+        lirpa.lirpa_ffn_forward(self.block, x, out, keep, *kept.raw()[1:], ws, need)
+        return out, kept
+
+    def backward(self, dout, kept, want=("dx", "dWg", "dWu", "dWd")):
+        """{name: gradient} of the wanted ones."""
+        model, hidden = self.block.n_model, self.block.n_hidden
+        shapes = {"dx": (dout.shape[0], model), "dWg": (hidden, model), "dWu": (hidden, model),
+                  "dWd": (model, hidden)}
+        grads = {k: torch.empty(shapes[k], dtype=dout.dtype, device=dout.device) for k in want}
+        ws, need = self._workspace(dout.shape[0], 1)
+        x, g, u = kept.raw()
+        lirpa.lirpa_ffn_backward(self.block, dout, kept.keep, x, g, u, *(
+            grads.get(k) for k in ("dx", "dWg", "dWu", "dWd")), ws, need)
+        return grads

@@ -1,0 +1,734 @@
+// The feed-forward block of a language model: host side of lirpa_q8_*, lirpa_norm_* and
+// lirpa_ffn_*.  Kernels: q8.hpp, norm.hpp, ffn_tile.hpp, ffn_few.hpp.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <exception>
+
+#include "host.hpp"
+#include "ffn_few.hpp"
+#include "ffn_tile.hpp"
+#include "lirpa.h"
+#include "norm.hpp"
+#include "q8.hpp"
+
+using namespace lirpa_host;
+using namespace lm;
+
+namespace {
+
+constexpr int kMaxWidth = 1 << 20;
+constexpr int64_t kMaxLd = (1 << 22) - 1;
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+bool is_dtype(int t) { return t == LIRPA_F32 || t == LIRPA_BF16 || t == LIRPA_F16; }
+size_t bytes_of(int dtype) { return dtype == LIRPA_F32 ? 4 : 2; }
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+// No C++ exception leaves a C entry.
+template <typename F>
+int guarded(F&& f) {
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    return fail(LIRPA_EDEVICE, "%s", e.what());
+  } catch (...) {
+    return fail(LIRPA_EDEVICE, "unexpected exception");
+  }
+}
+
+template <typename F>
+int by_type(int dtype, F&& f) {
+  switch (dtype) {
+    case LIRPA_F32: return f(float{});
+    case LIRPA_BF16: return f(bf16{});
+    default: return f(f16{});
+  }
+}
+
+int check_shape(const char* who, int dtype, int64_t rows, int n) {
+  if (!is_dtype(dtype)) return fail(LIRPA_EINVAL, "%s: dtype %d is none of lirpa_dtype", who, dtype);
+  if (rows < 0 || rows > kMaxRows)
+    return fail(LIRPA_EINVAL, "%s: rows = %lld is outside [0, 2^30]", who, (long long)rows);
+  if (n < 1 || n > kMaxWidth) return fail(LIRPA_EINVAL, "%s: width %d is outside [1, 2^20]", who, n);
+  return LIRPA_OK;
+}
+
+int check_rows(const char* who, const char* what, int dtype, const void* p, int64_t ld, int n) {
+  if (!p) return fail(LIRPA_EINVAL, "%s: %s is null", who, what);
+  if ((uintptr_t)p % bytes_of(dtype))
+    return fail(LIRPA_EINVAL, "%s: %s is not aligned to its type", who, what);
+  if (ld < n || ld > kMaxLd)
+    return fail(LIRPA_EINVAL, "%s: the row distance %lld of %s is outside [%d, 2^22)", who,
+                (long long)ld, what, n);
+  return LIRPA_OK;
+}
+
+#define TRY(x)                     \
+  do {                             \
+    int rc_ = (x);                 \
+    if (rc_ != LIRPA_OK) return rc_; \
+  } while (0)
+
+// ---------------------------------------------------------------------------------------------
+// 8 bits
+// ---------------------------------------------------------------------------------------------
+int64_t q8_exps_at(int64_t rows, int n) { return rows * groups_of(n) * kGroup; }
+size_t q8_bytes(int64_t rows, int n) { return (size_t)rows * groups_of(n) * (kGroup + 1); }
+
+int check_q8(const char* who, const char* what, const void* p) {
+  if (!p) return fail(LIRPA_EINVAL, "%s: %s is null", who, what);
+  if (!aligned16(p)) return fail(LIRPA_EINVAL, "%s: %s does not start on 16 bytes", who, what);
+  return LIRPA_OK;
+}
+
+template <typename T>
+int q8_pack(int64_t rows, int n, const T* x, int64_t ldx, void* q8, hipStream_t st) {
+  const int64_t blocks = (rows * groups_of(n) * 4 + 255) / 256;
+  if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "q8_pack: more than 2^42 values");
+  return launch_k("q8_pack", st, [&] {
+    k_q8_pack<T><<<(unsigned)blocks, 256, 0, st>>>(x, ldx, rows, n, (int8_t*)q8,
+                                                   (uint8_t*)q8 + q8_exps_at(rows, n));
+  });
+}
+
+template <typename T>
+int q8_unpack(int64_t rows, int n, int cols, const void* q8, T* x, int64_t ldx, hipStream_t st) {
+  const int64_t blocks = (rows * groups_of(n) * 4 + 255) / 256;
+  if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "q8_unpack: more than 2^42 values");
+  return launch_k("q8_unpack", st, [&] {
+    k_q8_unpack<T><<<(unsigned)blocks, 256, 0, st>>>(
+        (const int8_t*)q8, (const uint8_t*)q8 + q8_exps_at(rows, n), rows, n, cols, x, ldx);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// Norm
+// ---------------------------------------------------------------------------------------------
+// Threads a row and pieces of 8 columns a thread: one wave up to 2048 columns, then a block.  Rows
+// over 16384 columns are read twice: with four pieces the backward pass does not fit the registers
+// of 1024 threads.
+struct NormShape {
+  int threads, ch;
+};
+NormShape norm_shape(int n) {
+  const int pieces = (n + 7) / 8;
+  for (NormShape s : {NormShape{64, 1}, {64, 2}, {64, 4}, {256, 2}, {256, 4}, {1024, 2}})
+    if (pieces <= s.threads * s.ch) return s;
+  return {1024, 0};
+}
+
+template <typename F>
+int by_norm_shape(NormShape s, F&& f) {
+  using std::integral_constant;
+#define SHAPE(T, C) \
+  if (s.threads == T && s.ch == C) return f(integral_constant<int, T>{}, integral_constant<int, C>{})
+  SHAPE(64, 1);
+  SHAPE(64, 2);
+  SHAPE(64, 4);
+  SHAPE(256, 2);
+  SHAPE(256, 4);
+  SHAPE(1024, 2);
+#undef SHAPE
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
+}
+
+template <typename T>
+int norm_fwd(const NormFwd<T>& a, hipStream_t st) {
+  const NormShape s = norm_shape(a.n);
+  const int64_t blocks = s.threads == 64 ? (a.rows + 3) / 4 : a.rows;
+  return by_norm_shape(s, [&](auto th, auto ch) {
+    return launch_k("norm_forward", st, [&] {
+      k_norm_fwd<T, th.value, ch.value>
+          <<<(unsigned)blocks, th.value == 64 ? 256 : th.value, 0, st>>>(a);
+    });
+  });
+}
+
+// Blocks of the backward pass, and so partial sums of dw: enough to fill the chip.
+int64_t norm_bwd_blocks(int64_t rows, int n) {
+  const NormShape s = norm_shape(n);
+  const int64_t units = s.threads == 64 ? (rows + 3) / 4 : rows;
+  return std::min<int64_t>(units, s.threads == 64 ? 1024 : s.threads == 256 ? 1024 : 512);
+}
+
+template <typename T>
+int norm_bwd(NormBwd<T> a, T* dw, float* part, hipStream_t st) {
+  const NormShape s = norm_shape(a.n);
+  const int64_t blocks = norm_bwd_blocks(a.rows, a.n);
+  a.part = dw ? part : nullptr;
+  if (blocks > 0 && (a.dh || s.ch > 0)) {
+    TRY(by_norm_shape(s, [&](auto th, auto ch) {
+      return launch_k("norm_backward", st, [&] {
+        k_norm_bwd<T, th.value, ch.value>
+            <<<(unsigned)blocks, th.value == 64 ? 256 : th.value, 0, st>>>(a);
+      });
+    }));
+  }
+  if (dw && blocks > 0 && s.ch == 0)
+    TRY(launch_k("norm_backward", st, [&] {
+      k_norm_dw_wide<T><<<dim3((a.n + 2047) / 2048, (unsigned)blocks), 256, 0, st>>>(a);
+    }));
+  if (dw)
+    TRY(launch_k("norm_dw", st, [&] {
+      k_norm_dw<T><<<(a.n + 63) / 64, 1024, 0, st>>>(part, (int)blocks, a.n, dw);
+    }));
+  return LIRPA_OK;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Feed-forward block
+// ---------------------------------------------------------------------------------------------
+int check_ffn(const char* who, const lirpa_ffn* f) {
+  if (!f) return fail(LIRPA_EINVAL, "%s: the block is null", who);
+  TRY(check_shape(who, f->dtype, 0, f->n_model));
+  TRY(check_shape(who, f->dtype, 0, f->n_hidden));
+  if (f->gate != LIRPA_GATE_RELU && f->gate != LIRPA_GATE_SILU && f->gate != LIRPA_GATE_GELU)
+    return fail(LIRPA_EINVAL, "%s: gate %d is none of lirpa_gate", who, f->gate);
+  TRY(check_rows(who, "Wg", f->dtype, f->Wg, f->ldg, f->n_model));
+  TRY(check_rows(who, "Wu", f->dtype, f->Wu, f->ldu, f->n_model));
+  TRY(check_rows(who, "Wd", f->dtype, f->Wd, f->ldd, f->n_hidden));
+  return LIRPA_OK;
+}
+
+// An operand of the tile kernel: 16 bits, rows on 16 bytes, length a multiple of 8 or padded to
+// one with zeros.  `ld` in elements; parts of a 32-bit operand lie `plane` elements apart.
+struct Operand {
+  const char* p = nullptr;
+  int64_t ld = 0, plane = 0;
+};
+
+// Parts of the workspace, in order, each on 256 bytes.
+struct Carver {
+  char* base;
+  size_t at = 0;
+  void* take(size_t bytes) {
+    void* p = base ? base + at : nullptr;
+    at += (bytes + 255) / 256 * 256;
+    return p;
+  }
+};
+
+struct FfnPlan {
+  const lirpa_ffn* f;
+  int64_t rows;
+  bool f32;
+  int parts;
+  int64_t D, F, Dp, Fp;  // widths, and padded to 8
+  Carver ws;
+
+  FfnPlan(const lirpa_ffn* ffn, int64_t r, void* base)
+      : f(ffn), rows(r), f32(ffn->dtype == LIRPA_F32), parts(f32 ? 3 : 1), D(ffn->n_model),
+        F(ffn->n_hidden), Dp(up(D, 8)), Fp(up(F, 8)), ws{(char*)base} {}
+
+  // Room for an operand of the library's own.
+  Operand own(int64_t r, int64_t cols) {
+    Operand o;
+    o.ld = up(cols, 8);
+    o.plane = r * o.ld;
+    o.p = (const char*)ws.take((size_t)(parts * o.plane) * 2);
+    return o;
+  }
+  bool in_place(const void* p, int64_t ld, int64_t cols) const {
+    return !f32 && aligned16(p) && ld % 8 == 0 && cols % 8 == 0;
+  }
+};
+
+template <typename S, typename T, int PARTS>
+int copy_operand(const S* x, int64_t ldx, int64_t rows, int64_t n, const Operand& o,
+                 hipStream_t st) {
+  const int64_t blocks = (rows * (o.ld / 8) + 255) / 256;
+  return launch_k("ffn_operand", st, [&] {
+    k_operand<S, T, PARTS><<<(unsigned)blocks, 256, 0, st>>>(x, ldx, rows, (int)n, (T*)o.p,
+                                                            (int)o.ld, o.plane);
+  });
+}
+
+// The user's matrix as an operand: in place where the tile kernel can read it, else a copy in
+// `room`.
+int as_operand(const FfnPlan& pl, const void* x, int64_t ldx, int64_t rows, int64_t n,
+               Operand& o, hipStream_t st) {
+  if (pl.in_place(x, ldx, n)) {
+    o.p = (const char*)x;
+    o.ld = ldx;
+    o.plane = 0;
+    return LIRPA_OK;
+  }
+  if (rows == 0) return LIRPA_OK;
+  switch (pl.f->dtype) {
+    case LIRPA_F32: return copy_operand<float, bf16, 3>((const float*)x, ldx, rows, n, o, st);
+    case LIRPA_BF16: return copy_operand<bf16, bf16, 1>((const bf16*)x, ldx, rows, n, o, st);
+    default: return copy_operand<f16, f16, 1>((const f16*)x, ldx, rows, n, o, st);
+  }
+}
+
+// Parts (A, B) of the six products of 32-bit operands, smallest first.
+constexpr int kSixA[6] = {1, 0, 2, 0, 1, 0};
+constexpr int kSixB[6] = {1, 2, 0, 1, 0, 0};
+
+// Adds the segments of one product.
+void add_segs(const FfnPlan& pl, TileArgs& t, int batch, const Operand& A, const Operand& B,
+              const Operand* A2 = nullptr) {
+  const int n = pl.f32 ? 6 : 1, at = batch ? 0 : t.nseg;
+  for (int s = 0; s < n; ++s) {
+    const int64_t pa = pl.f32 ? kSixA[s] * 2 : 0, pb = pl.f32 ? kSixB[s] * 2 : 0;
+    t.A[at + s] = A.p + pa * A.plane;
+    if (A2) t.A2[at + s] = A2->p + pa * A2->plane;
+    t.B[batch][at + s] = B.p + pb * B.plane;
+  }
+  if (!batch) t.nseg += n;
+  t.lda = A.ld * 2;
+  t.ldb = B.ld * 2;
+}
+
+template <typename T, bool AKS, bool BKS, int EPI, int BI, int BJ, int WI, int WJ>
+int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
+  constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;
+  const int64_t ti = up(t.I, kFeat) / kFeat, tj = up(t.J, BJ) / BJ, total = ti * tj * t.batches;
+  if (total == 0) return LIRPA_OK;
+  if (total > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "%s: more than 2^31 tiles", name);
+  t.tiles_i = (int)ti;
+  t.tiles_j = (int)tj;
+  return launch_k(name, st, [&] {
+    k_ffn_tile<T, AKS, BKS, EPI, BI, BJ, WI, WJ>
+        <<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);
+  });
+}
+
+template <bool AKS, bool BKS, int EPI>
+int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, hipStream_t st) {
+  const int64_t feat = EPI == EPI_GATE ? 128 : 256;
+  const int64_t large = (up(t.I, feat) / feat) * (up(t.J, 256) / 256) * t.batches;
+  if (pl.f->dtype == LIRPA_F16) {
+    if (large >= 192) return launch_tile<f16, AKS, BKS, EPI, 256, 256, 2, 4>(name, t, st);
+    return launch_tile<f16, AKS, BKS, EPI, 128, 128, 2, 2>(name, t, st);
+  }
+  if (large >= 192) return launch_tile<bf16, AKS, BKS, EPI, 256, 256, 2, 4>(name, t, st);
+  return launch_tile<bf16, AKS, BKS, EPI, 128, 128, 2, 2>(name, t, st);
+}
+
+TileArgs tile_args(const FfnPlan& pl, int64_t I, int64_t J, int64_t KA, int64_t KB) {
+  TileArgs t{};
+  t.I = (int)I;
+  t.J = (int)J;
+  t.KA = (int)KA;
+  t.KB = (int)KB;
+  t.batches = 1;
+  t.parts = pl.parts;
+  t.keep = -1;
+  t.gate = pl.f->gate;
+  return t;
+}
+
+constexpr int kFewRows = 64;
+
+template <typename T, int TJ>
+int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, void* out,
+                int64_t ldo, void* hidden, hipStream_t st) {
+  FewArgs a{};
+  a.A = f->Wg;
+  a.A2 = f->Wu;
+  a.lda = f->ldg;
+  a.lda2 = f->ldu;
+  a.B = x;
+  a.ldb = ldx;
+  a.I = f->n_hidden;
+  a.J = (int)rows;
+  a.K = f->n_model;
+  a.gate = f->gate;
+  a.out = hidden;
+  a.ldo = f->n_hidden;
+  constexpr int UN = TJ == 1 ? 4 : 2;
+  TRY(launch_k("ffn_few_gate", st, [&] {
+    k_ffn_few<T, true, TJ, 8, UN><<<(a.I + 15) / 16, 8 * 64, 0, st>>>(a);
+  }));
+  a.A = f->Wd;
+  a.lda = f->ldd;
+  a.B = hidden;
+  a.ldb = f->n_hidden;
+  a.I = f->n_model;
+  a.K = f->n_hidden;
+  a.out = out;
+  a.ldo = ldo;
+  return launch_k("ffn_few_down", st, [&] {
+    k_ffn_few<T, false, TJ, 8, UN><<<(a.I + 15) / 16, 8 * 64, 0, st>>>(a);
+  });
+}
+
+struct ForwardRoom {
+  Operand x, wg, wu, wd, a;
+  size_t bytes;
+};
+ForwardRoom forward_room(FfnPlan& pl) {
+  const lirpa_ffn* f = pl.f;
+  ForwardRoom r;
+  r.x = pl.own(pl.rows, pl.D);
+  if (!pl.in_place(f->Wg, f->ldg, pl.D)) r.wg = pl.own(pl.F, pl.D);
+  if (!pl.in_place(f->Wu, f->ldu, pl.D)) r.wu = pl.own(pl.F, pl.D);
+  if (!pl.in_place(f->Wd, f->ldd, pl.F)) r.wd = pl.own(pl.D, pl.F);
+  r.a = pl.own(pl.rows, pl.F);
+  r.bytes = pl.ws.at;
+  return r;
+}
+
+int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, void* out,
+                int64_t ldo, int keep, void* g, void* u, void* ws, hipStream_t st) {
+  FfnPlan pl(f, rows, ws);
+  if (keep == LIRPA_KEEP_NONE && rows <= kFewRows)
+    return by_type(f->dtype, [&](auto t) {
+      using T = decltype(t);
+      if (rows <= 16) return few_forward<T, 1>(f, rows, x, ldx, out, ldo, ws, st);
+      if (rows <= 32) return few_forward<T, 2>(f, rows, x, ldx, out, ldo, ws, st);
+      return few_forward<T, 4>(f, rows, x, ldx, out, ldo, ws, st);
+    });
+  ForwardRoom r = forward_room(pl);
+  TRY(as_operand(pl, x, ldx, rows, pl.D, r.x, st));
+  TRY(as_operand(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg, st));
+  TRY(as_operand(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu, st));
+  TRY(as_operand(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd, st));
+
+  TileArgs t = tile_args(pl, pl.F, rows, pl.Dp, pl.Dp);
+  add_segs(pl, t, 0, r.wg, r.x, &r.wu);
+  t.lda2 = r.wu.ld * 2;
+  t.out[0] = (void*)r.a.p;
+  t.ldo = r.a.ld;
+  t.pad_i = (int)pl.Fp;
+  t.plane = r.a.plane;
+  t.keep = keep;
+  t.g = g;
+  t.u = u;
+  t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
+  t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
+  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, st)));
+
+  t = tile_args(pl, pl.D, rows, pl.Fp, pl.Fp);
+  add_segs(pl, t, 0, r.wd, r.a);
+  t.out[0] = out;
+  t.ldo = ldo;
+  return run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, st);
+}
+
+struct BackwardRoom {
+  Operand dout, x, wg, wu, wd, a, dg, du;
+  size_t bytes;
+};
+BackwardRoom backward_room(FfnPlan& pl) {
+  const lirpa_ffn* f = pl.f;
+  BackwardRoom r;
+  r.dout = pl.own(pl.rows, pl.D);
+  r.x = pl.own(pl.rows, pl.D);
+  if (!pl.in_place(f->Wg, f->ldg, pl.D)) r.wg = pl.own(pl.F, pl.D);
+  if (!pl.in_place(f->Wu, f->ldu, pl.D)) r.wu = pl.own(pl.F, pl.D);
+  if (!pl.in_place(f->Wd, f->ldd, pl.F)) r.wd = pl.own(pl.D, pl.F);
+  r.a = pl.own(pl.rows, pl.F);
+  r.dg = pl.own(pl.rows, pl.F);
+  r.du = pl.own(pl.rows, pl.F);
+  r.bytes = pl.ws.at;
+  return r;
+}
+
+int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t lddo, int keep,
+                 const void* x, int64_t ldx, const void* g, const void* u, void* dx, int64_t lddx,
+                 void* dWg, void* dWu, void* dWd, void* ws, hipStream_t st) {
+  FfnPlan pl(f, rows, ws);
+  BackwardRoom r = backward_room(pl);
+  TRY(as_operand(pl, dout, lddo, rows, pl.D, r.dout, st));
+  if (dx) {
+    TRY(as_operand(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg, st));
+    TRY(as_operand(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu, st));
+  }
+  TRY(as_operand(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd, st));
+  const bool wx = dWg || dWu;
+
+  // act(g) u, dg and du
+  TileArgs t = tile_args(pl, pl.F, rows, pl.D, pl.Dp);
+  add_segs(pl, t, 0, r.wd, r.dout);
+  t.out[0] = dWd ? (void*)r.a.p : nullptr;
+  t.dg = dx || dWg ? (void*)r.dg.p : nullptr;
+  t.du = dx || dWu ? (void*)r.du.p : nullptr;
+  t.ldo = r.a.ld;
+  t.plane = r.a.plane;
+  t.pad_i = (int)pl.Fp;
+  t.keep = keep;
+  t.g = (void*)g;
+  t.u = (void*)u;
+  t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
+  t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
+  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, st)));
+
+  if (dx) {
+    t = tile_args(pl, pl.D, rows, pl.F, pl.Fp);
+    add_segs(pl, t, 0, r.wg, r.dg);
+    const int64_t ldg = t.lda;
+    add_segs(pl, t, 0, r.wu, r.du);
+    t.lda2 = t.lda;
+    t.lda = ldg;
+    t.out[0] = dx;
+    t.ldo = lddx;
+    TRY((run_tile<true, false, EPI_STORE>(pl, "ffn_dx", t, st)));
+  }
+  if (wx) {
+    if (keep == LIRPA_KEEP_8) {
+      if (pl.f32) {
+        // 7 bits and a sign: the first part of three holds it, the other two are 0
+        if (rows) {
+          TRY(q8_unpack<bf16>(rows, (int)pl.D, (int)r.x.ld, x, (bf16*)r.x.p, r.x.ld, st));
+        }
+      } else if (rows) {
+        if (f->dtype == LIRPA_BF16)
+          TRY(q8_unpack<bf16>(rows, (int)pl.D, (int)r.x.ld, x, (bf16*)r.x.p, r.x.ld, st));
+        else
+          TRY(q8_unpack<f16>(rows, (int)pl.D, (int)r.x.ld, x, (f16*)r.x.p, r.x.ld, st));
+      }
+    } else {
+      TRY(as_operand(pl, x, ldx, rows, pl.D, r.x, st));
+    }
+    t = tile_args(pl, pl.D, pl.F, rows, rows);
+    const bool one_part = pl.f32 && keep == LIRPA_KEEP_8;
+    const Operand* d[2] = {&r.dg, &r.du};
+    void* out[2] = {dWg, dWu};
+    t.batches = 0;
+    for (int b = 0; b < 2; ++b) {
+      if (!out[b]) continue;
+      if (one_part) {  // x is exact in its first part: three products, smallest first
+        t.nseg = 3;
+        for (int s = 0; s < 3; ++s) {
+          t.A[s] = r.x.p;
+          t.B[t.batches][s] = d[b]->p + (2 - s) * 2 * d[b]->plane;
+        }
+        t.lda = r.x.ld * 2;
+        t.ldb = d[b]->ld * 2;
+      } else {
+        add_segs(pl, t, t.batches, r.x, *d[b]);
+      }
+      t.out[t.batches++] = out[b];
+    }
+    t.ldo = pl.D;
+    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_in", t, st)));
+  }
+  if (dWd) {
+    t = tile_args(pl, pl.F, pl.D, rows, rows);
+    add_segs(pl, t, 0, r.a, r.dout);
+    t.out[0] = dWd;
+    t.ldo = pl.F;
+    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_down", t, st)));
+  }
+  return LIRPA_OK;
+}
+
+size_t ffn_bytes(const lirpa_ffn* f, int64_t rows, bool backward) {
+  FfnPlan pl(f, rows, nullptr);
+  return backward ? backward_room(pl).bytes : forward_room(pl).bytes;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lirpa_q8_bytes(int64_t rows, int n) {
+  if (rows < 0 || rows > kMaxRows || n < 1 || n > kMaxWidth) return 0;
+  return q8_bytes(rows, n);
+}
+
+int lirpa_q8_pack(int dtype, int64_t rows, int n, const void* x, int64_t ldx, void* q8,
+                  hipStream_t stream) {
+  return guarded([&] {
+    TRY(check_shape("lirpa_q8_pack", dtype, rows, n));
+    if (rows == 0) return (int)LIRPA_OK;
+    TRY(check_rows("lirpa_q8_pack", "x", dtype, x, ldx, n));
+    TRY(check_q8("lirpa_q8_pack", "q8", q8));
+    return by_type(dtype, [&](auto t) {
+      return q8_pack(rows, n, (const decltype(t)*)x, ldx, q8, stream);
+    });
+  });
+}
+
+int lirpa_q8_unpack(int dtype, int64_t rows, int n, const void* q8, void* x, int64_t ldx,
+                    hipStream_t stream) {
+  return guarded([&] {
+    TRY(check_shape("lirpa_q8_unpack", dtype, rows, n));
+    if (rows == 0) return (int)LIRPA_OK;
+    TRY(check_rows("lirpa_q8_unpack", "x", dtype, x, ldx, n));
+    TRY(check_q8("lirpa_q8_unpack", "q8", q8));
+    return by_type(dtype, [&](auto t) {
+      return q8_unpack(rows, n, n, q8, (decltype(t)*)x, ldx, stream);
+    });
+  });
+}
+
+int lirpa_norm_forward(int dtype, int64_t rows, int n, const void* x, int64_t ldx,
+                       const void* res, int64_t ldr, const void* w, float eps, void* sum,
+                       int64_t lds, void* y, int64_t ldy, void* y8, float* rstd,
+                       hipStream_t stream) {
+  return guarded([&] {
+    const char* who = "lirpa_norm_forward";
+    TRY(check_shape(who, dtype, rows, n));
+    if (!(eps >= 0.f) || !std::isfinite(eps))
+      return fail(LIRPA_EINVAL, "%s: eps must be finite and >= 0", who);
+    if (rows == 0) return (int)LIRPA_OK;  // an empty buffer may be null
+    if (!sum && !y && !y8 && !rstd) return fail(LIRPA_EINVAL, "%s: no output is wanted", who);
+    TRY(check_rows(who, "x", dtype, x, ldx, n));
+    if (res) TRY(check_rows(who, "res", dtype, res, ldr, n));
+    TRY(check_rows(who, "w", dtype, w, n, n));
+    if (sum) TRY(check_rows(who, "sum", dtype, sum, lds, n));
+    if (y) TRY(check_rows(who, "y", dtype, y, ldy, n));
+    if (y8) TRY(check_q8(who, "y8", y8));
+    return by_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      NormFwd<T> a{};
+      a.x = (const T*)x;
+      a.res = (const T*)res;
+      a.w = (const T*)w;
+      a.ldx = ldx;
+      a.ldr = ldr;
+      a.lds = lds;
+      a.ldy = ldy;
+      a.rows = rows;
+      a.n = n;
+      a.eps = eps;
+      a.sum = (T*)sum;
+      a.y = (T*)y;
+      a.q = (int8_t*)y8;
+      a.exps = y8 ? (uint8_t*)y8 + q8_exps_at(rows, n) : nullptr;
+      a.rstd = rstd;
+      return norm_fwd(a, stream);
+    });
+  });
+}
+
+size_t lirpa_norm_workspace_bytes(int64_t rows, int n) {
+  if (rows < 0 || rows > kMaxRows || n < 1 || n > kMaxWidth) return 0;
+  return std::max<size_t>(256, (size_t)norm_bwd_blocks(rows, n) * n * sizeof(float));
+}
+
+int lirpa_norm_backward(int dtype, int64_t rows, int n, const void* dy, int64_t lddy,
+                        const void* dsum, int64_t ldds, const void* h, int64_t ldh,
+                        const void* w, const float* rstd, void* dh, int64_t lddh, void* dw,
+                        void* ws, size_t ws_bytes, hipStream_t stream) {
+  return guarded([&] {
+    const char* who = "lirpa_norm_backward";
+    TRY(check_shape(who, dtype, rows, n));
+    if (!dh && !dw && rows > 0) return fail(LIRPA_EINVAL, "%s: no output is wanted", who);
+    if (rows > 0) {
+      TRY(check_rows(who, "dy", dtype, dy, lddy, n));
+      if (dsum) TRY(check_rows(who, "dsum", dtype, dsum, ldds, n));
+      TRY(check_rows(who, "h", dtype, h, ldh, n));
+      TRY(check_rows(who, "w", dtype, w, n, n));
+      if (!rstd) return fail(LIRPA_EINVAL, "%s: rstd is null", who);
+      if (dh) TRY(check_rows(who, "dh", dtype, dh, lddh, n));
+    }
+    if (dw) {
+      TRY(check_rows(who, "dw", dtype, dw, n, n));
+      if (!ws) return fail(LIRPA_EINVAL, "%s: the workspace is null", who);
+      if (!aligned16(ws))
+        return fail(LIRPA_EINVAL, "%s: the workspace does not start on 16 bytes", who);
+      const size_t need = lirpa_norm_workspace_bytes(rows, n);
+      if (ws_bytes < need)
+        return fail(LIRPA_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes,
+                    need);
+    }
+    return by_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      NormBwd<T> a{};
+      a.dy = (const T*)dy;
+      a.dsum = (const T*)dsum;
+      a.h = (const T*)h;
+      a.w = (const T*)w;
+      a.lddy = lddy;
+      a.ldds = ldds;
+      a.ldh = ldh;
+      a.lddh = lddh;
+      a.rows = rows;
+      a.n = n;
+      a.rstd = rstd;
+      a.dh = (T*)dh;
+      return norm_bwd(a, (T*)dw, (float*)ws, stream);
+    });
+  });
+}
+
+size_t lirpa_ffn_workspace_bytes(const lirpa_ffn* ffn, int64_t rows, int backward) {
+  if (check_ffn("lirpa_ffn_workspace_bytes", ffn) != LIRPA_OK) return 0;
+  if (rows < 0 || rows > kMaxRows || (backward != 0 && backward != 1)) {
+    fail(LIRPA_EINVAL, "lirpa_ffn_workspace_bytes: rows or backward out of range");
+    return 0;
+  }
+  return std::max<size_t>(256, ffn_bytes(ffn, rows, backward == 1));
+}
+
+int lirpa_ffn_forward(const lirpa_ffn* ffn, int64_t rows, const void* x, int64_t ldx, void* out,
+                      int64_t ldo, int keep, void* g, void* u, void* ws, size_t ws_bytes,
+                      hipStream_t stream) {
+  return guarded([&] {
+    const char* who = "lirpa_ffn_forward";
+    TRY(check_ffn(who, ffn));
+    TRY(check_shape(who, ffn->dtype, rows, ffn->n_model));
+    if (keep != LIRPA_KEEP_NONE && keep != LIRPA_KEEP_FULL && keep != LIRPA_KEEP_8)
+      return fail(LIRPA_EINVAL, "%s: keep %d is none of lirpa_keep", who, keep);
+    if (keep == LIRPA_KEEP_NONE && (g || u))
+      return fail(LIRPA_EINVAL, "%s: g and u are null where nothing is kept", who);
+    if (rows == 0) return (int)LIRPA_OK;
+    TRY(check_rows(who, "x", ffn->dtype, x, ldx, ffn->n_model));
+    TRY(check_rows(who, "out", ffn->dtype, out, ldo, ffn->n_model));
+    if (keep == LIRPA_KEEP_8) {
+      TRY(check_q8(who, "g", g));
+      TRY(check_q8(who, "u", u));
+    } else if (keep == LIRPA_KEEP_FULL) {
+      TRY(check_rows(who, "g", ffn->dtype, g, ffn->n_hidden, ffn->n_hidden));
+      TRY(check_rows(who, "u", ffn->dtype, u, ffn->n_hidden, ffn->n_hidden));
+    }
+    if (!ws) return fail(LIRPA_EINVAL, "%s: the workspace is null", who);
+    if (!aligned16(ws))
+      return fail(LIRPA_EINVAL, "%s: the workspace does not start on 16 bytes", who);
+    const size_t need = lirpa_ffn_workspace_bytes(ffn, rows, 0);
+    if (ws_bytes < need)
+      return fail(LIRPA_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes,
+                  need);
+    return ffn_forward(ffn, rows, x, ldx, out, ldo, keep, g, u, ws, stream);
+  });
+}
+
+int lirpa_ffn_backward(const lirpa_ffn* ffn, int64_t rows, const void* dout, int64_t lddo,
+                       int keep, const void* x, int64_t ldx, const void* g, const void* u,
+                       void* dx, int64_t lddx, void* dWg, void* dWu, void* dWd, void* ws,
+                       size_t ws_bytes, hipStream_t stream) {
+  return guarded([&] {
+    const char* who = "lirpa_ffn_backward";
+    TRY(check_ffn(who, ffn));
+    const int t = ffn->dtype, D = ffn->n_model, F = ffn->n_hidden;
+    TRY(check_shape(who, t, rows, D));
+    if (keep != LIRPA_KEEP_FULL && keep != LIRPA_KEEP_8)
+      return fail(LIRPA_EINVAL, "%s: keep must be LIRPA_KEEP_FULL or LIRPA_KEEP_8", who);
+    if (!dx && !dWg && !dWu && !dWd && rows > 0)
+      return fail(LIRPA_EINVAL, "%s: no output is wanted", who);
+    if (rows > 0) {
+      TRY(check_rows(who, "dout", t, dout, lddo, D));
+      if (keep == LIRPA_KEEP_8) {
+        if (dWg || dWu) TRY(check_q8(who, "x", x));
+        TRY(check_q8(who, "g", g));
+        TRY(check_q8(who, "u", u));
+      } else {
+        if (dWg || dWu) TRY(check_rows(who, "x", t, x, ldx, D));
+        TRY(check_rows(who, "g", t, g, F, F));
+        TRY(check_rows(who, "u", t, u, F, F));
+      }
+      if (dx) TRY(check_rows(who, "dx", t, dx, lddx, D));
+    }
+    if (dWg) TRY(check_rows(who, "dWg", t, dWg, D, D));
+    if (dWu) TRY(check_rows(who, "dWu", t, dWu, D, D));
+    if (dWd) TRY(check_rows(who, "dWd", t, dWd, F, F));
+    if (!ws) return fail(LIRPA_EINVAL, "%s: the workspace is null", who);
+    if (!aligned16(ws))
+      return fail(LIRPA_EINVAL, "%s: the workspace does not start on 16 bytes", who);
+    const size_t need = lirpa_ffn_workspace_bytes(ffn, rows, 1);
+    if (ws_bytes < need)
+      return fail(LIRPA_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes,
+                  need);
+    return ffn_backward(ffn, rows, dout, lddo, keep, x, ldx, g, u, dx, lddx, dWg, dWu, dWd, ws,
+                        stream);
+  });
+}
+
+}  // extern "C"

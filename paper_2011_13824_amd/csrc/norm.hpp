@@ -1,0 +1,278 @@
+// Root-mean-square norm with the residual's addition, forward and backward.
+//
+//   h = x + res,  rstd = (mean h^2 + eps)^-1/2,  y = w h rstd
+//   dh = rstd (t - xhat mean(t xhat)) + dsum,  t = w dy,  xhat = h rstd;  dw = sum_rows dy xhat
+//
+// Bound by bytes: a row is read once, stays in registers (CH pieces of 8 columns a thread), is
+// reduced over its THREADS threads and written.  Rows too wide for the registers of 1024 threads
+// are read twice (CH = 0), the second time out of the caches.
+#pragma once
+
+#include "lm_types.hpp"
+
+namespace lm {
+
+// Sum over the THREADS threads that share a row; every thread gets it.  A row of one wave needs
+// no barrier; otherwise `part` holds a sum per wave, and the barrier before the write keeps a
+// wave of the next row from overwriting what a slower one still reads.
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float v, float* part) {
+#pragma unroll
+  for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
+  if constexpr (THREADS > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i) v += part[i];
+  }
+  return v;
+}
+
+template <typename T>
+struct NormFwd {
+  const T *x, *res, *w;
+  int64_t ldx, ldr, lds, ldy;
+  int64_t rows;
+  int n;
+  float eps;
+  T *sum, *y;
+  int8_t* q;
+  uint8_t* exps;
+  float* rstd;
+};
+
+// Writes one piece of h, y and the packed y.  `col` may lie past n (a thread without columns):
+// the lanes of a group still meet in the exchange.
+template <typename T>
+__device__ __forceinline__ void norm_piece(const NormFwd<T>& a, int64_t row, int col,
+                                           const float (&h)[8], float rstd, bool with_sum) {
+  float y[8], w[8];
+  load_row<T, 8>(a.w + col, a.n - col, w);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = h[i] * rstd * w[i];
+  if (with_sum && col < a.n) store_row<T, 8>(a.sum + row * a.lds + col, a.n - col, h);
+  if (a.y && col < a.n) store_row<T, 8>(a.y + row * a.ldy + col, a.n - col, y);
+  if (a.q) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude(y[i]));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    const int e = group_exponent(top);
+    const float inv = group_inverse(e);
+    const int groups = groups_of(a.n);
+    if (col < groups * kGroup) {
+      uint32_t p[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        p[i >> 2] |= (uint32_t)(to_int8(y[i], inv) & 255) << (8 * (i & 3));
+      *reinterpret_cast<uint2*>(a.q + row * groups * kGroup + col) = make_uint2(p[0], p[1]);
+      if ((threadIdx.x & 3) == 0) a.exps[row * groups + col / kGroup] = (uint8_t)e;
+    }
+  }
+}
+
+// THREADS threads a row (64: four rows a block), CH pieces of 8 columns each; CH = 0: any width.
+template <typename T, int THREADS, int CH>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_norm_fwd(NormFwd<T> a) {
+  __shared__ float part[THREADS / 64];
+  constexpr int kRows = THREADS == 64 ? 4 : 1;
+  const int t = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t row = (int64_t)blockIdx.x * kRows + (THREADS == 64 ? threadIdx.x >> 6 : 0);
+  if (row >= a.rows) return;
+  const T* x = a.x + row * a.ldx;
+  const T* res = a.res ? a.res + row * a.ldr : nullptr;
+  auto read = [&](int col, float(&h)[8]) {
+    load_row<T, 8>(x + col, a.n - col, h);
+    if (res) {
+      float r[8];
+      load_row<T, 8>(res + col, a.n - col, r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[i] += r[i];
+    }
+  };
+  float ss = 0.f;
+  if constexpr (CH > 0) {
+    float h[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) read((c * THREADS + t) * 8, h[c]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss += h[c][i] * h[c][i];
+    const float rstd = 1.f / sqrtf(row_sum<THREADS>(ss, part) / (float)a.n + a.eps);
+    if (a.rstd && t == 0) a.rstd[row] = rstd;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      norm_piece(a, row, (c * THREADS + t) * 8, h[c], rstd, a.sum != nullptr);
+  } else {
+    const int span = (a.n + THREADS * 8 - 1) / (THREADS * 8) * (THREADS * 8);
+    float h[8];
+    for (int col = t * 8; col < span; col += THREADS * 8) {
+      read(col, h);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss += h[i] * h[i];
+    }
+    const float rstd = 1.f / sqrtf(row_sum<THREADS>(ss, part) / (float)a.n + a.eps);
+    if (a.rstd && t == 0) a.rstd[row] = rstd;
+    for (int col = t * 8; col < span; col += THREADS * 8) {
+      read(col, h);
+      norm_piece(a, row, col, h, rstd, a.sum != nullptr);
+    }
+  }
+}
+
+template <typename T>
+struct NormBwd {
+  const T *dy, *dsum, *h, *w;
+  int64_t lddy, ldds, ldh, lddh;
+  int64_t rows;
+  int n;
+  const float* rstd;
+  T* dh;
+  float* part;  // [blocks][n] sums of dy * xhat over a block's rows; NULL: no dw
+};
+
+// A block walks over rows (blockIdx.x, + gridDim.x, ...), keeps the sums of dy * xhat of its
+// columns in registers and writes them once: dw needs no atomics, and its order is fixed by the
+// sizes alone.  CH as above; CH = 0 takes rows of any width and leaves dw to k_norm_dw_wide.
+template <typename T, int THREADS, int CH>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_norm_bwd(NormBwd<T> a) {
+  __shared__ float part[THREADS / 64];
+  constexpr int kRows = THREADS == 64 ? 4 : 1;
+  constexpr int kCh = CH ? CH : 1;
+  const int t = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
+  const int64_t first = (int64_t)blockIdx.x * kRows + (THREADS == 64 ? threadIdx.x >> 6 : 0);
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  const float inv_n = 1.f / (float)a.n;
+  if constexpr (CH > 0) {
+    float w[kCh][8], dw[kCh][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (c * THREADS + t) * 8;
+      load_row<T, 8>(a.w + col, a.n - col, w[c]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
+    }
+    for (int64_t row = first; row < a.rows; row += step) {
+      const float rstd = a.rstd[row];
+      float xhat[kCh][8], dy[kCh][8], dot = 0.f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int col = (c * THREADS + t) * 8;
+        load_row<T, 8>(a.h + row * a.ldh + col, a.n - col, xhat[c]);
+        load_row<T, 8>(a.dy + row * a.lddy + col, a.n - col, dy[c]);
+      }
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          xhat[c][i] *= rstd;
+          dw[c][i] += dy[c][i] * xhat[c][i];
+          dot += dy[c][i] * w[c][i] * xhat[c][i];
+        }
+      if (a.dh) {
+        dot = row_sum<THREADS>(dot, part) * inv_n;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const int col = (c * THREADS + t) * 8;
+          if (col >= a.n) continue;
+          float d[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[i] = rstd * (dy[c][i] * w[c][i] - xhat[c][i] * dot);
+          if (a.dsum) {
+            float s[8];
+            load_row<T, 8>(a.dsum + row * a.ldds + col, a.n - col, s);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] += s[i];
+          }
+          store_row<T, 8>(a.dh + row * a.lddh + col, a.n - col, d);
+        }
+      }
+    }
+    if (!a.part) return;
+    // the four waves of a block of one-wave rows hold sums of the same columns: added in order
+    if constexpr (THREADS == 64) {
+      __shared__ float all[4][64 * 8 * kCh];
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) all[threadIdx.x >> 6][(c * 64 + t) * 8 + i] = dw[c][i];
+      __syncthreads();
+      for (int col = threadIdx.x; col < a.n; col += 256)
+        a.part[(int64_t)blockIdx.x * a.n + col] =
+            (all[0][col] + all[1][col]) + (all[2][col] + all[3][col]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int col = (c * THREADS + t) * 8;
+        if (col < a.n)
+          store_row<float, 8>(a.part + (int64_t)blockIdx.x * a.n + col, a.n - col, dw[c]);
+      }
+    }
+  } else {
+    for (int64_t row = first; row < a.rows; row += step) {
+      const float rstd = a.rstd[row];
+      float h[8], dy[8], w[8], dot = 0.f;
+      for (int col = t * 8; col < a.n; col += THREADS * 8) {
+        load_row<T, 8>(a.h + row * a.ldh + col, a.n - col, h);
+        load_row<T, 8>(a.dy + row * a.lddy + col, a.n - col, dy);
+        load_row<T, 8>(a.w + col, a.n - col, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dot += dy[i] * w[i] * (h[i] * rstd);
+      }
+      dot = row_sum<THREADS>(dot, part) * inv_n;
+      for (int col = t * 8; col < a.n; col += THREADS * 8) {
+        load_row<T, 8>(a.h + row * a.ldh + col, a.n - col, h);
+        load_row<T, 8>(a.dy + row * a.lddy + col, a.n - col, dy);
+        load_row<T, 8>(a.w + col, a.n - col, w);
+        float s[8] = {};
+        if (a.dsum) load_row<T, 8>(a.dsum + row * a.ldds + col, a.n - col, s);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += rstd * (dy[i] * w[i] - h[i] * rstd * dot);
+        store_row<T, 8>(a.dh + row * a.lddh + col, a.n - col, s);
+      }
+    }
+  }
+}
+
+// Partial dw of rows wider than the registers hold: block (x, y) sums the rows y, y + gridDim.y,
+// ... of 2048 columns.
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_dw_wide(NormBwd<T> a) {
+  const int col = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (col >= a.n) return;
+  float dw[8] = {}, h[8], dy[8];
+  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    const float rstd = a.rstd[row];
+    load_row<T, 8>(a.h + row * a.ldh + col, a.n - col, h);
+    load_row<T, 8>(a.dy + row * a.lddy + col, a.n - col, dy);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dw[i] += dy[i] * (h[i] * rstd);
+  }
+  store_row<float, 8>(a.part + (int64_t)blockIdx.y * a.n + col, a.n - col, dw);
+}
+
+// dw = sum of the blocks' partial sums: a block takes 64 columns, its 16 waves every sixteenth
+// partial row, joined in order.
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_dw(const float* __restrict__ part, int blocks,
+                                                  int n, T* __restrict__ dw) {
+  __shared__ float all[16][64];
+  const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+  float s = 0.f;
+  if (col < n)
+    for (int b = wave; b < blocks; b += 16) s += part[(int64_t)b * n + col];
+  all[wave][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (wave == 0 && col < n) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += all[i][threadIdx.x];
+    dw[col] = (T)s;
+  }
+}
+
+}  // namespace lm

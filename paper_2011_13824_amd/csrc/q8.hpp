@@ -1,0 +1,73 @@
+// A matrix in 8 bits with a power-of-two scale per 32 columns, and back.
+//
+// q = rint(x * 2^-e): the scale is a power of two, so neither the product nor reading back rounds
+// (127 multiples fit the 8-bit significand of bf16).  Both kernels are bound by the bytes that
+// they move: a thread takes 8 columns (16 bytes of a 16-bit type, 8 of the packed values), four
+// neighbouring lanes make a group and find its largest magnitude with two lane exchanges.
+#pragma once
+
+#include "lm_types.hpp"
+
+namespace lm {
+
+// The 8 columns that thread `id` of a matrix with `per_row` pieces a row takes.  The block's first
+// piece is divided in 64 bits once (uniform), the thread's offset from it in 32.
+struct Piece {
+  int64_t row;
+  int col;
+};
+__device__ __forceinline__ Piece piece_of(int64_t first, int per_row) {
+  int64_t row0 = first / per_row;
+  uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x;
+  uint32_t down = at / (uint32_t)per_row;
+  return {row0 + down, (int)(at - down * (uint32_t)per_row) * 8};
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_q8_pack(const T* __restrict__ x, int64_t ldx,
+                                                 int64_t rows, int n, int8_t* __restrict__ q,
+                                                 uint8_t* __restrict__ exps) {
+  const int groups = groups_of(n);
+  Piece p = piece_of((int64_t)blockIdx.x * 256, groups * 4);
+  if (p.row >= rows) return;  // whole groups of lanes leave together
+  float v[8];
+  load_row<T, 8>(x + p.row * ldx + p.col, n - p.col, v);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  const int e = group_exponent(top);
+  const float inv = group_inverse(e);
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    w[h] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[h] |= (uint32_t)(to_int8(v[h * 4 + i], inv) & 255) << (8 * i);
+  }
+  *reinterpret_cast<uint2*>(q + p.row * groups * kGroup + p.col) = make_uint2(w[0], w[1]);
+  if ((threadIdx.x & 3) == 0) exps[p.row * groups + p.col / kGroup] = (uint8_t)e;
+}
+
+// Reads back; columns from n to `cols` (the padded width of an operand) come out as 0.
+template <typename T>
+__global__ __launch_bounds__(256) void k_q8_unpack(const int8_t* __restrict__ q,
+                                                   const uint8_t* __restrict__ exps,
+                                                   int64_t rows, int n, int cols,
+                                                   T* __restrict__ x, int64_t ldx) {
+  const int groups = groups_of(n);
+  Piece p = piece_of((int64_t)blockIdx.x * 256, groups * 4);
+  if (p.row >= rows || p.col >= cols) return;
+  const uint2 w = *reinterpret_cast<const uint2*>(q + p.row * groups * kGroup + p.col);
+  const float s = group_scale(exps[p.row * groups + p.col / kGroup]);
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = (float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * s;
+    if (p.col + i >= n) v[i] = 0.f;
+  }
+  store_row<T, 8>(x + p.row * ldx + p.col, cols - p.col, v);
+}
+
+}  // namespace lm

@@ -19,6 +19,10 @@ LIB_PATH = os.path.join(PKG, "liblirpa.so")
 LIRPA_OK, LIRPA_EINVAL, LIRPA_ENOMEM, LIRPA_EDEVICE, LIRPA_EUNSUPPORTED, LIRPA_EDATA = \
     0, -1, -2, -3, -4, -5
 LINEAR, CONV2D = 0, 1
+F32, BF16, F16 = 0, 1, 2
+DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+GATES = {"relu": 0, "silu": 1, "gelu": 2}
+KEEP_NONE, KEEP_FULL, KEEP_8 = -1, 0, 8
 
 
 class lirpa_layer(ctypes.Structure):
@@ -47,6 +51,13 @@ class lirpa_bab_result(ctypes.Structure):
                 ("domains_left", ctypes.c_int)]
 
 
+class lirpa_ffn(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("gate", ctypes.c_int), ("n_model", ctypes.c_int),
+                ("n_hidden", ctypes.c_int), ("Wg", ctypes.c_void_p), ("Wu", ctypes.c_void_p),
+                ("Wd", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("ldu", ctypes.c_int64),
+                ("ldd", ctypes.c_int64)]
+
+
 BAB_VERIFIED, BAB_VIOLATED, BAB_UNKNOWN_STUCK, BAB_UNKNOWN_LIMIT = 1, 2, 3, 4
 
 
@@ -60,6 +71,9 @@ SYMBOLS = ("lirpa_net_create", "lirpa_net_destroy", "lirpa_net_num_relu",
            "lirpa_bound_ul",
            "lirpa_bound_grad", "lirpa_optimize", "lirpa_optimize_ul",
            "lirpa_bab_workspace_bytes", "lirpa_bab",
+           "lirpa_q8_bytes", "lirpa_q8_pack", "lirpa_q8_unpack",
+           "lirpa_norm_forward", "lirpa_norm_workspace_bytes", "lirpa_norm_backward",
+           "lirpa_ffn_workspace_bytes", "lirpa_ffn_forward", "lirpa_ffn_backward",
            "lirpa_timing_begin", "lirpa_timing_end", "lirpa_last_error")
 
 _lib = None
@@ -104,6 +118,25 @@ def load() -> ctypes.CDLL:
     L.lirpa_optimize.argtypes = [P, P, f, P, i, i, P, P, P, P, ctypes.POINTER(lirpa_opt_params),
                                  P, P, P, sz, P]
     L.lirpa_optimize.restype = i
+    q, block = ctypes.c_int64, ctypes.POINTER(lirpa_ffn)
+    L.lirpa_q8_bytes.argtypes = [q, i]
+    L.lirpa_q8_bytes.restype = sz
+    L.lirpa_q8_pack.argtypes = [i, q, i, P, q, P, P]
+    L.lirpa_q8_pack.restype = i
+    L.lirpa_q8_unpack.argtypes = [i, q, i, P, P, q, P]
+    L.lirpa_q8_unpack.restype = i
+    L.lirpa_norm_forward.argtypes = [i, q, i, P, q, P, q, P, f, P, q, P, q, P, P, P]
+    L.lirpa_norm_forward.restype = i
+    L.lirpa_norm_workspace_bytes.argtypes = [q, i]
+    L.lirpa_norm_workspace_bytes.restype = sz
+    L.lirpa_norm_backward.argtypes = [i, q, i, P, q, P, q, P, q, P, P, P, q, P, P, sz, P]
+    L.lirpa_norm_backward.restype = i
+    L.lirpa_ffn_workspace_bytes.argtypes = [block, q, i]
+    L.lirpa_ffn_workspace_bytes.restype = sz
+    L.lirpa_ffn_forward.argtypes = [block, q, P, q, P, q, i, P, P, P, sz, P]
+    L.lirpa_ffn_forward.restype = i
+    L.lirpa_ffn_backward.argtypes = [block, q, P, q, i, P, q, P, P, P, q, P, P, P, P, sz, P]
+    L.lirpa_ffn_backward.restype = i
     L.lirpa_timing_begin.argtypes = []
     L.lirpa_timing_begin.restype = i
     L.lirpa_timing_end.argtypes = [ctypes.POINTER(lirpa_kernel_time), i, ctypes.POINTER(i)]
@@ -285,6 +318,146 @@ def lirpa_optimize(net, x0, eps, C, S, B, split, alpha, adam_m, adam_v, params, 
                                  _dev(lb_best, torch.float32, "lb_best"),
                                  _dev(lb_trace, torch.float32, "lb_trace"), _dev(ws, None, "ws"),
                                  int(ws_bytes), _stream(stream)))
+
+
+def _matrix(t, rows, n, dtype, what):
+    """(device pointer, row distance) of a [rows, n] CUDA tensor whose rows are contiguous
+    (None -> NULL)."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != n:
+        raise ValueError(f"{what} must be [{rows}, {n}], got {list(t.shape)}")
+    ld = t.stride(0)
+    if n > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    if rows <= 1:
+        ld = max(ld, n)
+    elif ld < n:
+        raise ValueError(f"rows of {what} overlap")
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, dtype, what):
+    """Device pointer of a contiguous CUDA tensor of n values (None -> NULL)."""
+    if t is not None and isinstance(t, torch.Tensor) and t.numel() != n:
+        raise ValueError(f"{what} must have {n} values, got {t.numel()}")
+    return _dev(t, dtype, what)
+
+
+def _packed(t, rows, n, what):
+    if t is None:
+        return None
+    need = rows * -(-n // 32) * 33
+    if isinstance(t, torch.Tensor) and t.numel() < need:
+        raise ValueError(f"{what} must have {need} bytes, got {t.numel()}")
+    return _dev(t, torch.uint8, what)
+
+
+def _dtype(t, what):
+    if not isinstance(t, torch.Tensor) or t.dtype not in DTYPES:
+        raise TypeError(f"{what} must be a float32, bfloat16 or float16 tensor")
+    return t.dtype
+
+
+def lirpa_q8_bytes(rows, n) -> int:
+    return int(load().lirpa_q8_bytes(int(rows), int(n)))
+
+
+def lirpa_q8_pack(x, q8, stream=None):
+    """x [rows, n] into the uint8 tensor q8."""
+    rows, n = x.shape
+    dt = _dtype(x, "x")
+    p, ld = _matrix(x, rows, n, dt, "x")
+    _check(load().lirpa_q8_pack(DTYPES[dt], rows, n, p, ld, _packed(q8, rows, n, "q8"),
+                                _stream(stream)))
+
+
+def lirpa_q8_unpack(q8, x, stream=None):
+    """The values of q8 into x [rows, n]."""
+    rows, n = x.shape
+    dt = _dtype(x, "x")
+    p, ld = _matrix(x, rows, n, dt, "x")
+    _check(load().lirpa_q8_unpack(DTYPES[dt], rows, n, _packed(q8, rows, n, "q8"), p, ld,
+                                  _stream(stream)))
+
+
+def lirpa_norm_forward(x, res, w, eps, sum, y, y8, rstd, stream=None):
+    rows, n = x.shape
+    dt = _dtype(x, "x")
+    _check(load().lirpa_norm_forward(
+        DTYPES[dt], rows, n, *_matrix(x, rows, n, dt, "x"), *_matrix(res, rows, n, dt, "res"),
+        _vector(w, n, dt, "w"), float(eps), *_matrix(sum, rows, n, dt, "sum"),
+        *_matrix(y, rows, n, dt, "y"), _packed(y8, rows, n, "y8"),
+        _vector(rstd, rows, torch.float32, "rstd"), _stream(stream)))
+
+
+def lirpa_norm_workspace_bytes(rows, n) -> int:
+    return int(load().lirpa_norm_workspace_bytes(int(rows), int(n)))
+
+
+def lirpa_norm_backward(dy, dsum, h, w, rstd, dh, dw, ws, ws_bytes, stream=None):
+    rows, n = dy.shape
+    dt = _dtype(dy, "dy")
+    _check(load().lirpa_norm_backward(
+        DTYPES[dt], rows, n, *_matrix(dy, rows, n, dt, "dy"), *_matrix(dsum, rows, n, dt, "dsum"),
+        *_matrix(h, rows, n, dt, "h"), _vector(w, n, dt, "w"),
+        _vector(rstd, rows, torch.float32, "rstd"), *_matrix(dh, rows, n, dt, "dh"),
+        _vector(dw, n, dt, "dw"), _dev(ws, None, "ws"), int(ws_bytes), _stream(stream)))
+
+
+def lirpa_ffn_block(Wg, Wu, Wd, gate):
+    """The lirpa_ffn of device weights, which have to outlive the calls that take it."""
+    dt = _dtype(Wg, "Wg")
+    if Wg.dim() != 2:
+        raise ValueError("Wg must be [n_hidden, n_model]")
+    if gate not in GATES:
+        raise ValueError(f"gate must be one of {sorted(GATES)}, got {gate!r}")
+    hidden, model = Wg.shape
+    g, ldg = _matrix(Wg, hidden, model, dt, "Wg")
+    u, ldu = _matrix(Wu, hidden, model, dt, "Wu")
+    d, ldd = _matrix(Wd, model, hidden, dt, "Wd")
+    return lirpa_ffn(DTYPES[dt], GATES[gate], model, hidden, g, u, d, ldg, ldu, ldd)
+
+
+def lirpa_ffn_workspace_bytes(ffn, rows, backward) -> int:
+    return int(load().lirpa_ffn_workspace_bytes(ctypes.byref(ffn), int(rows), int(backward)))
+
+
+def _kept(t, rows, n, dtype, keep, what):
+    if keep == KEEP_8:
+        return _packed(t, rows, n, what)
+    return _vector(t, rows * n, dtype, what)
+
+
+def lirpa_ffn_forward(ffn, x, out, keep, g, u, ws, ws_bytes, stream=None):
+    rows = x.shape[0]
+    dt = _dtype(x, "x")
+    if DTYPES[dt] != ffn.dtype:
+        raise TypeError(f"x is {dt}, the block's weights are not")
+    _check(load().lirpa_ffn_forward(
+        ctypes.byref(ffn), rows, *_matrix(x, rows, ffn.n_model, dt, "x"),
+        *_matrix(out, rows, ffn.n_model, dt, "out"), int(keep),
+        _kept(g, rows, ffn.n_hidden, dt, keep, "g"), _kept(u, rows, ffn.n_hidden, dt, keep, "u"),
+        _dev(ws, None, "ws"), int(ws_bytes), _stream(stream)))
+
+
+def lirpa_ffn_backward(ffn, dout, keep, x, g, u, dx, dWg, dWu, dWd, ws, ws_bytes, stream=None):
+    rows = dout.shape[0]
+    dt = _dtype(dout, "dout")
+    if DTYPES[dt] != ffn.dtype:
+        raise TypeError(f"dout is {dt}, the block's weights are not")
+    D, F = ffn.n_model, ffn.n_hidden
+    px, ldx = (_packed(x, rows, D, "x"), 0) if keep == KEEP_8 else _matrix(x, rows, D, dt, "x")
+    _check(load().lirpa_ffn_backward(
+        ctypes.byref(ffn), rows, *_matrix(dout, rows, D, dt, "dout"), int(keep), px, ldx,
+        _kept(g, rows, F, dt, keep, "g"), _kept(u, rows, F, dt, keep, "u"),
+        *_matrix(dx, rows, D, dt, "dx"), _vector(dWg, F * D, dt, "dWg"),
+        _vector(dWu, F * D, dt, "dWu"), _vector(dWd, D * F, dt, "dWd"), _dev(ws, None, "ws"),
+        int(ws_bytes), _stream(stream)))
 
 
 class Network:

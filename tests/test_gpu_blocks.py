@@ -1,0 +1,555 @@
+"""The feed-forward block's kernels against plain implementations in 64 bits.
+
+Tolerances are bounds, not measurements.  With u the rounding unit of the type (half the distance
+of neighbouring values, relative) and e = 2^-24 that of 32 bits:
+
+* a sum of K products in 32 bits is off by at most (K + 8) e times the sum of their magnitudes
+  (8: the products' own rounding, the parts of 32-bit operands that are left out, the join);
+* an intermediate that is rounded to the type is off by u of its magnitude, an output likewise;
+* a gate's value and slope are off by at most 16 e of theirs and move with their argument.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+UNIT = {t: torch.finfo(t).eps / 2 for t in (torch.float32, torch.bfloat16, torch.float16)}
+TINY = {torch.float32: 1e-37, torch.bfloat16: 1e-37, torch.float16: 2.0 ** -25}
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def ids(t):
+    return str(t).replace("torch.", "")
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2011_13824_amd import blocks
+    return blocks
+
+
+def rand(gen, *shape, dtype=torch.float32, pad=0, shift=0, scale=1.0):
+    """A [rows, n] view whose rows lie n + pad apart and start `shift` elements in."""
+    rows, n = shape
+    buf = torch.randn(rows * (n + pad) + shift, generator=gen, device="cuda") * scale
+    return buf.to(dtype)[shift:].view(rows, n + pad)[:, :n]
+
+
+def gen_of(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def check(got, want, tol, what):
+    got = got.double()
+    assert got.shape == want.shape, what
+    worst = ((got - want).abs() / tol.clamp(min=1e-300)).max().item() if got.numel() else 0.0
+    assert torch.isfinite(got).all() and worst <= 1.0, f"{what}: {worst:.3g} of the tolerance"
+
+
+# ---------------------------------------------------------------------------------------------
+# 8 bits
+# ---------------------------------------------------------------------------------------------
+def q8_parts(q):
+    groups = -(-q.n // 32)
+    buf = q.buf.cpu().numpy()
+    vals = buf[:q.rows * groups * 32].view(np.int8).reshape(q.rows, groups, 32)
+    return vals, buf[q.rows * groups * 32:].reshape(q.rows, groups)
+
+
+def q8_plain(x):
+    """Values and biased exponents in 64-bit numpy."""
+    x = x.double().cpu().numpy()
+    rows, n = x.shape
+    groups = -(-n // 32)
+    wide = np.zeros((rows, groups * 32))
+    wide[:, :n] = x
+    wide = wide.reshape(rows, groups, 32)
+    top = np.abs(wide).max(2)
+    part, e = np.frexp(top)
+    e = np.maximum(np.where(part > 127 / 128, e - 6, e - 7), -120)
+    e = np.where(top > 0, e, -120)  # the least there is for a group of zeros
+    return np.rint(np.ldexp(wide, -e[..., None])), e + 127
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,pad,shift", [(1, 1, 0, 0), (3, 31, 0, 1), (5, 32, 3, 0),
+                                              (17, 33, 0, 0), (64, 100, 5, 3), (9, 4096, 0, 0),
+                                              (700, 257, 1, 1)])
+def test_q8_is_the_definition(B, dtype, rows, n, pad, shift):
+    g = gen_of(rows * 1000 + n)
+    x = rand(g, rows, n, dtype=dtype, pad=pad, shift=shift)
+    x[0] = 0
+    if rows > 2:  # the ends of a group's range: 127, half steps, one past
+        x[1, :min(n, 4)] = torch.tensor([127.0, 63.5, -127.5, 0.5], device="cuda").to(dtype)[:n]
+        x[2] *= 2.0 ** -14
+    q = B.Q8.pack(x)
+    vals, exps = q8_parts(q)
+    want, wexp = q8_plain(x)
+    np.testing.assert_array_equal(exps, wexp)
+    np.testing.assert_array_equal(vals, want)  # columns past n are 0 on both sides
+    exact = np.ldexp(want, wexp[..., None] - 127).reshape(rows, -1)[:, :n]
+    for out in (torch.float32, torch.bfloat16):  # exact in both
+        np.testing.assert_array_equal(q.values(out).double().cpu().numpy(), exact)
+
+
+def test_q8_extremes(B):
+    x = torch.zeros(6, 64, device="cuda")
+    x[0, 3] = float("inf")
+    x[1, 40] = float("nan")
+    x[2, 5] = 3.4e38
+    x[3, 7] = 1e-45
+    x[4, 9] = -1e-36
+    x[5, 33] = -float("inf")
+    v = B.Q8.pack(x).values()
+    assert torch.isnan(v[0, :32]).all() and (v[0, 32:] == 0).all()
+    assert torch.isnan(v[1, 32:]).all() and (v[1, :32] == 0).all()
+    assert torch.isnan(v[5, 32:]).all() and (v[5, :32] == 0).all()
+    assert abs(v[2, 5].item() / 3.4e38 - 1) <= 2.0 ** -7
+    assert v[3, 7].item() == 0.0
+    assert abs(v[4, 9].item() + 1e-36) <= 2.0 ** -121
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+def test_q8_reads_into_strided_rows(B, dtype):
+    from paper_2011_13824_amd import lirpa
+    x = rand(gen_of(5), 33, 77)
+    q = B.Q8.pack(x)
+    out = torch.full((33, 90), 7.0, device="cuda", dtype=dtype)
+    lirpa.lirpa_q8_unpack(q.buf, out[:, 3:80])
+    assert (out[:, :3] == 7).all() and (out[:, 80:] == 7).all()
+    assert torch.equal(out[:, 3:80], q.values(dtype))
+
+
+def test_q8_no_rows(B):
+    assert B.Q8.pack(torch.empty(0, 40, device="cuda")).values().shape == (0, 40)
+
+
+# ---------------------------------------------------------------------------------------------
+# Norm
+# ---------------------------------------------------------------------------------------------
+NORM_SHAPES = [(1, 1, 0, 0), (2, 7, 1, 1), (5, 64, 0, 0), (67, 513, 3, 0), (9, 1025, 0, 1),
+               (33, 2048, 0, 0), (3, 2049, 0, 0), (5, 4096, 8, 0), (6, 8191, 0, 3), (4, 8200, 0, 0),
+               (2, 16385, 0, 0), (3, 40000, 4, 0), (2500, 96, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,pad,shift", NORM_SHAPES)
+@pytest.mark.parametrize("res", [True, False])
+def test_norm_forward(B, dtype, rows, n, pad, shift, res):
+    g = gen_of(rows + n)
+    x = rand(g, rows, n, dtype=dtype, pad=pad, shift=shift)
+    r = rand(g, rows, n, dtype=dtype, pad=pad + 1, scale=3.0) if res else None
+    w = (1 + 0.2 * torch.randn(n, generator=g, device="cuda")).to(dtype)
+    if rows > 1:
+        x[1] = 0  # a row without a direction: only eps is left
+        if res:
+            r[1] = 0
+    got = B.Norm(w, 1e-5).forward(x, r, want8=True)
+    h = x.double() + (r.double() if res else 0)
+    rstd = 1 / torch.sqrt(h.square().mean(1) + 1e-5)
+    y = h * rstd[:, None] * w.double()
+    u = UNIT[dtype]
+    # h is off by e, its square's mean by (n + 8) e at most, the root by half of that
+    rel = (n + 16) * E
+    check(got.rstd, rstd, rel * rstd, "rstd")
+    check(got.y, y, (u + rel) * y.abs() + TINY[dtype], "y")
+    if res:
+        check(got.sum, h, (u + 2 * E) * h.abs() + TINY[dtype], "sum")
+    else:
+        assert got.sum is x
+    # the packed y: within half a step of y, and its scale the least one that reaches the group
+    vals, exps = q8_parts(got.y8)
+    step = torch.from_numpy(np.exp2(exps.astype(np.float64) - 127)).cuda()
+    wide = torch.zeros(rows, step.shape[1] * 32, dtype=torch.float64, device="cuda")
+    wide[:, :n] = y
+    wide = wide.view(rows, -1, 32)
+    back = torch.from_numpy(vals.astype(np.float64)).cuda() * step[..., None]
+    check(back, wide, step[..., None] * 0.5 + rel * wide.abs() + 1e-300, "y8")
+    top = wide.abs().amax(2)
+    assert (127 * step >= top * (1 - rel)).all()
+    assert ((127 * step / 2 < top * (1 + rel)) | (exps_floor(exps))).all()
+
+
+def exps_floor(exps):
+    return torch.from_numpy(exps == 7).cuda()
+
+
+def test_norm_sum_in_place(B):
+    from paper_2011_13824_amd import lirpa
+    for n in (96, 4096, 20000):
+        g = gen_of(n)
+        x, r, w = rand(g, 9, n), rand(g, 9, n), torch.ones(n, device="cuda")
+        want = B.Norm(w).forward(x, r)
+        rstd = torch.empty(9, device="cuda")
+        y = torch.empty_like(x)
+        lirpa.lirpa_norm_forward(x, r, w, 1e-5, r, y, None, rstd)
+        assert torch.equal(r, want.sum) and torch.equal(y, want.y) and torch.equal(rstd, want.rstd)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,pad,shift", NORM_SHAPES)
+@pytest.mark.parametrize("past", [True, False])
+def test_norm_backward(B, dtype, rows, n, pad, shift, past):
+    g = gen_of(rows * 3 + n)
+    h = rand(g, rows, n, dtype=dtype, pad=pad, shift=shift, scale=2.0)
+    dy = rand(g, rows, n, dtype=dtype, pad=pad + 2)
+    dsum = rand(g, rows, n, dtype=dtype) if past else None
+    w = (1 + 0.2 * torch.randn(n, generator=g, device="cuda")).to(dtype)
+    rstd = torch.rsqrt(h.float().square().mean(1) + 1e-5)
+    dh, dw = B.Norm(w).backward(dy, h, rstd, dsum)
+    xhat, t, r = h.double() * rstd.double()[:, None], dy.double() * w.double(), rstd.double()
+    dot = (t * xhat).mean(1, keepdim=True)
+    want = r[:, None] * (t - xhat * dot)
+    size = r[:, None] * (t.abs() + xhat.abs() * (t * xhat).abs().mean(1, keepdim=True))
+    if past:
+        want = want + dsum.double()
+        size = size + dsum.double().abs()
+    u = UNIT[dtype]
+    check(dh, want, u * want.abs() + (n + 16) * E * size + TINY[dtype], "dh")
+    wdw = (dy.double() * xhat).sum(0)
+    check(dw, wdw, u * wdw.abs() + (rows + 16) * E * (dy.double() * xhat).abs().sum(0)
+          + TINY[dtype], "dw")
+
+
+def test_norm_backward_differences(B):
+    """<gradient, v> against central differences of the definition in 64 bits."""
+    g = gen_of(12)
+    rows, n = 7, 130
+    x, r, dy, dsum = (rand(g, rows, n) for _ in range(4))
+    w = 1 + 0.2 * torch.randn(n, generator=g, device="cuda")
+    norm = B.Norm(w)
+    f = norm.forward(x, r)
+    dh, dw = norm.backward(dy, f.sum, f.rstd, dsum)
+
+    def loss(a, ww):
+        h = a + r.double()
+        y = h / torch.sqrt(h.square().mean(1, keepdim=True) + 1e-5) * ww
+        return (y * dy.double()).sum() + (h * dsum.double()).sum()
+
+    va, vw = rand(g, rows, n).double(), torch.randn(n, generator=g, device="cuda").double()
+    s = 1e-5
+    num = (loss(x.double() + s * va, w.double() + s * vw)
+           - loss(x.double() - s * va, w.double() - s * vw)) / (2 * s)
+    got = (dh.double() * va).sum() + (dw.double() * vw).sum()
+    size = (dh.double() * va).abs().sum() + (dw.double() * vw).abs().sum()
+    assert abs(num - got) <= (n + rows + 32) * 4 * E * size + 1e-6
+
+
+def test_norm_in_place_gradient_and_parts(B):
+    from paper_2011_13824_amd import lirpa
+    g = gen_of(3)
+    for n in (200, 5000, 17000):
+        dy, h, ds = (rand(g, 11, n) for _ in range(3))
+        w, rstd = torch.ones(n, device="cuda"), torch.rsqrt(h.square().mean(1))
+        norm = B.Norm(w)
+        dh, dw = norm.backward(dy, h, rstd, ds)
+        only, none = norm.backward(dy, h, rstd, ds, want_dw=False)
+        assert none is None and torch.equal(only, dh)
+        need = lirpa.lirpa_norm_workspace_bytes(11, n)
+        ws, dw2 = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty_like(dw)
+        lirpa.lirpa_norm_backward(dy, ds, h, w, rstd, None, dw2, ws, need)
+        assert torch.equal(dw2, dw)
+        lirpa.lirpa_norm_backward(dy, ds, h, w, rstd, ds, None, None, 0)
+        assert torch.equal(ds, dh)
+
+
+def test_norm_no_rows(B):
+    x, w = torch.empty(0, 50, device="cuda"), torch.ones(50, device="cuda")
+    f = B.Norm(w).forward(x, x, want8=True)
+    assert f.y.shape == (0, 50)
+    dh, dw = B.Norm(w).backward(x, x, f.rstd)
+    assert dh.shape == (0, 50) and (dw == 0).all()
+
+
+# ---------------------------------------------------------------------------------------------
+# Gated block
+# ---------------------------------------------------------------------------------------------
+def act64(g, gate):
+    if gate == "relu":
+        return g.clamp(min=0), (g > 0).double()
+    if gate == "silu":
+        p = torch.sigmoid(g)
+        return g * p, p * (1 + g * (1 - p))
+    p = 0.5 * torch.special.erfc(-g / math.sqrt(2))
+    return g * p, p + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+
+
+def weights(gen, D, F, dtype, pad=0, shift=0):
+    return (rand(gen, F, D, dtype=dtype, pad=pad, shift=shift, scale=D ** -0.5),
+            rand(gen, F, D, dtype=dtype, pad=pad, shift=shift, scale=D ** -0.5),
+            rand(gen, D, F, dtype=dtype, pad=pad, shift=shift, scale=F ** -0.5))
+
+
+def forward64(x, W, gate, u):
+    """out, g, u and their tolerances."""
+    x, (Wg, Wu, Wd) = x.double(), [w.double() for w in W]
+    D, F = Wg.shape[1], Wg.shape[0]
+    g, p = x @ Wg.T, x @ Wu.T
+    tg, tp = ((D + 8) * E * (x.abs() @ w.abs().T) for w in (Wg, Wu))
+    act, _ = act64(g, gate)
+    a = act * p
+    # slopes of the three gates stay under 1.13
+    ta = 1.2 * tg * p.abs() + tp * act.abs() + 1.2 * tg * tp + (u + 20 * E) * a.abs()
+    out = a @ Wd.T
+    tol = u * out.abs() + (ta + (F + 8) * E * a.abs()) @ Wd.abs().T
+    return out, tol, g, tg, p, tp
+
+
+def backward64(dout, x, g, p, W, gate, u):
+    """Gradients and their tolerances."""
+    dout, x, (Wg, Wu, Wd) = dout.double(), x.double(), [w.double() for w in W]
+    rows, D, F = dout.shape[0], Wg.shape[1], Wg.shape[0]
+    act, slope = act64(g, gate)
+    da = dout @ Wd
+    tda = (D + 8) * E * (dout.abs() @ Wd.abs())
+    # a slope's terms may cancel: it is off by 16 e of at most 1 + |g|
+    tsl = 16 * E * (1 + g.abs())
+    dg, du, a = da * p * slope, da * act, act * p
+    tdg = (tda * slope.abs() + da.abs() * tsl) * p.abs() + (u + 8 * E) * dg.abs()
+    tdu = tda * act.abs() + (u + 24 * E) * du.abs()
+    ta = (u + 24 * E) * a.abs()
+    grads = {"dx": dg @ Wg + du @ Wu, "dWg": dg.T @ x, "dWu": du.T @ x, "dWd": dout.T @ a}
+    k = (2 * F + 8) * E
+    r = (rows + 8) * E
+    tols = {"dx": (tdg + k * dg.abs()) @ Wg.abs() + (tdu + k * du.abs()) @ Wu.abs(),
+            "dWg": (tdg + r * dg.abs()).T @ x.abs(), "dWu": (tdu + r * du.abs()).T @ x.abs(),
+            "dWd": dout.abs().T @ (ta + r * a.abs())}
+    return grads, {n: t + u * grads[n].abs() for n, t in tols.items()}
+
+
+# rows, model, hidden, row padding, element shift: one token to many, widths of no tile, one column
+FFN_SHAPES = [(1, 64, 96, 0, 0), (2, 1, 1, 0, 0), (3, 40, 24, 0, 0), (5, 7, 33, 1, 1),
+              (16, 129, 65, 0, 0), (17, 136, 264, 8, 0), (33, 72, 200, 0, 1), (64, 257, 130, 3, 0),
+              (65, 128, 128, 0, 0), (130, 100, 300, 0, 0), (257, 264, 136, 0, 0),
+              (100, 1001, 91, 0, 0), (300, 31, 517, 5, 0)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,D,F,pad,shift", FFN_SHAPES)
+@pytest.mark.parametrize("gate", ["silu", "gelu", "relu"])
+def test_ffn_forward(B, dtype, rows, D, F, pad, shift, gate):
+    g = gen_of(rows + D + F)
+    x = rand(g, rows, D, dtype=dtype, pad=pad, shift=shift)
+    W = weights(g, D, F, dtype, pad, shift)
+    ffn = B.FeedForward(*W, gate)
+    u = UNIT[dtype]
+    out, tol, wg, tg, wu, tu = forward64(x, W, gate, u)
+    tiny = TINY[dtype] * (1 + W[2].double().abs().sum(1))
+    check(ffn.forward(x), out, tol + tiny, "out")
+    got, kept = ffn.forward(x, keep=0)
+    check(got, out, tol + tiny, "out, projections kept")
+    check(kept.g, wg, tg + u * wg.abs() + TINY[dtype], "g")
+    check(kept.u, wu, tu + u * wu.abs() + TINY[dtype], "u")
+    got, kept = ffn.forward(x, keep=8)
+    check(got, out, tol + tiny, "out, 8 bits kept")
+    for q, want, t in ((kept.g, wg, tg), (kept.u, wu, tu)):
+        vals, exps = q8_parts(q)
+        assert (vals.reshape(rows, -1)[:, F:] == 0).all()
+        step = torch.from_numpy(np.exp2(exps.astype(np.float64) - 127)).cuda()
+        each = step.repeat_interleave(32, 1)[:, :F]
+        check(q.values(), want, 0.5 * each + t, "packed projection")
+        wide = torch.zeros(rows, step.shape[1] * 32, dtype=torch.float64, device="cuda")
+        wide[:, :F] = want.abs() + t
+        assert (127 * step < 2 * wide.view(rows, -1, 32).amax(2)).logical_or(exps_floor(exps)).all()
+    assert torch.equal(kept.x.values(), B.Q8.pack(x).values())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,D,F,pad,shift", FFN_SHAPES)
+@pytest.mark.parametrize("gate", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("keep", [8, 0])
+def test_ffn_backward(B, dtype, rows, D, F, pad, shift, gate, keep):
+    g = gen_of(rows + D + F + 1)
+    W = weights(g, D, F, dtype, pad, shift)
+    dout = rand(g, rows, D, dtype=dtype, pad=pad, shift=shift)
+    x = rand(g, rows, D, dtype=dtype, pad=pad, shift=shift)
+    kg, ku = rand(g, rows, F, dtype=dtype), rand(g, rows, F, dtype=dtype)
+    kg[0, 0] = 0  # relu's slope there is 0
+    if keep == 8:
+        kept = B.Kept(8, rows, *(B.Q8.pack(t) for t in (x, kg, ku)))
+        vx, vg, vu = (t.values() for t in (kept.x, kept.g, kept.u))
+    else:
+        kept = B.Kept(0, rows, x, kg.contiguous(), ku.contiguous())
+        vx, vg, vu = x, kg, ku
+    ffn = B.FeedForward(*W, gate)
+    got = ffn.backward(dout, kept)
+    want, tol = backward64(dout, vx, vg.double(), vu.double(), W, gate, UNIT[dtype])
+    tiny = TINY[dtype]
+    lost = {"dx": 2 * (W[0].double().abs() + W[1].double().abs()).sum(0),
+            "dWg": vx.double().abs().sum(0), "dWu": vx.double().abs().sum(0),
+            "dWd": dout.double().abs().sum(0)[:, None]}
+    for name in want:
+        check(got[name], want[name], tol[name] + tiny * (1 + lost[name]), name)
+    for name in want:  # each alone is what it is among the others
+        assert torch.equal(ffn.backward(dout, kept, want=(name,))[name], got[name]), name
+
+
+def test_ffn_backward_differences(B):
+    """<gradient, v> of a whole pass against central differences in 64 bits."""
+    g = gen_of(77)
+    rows, D, F = 19, 40, 72
+    x, dout, W = rand(g, rows, D), rand(g, rows, D), weights(g, D, F, torch.float32)
+    ffn = B.FeedForward(*W, "gelu")
+    _, kept = ffn.forward(x, keep=0)
+    got = ffn.backward(dout, kept)
+    at = [x.double()] + [w.double() for w in W]
+    to = [rand(g, *t.shape).double() for t in at]
+
+    def loss(s):
+        a, wg, wu, wd = (p + s * v for p, v in zip(at, to))
+        return (((act64(a @ wg.T, "gelu")[0] * (a @ wu.T)) @ wd.T) * dout.double()).sum()
+
+    s = 1e-5
+    num = (loss(s) - loss(-s)) / (2 * s)
+    parts = [got[k].double() * v for k, v in zip(("dx", "dWg", "dWu", "dWd"), to)]
+    size = sum(p.abs().sum() for p in parts)
+    assert abs(num - sum(p.sum() for p in parts)) <= (D + 2 * F + rows + 64) * 8 * E * size + 1e-5
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,D,F", [(2051, 72, 3083), (1030, 2060, 520)])
+def test_ffn_large_tiles(B, dtype, rows, D, F):
+    """Sizes that take the larger tiles, ragged on every side."""
+    g = gen_of(rows)
+    x, dout, W = rand(g, rows, D, dtype=dtype), rand(g, rows, D, dtype=dtype), weights(g, D, F,
+                                                                                     dtype)
+    ffn = B.FeedForward(*W, "silu")
+    out, tol, *_ = forward64(x, W, "silu", UNIT[dtype])
+    got, kept = ffn.forward(x, keep=8)
+    tiny = TINY[dtype] * 100
+    check(got, out, tol + tiny, "out")
+    grads = ffn.backward(dout, kept)
+    want, tol = backward64(dout, kept.x.values(), kept.g.values().double(),
+                           kept.u.values().double(), W, "silu", UNIT[dtype])
+    for name in want:
+        check(grads[name], want[name], tol[name] + tiny * 100, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+def test_ffn_no_rows(B, dtype):
+    W = weights(gen_of(1), 24, 40, dtype)
+    ffn = B.FeedForward(*W, "silu")
+    x = torch.empty(0, 24, dtype=dtype, device="cuda")
+    assert ffn.forward(x).shape == (0, 24)
+    for keep in (0, 8):
+        _, kept = ffn.forward(x, keep=keep)
+        grads = ffn.backward(x, kept)
+        assert grads["dx"].shape == (0, 24)
+        assert all((grads[k] == 0).all() for k in ("dWg", "dWu", "dWd"))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=ids)
+@pytest.mark.parametrize("rows", [12, 90])
+def test_ffn_rows_stay_apart(B, dtype, rows):
+    """A row of NaN and one of infinities spoil their own outputs alone."""
+    g = gen_of(8)
+    x, W = rand(g, rows, 72, dtype=dtype), weights(g, 72, 104, dtype)
+    ffn = B.FeedForward(*W, "silu")
+    clean = ffn.forward(x)
+    x[3] = float("nan")
+    x[7, 5] = float("inf")
+    out = ffn.forward(x)
+    others = [r for r in range(rows) if r not in (3, 7)]
+    assert torch.equal(out[others], clean[others])
+    assert torch.isnan(out[3]).all() and not torch.isfinite(out[7]).any()
+
+
+def test_ffn_strided_output_and_far_rows(B):
+    """Rows 2^22 - 8 elements apart: offsets pass 32 bits, and what lies between stays."""
+    from paper_2011_13824_amd import lirpa
+    rows, D, F, ld = 530, 64, 96, (1 << 22) - 8
+    g = gen_of(4)
+    W = weights(g, D, F, torch.bfloat16)
+    x = rand(g, rows, D, dtype=torch.bfloat16)
+    far = torch.zeros(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)
+    far[:, 8:8 + D] = x
+    ffn = B.FeedForward(*W, "silu")
+    want, kept = ffn.forward(x, keep=8)
+    ws, need = ffn._workspace(rows, 0)
+    lirpa.lirpa_ffn_forward(ffn.block, far[:, 8:8 + D], far[:, 128:128 + D], lirpa.KEEP_NONE, None,
+                            None, ws, need)
+    assert torch.equal(far[:, 128:128 + D], want)
+    assert (far[:, 120:128] == 0).all() and (far[:, 128 + D:136 + D] == 0).all()
+    q = B.Q8.pack(far[:, 8:8 + D])
+    assert torch.equal(q.buf, kept.x.buf)
+    w = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(B.Norm(w).forward(far[:, 8:8 + D]).y, B.Norm(w).forward(x).y)
+    grads = ffn.backward(want, kept)
+    there = ffn.backward(far[:, 128:128 + D], kept)
+    for k in grads:
+        assert torch.equal(grads[k], there[k]), k
+
+
+def test_calls_run_on_the_current_stream(B):
+    g = gen_of(21)
+    x, W = rand(g, 200, 128, dtype=torch.bfloat16), weights(g, 128, 256, torch.bfloat16)
+    norm, ffn = B.Norm(torch.ones(128, dtype=torch.bfloat16, device="cuda")), B.FeedForward(*W)
+
+    def block():
+        n = norm.forward(x, x, want8=True)
+        out, kept = ffn.forward(n.y, keep=8, x8=n.y8)
+        grads = ffn.backward(out, kept)
+        return [out, *grads.values(), *norm.backward(grads["dx"], n.sum, n.rstd, out)]
+
+    want = block()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = block()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_calls_replay_in_a_graph(B):
+    g = gen_of(22)
+    x, W = rand(g, 96, 136, dtype=torch.bfloat16), weights(g, 136, 200, torch.bfloat16)
+    few = x[:3]
+    norm, ffn = B.Norm(torch.ones(136, dtype=torch.bfloat16, device="cuda")), B.FeedForward(*W)
+
+    def block():
+        n = norm.forward(x, x, want8=True)
+        out, kept = ffn.forward(n.y, keep=8, x8=n.y8)
+        grads = ffn.backward(out, kept)
+        return [out, ffn.forward(few), *grads.values(),
+                *norm.backward(grads["dx"], n.sum, n.rstd, out)]
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        block()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = block()
+    for k in range(4):
+        x.copy_(rand(gen_of(100 + k), 96, 136, dtype=torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = block()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want)), k
+
+
+def test_binding_refusals(B):
+    from paper_2011_13824_amd import lirpa
+    g = gen_of(9)
+    W = weights(g, 24, 40, torch.bfloat16)
+    ffn = B.FeedForward(*W)
+    x = rand(g, 5, 24)
+    with pytest.raises(TypeError, match="weights are not"):
+        ffn.forward(x)
+    with pytest.raises(ValueError, match="must be"):
+        ffn.forward(rand(g, 5, 25, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="contiguous rows"):
+        ffn.forward(rand(g, 24, 5, dtype=torch.bfloat16).t())
+    with pytest.raises(ValueError, match="bytes"):
+        lirpa.lirpa_q8_unpack(torch.empty(10, dtype=torch.uint8, device="cuda"), x)
+    with pytest.raises(TypeError):
+        B.FeedForward(W[0], W[1].float(), W[2])
+    with pytest.raises(lirpa.LirpaError):
+        B.Norm(torch.ones(24, device="cuda"), eps=-1.0).forward(x)
