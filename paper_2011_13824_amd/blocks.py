@@ -53,8 +53,8 @@ class Norm:
         """Normed(y, sum, y8, rstd): sum is h (x itself without a residual); y8 a Q8 of y where
         wanted, else None; rstd is float32 [rows]."""
         rows, n = x.shape
-        y = torch.empty((rows, n), dtype=x.dtype, device=x.device) if want_y else None
-        h = torch.empty((rows, n), dtype=x.dtype, device=x.device) if res is not None else None
+        y = torch.empty_like(x) if want_y else None
+        h = torch.empty_like(x) if res is not None else None
         y8 = Q8(rows, n, device=x.device) if want8 else None
         rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
         lirpa.lirpa_norm_forward(x, res, self.w, self.eps, h, y, y8.buf if want8 else None, rstd)
@@ -63,11 +63,11 @@ class Norm:
     def backward(self, dy, h, rstd, dsum=None, want_dw=True):
         """(dh, dw): dh is the gradient of x and of res, dsum that of h past the norm."""
         rows, n = dy.shape
-        dh = torch.empty((rows, n), dtype=dy.dtype, device=dy.device)
+        dh = torch.empty_like(dy)
         dw = ws = None
         need = 0
         if want_dw:
-            dw = torch.empty(n, dtype=dy.dtype, device=dy.device)
+            dw = torch.empty_like(self.w)
             need = lirpa.lirpa_norm_workspace_bytes(rows, n)
             ws = torch.empty(need, dtype=torch.uint8, device=dy.device)
         lirpa.lirpa_norm_backward(dy, dsum, h, self.w, rstd, dh, dw, ws, need)
@@ -102,7 +102,7 @@ class FeedForward:
         """out; with ``keep`` (8 or 0) (out, Kept).  ``x8``: x in 8 bits where the caller has it
         (a norm's y8); it is packed here otherwise."""
         rows, dev, hidden = x.shape[0], x.device, self.block.n_hidden
-        out = torch.empty((rows, self.block.n_model), dtype=x.dtype, device=dev)
+        out = torch.empty_like(x)
         ws, need = self._workspace(rows, 0)
         if keep is None:
             lirpa.lirpa_ffn_forward(self.block, x, out, lirpa.KEEP_NONE, None, None, ws, need)

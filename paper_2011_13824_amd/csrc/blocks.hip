@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <exception>
+#include <type_traits>
 
 #include "host.hpp"
 #include "ffn_few.hpp"
@@ -283,7 +284,7 @@ void add_segs(const FfnPlan& pl, TileArgs& t, int batch, const Operand& A, const
   t.ldb = B.ld * 2;
 }
 
-template <typename T, bool AKS, bool BKS, int EPI, int BI, int BJ, int WI, int WJ>
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ>
 int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
   constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;
   const int64_t ti = up(t.I, kFeat) / kFeat, tj = up(t.J, BJ) / BJ, total = ti * tj * t.batches;
@@ -292,21 +293,35 @@ int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
   t.tiles_i = (int)ti;
   t.tiles_j = (int)tj;
   return launch_k(name, st, [&] {
-    k_ffn_tile<T, AKS, BKS, EPI, BI, BJ, WI, WJ>
+    k_ffn_tile<T, AKS, BKS, EPI, KEEP, BI, BJ, WI, WJ>
         <<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);
   });
 }
 
-template <bool AKS, bool BKS, int EPI>
-int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, hipStream_t st) {
+// The larger tile reads each operand half as often, once there are enough of them to fill the
+// chip; the epilogue of da in 32 bits does not fit its registers.
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP>
+int tile_of_size(const char* name, TileArgs& t, hipStream_t st) {
   const int64_t feat = EPI == EPI_GATE ? 128 : 256;
   const int64_t large = (up(t.I, feat) / feat) * (up(t.J, 256) / 256) * t.batches;
-  if (pl.f->dtype == LIRPA_F16) {
-    if (large >= 192) return launch_tile<f16, AKS, BKS, EPI, 256, 256, 2, 4>(name, t, st);
-    return launch_tile<f16, AKS, BKS, EPI, 128, 128, 2, 2>(name, t, st);
-  }
-  if (large >= 192) return launch_tile<bf16, AKS, BKS, EPI, 256, 256, 2, 4>(name, t, st);
-  return launch_tile<bf16, AKS, BKS, EPI, 128, 128, 2, 2>(name, t, st);
+  if constexpr (!(Kind<T>::kParts == 3 && EPI == EPI_BACK))
+    if (large >= 192) return launch_tile<T, AKS, BKS, EPI, KEEP, 256, 256, 2, 4>(name, t, st);
+  return launch_tile<T, AKS, BKS, EPI, KEEP, 128, 128, 2, 2>(name, t, st);
+}
+
+template <bool AKS, bool BKS, int EPI>
+int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, hipStream_t st) {
+  auto typed = [&](auto keep) {
+    constexpr int K = decltype(keep)::value;
+    switch (pl.f->dtype) {
+      case LIRPA_F32: return tile_of_size<Split, AKS, BKS, EPI, K>(name, t, st);
+      case LIRPA_BF16: return tile_of_size<bf16, AKS, BKS, EPI, K>(name, t, st);
+      default: return tile_of_size<f16, AKS, BKS, EPI, K>(name, t, st);
+    }
+  };
+  if constexpr (EPI == EPI_BACK)
+    if (t.keep == LIRPA_KEEP_8) return typed(std::integral_constant<int, 8>{});
+  return typed(std::integral_constant<int, 0>{});
 }
 
 TileArgs tile_args(const FfnPlan& pl, int64_t I, int64_t J, int64_t KA, int64_t KB) {
@@ -316,7 +331,6 @@ TileArgs tile_args(const FfnPlan& pl, int64_t I, int64_t J, int64_t KA, int64_t 
   t.KA = (int)KA;
   t.KB = (int)KB;
   t.batches = 1;
-  t.parts = pl.parts;
   t.keep = -1;
   t.gate = pl.f->gate;
   return t;

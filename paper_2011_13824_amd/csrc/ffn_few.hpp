@@ -22,11 +22,11 @@ template <typename T>
 struct Eight {
   typename Mfma<T>::x8 v;
   __device__ __forceinline__ void load(const T* p) {
-    v = __builtin_bit_cast(typename Mfma<T>::x8, *reinterpret_cast<const Vec<T, 8>*>(p));
+    v = load_global<Vec<T, 8>>(p);
   }
   __device__ __forceinline__ void load(const T* p, int valid) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : (T)0.f;
+    for (int i = 0; i < 8; ++i) v[i] = i < valid ? load_global<T>(p + i) : (T)0.f;
   }
   static __device__ __forceinline__ f32x4 mac(const Eight& a, const Eight& b, f32x4 c) {
     return Mfma<T>::mac(a.v, b.v, c);
@@ -36,13 +36,13 @@ template <>
 struct Eight<float> {
   float v[8];
   __device__ __forceinline__ void load(const float* p) {
-    const Vec<float, 8> t = *reinterpret_cast<const Vec<float, 8>*>(p);
+    const Vec<float, 8> t = load_global<Vec<float, 8>>(p);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = t.v[i];
+    for (int i = 0; i < 8; ++i) v[i] = t[i];
   }
   __device__ __forceinline__ void load(const float* p, int valid) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = i < valid ? load_global<float>(p + i) : 0.f;
   }
   static __device__ __forceinline__ f32x4 mac(const Eight& a, const Eight& b, f32x4 c) {
 #pragma unroll
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(FewArgs a) {
     }
     if constexpr (GATE) {
       float act, slope;
-      gate_fn(a.gate, v[0], act, slope);
+      gate_fn(a.gate, sizeof(T) == 2, v[0], act, slope);
       v[0] = act * v[1];
     }
     const int64_t token = t * 16 + j;

@@ -18,6 +18,8 @@
 // those of the largest parts, smallest first, and the error stays that of a 32-bit sum.
 #pragma once
 
+#include <type_traits>
+
 #include "lm_types.hpp"
 
 namespace lm {
@@ -26,7 +28,8 @@ enum Epi { EPI_STORE, EPI_GATE, EPI_BACK };
 enum Gate { RELU = 0, SILU = 1, GELU = 2 };
 
 constexpr int kMaxSegs = 12;
-constexpr int kBK = 64;  // k a tile step: 128 bytes of a k-contiguous row
+constexpr int kBK = 64;    // k a tile: 128 bytes of a k-contiguous row, the width of a cache line
+constexpr int kUnits = 5;  // tiles of one operand in LDS
 
 struct TileArgs {
   const char* A[kMaxSegs];
@@ -38,12 +41,10 @@ struct TileArgs {
   int KA, KB;                   // k extents (equal up to the zero padding of a packed operand)
   int I, J;                     // output sizes
   int tiles_i, tiles_j, batches;
-  // output: 16-bit or float; parts = 3 writes bf16 parts at distance `plane` elements
   void* out[2];
   int64_t ldo;                  // elements
-  int pad_i;                    // columns [I, pad_i) of 16-bit operand outputs are written as 0
-  int parts;
-  int64_t plane;
+  int pad_i;                    // columns [I, pad_i) of operand outputs are written as 0
+  int64_t plane;                // elements between the parts of a 32-bit operand
   // gate epilogues
   int gate, keep;               // keep: -1, 0, 8
   void *g, *u;                  // what is kept: [J][I] or packed
@@ -59,6 +60,24 @@ __device__ __forceinline__ void read8(const float* p, float (&x)[8]) {
   for (int r = 0; r < 4; ++r) x[r] = lo[r], x[4 + r] = hi[r];
 }
 
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+// Operands of the tile kernel: bf16, f16, or three bf16 parts of a float (Split).
+struct Split {};
+template <typename T>
+struct Kind {
+  using Half = T;  // what the matrix instruction takes
+  using Whole = T; // the tensors' type
+  static constexpr int kParts = 1;
+};
+template <>
+struct Kind<Split> {
+  using Half = bf16;
+  using Whole = float;
+  static constexpr int kParts = 3;
+};
+
 template <typename T>
 struct Mfma;
 template <>
@@ -67,6 +86,9 @@ struct Mfma<bf16> {
   static __device__ __forceinline__ f32x4 mac(x8 a, x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
+  static __device__ __forceinline__ void add(s16x8 a, s16x8 b, f32x4& c) {
+    c = mac(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c);
+  }
 };
 template <>
 struct Mfma<f16> {
@@ -74,22 +96,50 @@ struct Mfma<f16> {
   static __device__ __forceinline__ f32x4 mac(x8 a, x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
+  static __device__ __forceinline__ void add(s16x8 a, s16x8 b, f32x4& c) {
+    c = mac(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c);
+  }
 };
 
-// act(x) and act'(x).
-__device__ __forceinline__ void gate_fn(int gate, float x, float& act, float& slope) {
+// act(x) and act'(x).  `fast`: e^x and the reciprocal with the hardware's own instructions, 1e-6
+// off near 0 and x^2 2^-24 further out, far under the rounding of a 16-bit type.
+//
+// Phi(x) for x <= 0 is erfc(z) / 2 with z = |x| / sqrt(2), and erfc(z) e^(z^2) is t P(t) with
+// t = 1 / (1 + 0.4 z): P is a fit of degree 8 in the relative error (1.3e-7 over t in (0, 1]), made
+// for this file by reweighted least squares.  e^(-z^2) is the slope's too.
+__device__ __forceinline__ void gate_fn(int gate, bool fast, float x, float& act, float& slope) {
   if (gate == RELU) {
     act = fmaxf(x, 0.f);
     slope = x > 0.f ? 1.f : 0.f;
     if (x != x) act = slope = x;
   } else if (gate == SILU) {
-    const float p = 1.f / (1.f + expf(-x));
+    const float p = fast ? __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950409f * x))
+                         : 1.f / (1.f + expf(-x));
     act = x * p;
     slope = p * (1.f + x * (1.f - p));
   } else {
-    const float p = 0.5f * erfcf(-0.70710678118654752f * x);
+    const float below = 1.f + 0.28284271247f * fabsf(x), xx = x * x;
+    const float t = fast ? __builtin_amdgcn_rcpf(below) : 1.f / below;
+    float e;
+    if (fast) {
+      e = __builtin_amdgcn_exp2f(-0.72134752044f * xx);
+    } else {  // what the square's rounding leaves would be multiplied by the square
+      const float rest = xx < 1e30f ? fmaf(x, x, -xx) : 0.f;
+      e = expf(-0.5f * xx) * (1.f - 0.5f * rest);
+    }
+    float p = 0.050272651f;
+    p = fmaf(p, t, -0.182943851f);
+    p = fmaf(p, t, 0.169155225f);
+    p = fmaf(p, t, -0.00566805014f);
+    p = fmaf(p, t, 0.141461045f);
+    p = fmaf(p, t, 0.168533847f);
+    p = fmaf(p, t, 0.20784387f);
+    p = fmaf(p, t, 0.225669518f);
+    p = fmaf(p, t, 0.225675866f);
+    p *= 0.5f * t * e;
+    if (x > 0.f) p = 1.f - p;
     act = x * p;
-    slope = p + x * (0.39894228040143268f * expf(-0.5f * x * x));
+    slope = p + x * (0.39894228040143268f * e);
   }
 }
 
@@ -99,12 +149,12 @@ __device__ __forceinline__ void gate_fn(int gate, float x, float& act, float& sl
 constexpr uint32_t kOutside = 0x80000000u;
 constexpr uint32_t kExtent = 0x7fffffffu;
 
-__device__ __forceinline__ u32x4 descriptor(const char* p) {
+__device__ __forceinline__ u32x4 descriptor(const char* p, uint32_t bytes) {
   const uint64_t a = (uint64_t)p;
   u32x4 d;
   d[0] = (uint32_t)a;
   d[1] = (uint32_t)(a >> 32) & 0xffffu;
-  d[2] = kExtent;
+  d[2] = bytes;
   d[3] = 0x00020000u;
   return d;
 }
@@ -116,14 +166,17 @@ __device__ __forceinline__ void bring16(u32x4 desc, uint32_t offset, uint32_t ld
 __device__ __forceinline__ void wait_all() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
+// All but the newest N of this thread's copies have arrived, and then every thread's.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(N) : "memory");
+}
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) s16x8 lds_s16x8;
 
 // Where an operand's tile (R rows of i or j, kBK of k) lies in LDS.
-//   k-contiguous: row r is 8 pieces of 16 bytes, piece p at p ^ (r / 2 % 8): the 16 rows that one
+//   k-contiguous: row r is 4 pieces of 16 bytes, piece p at p ^ (r / 2 % 4): the 16 rows that one
 //   read takes then start in 16 different 16-byte columns of the 256 bytes of banks.
 //   k-strided: line k is R / 8 pieces, piece p at p ^ 2 f(k), f(k) = k % 4 + 4 (k / 8 % 2): a
 //   transposing read takes 32 bytes of 4 lines, from 2 groups of lanes at k and k + 8.
@@ -136,36 +189,35 @@ struct Lay {
   }
 };
 
-// One operand's copies: thread t of THREADS brings pieces t, t + THREADS, ... of a tile.
+// One operand's copies: thread t of THREADS brings pieces t, t + THREADS, ... of a tile.  Copy r
+// lies kLines lines after copy 0, at the same place of its line.
 template <bool KS, int R, int THREADS>
 struct Bringer {
   using L = Lay<KS, R>;
   static constexpr int kLoads = L::kBytes / 16 / THREADS;
-  uint32_t off[kLoads];  // byte offsets from the tile's corner; kOutside for rows past the end
-  int kk[kLoads];        // first k of the piece (k-contiguous) or the line's k
+  static constexpr int kLines = THREADS / L::kPieces;
+  static_assert(kLines % 16 == 0, "the swizzle repeats after 16 lines");
+  uint32_t off;    // from the tile's corner; kOutside for columns past the end (k-strided)
+  int k;           // first k of the piece (k-contiguous) or the line's k
+  int64_t step;    // bytes of kLines lines
+  uint32_t bytes;  // k-contiguous: of the rows that exist
 
   // `rows`: valid rows from the tile's corner on.
   __device__ __forceinline__ void init(int64_t ld, int rows) {
-#pragma unroll
-    for (int r = 0; r < kLoads; ++r) {
-      const int c = r * THREADS + threadIdx.x;
-      const int line = c / L::kPieces, p = (c % L::kPieces) ^ L::swizzle(line);
-      const bool in = KS ? p * 8 < rows : line < rows;
-      off[r] = in ? (uint32_t)(line * ld) + p * 16 : kOutside;
-      kk[r] = KS ? line : p * 8;
-    }
+    const int line = threadIdx.x / L::kPieces;
+    const int p = (threadIdx.x % L::kPieces) ^ L::swizzle(line);
+    k = KS ? line : p * 8;
+    off = !KS || p * 8 < rows ? (uint32_t)(line * ld) + p * 16 : kOutside;
+    step = kLines * ld;
+    bytes = __builtin_amdgcn_readfirstlane(
+        KS ? kExtent : (uint32_t)min((int64_t)min(rows, R) * ld, (int64_t)kExtent));
   }
-  // Brings k from the tile's step on, `left` of which exist.
-  __device__ __forceinline__ void bring(const char* base, int left, uint32_t lds,
-                                        int r0 = 0, int r1 = kLoads) const {
-    const u32x4 d = descriptor(base);
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
-#pragma unroll
-    for (int r = 0; r < kLoads; ++r) {
-      if (r < r0 || r >= r1) continue;
-      const uint32_t o = left >= kBK || kk[r] < left ? off[r] : kOutside;
-      bring16(d, o, lds + r * THREADS * 16 + wave);
-    }
+  // Copy r of the tile at `corner`, of which `left` k exist, none where it is <= 0.
+  __device__ __forceinline__ void bring(const char* corner, int left, uint32_t lds, int r) const {
+    const uint32_t skip = (uint32_t)(r * step);
+    const uint32_t left_bytes = __builtin_amdgcn_readfirstlane(bytes > skip ? bytes - skip : 0);
+    const u32x4 d = descriptor(corner + r * step, KS ? kExtent : left_bytes);
+    bring16(d, k + (KS ? r * kLines : 0) < left ? off : kOutside, lds + r * THREADS * 16);
   }
 };
 
@@ -173,126 +225,143 @@ struct Bringer {
 template <bool KS, int R>
 struct Reader {
   using L = Lay<KS, R>;
-  uint32_t at[KS ? R / 16 : 2];
+  uint32_t at;  // of fragment 0 of the first half of a tile at 0
   // `row0`: the wave's first row in the tile; fragments lie 16 rows apart.
-  __device__ __forceinline__ void init(int row0, int frags) {
+  __device__ __forceinline__ void init(int row0) {
     const int lane = threadIdx.x & 63, m = lane & 15, q = lane >> 4;
     if constexpr (KS) {
-      const int k = q * 8 + (m >> 2);
-#pragma unroll
-      for (int f = 0; f < R / 16; ++f)
-        if (f < frags) {
-          const int p = (row0 + f * 16) / 8 + ((m & 3) >> 1);
-          at[f] = k * R * 2 + (p ^ L::swizzle(k)) * 16 + (m & 1) * 8;
-        }
+      const int k = q * 8 + (m >> 2), p = row0 / 8 + ((m & 3) >> 1);
+      at = k * R * 2 + (p ^ L::swizzle(k)) * 16 + (m & 1) * 8;
     } else {
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-        at[ks] = (row0 + m) * 128 + ((ks * 4 + q) ^ L::swizzle(m)) * 16;
+      at = (row0 + m) * (kBK * 2) + (q ^ L::swizzle(m)) * 16;
     }
   }
+  // Fragment f of half ks of the tile at `tile`.  The bits that the swizzle mixes are changed
+  // with an exclusive or: pieces 2 f of up to 16 (k-strided), 4 ks of 8.
   __device__ __forceinline__ s16x8 read(uint32_t tile, int f, int ks) const {
     if constexpr (KS) {
-      const uint32_t a = tile + at[f] + ks * 32 * R * 2;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(a + 4 * R * 2));
+      const uint32_t a = (tile + at) ^ (f * 32);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4*)(uintptr_t)(a + ks * 32 * R * 2));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_s16x4*)(uintptr_t)(a + (ks * 32 + 4) * R * 2));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return *(lds_s16x8*)(uintptr_t)(tile + at[ks] + f * 2048);
+      const uint32_t a = (tile + at) ^ (ks * 64);
+      return *(lds_s16x8*)(uintptr_t)(a + f * (16 * kBK * 2));
     }
   }
 };
 
-// Eight consecutive features of a token, at any alignment of the output's rows.
+// Where a lane's piece, eight consecutive features of a token, lies in the arrays of an epilogue:
+// 32-bit offsets from the row that the wave has come to, whose address is uniform.
+struct Piece8 {
+  int col;          // of the first feature
+  uint32_t token;   // rows from the wave's row on
+  uint32_t q, e;    // bytes in a packed array and in its exponents
+};
 
 // An operand of a later product: 16 bits, or three bf16 parts of a 32-bit value.  The columns
 // [I, pad_i) are cleared.
 template <typename T>
-__device__ __forceinline__ void put_operand(const TileArgs& a, void* base, int64_t row, int col,
-                                            const float (&v)[8]) {
-  T* p = (T*)base + row * a.ldo + col;
-  float x[8], rest[8];
+__device__ __forceinline__ void put_operand(const TileArgs& a, void* base, int64_t row,
+                                            const Piece8& l, const float (&v)[8]) {
+  using H = typename Kind<T>::Half;
+  char* p = (char*)base + row * a.ldo * sizeof(H);
+  const uint32_t at = (l.token * (uint32_t)a.ldo + l.col) * sizeof(H);
+  float rest[8];
 #pragma unroll
-  for (int r = 0; r < 8; ++r) rest[r] = col + r < a.I ? v[r] : 0.f;
-  if (a.parts == 1) {
-    store_row<T, 8>(p, a.pad_i - col, rest);
-    return;
-  }
+  for (int r = 0; r < 8; ++r) rest[r] = l.col + r < a.I ? v[r] : 0.f;
+  if constexpr (Kind<T>::kParts == 1) {
+    store_row<H, 8>((H*)(p + at), a.pad_i - l.col, rest);
+  } else {
 #pragma unroll
-  for (int part = 0; part < 3; ++part) {
+    for (int part = 0; part < 3; ++part) {
+      float x[8];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      x[r] = (float)(T)rest[r];
-      rest[r] -= x[r];
-      if (!(fabsf(rest[r]) < INFINITY)) rest[r] = 0.f;  // the remainder of an infinity or a NaN
+      for (int r = 0; r < 8; ++r) {
+        x[r] = (float)(H)rest[r];
+        rest[r] -= x[r];
+        if (!(fabsf(rest[r]) < INFINITY)) rest[r] = 0.f;  // of an infinity or a NaN
+      }
+      store_row<H, 8>((H*)(p + part * a.plane * sizeof(H) + at), a.pad_i - l.col, x);
     }
-    store_row<T, 8>(p + part * a.plane, a.pad_i - col, x);
   }
 }
 
 template <typename T>
 __device__ __forceinline__ void put_output(const TileArgs& a, void* base, int64_t ld, int64_t row,
-                                           int col, const float (&v)[8]) {
-  if (a.parts == 3)
-    store_row<float, 8>((float*)base + row * ld + col, a.I - col, v);
-  else
-    store_row<T, 8>((T*)base + row * ld + col, a.I - col, v);
+                                           const Piece8& l, const float (&v)[8]) {
+  using W = typename Kind<T>::Whole;
+  char* p = (char*)base + row * ld * sizeof(W);
+  store_row<W, 8>((W*)(p + (l.token * (uint32_t)ld + l.col) * sizeof(W)), a.I - l.col, v);
 }
 
 // What the forward pass keeps: packed with a scale for 32 features (four neighbouring lanes), or
 // as it is.  Every lane of the wave comes here.
 template <typename T>
 __device__ __forceinline__ void keep8(const TileArgs& a, void* base, uint8_t* exps, int64_t row,
-                                      int col, const float (&v)[8]) {
-  const bool in = row < a.J && col < up32(a.I);
+                                      const Piece8& l, const float (&v)[8]) {
+  const bool in = row + l.token < a.J && l.col < up32(a.I);
   if (a.keep != 8) {
-    if (in) put_output<T>(a, base, a.I, row, col, v);
+    if (in) put_output<T>(a, base, a.I, row, l, v);
     return;
   }
-  uint32_t top = 0;
-#pragma unroll
-  for (int r = 0; r < 8; ++r)
-    if (col + r < a.I) top = max(top, magnitude(v[r]));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-  const int e = group_exponent(top);
-  const float inv = group_inverse(e);
-  const int groups = groups_of(a.I);
+  const int e = group_exponent4(v), groups = groups_of(a.I);
   if (!in) return;
-  uint32_t w[2] = {0, 0};
-#pragma unroll
-  for (int r = 0; r < 8; ++r)
-    if (col + r < a.I) w[r >> 2] |= (uint32_t)(to_int8(v[r], inv) & 255) << 8 * (r & 3);
-  *(uint2*)((int8_t*)base + row * groups * kGroup + col) = make_uint2(w[0], w[1]);
-  if ((col & 31) == 0) exps[row * groups + col / kGroup] = (uint8_t)e;
+  store_global((char*)base + row * groups * kGroup + l.q, pack8(v, e));
+  if ((l.col & 31) == 0) store_global(exps + row * groups + l.e, (uint8_t)e);
 }
 
-template <typename T>
-__device__ __forceinline__ void kept8(const TileArgs& a, const void* base, const uint8_t* exps,
-                                      int64_t row, int col, float (&v)[8]) {
-  if (a.keep == 8) {
-    const int groups = groups_of(a.I);
-    const uint2 w = *(const uint2*)((const int8_t*)base + row * groups * kGroup + col);
-    const float s = group_scale(exps[row * groups + col / kGroup]);
+// What was kept, loaded now and turned into values later.
+template <typename T, int KEEP>
+struct Kept8 {
+  using W = typename Kind<T>::Whole;
+  Vec<W, 8> raw;
+  __device__ __forceinline__ void load(const TileArgs& a, const void* base, const uint8_t*,
+                                       int64_t row, const Piece8& l) {
+    if (row + l.token >= a.J || l.col >= a.I) return;
+    const W* p = (const W*)((const char*)base + row * a.I * sizeof(W) +
+                            (l.token * (uint32_t)a.I + l.col) * sizeof(W));
+    if (a.I - l.col >= 8) {
+      raw = load_global<Vec<W, 8>>(p);
+    } else {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) v[r] = (float)(int8_t)((r < 4 ? w.x : w.y) >> 8 * (r & 3)) * s;
-  } else if (a.parts == 3) {
-    load_row<float, 8>((const float*)base + row * a.I + col, a.I - col, v);
-  } else {
-    load_row<T, 8>((const T*)base + row * a.I + col, a.I - col, v);
+      for (int r = 0; r < 8; ++r) raw[r] = l.col + r < a.I ? load_global<W>(p + r) : (W)0.f;
+    }
   }
-}
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] = (float)raw[r];
+  }
+};
+template <typename T>
+struct Kept8<T, 8> {
+  u32x2 w;
+  int e;
+  __device__ __forceinline__ void load(const TileArgs& a, const void* base, const uint8_t* exps,
+                                       int64_t row, const Piece8& l) {
+    // no branch: what lies past the end is read from the array's start, and not used
+    const int groups = groups_of(a.I);
+    const bool in = row + l.token < a.J && l.col < a.I;
+    const int64_t first = row < a.J ? row : 0;
+    w = load_global<u32x2>((const char*)base + first * groups * kGroup + (in ? l.q : 0));
+    e = load_global<uint8_t>(exps + first * groups + (in ? l.e : 0));
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const { unpack8(w, e, v); }
+};
 
 // BI x BJ output tile, WI x WJ waves.  EPI_GATE: the tile's A rows are BI / 2 of Wg and the same
 // BI / 2 of Wu, and a wave owns both projections of its features.
-template <typename T, bool AKS, bool BKS, int EPI, int BI, int BJ, int WI, int WJ>
-__global__ __launch_bounds__(WI* WJ * 64, WI* WJ == 8 ? 2 : 2) void k_ffn_tile(TileArgs a) {
+// KEEP: what was kept (EPI_BACK), 0 or 8.
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ>
+__global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 2) void k_ffn_tile(TileArgs a) {
   constexpr int kThreads = WI * WJ * 64;
   constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;  // fragments of a wave
   constexpr int kTileA = Lay<AKS, BI>::kBytes, kTileB = Lay<BKS, BJ>::kBytes;
-  constexpr int kStage = kTileA + kTileB;
+  constexpr int kUnit = kTileA > kTileB ? kTileA : kTileB;
   constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;  // features a tile
-  __shared__ __align__(256) char lds[2 * kStage];
+  __shared__ __align__(256) char lds[kUnits * kUnit];
 
   // tiles in an order that gives each of the 8 XCDs (blocks are dealt to them in turn) a run of
   // neighbouring tiles, in columns of 8 token tiles: they share operands in its L2
@@ -322,8 +391,8 @@ __global__ __launch_bounds__(WI* WJ * 64, WI* WJ == 8 ? 2 : 2) void k_ffn_tile(T
   bring_b.init(a.ldb, a.J - j0);
   Reader<AKS, BI> read_a;
   Reader<BKS, BJ> read_b;
-  read_a.init(EPI == EPI_GATE ? wi * (BI / 2 / WI) : wi * (BI / WI), FI);
-  read_b.init(wj * (BJ / WJ), FJ);
+  read_a.init(EPI == EPI_GATE ? wi * (BI / 2 / WI) : wi * (BI / WI));
+  read_b.init(wj * (BJ / WJ));
 
   f32x4 acc[FI][FJ];
 #pragma unroll
@@ -337,105 +406,219 @@ __global__ __launch_bounds__(WI* WJ * 64, WI* WJ == 8 ? 2 : 2) void k_ffn_tile(T
   const int64_t corner_b = BKS ? (int64_t)j0 * 2 : (int64_t)j0 * a.ldb;
   const int64_t next_a = AKS ? kBK * a.lda : kBK * 2, next_b = BKS ? kBK * a.ldb : kBK * 2;
 
-  int seg = 0, ks = 0;  // of the step that is brought next
-  auto bring = [&](int stage) {
-    const uint32_t to = base + stage * kStage;
-    const int k0 = ks * kBK;
-    bring_a.bring(a.A[seg] + corner_a + ks * next_a, a.KA - k0, to);
-    if constexpr (EPI == EPI_GATE)
-      bring_a.bring(a.A2[seg] + corner_a + ks * next_a, a.KA - k0, to + kTileA / 2);
-    bring_b.bring(a.B[batch][seg] + corner_b + ks * next_b, a.KB - k0, to + kTileA);
-    if (++ks == per_seg) ks = 0, ++seg;
+  // The operands' tiles A0 B0 A1 B1 ... take the units in turn; each has its next place in memory.
+  struct Next {
+    int seg, left;  // k that exist from the tile on; none are left after the last segment
+    const char *p, *p2;
+    uint32_t to;
   };
-
-  if (steps > 0) bring(0);
-  for (int step = 0; step < steps; ++step) {
-    wait_all();  // this step's tile is there, and nobody reads the other stage any more
-    if (step + 1 < steps) bring((step + 1) & 1);
-    const uint32_t ta = base + (step & 1) * kStage, tb = ta + kTileA;
-#pragma unroll
-    for (int kk = 0; kk < kBK / 32; ++kk) {
-      s16x8 fa[FI], fb[FJ];
-#pragma unroll
-      for (int j = 0; j < FJ; ++j) fb[j] = read_b.read(tb, j, kk);
-#pragma unroll
-      for (int i = 0; i < FI; ++i) {
-        if constexpr (EPI == EPI_GATE)
-          fa[i] = read_a.read(ta + (i >= FI / 2 ? kTileA / 2 : 0), i % (FI / 2), kk);
-        else
-          fa[i] = read_a.read(ta, i, kk);
-      }
-#pragma unroll
-      for (int i = 0; i < FI; ++i)
-#pragma unroll
-        for (int j = 0; j < FJ; ++j)
-          acc[i][j] = Mfma<T>::mac(__builtin_bit_cast(typename Mfma<T>::x8, fa[i]),
-                                   __builtin_bit_cast(typename Mfma<T>::x8, fb[j]), acc[i][j]);
+  const uint32_t first = base + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+  const uint32_t end = first + kUnits * kUnit;
+  Next na{0, a.nseg ? a.KA : 0, a.A[0] + corner_a, nullptr, first};
+  Next nb{0, a.nseg ? a.KB : 0, a.B[batch][0] + corner_b, nullptr, first + kUnit};
+  if constexpr (EPI == EPI_GATE) na.p2 = a.A2[0] + corner_a;
+  constexpr int kCopiesA = (EPI == EPI_GATE ? 2 : 1) * decltype(bring_a)::kLoads;
+  constexpr int kCopiesB = decltype(bring_b)::kLoads;
+  auto bring_a_part = [&](int r) {
+    constexpr int kHalf = decltype(bring_a)::kLoads;
+    if (EPI == EPI_GATE && r >= kHalf)
+      bring_a.bring(na.p2, na.left, na.to + kTileA / 2, r - kHalf);
+    else
+      bring_a.bring(na.p, na.left, na.to, r);
+  };
+  auto bring_b_part = [&](int r) { bring_b.bring(nb.p, nb.left, nb.to, r); };
+  auto unit_on = [&](uint32_t& u) {
+    u += 2 * kUnit;
+    if (u >= end) u -= kUnits * kUnit;
+  };
+  auto next_a_tile = [&]() {
+    unit_on(na.to);
+    na.p += next_a;
+    if constexpr (EPI == EPI_GATE) na.p2 += next_a;
+    na.left -= kBK;
+    if (na.left <= 0 && na.seg + 1 < a.nseg) {
+      ++na.seg;
+      na.left = a.KA;
+      na.p = a.A[na.seg] + corner_a;
+      if constexpr (EPI == EPI_GATE) na.p2 = a.A2[na.seg] + corner_a;
     }
-  }
-
+  };
+  auto next_b_tile = [&]() {
+    unit_on(nb.to);
+    nb.p += next_b;
+    nb.left -= kBK;
+    if (nb.left <= 0 && nb.seg + 1 < a.nseg) {
+      ++nb.seg;
+      nb.left = a.KB;
+      nb.p = a.B[batch][nb.seg] + corner_b;
+    }
+  };
+  struct Frags {
+    s16x8 a[FI], b[FJ];
+  };
+  uint32_t from_a = base, from_b = base + kUnit;  // of the tile that is read
+  auto unit_read = [&](uint32_t& u) {
+    u += 2 * kUnit;
+    if (u >= base + kUnits * kUnit) u -= kUnits * kUnit;
+  };
+  // 32 k: multiplies `now`, reads `next` and issues copies, all three spread over the rows of
+  // fragments: a copy that finds the address unit busy holds back what its wave issues next.
+  auto half = [&](const Frags& now, Frags& next, int ks, auto copies, auto&& copy) {
+    constexpr int kCopies = decltype(copies)::value;
+#pragma unroll
+    for (int i = 0; i < FI; ++i) {
+      if (i < FJ) next.b[i] = read_b.read(from_b, i, ks);
+      if constexpr (EPI == EPI_GATE)
+        next.a[i] = read_a.read(from_a + (i >= FI / 2 ? kTileA / 2 : 0), i % (FI / 2), ks);
+      else
+        next.a[i] = read_a.read(from_a, i, ks);
+#pragma unroll
+      for (int r = i * kCopies / FI; r < (i + 1) * kCopies / FI; ++r) copy(r);
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) Mfma<typename Kind<T>::Half>::add(now.a[i], now.b[j], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
   // A lane holds four consecutive features (4 (lane / 16) + 0..3 of 16) of token lane % 16.  The
-  // wave turns 16 tokens at a time in LDS of its own, so that a lane gets 8 consecutive features
-  // and neighbouring lanes the features beside them.
+  // wave turns kDump times 16 tokens at a time in LDS of its own, so that a lane gets 8
+  // consecutive features and neighbouring lanes the features beside them.
   constexpr int kWide = BI / WI;                  // accumulated rows of the wave
   constexpr int kPieces = kFeat / WI / 8;         // pieces of 8 features a token
   constexpr int kRow = kWide + 4;                 // floats; 4 more keep the banks apart
-  static_assert(WI * WJ * 16 * kRow * 4 <= 2 * kStage, "the turned tokens fit the stages");
-  wait_all();  // nobody reads the last tile any more
-  float* turn = (float*)lds + wave * 16 * kRow;
+  constexpr int kFit = kUnits * kUnit / (WI * WJ * 16 * kRow * 4);
+  constexpr int kDump = kFit >= FJ ? FJ : kFit >= FJ / 2 ? FJ / 2 : 1;
+  static_assert(kFit >= 1 && FJ % kDump == 0, "the turned tokens fit the units");
+  float* turn = (float*)lds + wave * kDump * 16 * kRow;
   const int lane = threadIdx.x & 63, q = lane >> 4;
   const int iw = i0 + wi * (kFeat / WI), jw = j0 + wj * (BJ / WJ);
+  constexpr int kTimes = kPieces * 16 / 64;  // pieces a lane of 16 tokens
+  const int f = (lane % kPieces) * 8;
+  Piece8 at;
+  at.col = iw + f;
+  at.token = lane / kPieces;
+  at.q = at.token * groups_of(a.I) * kGroup + at.col;
+  at.e = at.token * groups_of(a.I) + at.col / kGroup;
+  constexpr int kTokens = 64 / kPieces;  // the tokens of the wave's next pieces lie so far on
+  Kept8<T, KEEP> kg[kTimes], ku[kTimes];
+  auto load_kept = [&](int j) {
 #pragma unroll
-  for (int j = 0; j < FJ; ++j) {
+    for (int c = 0; c < kTimes; ++c) {
+      kg[c].load(a, a.g, a.ge, jw + j * 16 + c * kTokens, at);
+      ku[c].load(a, a.u, a.ue, jw + j * 16 + c * kTokens, at);
+    }
+  };
+
+  // Step n: tile n is there (its B was issued in step n - 1's first half, so A of n + 1 may still
+  // be on its way), every wave has read tile n - 1, whose units take B of n + 1 and A of n + 2.
+  // The second half of tile n - 1 is multiplied while the first of tile n is read.
+  {
+    Frags f0, f1;
+#pragma unroll
+    for (int i = 0; i < FI; ++i) f1.a[i] = s16x8{};
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) f1.b[j] = s16x8{};
+#pragma unroll
+    for (int r = 0; r < kCopiesA; ++r) bring_a_part(r);
+    next_a_tile();
+#pragma unroll
+    for (int r = 0; r < kCopiesB; ++r) bring_b_part(r);
+    next_b_tile();
+#pragma unroll
+    for (int r = 0; r < kCopiesA; ++r) bring_a_part(r);
+    next_a_tile();
+#pragma unroll 1
+    for (int n = 0; n < steps; ++n) {
+      wait_copies<kCopiesA>();
+      half(f1, f0, 0, std::integral_constant<int, kCopiesB>{}, bring_b_part);
+      next_b_tile();
+      half(f0, f1, 1, std::integral_constant<int, kCopiesA>{}, bring_a_part);
+      next_a_tile();
+      unit_read(from_a);
+      unit_read(from_b);
+    }
+    if constexpr (EPI == EPI_BACK) load_kept(0);
 #pragma unroll
     for (int i = 0; i < FI; ++i)
-      *(f32x4*)(turn + (lane & 15) * kRow + i * 16 + q * 4) = acc[i][j];
+#pragma unroll
+      for (int j = 0; j < FJ; ++j) Mfma<typename Kind<T>::Half>::add(f1.a[i], f1.b[j], acc[i][j]);
+  }
+  wait_all();  // nobody reads the last tile any more
+#pragma unroll
+  for (int j0 = 0; j0 < FJ; j0 += kDump) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the tokens before these are read
+#pragma unroll
+    for (int d = 0; d < kDump; ++d)
+#pragma unroll
+      for (int i = 0; i < FI; ++i)
+        *(f32x4*)(turn + (d * 16 + (lane & 15)) * kRow + i * 16 + q * 4) = acc[i][j0 + d];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the other lanes' values are there
 #pragma unroll 1
-    for (int c = lane; c < 16 * kPieces; c += 64) {
-      const int token = c / kPieces, f = (c % kPieces) * 8;
-      const int64_t row = jw + j * 16 + token;
-      const int col = iw + f;
-      float x[8];
-      read8(turn + token * kRow + f, x);
-      if constexpr (EPI == EPI_STORE) {
-        if (row < a.J) put_output<T>(a, a.out[batch], a.ldo, row, col, x);
-      } else if constexpr (EPI == EPI_GATE) {
-        float u[8];
-        read8(turn + token * kRow + kPieces * 8 + f, u);
-        if (a.keep >= 0) {
-          keep8<T>(a, a.g, a.ge, row, col, x);
-          keep8<T>(a, a.u, a.ue, row, col, u);
-        }
-        if (row >= a.J || col >= a.pad_i) continue;
+    for (int j = j0; j < j0 + kDump; ++j) {
+      const float* turned = turn + j % kDump * 16 * kRow;
+      Kept8<T, KEEP> g0[kTimes], u0[kTimes];
+      if constexpr (EPI == EPI_BACK) {  // the next tokens' are on their way meanwhile
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          float act, slope;
-          gate_fn(a.gate, x[r], act, slope);
-          u[r] *= act;
-        }
-        put_operand<T>(a, a.out[0], row, col, u);
-      } else {
-        if (row >= a.J || col >= a.pad_i) continue;
-        float g[8] = {}, u[8] = {}, v[8], du[8];
-        if (col < a.I) {
-          kept8<T>(a, a.g, a.ge, row, col, g);
-          kept8<T>(a, a.u, a.ue, row, col, u);
-        }
+        for (int c = 0; c < kTimes; ++c) g0[c] = kg[c], u0[c] = ku[c];
+        if (j + 1 < FJ) load_kept(j + 1);
+      }
+      auto piece = [&](int c, const Kept8<T, KEEP>& kept_g, const Kept8<T, KEEP>& kept_u) {
+        const int t = at.token + c * kTokens;
+        const int64_t row = jw + j * 16 + c * kTokens;
+        const bool in = row + at.token < a.J;
+        float x[8];
+        read8(turned + t * kRow + f, x);
+        if constexpr (EPI == EPI_STORE) {
+          if (in) put_output<T>(a, a.out[batch], a.ldo, row, at, x);
+        } else if constexpr (EPI == EPI_GATE) {
+          float u[8];
+          read8(turned + t * kRow + kPieces * 8 + f, u);
+          if (a.keep >= 0) {
+            keep8<T>(a, a.g, a.ge, row, at, x);
+            keep8<T>(a, a.u, a.ue, row, at, u);
+          }
+          if (!in || at.col >= a.pad_i) return;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          float act, slope;
-          gate_fn(a.gate, g[r], act, slope);
-          v[r] = act * u[r];
-          du[r] = x[r] * act;
-          x[r] *= u[r] * slope;
+          for (int r = 0; r < 8; ++r) {
+            float act, slope;
+            gate_fn(a.gate, Kind<T>::kParts == 1, x[r], act, slope);
+            u[r] *= act;
+          }
+          put_operand<T>(a, a.out[0], row, at, u);
+        } else {
+          if (!in || at.col >= a.pad_i) return;
+          float g[8], u[8], v[8];
+          kept_g.values(g);
+          kept_u.values(u);
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            float act, slope;
+            gate_fn(a.gate, Kind<T>::kParts == 1, g[r], act, slope);
+            v[r] = act * u[r];
+            g[r] = x[r] * act;
+            x[r] *= u[r] * slope;
+          }
+          if (a.out[0]) put_operand<T>(a, a.out[0], row, at, v);
+          if (a.dg) put_operand<T>(a, a.dg, row, at, x);
+          if (a.du) put_operand<T>(a, a.du, row, at, g);
         }
-        if (a.out[0]) put_operand<T>(a, a.out[0], row, col, v);
-        if (a.dg) put_operand<T>(a, a.dg, row, col, x);
-        if (a.du) put_operand<T>(a, a.du, row, col, du);
+      };
+      if constexpr (Kind<T>::kParts == 1) {
+#pragma unroll
+        for (int c = 0; c < kTimes; ++c) {
+          piece(c, g0[c], u0[c]);
+          __builtin_amdgcn_sched_barrier(0);  // two at once need more registers than there are
+        }
+      } else {  // three parts an output: too much code to be unrolled
+#pragma unroll 1
+        for (int c = 0; c < kTimes; ++c) {
+          Kept8<T, KEEP> kept_g, kept_u;
+#pragma unroll
+          for (int cc = 0; cc < kTimes; ++cc)
+            if (cc == c) kept_g = g0[cc], kept_u = u0[cc];
+          piece(c, kept_g, kept_u);
+        }
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read before the next tokens arrive
   }
 }
 

@@ -11,39 +11,49 @@ using bf16 = __bf16;
 using f16 = _Float16;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 // N elements of a row at any element alignment: one wide load or store (the hardware takes
-// unaligned global accesses), where a typed vector access would promise an alignment that a
-// tensor of odd width does not have.
+// unaligned global accesses), where a plain vector type would promise an alignment that a tensor
+// of odd width does not have.
 template <typename T, int N>
-struct __attribute__((packed, aligned(sizeof(T)))) Vec {
-  T v[N];
-};
+using Vec = T __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+
+// Global memory: a pointer that comes out of an array in a kernel's arguments is otherwise taken
+// for one that may point anywhere, and its accesses for LDS traffic too.
+template <typename V>
+__device__ __forceinline__ V load_global(const void* p) {
+  return *(const __attribute__((address_space(1))) V*)p;
+}
+template <typename V>
+__device__ __forceinline__ void store_global(void* p, V v) {
+  *(__attribute__((address_space(1))) V*)p = v;
+}
 
 template <typename T, int N>
 __device__ __forceinline__ void load_row(const T* p, int valid, float (&out)[N]) {
   if (valid >= N) {
-    Vec<T, N> t = *reinterpret_cast<const Vec<T, N>*>(p);
+    const Vec<T, N> t = load_global<Vec<T, N>>(p);
 #pragma unroll
-    for (int i = 0; i < N; ++i) out[i] = (float)t.v[i];
+    for (int i = 0; i < N; ++i) out[i] = (float)t[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) out[i] = i < valid ? (float)p[i] : 0.f;
+    for (int i = 0; i < N; ++i) out[i] = i < valid ? (float)load_global<T>(p + i) : 0.f;
   }
 }
 
 template <typename T, int N>
 __device__ __forceinline__ void store_row(T* p, int valid, const float (&x)[N]) {
-  if (valid >= N) {
-    Vec<T, N> t;
+  Vec<T, N> t;
 #pragma unroll
-    for (int i = 0; i < N; ++i) t.v[i] = (T)x[i];
-    *reinterpret_cast<Vec<T, N>*>(p) = t;
+  for (int i = 0; i < N; ++i) t[i] = (T)x[i];
+  if (valid >= N) {
+    store_global(p, t);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (i < valid) p[i] = (T)x[i];
+      if (i < valid) store_global<T>(p + i, t[i]);
   }
 }
 
@@ -76,12 +86,53 @@ __device__ __forceinline__ float group_scale(int biased) {
                             : __uint_as_float((uint32_t)biased << 23);
 }
 
-// x * 2^-e to the nearest whole number in [-127, 127]; any number for a NaN (the exponent marks
-// its group).
-__device__ __forceinline__ int to_int8(float x, float inverse) {
-  return (int)__builtin_amdgcn_fmed3f(rintf(x * inverse), -127.f, 127.f);
+// The largest magnitude of eight values; a NaN among them is the result.
+__device__ __forceinline__ float largest8(const float (&x)[8]) {
+  float m = fabsf(x[0]);
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = __builtin_elementwise_maximum(m, fabsf(x[i]));
+  return m;
 }
 
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// Biased exponent of the group that four neighbouring lanes hold, eight values each.
+__device__ __forceinline__ int group_exponent4(const float (&x)[8]) {
+  // the sign is off, so the bits order as the values do, and a NaN comes last
+  uint32_t top = __float_as_uint(largest8(x)) & 0x7fffffffu;
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  return group_exponent(top);
+}
+
+// Eight values as multiples of 2^e, rounded to the nearest (ties to even) by the addition of
+// 1.5 * 2^23: the sum's low byte is the multiple in two's complement.  Only under the largest
+// exponent a multiple can pass 127.  In a group without values any byte comes out.
+__device__ __forceinline__ u32x2 pack8(const float (&x)[8], int biased) {
+  constexpr float kWhole = 12582912.f;
+  const float inv = group_inverse(biased);
+  uint32_t b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(x[i], inv, kWhole));
+  if (biased == kMostExp + 127) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      b[i] = (uint32_t)(int)__builtin_amdgcn_fmed3f(rintf(x[i] * inv), -127.f, 127.f);
+  }
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    // bytes 0 of two words side by side, then of both pairs
+    const uint32_t lo = __builtin_amdgcn_perm(b[4 * h + 1], b[4 * h], 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(b[4 * h + 3], b[4 * h + 2], 0x0c0c0400u);
+    w[h] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+  }
+  return u32x2{w[0], w[1]};
+}
+
+// Eight multiples as values.
+__device__ __forceinline__ void unpack8(u32x2 w, int biased, float (&x)[8]) {
+  const float s = group_scale(biased);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = (float)(int8_t)(w[i >> 2] >> 8 * (i & 3)) * s;
+}
 
 }  // namespace lm

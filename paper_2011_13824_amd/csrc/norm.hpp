@@ -55,21 +55,12 @@ __device__ __forceinline__ void norm_piece(const NormFwd<T>& a, int64_t row, int
   if (with_sum && col < a.n) store_row<T, 8>(a.sum + row * a.lds + col, a.n - col, h);
   if (a.y && col < a.n) store_row<T, 8>(a.y + row * a.ldy + col, a.n - col, y);
   if (a.q) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, magnitude(y[i]));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    const int e = group_exponent(top);
-    const float inv = group_inverse(e);
+    const int e = group_exponent4(y);
     const int groups = groups_of(a.n);
     if (col < groups * kGroup) {
-      uint32_t p[2] = {0, 0};
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        p[i >> 2] |= (uint32_t)(to_int8(y[i], inv) & 255) << (8 * (i & 3));
-      *reinterpret_cast<uint2*>(a.q + row * groups * kGroup + col) = make_uint2(p[0], p[1]);
-      if ((threadIdx.x & 3) == 0) a.exps[row * groups + col / kGroup] = (uint8_t)e;
+      store_global(a.q + row * groups * kGroup + col, pack8(y, e));
+      if ((threadIdx.x & 3) == 0)
+        store_global(a.exps + row * groups + col / kGroup, (uint8_t)e);
     }
   }
 }

@@ -32,22 +32,10 @@ __global__ __launch_bounds__(256) void k_q8_pack(const T* __restrict__ x, int64_
   if (p.row >= rows) return;  // whole groups of lanes leave together
   float v[8];
   load_row<T, 8>(x + p.row * ldx + p.col, n - p.col, v);
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, magnitude(v[i]));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-  const int e = group_exponent(top);
-  const float inv = group_inverse(e);
-  uint32_t w[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    w[h] = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[h] |= (uint32_t)(to_int8(v[h * 4 + i], inv) & 255) << (8 * i);
-  }
-  *reinterpret_cast<uint2*>(q + p.row * groups * kGroup + p.col) = make_uint2(w[0], w[1]);
-  if ((threadIdx.x & 3) == 0) exps[p.row * groups + p.col / kGroup] = (uint8_t)e;
+  const int e = group_exponent4(v);
+  store_global(q + p.row * groups * kGroup + p.col, pack8(v, e));
+  if ((threadIdx.x & 3) == 0)
+    store_global(exps + p.row * groups + p.col / kGroup, (uint8_t)e);
 }
 
 // Reads back; columns from n to `cols` (the padded width of an operand) come out as 0.
@@ -59,14 +47,12 @@ __global__ __launch_bounds__(256) void k_q8_unpack(const int8_t* __restrict__ q,
   const int groups = groups_of(n);
   Piece p = piece_of((int64_t)blockIdx.x * 256, groups * 4);
   if (p.row >= rows || p.col >= cols) return;
-  const uint2 w = *reinterpret_cast<const uint2*>(q + p.row * groups * kGroup + p.col);
-  const float s = group_scale(exps[p.row * groups + p.col / kGroup]);
+  const u32x2 w = load_global<u32x2>(q + p.row * groups * kGroup + p.col);
   float v[8];
+  unpack8(w, load_global<uint8_t>(exps + p.row * groups + p.col / kGroup), v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = (float)(int8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3))) * s;
+  for (int i = 0; i < 8; ++i)
     if (p.col + i >= n) v[i] = 0.f;
-  }
   store_row<T, 8>(x + p.row * ldx + p.col, cols - p.col, v);
 }
 

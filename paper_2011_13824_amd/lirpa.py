@@ -154,7 +154,7 @@ class LirpaError(RuntimeError):
 
 
 def _check(rc):
-    if rc != LIRPA_OK:
+    if rc:
         raise LirpaError(rc, load().lirpa_last_error().decode())
 
 
@@ -172,8 +172,8 @@ def _dev(t, dtype=None, what="tensor"):
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:  # the raw handle: a torch.cuda.Stream object costs more than a small call
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -329,15 +329,15 @@ def _matrix(t, rows, n, dtype, what):
         raise TypeError(f"{what} must be a CUDA tensor")
     if t.dtype != dtype:
         raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != n:
+    if t.shape != (rows, n):
         raise ValueError(f"{what} must be [{rows}, {n}], got {list(t.shape)}")
-    ld = t.stride(0)
-    if n > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and n > 1:
         raise ValueError(f"{what} must have contiguous rows")
-    if rows <= 1:
-        ld = max(ld, n)
-    elif ld < n:
-        raise ValueError(f"rows of {what} overlap")
+    if ld < n:
+        if rows > 1:
+            raise ValueError(f"rows of {what} overlap")
+        ld = n
     return t.data_ptr(), ld
 
 
