@@ -287,7 +287,7 @@ void add_segs(const FfnPlan& pl, TileArgs& t, int batch, const Operand& A, const
 template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ>
 int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
   constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;
-  const int64_t ti = up(t.I, kFeat) / kFeat, tj = up(t.J, BJ) / BJ, total = ti * tj * t.batches;
+  const int64_t ti = up(t.I, kFeat) / kFeat, tj = up(t.J, BJ) / BJ, total = ti * tj * t.batches * t.splits;
   if (total == 0) return LIRPA_OK;
   if (total > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "%s: more than 2^31 tiles", name);
   t.tiles_i = (int)ti;
@@ -298,25 +298,86 @@ int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
   });
 }
 
-// The larger tile reads each operand half as often, once there are enough of them to fill the
-// chip; the epilogue of da in 32 bits does not fit its registers.
+// How a product is cut: tiles of 256 x 256 (one block a CU) or 128 x 128 (two), and the number of
+// blocks that share a tile's k, whose sums are then added by k_ffn_join.
+struct Cut {
+  bool large = false;
+  int splits = 1;
+};
+
+// The cut of least estimated time.  A round of blocks over the 256 CUs takes, for k in thousands:
+//   256 x 256: 10 + 23.5 k us; 128 x 128, two a CU: 5 + 15 k us, one a CU: 4 + 9.5 k us
+// (measured at k = 64 to 4096, in bf16; what a round computes is 1, 1/2 and 1/4), and joining moves
+// the sums twice at 4 TB/s and costs a launch.  So few tiles over a long k are split, and tiles
+// that leave a round nearly empty are made smaller.
+Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, bool gate, bool may_split,
+           bool may_large) {
+  auto tiles = [&](int64_t size) {
+    const int64_t feat = gate ? size / 2 : size;
+    return (up(I, feat) / feat) * (up(J, size) / size) * batches;
+  };
+  Cut best;
+  double least = 1e300;
+  for (int large = 0; large <= (may_large ? 1 : 0); ++large)
+    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      if (splits > 1 && (!may_split || steps < 4 * splits)) break;
+      const int64_t n = tiles(large ? 256 : 128) * splits, per = large ? 256 : 512;
+      const double k = (double)((steps + splits - 1) / splits) * kBK / 1024.0;
+      const int64_t whole = n / per, rest = n % per;
+      double t;
+      if (large)
+        t = (double)(whole + (rest > 0)) * (10 + 23.5 * k);
+      else
+        t = (double)(whole + (rest > 256)) * (5 + 15 * k) +
+            (rest > 0 && rest <= 256 ? 4 + 9.5 * k : 0);
+      if (splits > 1) t += 5 + (double)I * J * batches * 4 * splits * 2 / 4e6;
+      if (t < least) {
+        least = t;
+        best.large = large;
+        best.splits = splits;
+      }
+    }
+  return best;
+}
+
+int64_t part_ld(int64_t I) { return up(I, 8); }
+size_t part_bytes(const Cut& c, int64_t I, int64_t J, int batches) {
+  return c.splits > 1 ? (size_t)c.splits * batches * J * part_ld(I) * sizeof(float) : 0;
+}
+int64_t steps_of(int64_t k, int nseg) { return up(k, kBK) / kBK * nseg; }
+
 template <typename T, bool AKS, bool BKS, int EPI, int KEEP>
-int tile_of_size(const char* name, TileArgs& t, hipStream_t st) {
-  const int64_t feat = EPI == EPI_GATE ? 128 : 256;
-  const int64_t large = (up(t.I, feat) / feat) * (up(t.J, 256) / 256) * t.batches;
-  if constexpr (!(Kind<T>::kParts == 3 && EPI == EPI_BACK))
-    if (large >= 192) return launch_tile<T, AKS, BKS, EPI, KEEP, 256, 256, 2, 4>(name, t, st);
-  return launch_tile<T, AKS, BKS, EPI, KEEP, 128, 128, 2, 2>(name, t, st);
+int tile_of_size(const char* name, TileArgs& t, void* part, hipStream_t st) {
+  // the epilogue of da in 32 bits does not fit the registers of the larger tile
+  constexpr bool kLarge = !(Kind<T>::kParts == 3 && EPI == EPI_BACK);
+  using W = typename Kind<T>::Whole;
+  const Cut c = cut_of(t.I, t.J, t.batches, steps_of(std::max(t.KA, t.KB), t.nseg),
+                       EPI == EPI_GATE, EPI == EPI_STORE, kLarge);
+  t.splits = c.splits;
+  t.part = (float*)part;
+  t.part_ld = part_ld(t.I);
+  if (c.large) {
+    if constexpr (kLarge)
+      TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 256, 256, 2, 4>(name, t, st)));
+  } else {
+    TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 128, 128, 2, 2>(name, t, st)));
+  }
+  if (EPI != EPI_STORE || c.splits == 1) return LIRPA_OK;
+  const int64_t blocks = ((int64_t)t.batches * t.J * ((t.I + 7) / 8) + 255) / 256;
+  return launch_k("ffn_join", st, [&] {
+    k_ffn_join<W><<<(unsigned)blocks, 256, 0, st>>>(t.part, t.part_ld, t.splits, t.batches, t.J,
+                                                    t.I, (W*)t.out[0], (W*)t.out[1], t.ldo);
+  });
 }
 
 template <bool AKS, bool BKS, int EPI>
-int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, hipStream_t st) {
+int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, void* part, hipStream_t st) {
   auto typed = [&](auto keep) {
     constexpr int K = decltype(keep)::value;
     switch (pl.f->dtype) {
-      case LIRPA_F32: return tile_of_size<Split, AKS, BKS, EPI, K>(name, t, st);
-      case LIRPA_BF16: return tile_of_size<bf16, AKS, BKS, EPI, K>(name, t, st);
-      default: return tile_of_size<f16, AKS, BKS, EPI, K>(name, t, st);
+      case LIRPA_F32: return tile_of_size<Split, AKS, BKS, EPI, K>(name, t, part, st);
+      case LIRPA_BF16: return tile_of_size<bf16, AKS, BKS, EPI, K>(name, t, part, st);
+      default: return tile_of_size<f16, AKS, BKS, EPI, K>(name, t, part, st);
     }
   };
   if constexpr (EPI == EPI_BACK)
@@ -371,8 +432,14 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   });
 }
 
+// Room for the sums of a product that is split.
+size_t part_room(const FfnPlan& pl, int64_t I, int64_t J, int batches, int64_t k, int nseg) {
+  return part_bytes(cut_of(I, J, batches, steps_of(k, nseg), false, true, true), I, J, batches);
+}
+
 struct ForwardRoom {
   Operand x, wg, wu, wd, a;
+  void* part;
   size_t bytes;
 };
 ForwardRoom forward_room(FfnPlan& pl) {
@@ -383,6 +450,7 @@ ForwardRoom forward_room(FfnPlan& pl) {
   if (!pl.in_place(f->Wu, f->ldu, pl.D)) r.wu = pl.own(pl.F, pl.D);
   if (!pl.in_place(f->Wd, f->ldd, pl.F)) r.wd = pl.own(pl.D, pl.F);
   r.a = pl.own(pl.rows, pl.F);
+  r.part = pl.ws.take(part_room(pl, pl.D, pl.rows, 1, pl.Fp, pl.f32 ? 6 : 1));
   r.bytes = pl.ws.at;
   return r;
 }
@@ -415,17 +483,18 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   t.u = u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, st)));
+  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, r.part, st)));
 
   t = tile_args(pl, pl.D, rows, pl.Fp, pl.Fp);
   add_segs(pl, t, 0, r.wd, r.a);
   t.out[0] = out;
   t.ldo = ldo;
-  return run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, st);
+  return run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, r.part, st);
 }
 
 struct BackwardRoom {
   Operand dout, x, wg, wu, wd, a, dg, du;
+  void* part;
   size_t bytes;
 };
 BackwardRoom backward_room(FfnPlan& pl) {
@@ -439,6 +508,13 @@ BackwardRoom backward_room(FfnPlan& pl) {
   r.a = pl.own(pl.rows, pl.F);
   r.dg = pl.own(pl.rows, pl.F);
   r.du = pl.own(pl.rows, pl.F);
+  const int n = pl.f32 ? 6 : 1;
+  size_t part = part_room(pl, pl.D, pl.rows, 1, pl.Fp, 2 * n);
+  for (int batches : {1, 2})      // dWg and dWu, or one of them,
+    for (int seg : {n, pl.f32 ? 3 : 1})  // from x in 32 or in 8 bits
+      part = std::max(part, part_room(pl, pl.D, pl.F, batches, pl.rows, seg));
+  part = std::max(part, part_room(pl, pl.F, pl.D, 1, pl.rows, n));
+  r.part = pl.ws.take(part);
   r.bytes = pl.ws.at;
   return r;
 }
@@ -470,7 +546,7 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
   t.u = (void*)u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, st)));
+  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, r.part, st)));
 
   if (dx) {
     t = tile_args(pl, pl.D, rows, pl.F, pl.Fp);
@@ -481,7 +557,7 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
     t.lda = ldg;
     t.out[0] = dx;
     t.ldo = lddx;
-    TRY((run_tile<true, false, EPI_STORE>(pl, "ffn_dx", t, st)));
+    TRY((run_tile<true, false, EPI_STORE>(pl, "ffn_dx", t, r.part, st)));
   }
   if (wx) {
     if (keep == LIRPA_KEEP_8) {
@@ -520,14 +596,14 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
       t.out[t.batches++] = out[b];
     }
     t.ldo = pl.D;
-    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_in", t, st)));
+    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_in", t, r.part, st)));
   }
   if (dWd) {
     t = tile_args(pl, pl.F, pl.D, rows, rows);
     add_segs(pl, t, 0, r.a, r.dout);
     t.out[0] = dWd;
     t.ldo = pl.F;
-    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_down", t, st)));
+    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_down", t, r.part, st)));
   }
   return LIRPA_OK;
 }

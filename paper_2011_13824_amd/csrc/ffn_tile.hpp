@@ -41,6 +41,9 @@ struct TileArgs {
   int KA, KB;                   // k extents (equal up to the zero padding of a packed operand)
   int I, J;                     // output sizes
   int tiles_i, tiles_j, batches;
+  int splits;                   // EPI_STORE: blocks that share a tile's k; over 1, their sums go to
+  float* part;                  // part[split][batch][J][part_ld] and are added by k_ffn_join
+  int64_t part_ld;
   void* out[2];
   int64_t ldo;                  // elements
   int pad_i;                    // columns [I, pad_i) of operand outputs are written as 0
@@ -372,6 +375,11 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     id = x * per + min(x, more) + (blockIdx.x >> 3);
   }
   const int per_batch = a.tiles_i * a.tiles_j;
+  int split = 0;
+  if constexpr (EPI == EPI_STORE) {
+    split = id / (per_batch * a.batches);
+    id -= split * (per_batch * a.batches);
+  }
   const int batch = id / per_batch;
   id -= batch * per_batch;
   constexpr int kBand = 8;
@@ -401,7 +409,15 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const int K = max(a.KA, a.KB);
-  const int per_seg = (K + kBK - 1) / kBK, steps = per_seg * a.nseg;
+  const int per_seg = (K + kBK - 1) / kBK;
+  int steps = per_seg * a.nseg, first_seg = 0, first_k = 0;
+  if constexpr (EPI == EPI_STORE) {
+    if (a.splits > 1) {
+      const int each = (steps + a.splits - 1) / a.splits, from = min(split * each, steps);
+      steps = min(each, steps - from);
+      if (steps > 0) first_seg = from / per_seg, first_k = from % per_seg;
+    }
+  }
   const int64_t corner_a = AKS ? (int64_t)i0 * 2 : (int64_t)i0 * a.lda;
   const int64_t corner_b = BKS ? (int64_t)j0 * 2 : (int64_t)j0 * a.ldb;
   const int64_t next_a = AKS ? kBK * a.lda : kBK * 2, next_b = BKS ? kBK * a.ldb : kBK * 2;
@@ -414,8 +430,10 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
   };
   const uint32_t first = base + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
   const uint32_t end = first + kUnits * kUnit;
-  Next na{0, a.nseg ? a.KA : 0, a.A[0] + corner_a, nullptr, first};
-  Next nb{0, a.nseg ? a.KB : 0, a.B[batch][0] + corner_b, nullptr, first + kUnit};
+  Next na{first_seg, a.KA - first_k * kBK, a.A[first_seg] + corner_a + first_k * next_a, nullptr,
+          first};
+  Next nb{first_seg, a.KB - first_k * kBK, a.B[batch][first_seg] + corner_b + first_k * next_b,
+          nullptr, first + kUnit};
   if constexpr (EPI == EPI_GATE) na.p2 = a.A2[0] + corner_a;
   constexpr int kCopiesA = (EPI == EPI_GATE ? 2 : 1) * decltype(bring_a)::kLoads;
   constexpr int kCopiesB = decltype(bring_b)::kLoads;
@@ -568,7 +586,13 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
         float x[8];
         read8(turned + t * kRow + f, x);
         if constexpr (EPI == EPI_STORE) {
-          if (in) put_output<T>(a, a.out[batch], a.ldo, row, at, x);
+          if (!in) return;
+          if (a.splits > 1) {
+            float* p = a.part + ((int64_t)(split * a.batches + batch) * a.J + row) * a.part_ld;
+            store_row<float, 8>(p + (at.token * (uint32_t)a.part_ld + at.col), a.I - at.col, x);
+          } else {
+            put_output<T>(a, a.out[batch], a.ldo, row, at, x);
+          }
         } else if constexpr (EPI == EPI_GATE) {
           float u[8];
           read8(turned + t * kRow + kPieces * 8 + f, u);
@@ -620,6 +644,29 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
       }
     }
   }
+}
+
+// Adds the sums of the blocks that shared a tile's k, in order.  Bound by bytes.
+template <typename W>
+__global__ __launch_bounds__(256) void k_ffn_join(const float* __restrict__ part, int64_t part_ld,
+                                                  int splits, int batches, int64_t J, int I,
+                                                  W* out0, W* out1, int64_t ldo) {
+  const int per_row = (I + 7) / 8;
+  const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;
+  const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x;
+  const uint32_t down = at / (uint32_t)per_row;
+  const int64_t row = row0 + down;  // of all batches' rows
+  const int col = (int)(at - down * (uint32_t)per_row) * 8;
+  if (row >= J * batches) return;
+  float sum[8] = {};
+  for (int s = 0; s < splits; ++s) {
+    float x[8];
+    load_row<float, 8>(part + ((int64_t)s * batches * J + row) * part_ld + col, 8, x);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sum[r] += x[r];
+  }
+  W* out = row < J ? out0 + row * ldo : out1 + (row - J) * ldo;
+  store_row<W, 8>(out + col, I - col, sum);
 }
 
 // Copies [rows][n] into [rows][ld] 16-bit operands, columns from n to ld cleared; a 32-bit source
