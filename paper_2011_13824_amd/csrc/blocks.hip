@@ -174,7 +174,7 @@ int norm_bwd(NormBwd<T> a, T* dw, float* part, hipStream_t st) {
     }));
   if (dw)
     TRY(launch_k("norm_dw", st, [&] {
-      k_norm_dw<T><<<(a.n + 63) / 64, 1024, 0, st>>>(part, (int)blocks, a.n, dw);
+      k_norm_dw<T><<<(a.n + 31) / 32, 256, 0, st>>>(part, (int)blocks, a.n, dw);
     }));
   return LIRPA_OK;
 }
@@ -237,33 +237,36 @@ struct FfnPlan {
   }
 };
 
-template <typename S, typename T, int PARTS>
-int copy_operand(const S* x, int64_t ldx, int64_t rows, int64_t n, const Operand& o,
-                 hipStream_t st) {
-  const int64_t blocks = (rows * (o.ld / 8) + 255) / 256;
-  return launch_k("ffn_operand", st, [&] {
-    k_operand<S, T, PARTS><<<(unsigned)blocks, 256, 0, st>>>(x, ldx, rows, (int)n, (T*)o.p,
-                                                            (int)o.ld, o.plane);
-  });
-}
+// The user's matrices as operands: in place where the tile kernel can read them, else copies in
+// their rooms, all made by one launch.
+struct Copies {
+  OperandJobs jobs{};
+  int64_t blocks = 0;
 
-// The user's matrix as an operand: in place where the tile kernel can read it, else a copy in
-// `room`.
-int as_operand(const FfnPlan& pl, const void* x, int64_t ldx, int64_t rows, int64_t n,
-               Operand& o, hipStream_t st) {
-  if (pl.in_place(x, ldx, n)) {
-    o.p = (const char*)x;
-    o.ld = ldx;
-    o.plane = 0;
-    return LIRPA_OK;
+  void add(const FfnPlan& pl, const void* x, int64_t ldx, int64_t rows, int64_t n, Operand& o) {
+    if (pl.in_place(x, ldx, n)) {
+      o.p = (const char*)x;
+      o.ld = ldx;
+      o.plane = 0;
+      return;
+    }
+    if (rows == 0) return;
+    jobs.job[jobs.count++] = {x, ldx, rows, o.plane, (void*)o.p, (int)n, (int)o.ld,
+                              (unsigned)blocks};
+    blocks += (rows * (o.ld / 8) + 255) / 256;
   }
-  if (rows == 0) return LIRPA_OK;
-  switch (pl.f->dtype) {
-    case LIRPA_F32: return copy_operand<float, bf16, 3>((const float*)x, ldx, rows, n, o, st);
-    case LIRPA_BF16: return copy_operand<bf16, bf16, 1>((const bf16*)x, ldx, rows, n, o, st);
-    default: return copy_operand<f16, f16, 1>((const f16*)x, ldx, rows, n, o, st);
+  int run(const FfnPlan& pl, hipStream_t st) const {
+    if (blocks == 0) return LIRPA_OK;
+    if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "ffn_operands: more than 2^42 values");
+    return launch_k("ffn_operands", st, [&] {
+      switch (pl.f->dtype) {
+        case LIRPA_F32: k_ffn_operands<Split><<<(unsigned)blocks, 256, 0, st>>>(jobs); break;
+        case LIRPA_BF16: k_ffn_operands<bf16><<<(unsigned)blocks, 256, 0, st>>>(jobs); break;
+        default: k_ffn_operands<f16><<<(unsigned)blocks, 256, 0, st>>>(jobs);
+      }
+    });
   }
-}
+};
 
 // Parts (A, B) of the six products of 32-bit operands, smallest first.
 constexpr int kSixA[6] = {1, 0, 2, 0, 1, 0};
@@ -466,10 +469,12 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
       return few_forward<T, 4>(f, rows, x, ldx, out, ldo, ws, st);
     });
   ForwardRoom r = forward_room(pl);
-  TRY(as_operand(pl, x, ldx, rows, pl.D, r.x, st));
-  TRY(as_operand(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg, st));
-  TRY(as_operand(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu, st));
-  TRY(as_operand(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd, st));
+  Copies copies;
+  copies.add(pl, x, ldx, rows, pl.D, r.x);
+  copies.add(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg);
+  copies.add(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu);
+  copies.add(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd);
+  TRY(copies.run(pl, st));
 
   TileArgs t = tile_args(pl, pl.F, rows, pl.Dp, pl.Dp);
   add_segs(pl, t, 0, r.wg, r.x, &r.wu);
@@ -524,13 +529,16 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
                  void* dWg, void* dWu, void* dWd, void* ws, hipStream_t st) {
   FfnPlan pl(f, rows, ws);
   BackwardRoom r = backward_room(pl);
-  TRY(as_operand(pl, dout, lddo, rows, pl.D, r.dout, st));
-  if (dx) {
-    TRY(as_operand(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg, st));
-    TRY(as_operand(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu, st));
-  }
-  TRY(as_operand(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd, st));
   const bool wx = dWg || dWu;
+  Copies copies;
+  copies.add(pl, dout, lddo, rows, pl.D, r.dout);
+  if (dx) {
+    copies.add(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg);
+    copies.add(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu);
+  }
+  copies.add(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd);
+  if (wx && keep == LIRPA_KEEP_FULL) copies.add(pl, x, ldx, rows, pl.D, r.x);
+  TRY(copies.run(pl, st));
 
   // act(g) u, dg and du
   TileArgs t = tile_args(pl, pl.F, rows, pl.D, pl.Dp);
@@ -560,20 +568,11 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
     TRY((run_tile<true, false, EPI_STORE>(pl, "ffn_dx", t, r.part, st)));
   }
   if (wx) {
-    if (keep == LIRPA_KEEP_8) {
-      if (pl.f32) {
-        // 7 bits and a sign: the first part of three holds it, the other two are 0
-        if (rows) {
-          TRY(q8_unpack<bf16>(rows, (int)pl.D, (int)r.x.ld, x, (bf16*)r.x.p, r.x.ld, st));
-        }
-      } else if (rows) {
-        if (f->dtype == LIRPA_BF16)
-          TRY(q8_unpack<bf16>(rows, (int)pl.D, (int)r.x.ld, x, (bf16*)r.x.p, r.x.ld, st));
-        else
-          TRY(q8_unpack<f16>(rows, (int)pl.D, (int)r.x.ld, x, (f16*)r.x.p, r.x.ld, st));
-      }
-    } else {
-      TRY(as_operand(pl, x, ldx, rows, pl.D, r.x, st));
+    if (keep == LIRPA_KEEP_8 && rows) {  // f32: in the first of three parts, which holds 8 bits
+      if (f->dtype == LIRPA_F16)
+        TRY(q8_unpack<f16>(rows, (int)pl.D, (int)r.x.ld, x, (f16*)r.x.p, r.x.ld, st));
+      else
+        TRY(q8_unpack<bf16>(rows, (int)pl.D, (int)r.x.ld, x, (bf16*)r.x.p, r.x.ld, st));
     }
     t = tile_args(pl, pl.D, pl.F, rows, rows);
     const bool one_part = pl.f32 && keep == LIRPA_KEEP_8;

@@ -670,30 +670,46 @@ __global__ __launch_bounds__(256) void k_ffn_join(const float* __restrict__ part
 }
 
 // Copies [rows][n] into [rows][ld] 16-bit operands, columns from n to ld cleared; a 32-bit source
-// becomes three bf16 parts.  Bound by bytes.
-template <typename S, typename T, int PARTS>
-__global__ __launch_bounds__(256) void k_operand(const S* __restrict__ x, int64_t ldx,
-                                                 int64_t rows, int n, T* __restrict__ out, int ld,
-                                                 int64_t plane) {
-  const int per_row = (ld + 7) / 8;
-  const int64_t first = (int64_t)blockIdx.x * 256;
-  const int64_t row0 = first / per_row;
+// becomes three bf16 parts.  All operands of a call in one launch: they are often small, and a
+// launch then costs more than the copy.  Bound by bytes.
+struct OperandJob {
+  const void* x;
+  int64_t ldx, rows, plane;
+  void* out;
+  int n, ld;
+  unsigned first;  // block
+};
+constexpr int kMaxJobs = 5;
+struct OperandJobs {
+  OperandJob job[kMaxJobs];
+  int count;
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_ffn_operands(OperandJobs jobs) {
+  using H = typename Kind<T>::Half;
+  using W = typename Kind<T>::Whole;
+  int j = 0;
+  while (j + 1 < jobs.count && blockIdx.x >= jobs.job[j + 1].first) ++j;
+  const OperandJob& o = jobs.job[j];
+  const int per_row = o.ld / 8;
+  const int64_t first = (int64_t)(blockIdx.x - o.first) * 256, row0 = first / per_row;
   const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x;
   const uint32_t down = at / (uint32_t)per_row;
   const int64_t row = row0 + down;
   const int col = (int)(at - down * (uint32_t)per_row) * 8;
-  if (row >= rows) return;
+  if (row >= o.rows) return;
   float v[8], p[8];
-  load_row<S, 8>(x + row * ldx + col, n - col, v);
+  load_row<W, 8>((const W*)o.x + row * o.ldx + col, o.n - col, v);
 #pragma unroll
-  for (int part = 0; part < PARTS; ++part) {
+  for (int part = 0; part < Kind<T>::kParts; ++part) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = (float)(T)v[i];
+      p[i] = (float)(H)v[i];
       v[i] -= p[i];
       if (!(fabsf(v[i]) < INFINITY)) v[i] = 0.f;
     }
-    store_row<T, 8>(out + part * plane + row * ld + col, ld - col, p);
+    store_row<H, 8>((H*)o.out + part * o.plane + row * o.ld + col, 8, p);
   }
 }
 

@@ -246,24 +246,40 @@ __global__ __launch_bounds__(256) void k_norm_dw_wide(NormBwd<T> a) {
   store_row<float, 8>(a.part + (int64_t)blockIdx.y * a.n + col, a.n - col, dw);
 }
 
-// dw = sum of the blocks' partial sums: a block takes 64 columns, its 16 waves every sixteenth
-// partial row, joined in order.
+// dw = sum of the blocks' partial sums: a block takes 32 columns, each of its 32 groups of 8 threads
+// every 32nd partial row, eight of them on their way at a time; the groups' sums are joined in
+// order.  Bound by the latency of a few loads.
 template <typename T>
-__global__ __launch_bounds__(1024) void k_norm_dw(const float* __restrict__ part, int blocks,
-                                                  int n, T* __restrict__ dw) {
-  __shared__ float all[16][64];
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
-  float s = 0.f;
-  if (col < n)
-    for (int b = wave; b < blocks; b += 16) s += part[(int64_t)b * n + col];
-  all[wave][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (wave == 0 && col < n) {
-    s = 0.f;
+__global__ __launch_bounds__(256) void k_norm_dw(const float* __restrict__ part, int blocks,
+                                                 int n, T* __restrict__ dw) {
+  __shared__ float all[32][33];
+  const int c = threadIdx.x & 7, g = threadIdx.x >> 3, col = blockIdx.x * 32 + c * 4;
+  float s[4] = {};
+  int b = g;
+  for (; b + 7 * 32 < blocks; b += 8 * 32) {
+    float x[8][4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += all[i][threadIdx.x];
-    dw[col] = (T)s;
+    for (int i = 0; i < 8; ++i)
+      load_row<float, 4>(part + (int64_t)(b + i * 32) * n + col, n - col, x[i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k] += x[i][k];
   }
+  for (; b < blocks; b += 32) {
+    float x[4];
+    load_row<float, 4>(part + (int64_t)b * n + col, n - col, x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] += x[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) all[g][c * 4 + k] = s[k];
+  __syncthreads();
+  if (threadIdx.x >= 32 || blockIdx.x * 32 + threadIdx.x >= n) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) sum += all[i][threadIdx.x];
+  dw[blockIdx.x * 32 + threadIdx.x] = (T)sum;
 }
 
 }  // namespace lm
