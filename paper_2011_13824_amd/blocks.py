@@ -19,14 +19,16 @@ import torch
 from . import lirpa
 
 
+def _bytes(n, device):
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
 class Q8:
     """A matrix [rows, n] in 8 bits with a power-of-two scale per 32 columns of a row."""
 
     def __init__(self, rows, n, buf=None, device="cuda"):
         self.rows, self.n = rows, n
-        if buf is None:
-            buf = torch.empty(lirpa.lirpa_q8_bytes(rows, n), dtype=torch.uint8, device=device)
-        self.buf = buf
+        self.buf = _bytes(rows * -(-n // 32) * 33, device) if buf is None else buf
 
     @staticmethod
     def pack(x):
@@ -69,7 +71,7 @@ class Norm:
         if want_dw:
             dw = torch.empty_like(self.w)
             need = lirpa.lirpa_norm_workspace_bytes(rows, n)
-            ws = torch.empty(need, dtype=torch.uint8, device=dy.device)
+            ws = _bytes(need, dy.device)
         lirpa.lirpa_norm_backward(dy, dsum, h, self.w, rstd, dh, dw, ws, need)
         return dh, dw
 
@@ -93,10 +95,16 @@ class FeedForward:
     def __init__(self, Wg, Wu, Wd, gate="silu"):
         self.weights = (Wg, Wu, Wd)
         self.block = lirpa.lirpa_ffn_block(Wg, Wu, Wd, gate)
+        self._need = {}  # workspace bytes by (rows, backward): they follow from the sizes
 
     def _workspace(self, rows, backward):
-        need = lirpa.lirpa_ffn_workspace_bytes(self.block, rows, backward)
-        return torch.empty(need, dtype=torch.uint8, device=self.weights[0].device), need
+        need = self._need.get((rows, backward))
+        if need is None:
+            need = lirpa.lirpa_ffn_workspace_bytes(self.block, rows, backward)
+            if len(self._need) > 1024:
+                self._need.clear()
+            self._need[rows, backward] = need
+        return _bytes(need, self.weights[0].device), need
 
     def forward(self, x, keep=None, x8=None):
         """out; with ``keep`` (8 or 0) (out, Kept).  ``x8``: x in 8 bits where the caller has it
@@ -118,10 +126,10 @@ class FeedForward:
 
     def backward(self, dout, kept, want=("dx", "dWg", "dWu", "dWd")):
         """{name: gradient} of the wanted ones."""
-        model, hidden = self.block.n_model, self.block.n_hidden
-        shapes = {"dx": (dout.shape[0], model), "dWg": (hidden, model), "dWu": (hidden, model),
-                  "dWd": (model, hidden)}
-        grads = {k: torch.empty(shapes[k], dtype=dout.dtype, device=dout.device) for k in want}
+        like = {"dx": dout, "dWg": self.weights[0], "dWu": self.weights[1],
+                "dWd": self.weights[2]}
+        grads = {k: torch.empty(like[k].shape, dtype=dout.dtype, device=dout.device)
+                 for k in want}
         ws, need = self._workspace(dout.shape[0], 1)
         x, g, u = kept.raw()
         lirpa.lirpa_ffn_backward(self.block, dout, kept.keep, x, g, u, *(

@@ -287,7 +287,8 @@ void add_segs(const FfnPlan& pl, TileArgs& t, int batch, const Operand& A, const
   t.ldb = B.ld * 2;
 }
 
-template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ>
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ,
+          int AHEAD = 1>
 int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
   constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;
   const int64_t ti = up(t.I, kFeat) / kFeat, tj = up(t.J, BJ) / BJ, total = ti * tj * t.batches * t.splits;
@@ -296,15 +297,15 @@ int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
   t.tiles_i = (int)ti;
   t.tiles_j = (int)tj;
   return launch_k(name, st, [&] {
-    k_ffn_tile<T, AKS, BKS, EPI, KEEP, BI, BJ, WI, WJ>
+    k_ffn_tile<T, AKS, BKS, EPI, KEEP, BI, BJ, WI, WJ, AHEAD>
         <<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);
   });
 }
 
-// How a product is cut: tiles of 256 x 256 (one block a CU) or 128 x 128 (two), and the number of
-// blocks that share a tile's k, whose sums are then added by k_ffn_join.
+// How a product is cut: tiles of 256 x 256 (one block a CU), 128 x 128 or 64 x 64 (two), and the
+// number of blocks that share a tile's k, whose sums are then added by k_ffn_join.
 struct Cut {
-  bool large = false;
+  int size = 128;
   int splits = 1;
 };
 
@@ -313,8 +314,18 @@ struct Cut {
 // (measured at k = 64 to 4096, in bf16; what a round computes is 1, 1/2 and 1/4), and joining moves
 // the sums twice at 4 TB/s and costs a launch.  So few tiles over a long k are split, and tiles
 // that leave a round nearly empty are made smaller.
+//
+// Up to 64 tokens (`few`: both operands k-contiguous) it is the weights' bytes that count: tiles of
+// 64, three more on their way, in about 512 blocks.  4096 x 10944 in bf16: gate and up 34 us
+// against 39-43 with tiles of 128, down 17 us in 8 parts, 22 in 4, 19 in 16.
 Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, bool gate, bool may_split,
-           bool may_large) {
+           bool may_large, bool few) {
+  if (few && J <= 64) {
+    const int64_t n = up(I, gate ? 32 : 64) / (gate ? 32 : 64);
+    int splits = 1;
+    while (may_split && splits < 16 && n * splits * 2 <= 640 && steps >= 16 * splits) splits *= 2;
+    return {64, splits};
+  }
   auto tiles = [&](int64_t size) {
     const int64_t feat = gate ? size / 2 : size;
     return (up(I, feat) / feat) * (up(J, size) / size) * batches;
@@ -336,7 +347,7 @@ Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, bool gate, bool may
       if (splits > 1) t += 5 + (double)I * J * batches * 4 * splits * 2 / 4e6;
       if (t < least) {
         least = t;
-        best.large = large;
+        best.size = large ? 256 : 128;
         best.splits = splits;
       }
     }
@@ -355,11 +366,14 @@ int tile_of_size(const char* name, TileArgs& t, void* part, hipStream_t st) {
   constexpr bool kLarge = !(Kind<T>::kParts == 3 && EPI == EPI_BACK);
   using W = typename Kind<T>::Whole;
   const Cut c = cut_of(t.I, t.J, t.batches, steps_of(std::max(t.KA, t.KB), t.nseg),
-                       EPI == EPI_GATE, EPI == EPI_STORE, kLarge);
+                       EPI == EPI_GATE, EPI == EPI_STORE, kLarge, !AKS && !BKS);
   t.splits = c.splits;
   t.part = (float*)part;
   t.part_ld = part_ld(t.I);
-  if (c.large) {
+  if (c.size == 64) {
+    if constexpr (!AKS && !BKS)
+      TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 64, 64, 1, 4, 3>(name, t, st)));
+  } else if (c.size == 256) {
     if constexpr (kLarge)
       TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 256, 256, 2, 4>(name, t, st)));
   } else {
@@ -400,7 +414,11 @@ TileArgs tile_args(const FfnPlan& pl, int64_t I, int64_t J, int64_t KA, int64_t 
   return t;
 }
 
-constexpr int kFewRows = 64;
+// Up to kFewest tokens k_ffn_few is the faster one (us in bf16, against the tile kernel: 4096 x
+// 10944, 1 token 59 and 66, 4 tokens 65 and 70, 8 the same; 1024 x 2752, 8 tokens 16 and 20).
+// Weights that the tile kernel cannot read in place it reads up to kFewRows, rather than that they
+// are copied.
+constexpr int kFewest = 8, kFewRows = 64;
 
 template <typename T, int TJ>
 int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, void* out,
@@ -418,9 +436,11 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   a.gate = f->gate;
   a.out = hidden;
   a.ldo = f->n_hidden;
-  constexpr int UN = TJ == 1 ? 4 : 2;
+  // waves a block and steps in flight, in us for 1 token of 4096 x 10944 in bf16: gate 16 waves
+  // 36.5, 8 39.5; both 16: 57.1, both 8: 62.6; with 64 tokens 4 and 16: 129, both 8: 166
+  constexpr int UN = TJ == 1 ? 4 : 2, kGate = TJ == 1 ? 16 : TJ == 2 ? 8 : 4;
   TRY(launch_k("ffn_few_gate", st, [&] {
-    k_ffn_few<T, true, TJ, 8, UN><<<(a.I + 15) / 16, 8 * 64, 0, st>>>(a);
+    k_ffn_few<T, true, TJ, kGate, UN><<<(a.I + 15) / 16, kGate * 64, 0, st>>>(a);
   }));
   a.A = f->Wd;
   a.lda = f->ldd;
@@ -431,13 +451,14 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   a.out = out;
   a.ldo = ldo;
   return launch_k("ffn_few_down", st, [&] {
-    k_ffn_few<T, false, TJ, 8, UN><<<(a.I + 15) / 16, 8 * 64, 0, st>>>(a);
+    k_ffn_few<T, false, TJ, 16, UN><<<(a.I + 15) / 16, 16 * 64, 0, st>>>(a);
   });
 }
 
 // Room for the sums of a product that is split.
-size_t part_room(const FfnPlan& pl, int64_t I, int64_t J, int batches, int64_t k, int nseg) {
-  return part_bytes(cut_of(I, J, batches, steps_of(k, nseg), false, true, true), I, J, batches);
+size_t part_room(int64_t I, int64_t J, int batches, int64_t k, int nseg, bool few) {
+  return part_bytes(cut_of(I, J, batches, steps_of(k, nseg), false, true, true, few), I, J,
+                    batches);
 }
 
 struct ForwardRoom {
@@ -453,7 +474,7 @@ ForwardRoom forward_room(FfnPlan& pl) {
   if (!pl.in_place(f->Wu, f->ldu, pl.D)) r.wu = pl.own(pl.F, pl.D);
   if (!pl.in_place(f->Wd, f->ldd, pl.F)) r.wd = pl.own(pl.D, pl.F);
   r.a = pl.own(pl.rows, pl.F);
-  r.part = pl.ws.take(part_room(pl, pl.D, pl.rows, 1, pl.Fp, pl.f32 ? 6 : 1));
+  r.part = pl.ws.take(part_room(pl.D, pl.rows, 1, pl.Fp, pl.f32 ? 6 : 1, true));
   r.bytes = pl.ws.at;
   return r;
 }
@@ -461,7 +482,9 @@ ForwardRoom forward_room(FfnPlan& pl) {
 int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, void* out,
                 int64_t ldo, int keep, void* g, void* u, void* ws, hipStream_t st) {
   FfnPlan pl(f, rows, ws);
-  if (keep == LIRPA_KEEP_NONE && rows <= kFewRows)
+  const bool in_place = pl.in_place(f->Wg, f->ldg, pl.D) && pl.in_place(f->Wu, f->ldu, pl.D) &&
+                        pl.in_place(f->Wd, f->ldd, pl.F);
+  if (keep == LIRPA_KEEP_NONE && rows <= (in_place ? kFewest : kFewRows))
     return by_type(f->dtype, [&](auto t) {
       using T = decltype(t);
       if (rows <= 16) return few_forward<T, 1>(f, rows, x, ldx, out, ldo, ws, st);
@@ -514,11 +537,11 @@ BackwardRoom backward_room(FfnPlan& pl) {
   r.dg = pl.own(pl.rows, pl.F);
   r.du = pl.own(pl.rows, pl.F);
   const int n = pl.f32 ? 6 : 1;
-  size_t part = part_room(pl, pl.D, pl.rows, 1, pl.Fp, 2 * n);
+  size_t part = part_room(pl.D, pl.rows, 1, pl.Fp, 2 * n, false);
   for (int batches : {1, 2})      // dWg and dWu, or one of them,
     for (int seg : {n, pl.f32 ? 3 : 1})  // from x in 32 or in 8 bits
-      part = std::max(part, part_room(pl, pl.D, pl.F, batches, pl.rows, seg));
-  part = std::max(part, part_room(pl, pl.F, pl.D, 1, pl.rows, n));
+      part = std::max(part, part_room(pl.D, pl.F, batches, pl.rows, seg, false));
+  part = std::max(part, part_room(pl.F, pl.D, 1, pl.rows, n, false));
   r.part = pl.ws.take(part);
   r.bytes = pl.ws.at;
   return r;

@@ -74,12 +74,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(FewArgs a) {
     for (int t = 0; t < TJ; ++t) acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const int full = a.K / 32;  // whole steps; wave w takes w, w + WAVES, ...
-  int s = wave;
-  for (; s + (UN - 1) * WAVES < full; s += UN * WAVES) {
+  for (int s = wave; s < full; s += UN * WAVES) {
     Eight<T> fw[UN][kMats], fx[UN][TJ];
 #pragma unroll
     for (int n = 0; n < UN; ++n) {
-      const int k = (s + n * WAVES) * 32;
+      const int k = min(s + n * WAVES, full - 1) * 32;  // past the end: loaded, not multiplied
 #pragma unroll
       for (int c = 0; c < kMats; ++c) fw[n][c].load(w[c] + k);
 #pragma unroll
@@ -87,13 +86,15 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(FewArgs a) {
     }
 #pragma unroll
     for (int n = 0; n < UN; ++n)
+      if (s + n * WAVES < full) {
 #pragma unroll
-      for (int c = 0; c < kMats; ++c)
+        for (int c = 0; c < kMats; ++c)
 #pragma unroll
-        for (int t = 0; t < TJ; ++t) acc[c][t] = Eight<T>::mac(fw[n][c], fx[n][t], acc[c][t]);
+          for (int t = 0; t < TJ; ++t) acc[c][t] = Eight<T>::mac(fw[n][c], fx[n][t], acc[c][t]);
+      }
   }
-  for (; s * 32 < a.K; s += WAVES) {
-    const int k = s * 32, valid = a.K - k - q * 8;
+  if (full * 32 < a.K && wave == full % WAVES) {  // the last, partial step
+    const int k = full * 32, valid = a.K - k - q * 8;
     Eight<T> fw[kMats], fx[TJ];
 #pragma unroll
     for (int c = 0; c < kMats; ++c) fw[c].load(w[c] + k, valid);

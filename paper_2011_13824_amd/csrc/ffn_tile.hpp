@@ -29,7 +29,6 @@ enum Gate { RELU = 0, SILU = 1, GELU = 2 };
 
 constexpr int kMaxSegs = 12;
 constexpr int kBK = 64;    // k a tile: 128 bytes of a k-contiguous row, the width of a cache line
-constexpr int kUnits = 5;  // tiles of one operand in LDS
 
 struct TileArgs {
   const char* A[kMaxSegs];
@@ -357,12 +356,13 @@ struct Kept8<T, 8> {
 // BI x BJ output tile, WI x WJ waves.  EPI_GATE: the tile's A rows are BI / 2 of Wg and the same
 // BI / 2 of Wu, and a wave owns both projections of its features.
 // KEEP: what was kept (EPI_BACK), 0 or 8.
-template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ>
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ, int AHEAD>
 __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 2) void k_ffn_tile(TileArgs a) {
   constexpr int kThreads = WI * WJ * 64;
   constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;  // fragments of a wave
   constexpr int kTileA = Lay<AKS, BI>::kBytes, kTileB = Lay<BKS, BJ>::kBytes;
   constexpr int kUnit = kTileA > kTileB ? kTileA : kTileB;
+  constexpr int kUnits = 2 * AHEAD + 3;  // tiles of one operand in LDS
   constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;  // features a tile
   __shared__ __align__(256) char lds[kUnits * kUnit];
 
@@ -526,9 +526,10 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     }
   };
 
-  // Step n: tile n is there (its B was issued in step n - 1's first half, so A of n + 1 may still
-  // be on its way), every wave has read tile n - 1, whose units take B of n + 1 and A of n + 2.
-  // The second half of tile n - 1 is multiplied while the first of tile n is read.
+  // Step n: tile n is there; after its B, which was issued in step n - AHEAD, came AHEAD more of A
+  // and AHEAD - 1 of B, which may still be on their way.  Every wave has read tile n - 1, whose
+  // units take B of n + AHEAD and A of n + AHEAD + 1.  The second half of tile n - 1 is multiplied
+  // while the first of tile n is read.
   {
     Frags f0, f1;
 #pragma unroll
@@ -536,17 +537,18 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
 #pragma unroll
     for (int j = 0; j < FJ; ++j) f1.b[j] = s16x8{};
 #pragma unroll
-    for (int r = 0; r < kCopiesA; ++r) bring_a_part(r);
-    next_a_tile();
+    for (int ahead = 0; ahead <= AHEAD; ++ahead) {
 #pragma unroll
-    for (int r = 0; r < kCopiesB; ++r) bring_b_part(r);
-    next_b_tile();
+      for (int r = 0; r < kCopiesA; ++r) bring_a_part(r);
+      next_a_tile();
+      if (ahead == AHEAD) break;
 #pragma unroll
-    for (int r = 0; r < kCopiesA; ++r) bring_a_part(r);
-    next_a_tile();
+      for (int r = 0; r < kCopiesB; ++r) bring_b_part(r);
+      next_b_tile();
+    }
 #pragma unroll 1
     for (int n = 0; n < steps; ++n) {
-      wait_copies<kCopiesA>();
+      wait_copies<(AHEAD - 1) * (kCopiesA + kCopiesB) + kCopiesA>();
       half(f1, f0, 0, std::integral_constant<int, kCopiesB>{}, bring_b_part);
       next_b_tile();
       half(f0, f1, 1, std::integral_constant<int, kCopiesA>{}, bring_a_part);
