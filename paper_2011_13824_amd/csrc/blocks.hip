@@ -309,48 +309,56 @@ struct Cut {
   int splits = 1;
 };
 
-// The cut of least estimated time.  A round of blocks over the 256 CUs takes, for k in thousands:
-//   256 x 256: 10 + 23.5 k us; 128 x 128, two a CU: 5 + 15 k us, one a CU: 4 + 9.5 k us
-// (measured at k = 64 to 4096, in bf16; what a round computes is 1, 1/2 and 1/4), and joining moves
-// the sums twice at 4 TB/s and costs a launch.  So few tiles over a long k are split, and tiles
-// that leave a round nearly empty are made smaller.
+// What a round of blocks over the 256 CUs takes: fixed + slope * k us for k in thousands, when it is
+// full and when it is at most half full, and what the other epilogues add.  Measured at k = 64 to
+// 4096 in bf16; a full round computes 1, 2 and 4 tiles of 128 x 128 a CU.
+struct Round {
+  int size, full;  // tile, blocks
+  double fixed, slope, half_fixed, half_slope, gate, back;
+};
+constexpr Round kRounds[3] = {{64, 1024, 6.0, 11.8, 4.5, 7.4, 1, 4},
+                              {128, 512, 8.0, 14.3, 6.0, 8.7, 4.5, 12},
+                              {256, 256, 10.0, 23.5, 10.0, 23.5, 8.6, 30}};
+
+// The cut of least estimated time.  Joining moves the sums twice at 4 TB/s and costs a launch.  So
+// few tiles over a long k are split, and tiles that would leave a round nearly empty, or most of
+// its time to epilogues, are made smaller.
 //
 // Up to 64 tokens (`few`: both operands k-contiguous) it is the weights' bytes that count: tiles of
 // 64, three more on their way, in about 512 blocks.  4096 x 10944 in bf16: gate and up 34 us
 // against 39-43 with tiles of 128, down 17 us in 8 parts, 22 in 4, 19 in 16.
-Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, bool gate, bool may_split,
-           bool may_large, bool few) {
+Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, int epi, bool may_large, bool few) {
+  const bool gate = epi == EPI_GATE, may_split = epi == EPI_STORE;
   if (few && J <= 64) {
     const int64_t n = up(I, gate ? 32 : 64) / (gate ? 32 : 64);
     int splits = 1;
     while (may_split && splits < 16 && n * splits * 2 <= 640 && steps >= 16 * splits) splits *= 2;
     return {64, splits};
   }
-  auto tiles = [&](int64_t size) {
-    const int64_t feat = gate ? size / 2 : size;
-    return (up(I, feat) / feat) * (up(J, size) / size) * batches;
-  };
   Cut best;
   double least = 1e300;
-  for (int large = 0; large <= (may_large ? 1 : 0); ++large)
+  for (const Round& r : kRounds) {
+    if (r.size == 256 && !may_large) continue;
+    const int64_t feat = gate ? r.size / 2 : r.size;
+    const int64_t tiles = (up(I, feat) / feat) * (up(J, r.size) / r.size) * batches;
+    const double more = gate ? r.gate : epi == EPI_BACK ? r.back : 0;
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (splits > 1 && (!may_split || steps < 4 * splits)) break;
-      const int64_t n = tiles(large ? 256 : 128) * splits, per = large ? 256 : 512;
       const double k = (double)((steps + splits - 1) / splits) * kBK / 1024.0;
-      const int64_t whole = n / per, rest = n % per;
-      double t;
-      if (large)
-        t = (double)(whole + (rest > 0)) * (10 + 23.5 * k);
-      else
-        t = (double)(whole + (rest > 256)) * (5 + 15 * k) +
-            (rest > 0 && rest <= 256 ? 4 + 9.5 * k : 0);
+      const int64_t whole = tiles * splits / r.full, rest = tiles * splits % r.full;
+      double t = (double)whole * (r.fixed + more + r.slope * k);
+      if (rest > r.full / 2)
+        t += r.fixed + more + r.slope * k;
+      else if (rest > 0)
+        t += r.half_fixed + more + r.half_slope * k;
       if (splits > 1) t += 5 + (double)I * J * batches * 4 * splits * 2 / 4e6;
       if (t < least) {
         least = t;
-        best.size = large ? 256 : 128;
+        best.size = r.size;
         best.splits = splits;
       }
     }
+  }
   return best;
 }
 
@@ -366,13 +374,14 @@ int tile_of_size(const char* name, TileArgs& t, void* part, hipStream_t st) {
   constexpr bool kLarge = !(Kind<T>::kParts == 3 && EPI == EPI_BACK);
   using W = typename Kind<T>::Whole;
   const Cut c = cut_of(t.I, t.J, t.batches, steps_of(std::max(t.KA, t.KB), t.nseg),
-                       EPI == EPI_GATE, EPI == EPI_STORE, kLarge, !AKS && !BKS);
+                       EPI, kLarge, !AKS && !BKS);
   t.splits = c.splits;
   t.part = (float*)part;
   t.part_ld = part_ld(t.I);
   if (c.size == 64) {
-    if constexpr (!AKS && !BKS)
-      TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 64, 64, 1, 4, 3>(name, t, st)));
+    // k-contiguous: for few tokens, where three more tiles on their way are worth their LDS
+    constexpr int kAhead = !AKS && !BKS ? 3 : 1;
+    TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 64, 64, 1, 4, kAhead>(name, t, st)));
   } else if (c.size == 256) {
     if constexpr (kLarge)
       TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 256, 256, 2, 4>(name, t, st)));
@@ -457,8 +466,7 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
 
 // Room for the sums of a product that is split.
 size_t part_room(int64_t I, int64_t J, int batches, int64_t k, int nseg, bool few) {
-  return part_bytes(cut_of(I, J, batches, steps_of(k, nseg), false, true, true, few), I, J,
-                    batches);
+  return part_bytes(cut_of(I, J, batches, steps_of(k, nseg), EPI_STORE, true, few), I, J, batches);
 }
 
 struct ForwardRoom {

@@ -181,13 +181,16 @@ typedef __attribute__((address_space(3))) s16x8 lds_s16x8;
 //   k-contiguous: row r is 4 pieces of 16 bytes, piece p at p ^ (r / 2 % 4): the 16 rows that one
 //   read takes then start in 16 different 16-byte columns of the 256 bytes of banks.
 //   k-strided: line k is R / 8 pieces, piece p at p ^ 2 f(k), f(k) = k % 4 + 4 (k / 8 % 2): a
-//   transposing read takes 32 bytes of 4 lines, from 2 groups of lanes at k and k + 8.
+//   transposing read takes 32 bytes of 4 lines, from 2 groups of lanes at k and k + 8.  Two lines
+//   of 8 pieces fill the banks, and f(k) = k / 2 % 2 + 2 (k / 8 % 2) does.
 template <bool KS, int R>
 struct Lay {
   static constexpr int kPieces = KS ? R / 8 : kBK / 8;  // of a line
   static constexpr int kBytes = R * kBK * 2;
   static __device__ __forceinline__ int swizzle(int line) {
-    return KS ? ((line & 3) | ((line >> 3) & 1) << 2) << 1 : (line >> 1) & 7;
+    if (!KS) return (line >> 1) & 7;
+    if (R == 64) return (((line >> 1) & 1) | ((line >> 3) & 1) << 1) << 1;
+    return ((line & 3) | ((line >> 3) & 1) << 2) << 1;
   }
 };
 
