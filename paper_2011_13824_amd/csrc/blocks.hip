@@ -96,12 +96,12 @@ int q8_pack(int64_t rows, int n, const T* x, int64_t ldx, void* q8, hipStream_t 
 }
 
 template <typename T>
-int q8_unpack(int64_t rows, int n, int cols, const void* q8, T* x, int64_t ldx, hipStream_t st) {
+int q8_unpack(int64_t rows, int n, const void* q8, T* x, int64_t ldx, hipStream_t st) {
   const int64_t blocks = (rows * groups_of(n) * 4 + 255) / 256;
   if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "q8_unpack: more than 2^42 values");
   return launch_k("q8_unpack", st, [&] {
     k_q8_unpack<T><<<(unsigned)blocks, 256, 0, st>>>(
-        (const int8_t*)q8, (const uint8_t*)q8 + q8_exps_at(rows, n), rows, n, cols, x, ldx);
+        (const int8_t*)q8, (const uint8_t*)q8 + q8_exps_at(rows, n), rows, n, x, ldx);
   });
 }
 
@@ -235,23 +235,34 @@ struct FfnPlan {
   bool in_place(const void* p, int64_t ld, int64_t cols) const {
     return !f32 && aligned16(p) && ld % 8 == 0 && cols % 8 == 0;
   }
+  // Wg and Wu are read side by side, with one row distance.
+  bool in_in_place() const {
+    return in_place(f->Wg, f->ldg, D) && in_place(f->Wu, f->ldu, D) && f->ldg == f->ldu;
+  }
+  bool down_in_place() const { return in_place(f->Wd, f->ldd, F); }
 };
 
-// The user's matrices as operands: in place where the tile kernel can read them, else copies in
-// their rooms, all made by one launch.
+// The operands that the tile kernel cannot read in place, copied into their rooms by one launch.
 struct Copies {
   OperandJobs jobs{};
   int64_t blocks = 0;
 
-  void add(const FfnPlan& pl, const void* x, int64_t ldx, int64_t rows, int64_t n, Operand& o) {
-    if (pl.in_place(x, ldx, n)) {
+  void add(bool in_place, const void* x, int64_t ldx, int64_t rows, int64_t n, Operand& o) {
+    if (in_place) {
       o.p = (const char*)x;
       o.ld = ldx;
       o.plane = 0;
-      return;
+    } else {
+      job(x, nullptr, ldx, rows, n, o);
     }
+  }
+  void add_packed(const void* q8, int64_t rows, int64_t n, const Operand& o) {
+    job(q8, (const uint8_t*)q8 + q8_exps_at(rows, (int)n), 0, rows, n, o);
+  }
+  void job(const void* x, const uint8_t* exps, int64_t ldx, int64_t rows, int64_t n,
+           const Operand& o) {
     if (rows == 0) return;
-    jobs.job[jobs.count++] = {x, ldx, rows, o.plane, (void*)o.p, (int)n, (int)o.ld,
+    jobs.job[jobs.count++] = {x, exps, ldx, rows, o.plane, (void*)o.p, (int)n, (int)o.ld,
                               (unsigned)blocks};
     blocks += (rows * (o.ld / 8) + 255) / 256;
   }
@@ -272,34 +283,36 @@ struct Copies {
 constexpr int kSixA[6] = {1, 0, 2, 0, 1, 0};
 constexpr int kSixB[6] = {1, 2, 0, 1, 0, 0};
 
-// Adds the segments of one product.
-void add_segs(const FfnPlan& pl, TileArgs& t, int batch, const Operand& A, const Operand& B,
-              const Operand* A2 = nullptr) {
-  const int n = pl.f32 ? 6 : 1, at = batch ? 0 : t.nseg;
-  for (int s = 0; s < n; ++s) {
-    const int64_t pa = pl.f32 ? kSixA[s] * 2 : 0, pb = pl.f32 ? kSixB[s] * 2 : 0;
-    t.A[at + s] = A.p + pa * A.plane;
-    if (A2) t.A2[at + s] = A2->p + pa * A2->plane;
-    t.B[batch][at + s] = B.p + pb * B.plane;
-  }
-  if (!batch) t.nseg += n;
-  t.lda = A.ld * 2;
-  t.ldb = B.ld * 2;
+// A product without its segments and output.
+TileProblem problem(int64_t I, int64_t J, int64_t KA, int64_t KB) {
+  TileProblem p{};
+  p.I = (int)I;
+  p.J = (int)J;
+  p.KA = (int)KA;
+  p.KB = (int)KB;
+  p.splits = 1;
+  return p;
 }
 
-template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ,
-          int AHEAD = 1>
-int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
-  constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;
-  const int64_t ti = up(t.I, kFeat) / kFeat, tj = up(t.J, BJ) / BJ, total = ti * tj * t.batches * t.splits;
-  if (total == 0) return LIRPA_OK;
-  if (total > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "%s: more than 2^31 tiles", name);
-  t.tiles_i = (int)ti;
-  t.tiles_j = (int)tj;
-  return launch_k(name, st, [&] {
-    k_ffn_tile<T, AKS, BKS, EPI, KEEP, BI, BJ, WI, WJ, AHEAD>
-        <<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);
-  });
+// Adds the segments of one product.  `one_part`: A is exact in its first part.
+void add_segs(const FfnPlan& pl, TileProblem& p, const Operand& A, const Operand& B,
+              bool one_part = false) {
+  const int n = !pl.f32 ? 1 : one_part ? 3 : 6;
+  for (int s = 0; s < n; ++s) {
+    const int64_t pa = n == 6 ? kSixA[s] : 0, pb = n == 6 ? kSixB[s] : n == 3 ? 2 - s : 0;
+    p.A[p.nseg] = A.p + pa * 2 * A.plane;
+    p.B[p.nseg++] = B.p + pb * 2 * B.plane;
+  }
+  p.lda = A.ld * 2;
+  p.ldb = B.ld * 2;
+}
+
+TileArgs tile_args(const FfnPlan& pl, int keep) {
+  TileArgs t{};
+  t.count = 1;
+  t.keep = keep;
+  t.gate = pl.f->gate;
+  return t;
 }
 
 // How a product is cut: tiles of 256 x 256 (one block a CU), 128 x 128 or 64 x 64 (two), and the
@@ -320,17 +333,32 @@ constexpr Round kRounds[3] = {{64, 1024, 6.0, 11.8, 4.5, 7.4, 1, 4},
                               {128, 512, 8.0, 14.3, 6.0, 8.7, 4.5, 12},
                               {256, 256, 10.0, 23.5, 10.0, 23.5, 8.6, 30}};
 
-// The cut of least estimated time.  Joining moves the sums twice at 4 TB/s and costs a launch.  So
-// few tiles over a long k are split, and tiles that would leave a round nearly empty, or most of
-// its time to epilogues, are made smaller.
+// The cut of least estimated time for the products of a launch.  Joining moves the sums twice at
+// 4 TB/s and costs a launch.  So few tiles over a long k are split, and tiles that would leave a
+// round nearly empty, or most of its time to epilogues, are made smaller.
 //
 // Up to 64 tokens (`few`: both operands k-contiguous) it is the weights' bytes that count: tiles of
 // 64, three more on their way, in about 512 blocks.  4096 x 10944 in bf16: gate and up 34 us
 // against 39-43 with tiles of 128, down 17 us in 8 parts, 22 in 4, 19 in 16.
-Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, int epi, bool may_large, bool few) {
+int64_t tiles_of(const TileProblem& p, int64_t size, bool gate) {
+  const int64_t feat = gate ? size / 2 : size;
+  return (up(p.I, feat) / feat) * (up(p.J, size) / size);
+}
+int64_t steps_of(const TileProblem& p) {
+  return up(std::max(p.KA, p.KB), kBK) / kBK * p.nseg;
+}
+
+// `may_large`: not the epilogue of da in 32 bits, which does not fit the larger tile's registers.
+Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool few) {
   const bool gate = epi == EPI_GATE, may_split = epi == EPI_STORE;
-  if (few && J <= 64) {
-    const int64_t n = up(I, gate ? 32 : 64) / (gate ? 32 : 64);
+  int64_t steps = 0;
+  double outs = 0;
+  for (int i = 0; i < count; ++i) {
+    steps = std::max(steps, steps_of(probs[i]));
+    outs += (double)probs[i].I * probs[i].J;
+  }
+  if (few && probs[0].J <= 64) {
+    const int64_t n = tiles_of(probs[0], 64, gate);
     int splits = 1;
     while (may_split && splits < 16 && n * splits * 2 <= 640 && steps >= 16 * splits) splits *= 2;
     return {64, splits};
@@ -339,8 +367,8 @@ Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, int epi, bool may_l
   double least = 1e300;
   for (const Round& r : kRounds) {
     if (r.size == 256 && !may_large) continue;
-    const int64_t feat = gate ? r.size / 2 : r.size;
-    const int64_t tiles = (up(I, feat) / feat) * (up(J, r.size) / r.size) * batches;
+    int64_t tiles = 0;
+    for (int i = 0; i < count; ++i) tiles += tiles_of(probs[i], r.size, gate);
     const double more = gate ? r.gate : epi == EPI_BACK ? r.back : 0;
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
       if (splits > 1 && (!may_split || steps < 4 * splits)) break;
@@ -351,7 +379,7 @@ Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, int epi, bool may_l
         t += r.fixed + more + r.slope * k;
       else if (rest > 0)
         t += r.half_fixed + more + r.half_slope * k;
-      if (splits > 1) t += 5 + (double)I * J * batches * 4 * splits * 2 / 4e6;
+      if (splits > 1) t += 5 + outs * 4 * splits * 2 / 4e6;
       if (t < least) {
         least = t;
         best.size = r.size;
@@ -363,64 +391,94 @@ Cut cut_of(int64_t I, int64_t J, int batches, int64_t steps, int epi, bool may_l
 }
 
 int64_t part_ld(int64_t I) { return up(I, 8); }
-size_t part_bytes(const Cut& c, int64_t I, int64_t J, int batches) {
-  return c.splits > 1 ? (size_t)c.splits * batches * J * part_ld(I) * sizeof(float) : 0;
-}
-int64_t steps_of(int64_t k, int nseg) { return up(k, kBK) / kBK * nseg; }
 
-template <typename T, bool AKS, bool BKS, int EPI, int KEEP>
-int tile_of_size(const char* name, TileArgs& t, void* part, hipStream_t st) {
-  // the epilogue of da in 32 bits does not fit the registers of the larger tile
-  constexpr bool kLarge = !(Kind<T>::kParts == 3 && EPI == EPI_BACK);
-  using W = typename Kind<T>::Whole;
-  const Cut c = cut_of(t.I, t.J, t.batches, steps_of(std::max(t.KA, t.KB), t.nseg),
-                       EPI, kLarge, !AKS && !BKS);
-  t.splits = c.splits;
-  t.part = (float*)part;
-  t.part_ld = part_ld(t.I);
-  if (c.size == 64) {
-    // k-contiguous: for few tokens, where three more tiles on their way are worth their LDS
-    constexpr int kAhead = !AKS && !BKS ? 3 : 1;
-    TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 64, 64, 1, 4, kAhead>(name, t, st)));
-  } else if (c.size == 256) {
-    if constexpr (kLarge)
-      TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 256, 256, 2, 4>(name, t, st)));
-  } else {
-    TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 128, 128, 2, 2>(name, t, st)));
+// Room for the sums of products that are split.
+size_t part_room(const Cut& c, const TileProblem* probs, int count) {
+  size_t bytes = 0;
+  for (int i = 0; c.splits > 1 && i < count; ++i)
+    bytes += up((size_t)c.splits * probs[i].J * part_ld(probs[i].I) * sizeof(float), 256);
+  return bytes;
+}
+
+// What the split products of a call leave to be added.
+struct Joins {
+  JoinJobs jobs{};
+  int64_t blocks = 0;
+
+  void add(const TileProblem& p) {
+    jobs.job[jobs.count++] = {p.part, p.out, p.part_ld, p.ldo, p.J, p.I, p.splits,
+                              (unsigned)blocks};
+    blocks += ((int64_t)p.J * ((p.I + 7) / 8) + 255) / 256;
   }
-  if (EPI != EPI_STORE || c.splits == 1) return LIRPA_OK;
-  const int64_t blocks = ((int64_t)t.batches * t.J * ((t.I + 7) / 8) + 255) / 256;
-  return launch_k("ffn_join", st, [&] {
-    k_ffn_join<W><<<(unsigned)blocks, 256, 0, st>>>(t.part, t.part_ld, t.splits, t.batches, t.J,
-                                                    t.I, (W*)t.out[0], (W*)t.out[1], t.ldo);
+  int run(const FfnPlan& pl, hipStream_t st) const {
+    if (blocks == 0) return LIRPA_OK;
+    if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "ffn_join: more than 2^42 values");
+    return launch_k("ffn_join", st, [&] {
+      switch (pl.f->dtype) {
+        case LIRPA_F32: k_ffn_join<float><<<(unsigned)blocks, 256, 0, st>>>(jobs); break;
+        case LIRPA_BF16: k_ffn_join<bf16><<<(unsigned)blocks, 256, 0, st>>>(jobs); break;
+        default: k_ffn_join<f16><<<(unsigned)blocks, 256, 0, st>>>(jobs);
+      }
+    });
+  }
+};
+
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int SIZE, int WI, int WJ, int AHEAD>
+int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
+  int64_t total = 0;
+  for (int i = 0; i < t.count; ++i) {
+    TileProblem& p = t.prob[i];
+    const int64_t feat = EPI == EPI_GATE ? SIZE / 2 : SIZE;
+    const int64_t ti = up(p.I, feat) / feat, tj = up(p.J, SIZE) / SIZE;
+    if (total + ti * tj * p.splits > 0x7fffffff)
+      return fail(LIRPA_EUNSUPPORTED, "%s: more than 2^31 tiles", name);
+    p.tiles_i = (int)ti;
+    p.tiles_j = (int)tj;
+    p.first = (int)total;
+    total += ti * tj * p.splits;
+  }
+  if (total == 0) return LIRPA_OK;
+  return launch_k(name, st, [&] {
+    k_ffn_tile<T, AKS, BKS, EPI, KEEP, SIZE, SIZE, WI, WJ, AHEAD>
+        <<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);
   });
 }
 
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP>
+int tile_of_size(const char* name, TileArgs& t, const Cut& c, char* part, Joins* joins,
+                 hipStream_t st) {
+  for (int i = 0; c.splits > 1 && i < t.count; ++i) {
+    TileProblem& p = t.prob[i];
+    p.splits = c.splits;
+    p.part = (float*)part;
+    p.part_ld = part_ld(p.I);
+    part += up((size_t)c.splits * p.J * p.part_ld * sizeof(float), 256);
+    joins->add(p);
+  }
+  if (c.size == 64) {
+    // k-contiguous: for few tokens, where three more tiles on their way are worth their LDS
+    constexpr int kAhead = !AKS && !BKS ? 3 : 1;
+    return launch_tile<T, AKS, BKS, EPI, KEEP, 64, 1, 4, kAhead>(name, t, st);
+  }
+  if constexpr (!(Kind<T>::kParts == 3 && EPI == EPI_BACK))
+    if (c.size == 256) return launch_tile<T, AKS, BKS, EPI, KEEP, 256, 2, 4, 1>(name, t, st);
+  return launch_tile<T, AKS, BKS, EPI, KEEP, 128, 2, 2, 1>(name, t, st);
+}
+
 template <bool AKS, bool BKS, int EPI>
-int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, void* part, hipStream_t st) {
+int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, const Cut& cut, void* part,
+             Joins* joins, hipStream_t st) {
   auto typed = [&](auto keep) {
     constexpr int K = decltype(keep)::value;
     switch (pl.f->dtype) {
-      case LIRPA_F32: return tile_of_size<Split, AKS, BKS, EPI, K>(name, t, part, st);
-      case LIRPA_BF16: return tile_of_size<bf16, AKS, BKS, EPI, K>(name, t, part, st);
-      default: return tile_of_size<f16, AKS, BKS, EPI, K>(name, t, part, st);
+      case LIRPA_F32: return tile_of_size<Split, AKS, BKS, EPI, K>(name, t, cut, (char*)part, joins, st);
+      case LIRPA_BF16: return tile_of_size<bf16, AKS, BKS, EPI, K>(name, t, cut, (char*)part, joins, st);
+      default: return tile_of_size<f16, AKS, BKS, EPI, K>(name, t, cut, (char*)part, joins, st);
     }
   };
   if constexpr (EPI == EPI_BACK)
     if (t.keep == LIRPA_KEEP_8) return typed(std::integral_constant<int, 8>{});
   return typed(std::integral_constant<int, 0>{});
-}
-
-TileArgs tile_args(const FfnPlan& pl, int64_t I, int64_t J, int64_t KA, int64_t KB) {
-  TileArgs t{};
-  t.I = (int)I;
-  t.J = (int)J;
-  t.KA = (int)KA;
-  t.KB = (int)KB;
-  t.batches = 1;
-  t.keep = -1;
-  t.gate = pl.f->gate;
-  return t;
 }
 
 // Up to kFewest tokens k_ffn_few is the faster one (us in bf16, against the tile kernel: 4096 x
@@ -464,25 +522,26 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   });
 }
 
-// Room for the sums of a product that is split.
-size_t part_room(int64_t I, int64_t J, int batches, int64_t k, int nseg, bool few) {
-  return part_bytes(cut_of(I, J, batches, steps_of(k, nseg), EPI_STORE, true, few), I, J, batches);
-}
-
 struct ForwardRoom {
   Operand x, wg, wu, wd, a;
+  Cut cut_down;
   void* part;
   size_t bytes;
 };
+TileProblem down_problem(const FfnPlan& pl, const ForwardRoom& r) {
+  TileProblem p = problem(pl.D, pl.rows, pl.Fp, pl.Fp);
+  add_segs(pl, p, r.wd, r.a);
+  return p;
+}
 ForwardRoom forward_room(FfnPlan& pl) {
-  const lirpa_ffn* f = pl.f;
   ForwardRoom r;
   r.x = pl.own(pl.rows, pl.D);
-  if (!pl.in_place(f->Wg, f->ldg, pl.D)) r.wg = pl.own(pl.F, pl.D);
-  if (!pl.in_place(f->Wu, f->ldu, pl.D)) r.wu = pl.own(pl.F, pl.D);
-  if (!pl.in_place(f->Wd, f->ldd, pl.F)) r.wd = pl.own(pl.D, pl.F);
+  if (!pl.in_in_place()) r.wg = pl.own(pl.F, pl.D), r.wu = pl.own(pl.F, pl.D);
+  if (!pl.down_in_place()) r.wd = pl.own(pl.D, pl.F);
   r.a = pl.own(pl.rows, pl.F);
-  r.part = pl.ws.take(part_room(pl.D, pl.rows, 1, pl.Fp, pl.f32 ? 6 : 1, true));
+  const TileProblem down = down_problem(pl, r);
+  r.cut_down = cut_of(&down, 1, EPI_STORE, true, true);
+  r.part = pl.ws.take(part_room(r.cut_down, &down, 1));
   r.bytes = pl.ws.at;
   return r;
 }
@@ -490,9 +549,8 @@ ForwardRoom forward_room(FfnPlan& pl) {
 int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, void* out,
                 int64_t ldo, int keep, void* g, void* u, void* ws, hipStream_t st) {
   FfnPlan pl(f, rows, ws);
-  const bool in_place = pl.in_place(f->Wg, f->ldg, pl.D) && pl.in_place(f->Wu, f->ldu, pl.D) &&
-                        pl.in_place(f->Wd, f->ldd, pl.F);
-  if (keep == LIRPA_KEEP_NONE && rows <= (in_place ? kFewest : kFewRows))
+  const bool in = pl.in_in_place(), down = pl.down_in_place();
+  if (keep == LIRPA_KEEP_NONE && rows <= (in && down ? kFewest : kFewRows))
     return by_type(f->dtype, [&](auto t) {
       using T = decltype(t);
       if (rows <= 16) return few_forward<T, 1>(f, rows, x, ldx, out, ldo, ws, st);
@@ -501,56 +559,88 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
     });
   ForwardRoom r = forward_room(pl);
   Copies copies;
-  copies.add(pl, x, ldx, rows, pl.D, r.x);
-  copies.add(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg);
-  copies.add(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu);
-  copies.add(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd);
+  copies.add(pl.in_place(x, ldx, pl.D), x, ldx, rows, pl.D, r.x);
+  copies.add(in, f->Wg, f->ldg, pl.F, pl.D, r.wg);
+  copies.add(in, f->Wu, f->ldu, pl.F, pl.D, r.wu);
+  copies.add(down, f->Wd, f->ldd, pl.D, pl.F, r.wd);
   TRY(copies.run(pl, st));
 
-  TileArgs t = tile_args(pl, pl.F, rows, pl.Dp, pl.Dp);
-  add_segs(pl, t, 0, r.wg, r.x, &r.wu);
-  t.lda2 = r.wu.ld * 2;
-  t.out[0] = (void*)r.a.p;
-  t.ldo = r.a.ld;
-  t.pad_i = (int)pl.Fp;
-  t.plane = r.a.plane;
-  t.keep = keep;
+  TileArgs t = tile_args(pl, keep);
+  TileProblem& p = t.prob[0];
+  p = problem(pl.F, rows, pl.Dp, pl.Dp);
+  add_segs(pl, p, r.wg, r.x);
+  for (int s = 0; s < p.nseg; ++s) t.A2[s] = r.wu.p + (p.A[s] - r.wg.p);
+  p.out = (void*)r.a.p;
+  p.ldo = r.a.ld;
+  p.pad_i = (int)pl.Fp;
+  p.plane = r.a.plane;
   t.g = g;
   t.u = u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, r.part, st)));
+  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, cut_of(&p, 1, EPI_GATE, true, true),
+                                          nullptr, nullptr, st)));
 
-  t = tile_args(pl, pl.D, rows, pl.Fp, pl.Fp);
-  add_segs(pl, t, 0, r.wd, r.a);
-  t.out[0] = out;
-  t.ldo = ldo;
-  return run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, r.part, st);
+  Joins joins;
+  t = tile_args(pl, LIRPA_KEEP_NONE);
+  t.prob[0] = down_problem(pl, r);
+  t.prob[0].out = out;
+  t.prob[0].ldo = ldo;
+  TRY((run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, r.cut_down, r.part, &joins, st)));
+  return joins.run(pl, st);
 }
 
 struct BackwardRoom {
   Operand dout, x, wg, wu, wd, a, dg, du;
-  void* part;
+  Cut cut_dx, cut_dw;
+  void *part_dx, *part_dw;
   size_t bytes;
 };
-BackwardRoom backward_room(FfnPlan& pl) {
-  const lirpa_ffn* f = pl.f;
+TileProblem dx_problem(const FfnPlan& pl, const BackwardRoom& r) {
+  TileProblem p = problem(pl.D, pl.rows, pl.F, pl.Fp);
+  add_segs(pl, p, r.wg, r.dg);
+  add_segs(pl, p, r.wu, r.du);
+  return p;
+}
+// The wanted ones of dWg, dWu and dWd.
+int dw_problems(const FfnPlan& pl, const BackwardRoom& r, bool packed_x, void* dWg, void* dWu,
+                void* dWd, TileProblem* probs) {
+  int n = 0;
+  for (int b = 0; b < 2; ++b) {
+    if (!(b ? dWu : dWg)) continue;
+    TileProblem& p = probs[n++];
+    p = problem(pl.D, pl.F, pl.rows, pl.rows);
+    add_segs(pl, p, r.x, b ? r.du : r.dg, packed_x);
+    p.out = b ? dWu : dWg;
+    p.ldo = pl.D;
+  }
+  if (dWd) {
+    TileProblem& p = probs[n++];
+    p = problem(pl.F, pl.D, pl.rows, pl.rows);
+    add_segs(pl, p, r.a, r.dout);
+    p.out = dWd;
+    p.ldo = pl.F;
+  }
+  return n;
+}
+BackwardRoom backward_room(FfnPlan& pl, bool packed_x) {
   BackwardRoom r;
   r.dout = pl.own(pl.rows, pl.D);
   r.x = pl.own(pl.rows, pl.D);
-  if (!pl.in_place(f->Wg, f->ldg, pl.D)) r.wg = pl.own(pl.F, pl.D);
-  if (!pl.in_place(f->Wu, f->ldu, pl.D)) r.wu = pl.own(pl.F, pl.D);
-  if (!pl.in_place(f->Wd, f->ldd, pl.F)) r.wd = pl.own(pl.D, pl.F);
+  if (!pl.in_in_place()) r.wg = pl.own(pl.F, pl.D), r.wu = pl.own(pl.F, pl.D);
+  if (!pl.down_in_place()) r.wd = pl.own(pl.D, pl.F);
   r.a = pl.own(pl.rows, pl.F);
   r.dg = pl.own(pl.rows, pl.F);
   r.du = pl.own(pl.rows, pl.F);
-  const int n = pl.f32 ? 6 : 1;
-  size_t part = part_room(pl.D, pl.rows, 1, pl.Fp, 2 * n, false);
-  for (int batches : {1, 2})      // dWg and dWu, or one of them,
-    for (int seg : {n, pl.f32 ? 3 : 1})  // from x in 32 or in 8 bits
-      part = std::max(part, part_room(pl.D, pl.F, batches, pl.rows, seg, false));
-  part = std::max(part, part_room(pl.F, pl.D, 1, pl.rows, n, false));
-  r.part = pl.ws.take(part);
+  const TileProblem dx = dx_problem(pl, r);
+  r.cut_dx = cut_of(&dx, 1, EPI_STORE, true, false);
+  r.part_dx = pl.ws.take(part_room(r.cut_dx, &dx, 1));
+  // cut as if all three were wanted: a gradient does not depend on which others are
+  char all;
+  TileProblem dw[3];
+  const int n = dw_problems(pl, r, packed_x, &all, &all, &all, dw);
+  r.cut_dw = cut_of(dw, n, EPI_STORE, true, false);
+  r.part_dw = pl.ws.take(part_room(r.cut_dw, dw, n));
   r.bytes = pl.ws.at;
   return r;
 }
@@ -559,88 +649,64 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
                  const void* x, int64_t ldx, const void* g, const void* u, void* dx, int64_t lddx,
                  void* dWg, void* dWu, void* dWd, void* ws, hipStream_t st) {
   FfnPlan pl(f, rows, ws);
-  BackwardRoom r = backward_room(pl);
-  const bool wx = dWg || dWu;
+  const bool packed = keep == LIRPA_KEEP_8;
+  BackwardRoom r = backward_room(pl, packed);
   Copies copies;
-  copies.add(pl, dout, lddo, rows, pl.D, r.dout);
+  copies.add(pl.in_place(dout, lddo, pl.D), dout, lddo, rows, pl.D, r.dout);
   if (dx) {
-    copies.add(pl, f->Wg, f->ldg, pl.F, pl.D, r.wg);
-    copies.add(pl, f->Wu, f->ldu, pl.F, pl.D, r.wu);
+    copies.add(pl.in_in_place(), f->Wg, f->ldg, pl.F, pl.D, r.wg);
+    copies.add(pl.in_in_place(), f->Wu, f->ldu, pl.F, pl.D, r.wu);
   }
-  copies.add(pl, f->Wd, f->ldd, pl.D, pl.F, r.wd);
-  if (wx && keep == LIRPA_KEEP_FULL) copies.add(pl, x, ldx, rows, pl.D, r.x);
+  copies.add(pl.down_in_place(), f->Wd, f->ldd, pl.D, pl.F, r.wd);
+  if (dWg || dWu) {
+    if (packed)
+      copies.add_packed(x, rows, pl.D, r.x);
+    else
+      copies.add(pl.in_place(x, ldx, pl.D), x, ldx, rows, pl.D, r.x);
+  }
   TRY(copies.run(pl, st));
 
   // act(g) u, dg and du
-  TileArgs t = tile_args(pl, pl.F, rows, pl.D, pl.Dp);
-  add_segs(pl, t, 0, r.wd, r.dout);
-  t.out[0] = dWd ? (void*)r.a.p : nullptr;
+  TileArgs t = tile_args(pl, keep);
+  TileProblem& p = t.prob[0];
+  p = problem(pl.F, rows, pl.D, pl.Dp);
+  add_segs(pl, p, r.wd, r.dout);
+  p.out = dWd ? (void*)r.a.p : nullptr;
+  p.ldo = r.a.ld;
+  p.plane = r.a.plane;
+  p.pad_i = (int)pl.Fp;
   t.dg = dx || dWg ? (void*)r.dg.p : nullptr;
   t.du = dx || dWu ? (void*)r.du.p : nullptr;
-  t.ldo = r.a.ld;
-  t.plane = r.a.plane;
-  t.pad_i = (int)pl.Fp;
-  t.keep = keep;
   t.g = (void*)g;
   t.u = (void*)u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, r.part, st)));
+  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, cut_of(&p, 1, EPI_BACK, !pl.f32, false),
+                                         nullptr, nullptr, st)));
 
+  Joins joins;
   if (dx) {
-    t = tile_args(pl, pl.D, rows, pl.F, pl.Fp);
-    add_segs(pl, t, 0, r.wg, r.dg);
-    const int64_t ldg = t.lda;
-    add_segs(pl, t, 0, r.wu, r.du);
-    t.lda2 = t.lda;
-    t.lda = ldg;
-    t.out[0] = dx;
-    t.ldo = lddx;
-    TRY((run_tile<true, false, EPI_STORE>(pl, "ffn_dx", t, r.part, st)));
+    t = tile_args(pl, LIRPA_KEEP_NONE);
+    t.prob[0] = dx_problem(pl, r);
+    t.prob[0].out = dx;
+    t.prob[0].ldo = lddx;
+    TRY((run_tile<true, false, EPI_STORE>(pl, "ffn_dx", t, r.cut_dx, r.part_dx, &joins, st)));
   }
-  if (wx) {
-    if (keep == LIRPA_KEEP_8 && rows) {  // f32: in the first of three parts, which holds 8 bits
-      if (f->dtype == LIRPA_F16)
-        TRY(q8_unpack<f16>(rows, (int)pl.D, (int)r.x.ld, x, (f16*)r.x.p, r.x.ld, st));
-      else
-        TRY(q8_unpack<bf16>(rows, (int)pl.D, (int)r.x.ld, x, (bf16*)r.x.p, r.x.ld, st));
-    }
-    t = tile_args(pl, pl.D, pl.F, rows, rows);
-    const bool one_part = pl.f32 && keep == LIRPA_KEEP_8;
-    const Operand* d[2] = {&r.dg, &r.du};
-    void* out[2] = {dWg, dWu};
-    t.batches = 0;
-    for (int b = 0; b < 2; ++b) {
-      if (!out[b]) continue;
-      if (one_part) {  // x is exact in its first part: three products, smallest first
-        t.nseg = 3;
-        for (int s = 0; s < 3; ++s) {
-          t.A[s] = r.x.p;
-          t.B[t.batches][s] = d[b]->p + (2 - s) * 2 * d[b]->plane;
-        }
-        t.lda = r.x.ld * 2;
-        t.ldb = d[b]->ld * 2;
-      } else {
-        add_segs(pl, t, t.batches, r.x, *d[b]);
-      }
-      t.out[t.batches++] = out[b];
-    }
-    t.ldo = pl.D;
-    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_in", t, r.part, st)));
+  if (dWg || dWu || dWd) {
+    t = tile_args(pl, LIRPA_KEEP_NONE);
+    t.count = dw_problems(pl, r, packed, dWg, dWu, dWd, t.prob);
+    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw", t, r.cut_dw, r.part_dw, &joins, st)));
   }
-  if (dWd) {
-    t = tile_args(pl, pl.F, pl.D, rows, rows);
-    add_segs(pl, t, 0, r.a, r.dout);
-    t.out[0] = dWd;
-    t.ldo = pl.F;
-    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw_down", t, r.part, st)));
-  }
-  return LIRPA_OK;
+  return joins.run(pl, st);
 }
 
 size_t ffn_bytes(const lirpa_ffn* f, int64_t rows, bool backward) {
-  FfnPlan pl(f, rows, nullptr);
-  return backward ? backward_room(pl).bytes : forward_room(pl).bytes;
+  if (!backward) {
+    FfnPlan pl(f, rows, nullptr);
+    return forward_room(pl).bytes;
+  }
+  FfnPlan full(f, rows, nullptr), packed(f, rows, nullptr);
+  return std::max(backward_room(full, false).bytes, backward_room(packed, true).bytes);
 }
 
 }  // namespace
@@ -673,7 +739,7 @@ int lirpa_q8_unpack(int dtype, int64_t rows, int n, const void* q8, void* x, int
     TRY(check_rows("lirpa_q8_unpack", "x", dtype, x, ldx, n));
     TRY(check_q8("lirpa_q8_unpack", "q8", q8));
     return by_type(dtype, [&](auto t) {
-      return q8_unpack(rows, n, n, q8, (decltype(t)*)x, ldx, stream);
+      return q8_unpack(rows, n, q8, (decltype(t)*)x, ldx, stream);
     });
   });
 }

@@ -30,28 +30,36 @@ enum Gate { RELU = 0, SILU = 1, GELU = 2 };
 constexpr int kMaxSegs = 12;
 constexpr int kBK = 64;    // k a tile: 128 bytes of a k-contiguous row, the width of a cache line
 
-struct TileArgs {
+constexpr int kMaxProblems = 3;
+
+// One product.
+struct TileProblem {
   const char* A[kMaxSegs];
-  const char* A2[kMaxSegs];     // EPI_GATE: the rows of Wu
-  const char* B[2][kMaxSegs];   // per batch
-  int64_t lda, ldb;             // bytes between rows
-  int64_t lda2;
+  const char* B[kMaxSegs];
+  int64_t lda, ldb;    // bytes between rows, the same for all segments
   int nseg;
-  int KA, KB;                   // k extents (equal up to the zero padding of a packed operand)
-  int I, J;                     // output sizes
-  int tiles_i, tiles_j, batches;
-  int splits;                   // EPI_STORE: blocks that share a tile's k; over 1, their sums go to
-  float* part;                  // part[split][batch][J][part_ld] and are added by k_ffn_join
+  int KA, KB;          // k extents (equal up to the zero padding of a packed operand)
+  int I, J;            // output sizes
+  int tiles_i, tiles_j;
+  int first;           // block of its first tile
+  int splits;          // EPI_STORE: blocks that share a tile's k; over 1, their sums go to
+  float* part;         // part[split][J][part_ld] and are added by k_ffn_join
   int64_t part_ld;
-  void* out[2];
-  int64_t ldo;                  // elements
-  int pad_i;                    // columns [I, pad_i) of operand outputs are written as 0
-  int64_t plane;                // elements between the parts of a 32-bit operand
-  // gate epilogues
-  int gate, keep;               // keep: -1, 0, 8
-  void *g, *u;                  // what is kept: [J][I] or packed
-  uint8_t *ge, *ue;             // exponents of the packed form
-  void *dg, *du;                // EPI_BACK
+  void* out;           // the tensors' type (EPI_STORE), else an operand of a later product
+  int64_t ldo;         // elements
+  int pad_i;           // columns [I, pad_i) of an operand are written as 0
+  int64_t plane;       // elements between the parts of a 32-bit operand
+};
+
+// A launch: products that do not depend on one another (EPI_STORE), or one with its epilogue.
+struct TileArgs {
+  TileProblem prob[kMaxProblems];
+  int count;
+  const char* A2[kMaxSegs];  // EPI_GATE: the rows of Wu, as those of Wg
+  int gate, keep;            // keep: -1, 0, 8
+  void *g, *u;               // what is kept: [J][I] or packed
+  uint8_t *ge, *ue;          // exponents of the packed form
+  void *dg, *du;             // EPI_BACK
 };
 
 __device__ __forceinline__ int up32(int n) { return (n + 31) & ~31; }
@@ -269,16 +277,16 @@ struct Piece8 {
 // An operand of a later product: 16 bits, or three bf16 parts of a 32-bit value.  The columns
 // [I, pad_i) are cleared.
 template <typename T>
-__device__ __forceinline__ void put_operand(const TileArgs& a, void* base, int64_t row,
+__device__ __forceinline__ void put_operand(const TileProblem& p, void* base, int64_t row,
                                             const Piece8& l, const float (&v)[8]) {
   using H = typename Kind<T>::Half;
-  char* p = (char*)base + row * a.ldo * sizeof(H);
-  const uint32_t at = (l.token * (uint32_t)a.ldo + l.col) * sizeof(H);
+  char* to = (char*)base + row * p.ldo * sizeof(H);
+  const uint32_t at = (l.token * (uint32_t)p.ldo + l.col) * sizeof(H);
   float rest[8];
 #pragma unroll
-  for (int r = 0; r < 8; ++r) rest[r] = l.col + r < a.I ? v[r] : 0.f;
+  for (int r = 0; r < 8; ++r) rest[r] = l.col + r < p.I ? v[r] : 0.f;
   if constexpr (Kind<T>::kParts == 1) {
-    store_row<H, 8>((H*)(p + at), a.pad_i - l.col, rest);
+    store_row<H, 8>((H*)(to + at), p.pad_i - l.col, rest);
   } else {
 #pragma unroll
     for (int part = 0; part < 3; ++part) {
@@ -289,30 +297,30 @@ __device__ __forceinline__ void put_operand(const TileArgs& a, void* base, int64
         rest[r] -= x[r];
         if (!(fabsf(rest[r]) < INFINITY)) rest[r] = 0.f;  // of an infinity or a NaN
       }
-      store_row<H, 8>((H*)(p + part * a.plane * sizeof(H) + at), a.pad_i - l.col, x);
+      store_row<H, 8>((H*)(to + part * p.plane * sizeof(H) + at), p.pad_i - l.col, x);
     }
   }
 }
 
 template <typename T>
-__device__ __forceinline__ void put_output(const TileArgs& a, void* base, int64_t ld, int64_t row,
+__device__ __forceinline__ void put_output(const TileProblem& p, void* base, int64_t ld, int64_t row,
                                            const Piece8& l, const float (&v)[8]) {
   using W = typename Kind<T>::Whole;
-  char* p = (char*)base + row * ld * sizeof(W);
-  store_row<W, 8>((W*)(p + (l.token * (uint32_t)ld + l.col) * sizeof(W)), a.I - l.col, v);
+  char* to = (char*)base + row * ld * sizeof(W);
+  store_row<W, 8>((W*)(to + (l.token * (uint32_t)ld + l.col) * sizeof(W)), p.I - l.col, v);
 }
 
 // What the forward pass keeps: packed with a scale for 32 features (four neighbouring lanes), or
 // as it is.  Every lane of the wave comes here.
 template <typename T>
-__device__ __forceinline__ void keep8(const TileArgs& a, void* base, uint8_t* exps, int64_t row,
+__device__ __forceinline__ void keep8(const TileProblem& p, int keep, void* base, uint8_t* exps, int64_t row,
                                       const Piece8& l, const float (&v)[8]) {
-  const bool in = row + l.token < a.J && l.col < up32(a.I);
-  if (a.keep != 8) {
-    if (in) put_output<T>(a, base, a.I, row, l, v);
+  const bool in = row + l.token < p.J && l.col < up32(p.I);
+  if (keep != 8) {
+    if (in) put_output<T>(p, base, p.I, row, l, v);
     return;
   }
-  const int e = group_exponent4(v), groups = groups_of(a.I);
+  const int e = group_exponent4(v), groups = groups_of(p.I);
   if (!in) return;
   store_global((char*)base + row * groups * kGroup + l.q, pack8(v, e));
   if ((l.col & 31) == 0) store_global(exps + row * groups + l.e, (uint8_t)e);
@@ -323,16 +331,16 @@ template <typename T, int KEEP>
 struct Kept8 {
   using W = typename Kind<T>::Whole;
   Vec<W, 8> raw;
-  __device__ __forceinline__ void load(const TileArgs& a, const void* base, const uint8_t*,
+  __device__ __forceinline__ void load(const TileProblem& p, const void* base, const uint8_t*,
                                        int64_t row, const Piece8& l) {
-    if (row + l.token >= a.J || l.col >= a.I) return;
-    const W* p = (const W*)((const char*)base + row * a.I * sizeof(W) +
-                            (l.token * (uint32_t)a.I + l.col) * sizeof(W));
-    if (a.I - l.col >= 8) {
-      raw = load_global<Vec<W, 8>>(p);
+    if (row + l.token >= p.J || l.col >= p.I) return;
+    const W* from = (const W*)((const char*)base + row * p.I * sizeof(W) +
+                            (l.token * (uint32_t)p.I + l.col) * sizeof(W));
+    if (p.I - l.col >= 8) {
+      raw = load_global<Vec<W, 8>>(from);
     } else {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) raw[r] = l.col + r < a.I ? load_global<W>(p + r) : (W)0.f;
+      for (int r = 0; r < 8; ++r) raw[r] = l.col + r < p.I ? load_global<W>(from + r) : (W)0.f;
     }
   }
   __device__ __forceinline__ void values(float (&v)[8]) const {
@@ -344,12 +352,12 @@ template <typename T>
 struct Kept8<T, 8> {
   u32x2 w;
   int e;
-  __device__ __forceinline__ void load(const TileArgs& a, const void* base, const uint8_t* exps,
+  __device__ __forceinline__ void load(const TileProblem& p, const void* base, const uint8_t* exps,
                                        int64_t row, const Piece8& l) {
     // no branch: what lies past the end is read from the array's start, and not used
-    const int groups = groups_of(a.I);
-    const bool in = row + l.token < a.J && l.col < a.I;
-    const int64_t first = row < a.J ? row : 0;
+    const int groups = groups_of(p.I);
+    const bool in = row + l.token < p.J && l.col < p.I;
+    const int64_t first = row < p.J ? row : 0;
     w = load_global<u32x2>((const char*)base + first * groups * kGroup + (in ? l.q : 0));
     e = load_global<uint8_t>(exps + first * groups + (in ? l.e : 0));
   }
@@ -377,17 +385,19 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     const int x = blockIdx.x & 7, per = total >> 3, more = total & 7;
     id = x * per + min(x, more) + (blockIdx.x >> 3);
   }
-  const int per_batch = a.tiles_i * a.tiles_j;
+  int which = 0;
+  if constexpr (EPI == EPI_STORE)
+    while (which + 1 < a.count && id >= a.prob[which + 1].first) ++which;
+  const TileProblem& p = a.prob[which];
+  id -= p.first;
   int split = 0;
   if constexpr (EPI == EPI_STORE) {
-    split = id / (per_batch * a.batches);
-    id -= split * (per_batch * a.batches);
+    split = id / (p.tiles_i * p.tiles_j);
+    id -= split * (p.tiles_i * p.tiles_j);
   }
-  const int batch = id / per_batch;
-  id -= batch * per_batch;
   constexpr int kBand = 8;
-  const int band = id / (kBand * a.tiles_i), in_band = id - band * kBand * a.tiles_i;
-  const int height = min(kBand, a.tiles_j - band * kBand);
+  const int band = id / (kBand * p.tiles_i), in_band = id - band * kBand * p.tiles_i;
+  const int height = min(kBand, p.tiles_j - band * kBand);
   const int ti = in_band / height, tj = band * kBand + in_band - ti * height;
   const int i0 = ti * kFeat, j0 = tj * BJ;
 
@@ -398,8 +408,8 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
   constexpr int RA = EPI == EPI_GATE ? BI / 2 : BI;
   Bringer<AKS, RA, kThreads> bring_a;
   Bringer<BKS, BJ, kThreads> bring_b;
-  bring_a.init(a.lda, a.I - i0);
-  bring_b.init(a.ldb, a.J - j0);
+  bring_a.init(p.lda, p.I - i0);
+  bring_b.init(p.ldb, p.J - j0);
   Reader<AKS, BI> read_a;
   Reader<BKS, BJ> read_b;
   read_a.init(EPI == EPI_GATE ? wi * (BI / 2 / WI) : wi * (BI / WI));
@@ -411,19 +421,19 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
 #pragma unroll
     for (int j = 0; j < FJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  const int K = max(a.KA, a.KB);
+  const int K = max(p.KA, p.KB);
   const int per_seg = (K + kBK - 1) / kBK;
-  int steps = per_seg * a.nseg, first_seg = 0, first_k = 0;
+  int steps = per_seg * p.nseg, first_seg = 0, first_k = 0;
   if constexpr (EPI == EPI_STORE) {
-    if (a.splits > 1) {
-      const int each = (steps + a.splits - 1) / a.splits, from = min(split * each, steps);
+    if (p.splits > 1) {
+      const int each = (steps + p.splits - 1) / p.splits, from = min(split * each, steps);
       steps = min(each, steps - from);
       if (steps > 0) first_seg = from / per_seg, first_k = from % per_seg;
     }
   }
-  const int64_t corner_a = AKS ? (int64_t)i0 * 2 : (int64_t)i0 * a.lda;
-  const int64_t corner_b = BKS ? (int64_t)j0 * 2 : (int64_t)j0 * a.ldb;
-  const int64_t next_a = AKS ? kBK * a.lda : kBK * 2, next_b = BKS ? kBK * a.ldb : kBK * 2;
+  const int64_t corner_a = AKS ? (int64_t)i0 * 2 : (int64_t)i0 * p.lda;
+  const int64_t corner_b = BKS ? (int64_t)j0 * 2 : (int64_t)j0 * p.ldb;
+  const int64_t next_a = AKS ? kBK * p.lda : kBK * 2, next_b = BKS ? kBK * p.ldb : kBK * 2;
 
   // The operands' tiles A0 B0 A1 B1 ... take the units in turn; each has its next place in memory.
   struct Next {
@@ -433,9 +443,9 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
   };
   const uint32_t first = base + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
   const uint32_t end = first + kUnits * kUnit;
-  Next na{first_seg, a.KA - first_k * kBK, a.A[first_seg] + corner_a + first_k * next_a, nullptr,
+  Next na{first_seg, p.KA - first_k * kBK, p.A[first_seg] + corner_a + first_k * next_a, nullptr,
           first};
-  Next nb{first_seg, a.KB - first_k * kBK, a.B[batch][first_seg] + corner_b + first_k * next_b,
+  Next nb{first_seg, p.KB - first_k * kBK, p.B[first_seg] + corner_b + first_k * next_b,
           nullptr, first + kUnit};
   if constexpr (EPI == EPI_GATE) na.p2 = a.A2[0] + corner_a;
   constexpr int kCopiesA = (EPI == EPI_GATE ? 2 : 1) * decltype(bring_a)::kLoads;
@@ -457,10 +467,10 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     na.p += next_a;
     if constexpr (EPI == EPI_GATE) na.p2 += next_a;
     na.left -= kBK;
-    if (na.left <= 0 && na.seg + 1 < a.nseg) {
+    if (na.left <= 0 && na.seg + 1 < p.nseg) {
       ++na.seg;
-      na.left = a.KA;
-      na.p = a.A[na.seg] + corner_a;
+      na.left = p.KA;
+      na.p = p.A[na.seg] + corner_a;
       if constexpr (EPI == EPI_GATE) na.p2 = a.A2[na.seg] + corner_a;
     }
   };
@@ -468,10 +478,10 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     unit_on(nb.to);
     nb.p += next_b;
     nb.left -= kBK;
-    if (nb.left <= 0 && nb.seg + 1 < a.nseg) {
+    if (nb.left <= 0 && nb.seg + 1 < p.nseg) {
       ++nb.seg;
-      nb.left = a.KB;
-      nb.p = a.B[batch][nb.seg] + corner_b;
+      nb.left = p.KB;
+      nb.p = p.B[nb.seg] + corner_b;
     }
   };
   struct Frags {
@@ -517,15 +527,15 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
   Piece8 at;
   at.col = iw + f;
   at.token = lane / kPieces;
-  at.q = at.token * groups_of(a.I) * kGroup + at.col;
-  at.e = at.token * groups_of(a.I) + at.col / kGroup;
+  at.q = at.token * groups_of(p.I) * kGroup + at.col;
+  at.e = at.token * groups_of(p.I) + at.col / kGroup;
   constexpr int kTokens = 64 / kPieces;  // the tokens of the wave's next pieces lie so far on
   Kept8<T, KEEP> kg[kTimes], ku[kTimes];
   auto load_kept = [&](int j) {
 #pragma unroll
     for (int c = 0; c < kTimes; ++c) {
-      kg[c].load(a, a.g, a.ge, jw + j * 16 + c * kTokens, at);
-      ku[c].load(a, a.u, a.ue, jw + j * 16 + c * kTokens, at);
+      kg[c].load(p, a.g, a.ge, jw + j * 16 + c * kTokens, at);
+      ku[c].load(p, a.u, a.ue, jw + j * 16 + c * kTokens, at);
     }
   };
 
@@ -587,34 +597,34 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
       auto piece = [&](int c, const Kept8<T, KEEP>& kept_g, const Kept8<T, KEEP>& kept_u) {
         const int t = at.token + c * kTokens;
         const int64_t row = jw + j * 16 + c * kTokens;
-        const bool in = row + at.token < a.J;
+        const bool in = row + at.token < p.J;
         float x[8];
         read8(turned + t * kRow + f, x);
         if constexpr (EPI == EPI_STORE) {
           if (!in) return;
-          if (a.splits > 1) {
-            float* p = a.part + ((int64_t)(split * a.batches + batch) * a.J + row) * a.part_ld;
-            store_row<float, 8>(p + (at.token * (uint32_t)a.part_ld + at.col), a.I - at.col, x);
+          if (p.splits > 1) {
+            float* to = p.part + ((int64_t)split * p.J + row) * p.part_ld;
+            store_row<float, 8>(to + (at.token * (uint32_t)p.part_ld + at.col), p.I - at.col, x);
           } else {
-            put_output<T>(a, a.out[batch], a.ldo, row, at, x);
+            put_output<T>(p, p.out, p.ldo, row, at, x);
           }
         } else if constexpr (EPI == EPI_GATE) {
           float u[8];
           read8(turned + t * kRow + kPieces * 8 + f, u);
           if (a.keep >= 0) {
-            keep8<T>(a, a.g, a.ge, row, at, x);
-            keep8<T>(a, a.u, a.ue, row, at, u);
+            keep8<T>(p, a.keep, a.g, a.ge, row, at, x);
+            keep8<T>(p, a.keep, a.u, a.ue, row, at, u);
           }
-          if (!in || at.col >= a.pad_i) return;
+          if (!in || at.col >= p.pad_i) return;
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
             float act, slope;
             gate_fn(a.gate, Kind<T>::kParts == 1, x[r], act, slope);
             u[r] *= act;
           }
-          put_operand<T>(a, a.out[0], row, at, u);
+          put_operand<T>(p, p.out, row, at, u);
         } else {
-          if (!in || at.col >= a.pad_i) return;
+          if (!in || at.col >= p.pad_i) return;
           float g[8], u[8], v[8];
           kept_g.values(g);
           kept_u.values(u);
@@ -626,9 +636,9 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
             g[r] = x[r] * act;
             x[r] *= u[r] * slope;
           }
-          if (a.out[0]) put_operand<T>(a, a.out[0], row, at, v);
-          if (a.dg) put_operand<T>(a, a.dg, row, at, x);
-          if (a.du) put_operand<T>(a, a.du, row, at, g);
+          if (p.out) put_operand<T>(p, p.out, row, at, v);
+          if (a.dg) put_operand<T>(p, a.dg, row, at, x);
+          if (a.du) put_operand<T>(p, a.du, row, at, g);
         }
       };
       if constexpr (Kind<T>::kParts == 1) {
@@ -651,34 +661,56 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
   }
 }
 
-// Adds the sums of the blocks that shared a tile's k, in order.  Bound by bytes.
+// Adds the sums of the blocks that shared a tile's k, in order, for all split products of a call.
+// Bound by bytes.
+struct JoinJob {
+  const float* part;
+  void* out;
+  int64_t part_ld, ldo, J;
+  int I, splits;
+  unsigned first;  // block
+};
+struct JoinJobs {
+  JoinJob job[kMaxProblems + 1];
+  int count;
+};
+
 template <typename W>
-__global__ __launch_bounds__(256) void k_ffn_join(const float* __restrict__ part, int64_t part_ld,
-                                                  int splits, int batches, int64_t J, int I,
-                                                  W* out0, W* out1, int64_t ldo) {
-  const int per_row = (I + 7) / 8;
-  const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;
+__global__ __launch_bounds__(256) void k_ffn_join(JoinJobs jobs) {
+  int j = 0;
+  while (j + 1 < jobs.count && blockIdx.x >= jobs.job[j + 1].first) ++j;
+  const JoinJob& o = jobs.job[j];
+  const int per_row = (o.I + 7) / 8;
+  const int64_t first = (int64_t)(blockIdx.x - o.first) * 256, row0 = first / per_row;
   const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x;
   const uint32_t down = at / (uint32_t)per_row;
-  const int64_t row = row0 + down;  // of all batches' rows
+  const int64_t row = row0 + down;
   const int col = (int)(at - down * (uint32_t)per_row) * 8;
-  if (row >= J * batches) return;
+  if (row >= o.J) return;
   float sum[8] = {};
-  for (int s = 0; s < splits; ++s) {
-    float x[8];
-    load_row<float, 8>(part + ((int64_t)s * batches * J + row) * part_ld + col, 8, x);
+  const float* from = o.part + row * o.part_ld + col;
+  const int64_t next = o.J * o.part_ld;
+  for (int s = 0; s < o.splits; s += 4) {  // four on their way; past the end the last one again
+    float x[4][8];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) sum[r] += x[r];
+    for (int i = 0; i < 4; ++i)
+      load_row<float, 8>(from + min(s + i, o.splits - 1) * next, 8, x[i]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (s + i < o.splits) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) sum[r] += x[i][r];
+      }
   }
-  W* out = row < J ? out0 + row * ldo : out1 + (row - J) * ldo;
-  store_row<W, 8>(out + col, I - col, sum);
+  store_row<W, 8>((W*)o.out + row * o.ldo + col, o.I - col, sum);
 }
 
 // Copies [rows][n] into [rows][ld] 16-bit operands, columns from n to ld cleared; a 32-bit source
-// becomes three bf16 parts.  All operands of a call in one launch: they are often small, and a
-// launch then costs more than the copy.  Bound by bytes.
+// becomes three bf16 parts, a packed one (8 bits) is read back.  All operands of a call in one
+// launch: they are often small, and a launch then costs more than the copy.  Bound by bytes.
 struct OperandJob {
   const void* x;
+  const uint8_t* exps;  // of a packed source (x: its int8 values), which one part holds
   int64_t ldx, rows, plane;
   void* out;
   int n, ld;
@@ -705,6 +737,16 @@ __global__ __launch_bounds__(256) void k_ffn_operands(OperandJobs jobs) {
   const int col = (int)(at - down * (uint32_t)per_row) * 8;
   if (row >= o.rows) return;
   float v[8], p[8];
+  if (o.exps) {
+    const int groups = groups_of(o.n);
+    unpack8(load_global<u32x2>((const int8_t*)o.x + row * groups * kGroup + col),
+            load_global<uint8_t>(o.exps + row * groups + col / kGroup), v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i >= o.n) v[i] = 0.f;
+    store_row<H, 8>((H*)o.out + row * o.ld + col, 8, v);
+    return;
+  }
   load_row<W, 8>((const W*)o.x + row * o.ldx + col, o.n - col, v);
 #pragma unroll
   for (int part = 0; part < Kind<T>::kParts; ++part) {

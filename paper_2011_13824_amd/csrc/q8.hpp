@@ -38,22 +38,18 @@ __global__ __launch_bounds__(256) void k_q8_pack(const T* __restrict__ x, int64_
     store_global(exps + p.row * groups + p.col / kGroup, (uint8_t)e);
 }
 
-// Reads back; columns from n to `cols` (the padded width of an operand) come out as 0.
 template <typename T>
 __global__ __launch_bounds__(256) void k_q8_unpack(const int8_t* __restrict__ q,
                                                    const uint8_t* __restrict__ exps,
-                                                   int64_t rows, int n, int cols,
-                                                   T* __restrict__ x, int64_t ldx) {
+                                                   int64_t rows, int n, T* __restrict__ x,
+                                                   int64_t ldx) {
   const int groups = groups_of(n);
   Piece p = piece_of((int64_t)blockIdx.x * 256, groups * 4);
-  if (p.row >= rows || p.col >= cols) return;
+  if (p.row >= rows || p.col >= n) return;
   const u32x2 w = load_global<u32x2>(q + p.row * groups * kGroup + p.col);
   float v[8];
   unpack8(w, load_global<uint8_t>(exps + p.row * groups + p.col / kGroup), v);
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (p.col + i >= n) v[i] = 0.f;
-  store_row<T, 8>(x + p.row * ldx + p.col, cols - p.col, v);
+  store_row<T, 8>(x + p.row * ldx + p.col, n - p.col, v);
 }
 
 }  // namespace lm

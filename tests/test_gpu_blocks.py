@@ -432,6 +432,28 @@ def test_ffn_large_tiles(B, dtype, rows, D, F):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows", [3, 90])
+def test_ffn_weights_of_different_strides(B, dtype, rows):
+    """Wg and Wu with row distances of their own, one of them unaligned, Wd a view of a wider one."""
+    g = gen_of(31)
+    D, F = 72, 104
+    x, dout = rand(g, rows, D, dtype=dtype), rand(g, rows, D, dtype=dtype)
+    for pads in ((0, 8, 16), (8, 0, 0), (0, 3, 0), (5, 0, 8), (0, 0, 1)):
+        W = [rand(g, *s, dtype=dtype, pad=p, scale=0.1)
+             for s, p in zip(((F, D), (F, D), (D, F)), pads)]
+        ffn = B.FeedForward(*W, "silu")
+        same = B.FeedForward(*(w.contiguous() for w in W), "silu")
+        out, kept = ffn.forward(x, keep=8)
+        want, _ = same.forward(x, keep=8)
+        assert torch.equal(out, want), pads
+        o, tol, *_ = forward64(x, W, "silu", UNIT[dtype])
+        check(ffn.forward(x), o, tol + 10 * TINY[dtype], "out")
+        got, grads = ffn.backward(dout, kept), same.backward(dout, kept)
+        for k in grads:
+            assert torch.equal(got[k], grads[k]), (pads, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
 def test_ffn_no_rows(B, dtype):
     W = weights(gen_of(1), 24, 40, dtype)
     ffn = B.FeedForward(*W, "silu")
