@@ -17,10 +17,19 @@ import collections
 import torch
 
 from . import lirpa
+from .lirpa import DTYPES, _check, _matrix, _stream, _vector, load
+
+# What a caller hands in is checked as in lirpa's functions of the same names; outputs that are
+# allocated here are not checked again: a small call costs little more than its Python.
 
 
 def _bytes(n, device):
     return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _type(t, what):
+    """(dtype, its code in the library)"""
+    return lirpa._dtype(t, what), DTYPES[t.dtype]
 
 
 class Q8:
@@ -32,13 +41,19 @@ class Q8:
 
     @staticmethod
     def pack(x):
-        q = Q8(x.shape[0], x.shape[1], device=x.device)
-        lirpa.lirpa_q8_pack(x, q.buf)
+        rows, n = x.shape
+        dt, code = _type(x, "x")
+        p, ld = _matrix(x, rows, n, dt, "x")
+        q = Q8(rows, n, device=x.device)
+        _check(load().lirpa_q8_pack(code, rows, n, p, ld, q.buf.data_ptr(), _stream(None)))
         return q
 
     def values(self, dtype=torch.float32):
-        x = torch.empty((self.rows, self.n), dtype=dtype, device=self.buf.device)
-        lirpa.lirpa_q8_unpack(self.buf, x)
+        rows, n = self.rows, self.n
+        p = lirpa._packed(self.buf, rows, n, "buf")
+        x = torch.empty((rows, n), dtype=dtype, device=self.buf.device)
+        code = _type(x, "dtype")[1]
+        _check(load().lirpa_q8_unpack(code, rows, n, p, x.data_ptr(), n, _stream(None)))
         return x
 
 
@@ -55,24 +70,39 @@ class Norm:
         """Normed(y, sum, y8, rstd): sum is h (x itself without a residual); y8 a Q8 of y where
         wanted, else None; rstd is float32 [rows]."""
         rows, n = x.shape
+        dt, code = _type(x, "x")
+        px, ldx = _matrix(x, rows, n, dt, "x")
+        pr, ldr = _matrix(res, rows, n, dt, "res")
+        pw = _vector(self.w, n, dt, "w")
         y = torch.empty_like(x) if want_y else None
         h = torch.empty_like(x) if res is not None else None
         y8 = Q8(rows, n, device=x.device) if want8 else None
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        lirpa.lirpa_norm_forward(x, res, self.w, self.eps, h, y, y8.buf if want8 else None, rstd)
+        rstd = x.new_empty(rows, dtype=torch.float32)
+        _check(load().lirpa_norm_forward(
+            code, rows, n, px, ldx, pr, ldr, pw, self.eps, None if h is None else h.data_ptr(), n,
+            None if y is None else y.data_ptr(), n, y8.buf.data_ptr() if want8 else None,
+            rstd.data_ptr(), _stream(None)))
         return Normed(y, x if h is None else h, y8, rstd)
 
     def backward(self, dy, h, rstd, dsum=None, want_dw=True):
         """(dh, dw): dh is the gradient of x and of res, dsum that of h past the norm."""
         rows, n = dy.shape
+        dt, code = _type(dy, "dy")
+        pdy, lddy = _matrix(dy, rows, n, dt, "dy")
+        pds, ldds = _matrix(dsum, rows, n, dt, "dsum")
+        ph, ldh = _matrix(h, rows, n, dt, "h")
+        pw, pr = _vector(self.w, n, dt, "w"), _vector(rstd, rows, torch.float32, "rstd")
         dh = torch.empty_like(dy)
         dw = ws = None
         need = 0
         if want_dw:
             dw = torch.empty_like(self.w)
-            need = lirpa.lirpa_norm_workspace_bytes(rows, n)
+            need = load().lirpa_norm_workspace_bytes(rows, n)
             ws = _bytes(need, dy.device)
-        lirpa.lirpa_norm_backward(dy, dsum, h, self.w, rstd, dh, dw, ws, need)
+        _check(load().lirpa_norm_backward(
+            code, rows, n, pdy, lddy, pds, ldds, ph, ldh, pw, pr, dh.data_ptr(), n,
+            dw.data_ptr() if want_dw else None, ws.data_ptr() if want_dw else None, need,
+            _stream(None)))
         return dh, dw
 
 
