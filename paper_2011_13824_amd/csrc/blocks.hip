@@ -334,12 +334,12 @@ constexpr Round kRounds[3] = {{64, 1024, 6.0, 11.8, 4.5, 7.4, 1, 4},
                               {256, 256, 10.0, 23.5, 10.0, 23.5, 8.6, 30}};
 
 // The cut of least estimated time for the products of a launch.  Joining moves the sums twice at
-// 4 TB/s and costs a launch.  So few tiles over a long k are split, and tiles that would leave a
+// 4 TB/s and costs a launch (5 us; 10 with an epilogue, which then reads memory cold).  So few tiles over a long k are split, and tiles that would leave a
 // round nearly empty, or most of its time to epilogues, are made smaller.
 //
 // Up to 64 tokens (`few`: both operands k-contiguous) it is the weights' bytes that count: tiles of
-// 64, three more on their way, in about 512 blocks.  4096 x 10944 in bf16: gate and up 34 us
-// against 39-43 with tiles of 128, down 17 us in 8 parts, 22 in 4, 19 in 16.
+// 64, three more on their way, two blocks a CU.  4096 x 10944 in bf16: gate and up 34 us against
+// 39-43 with tiles of 128, down 17 us in 8 parts, 22 in 4, 19 in 16.
 int64_t tiles_of(const TileProblem& p, int64_t size, bool gate) {
   const int64_t feat = gate ? size / 2 : size;
   return (up(p.I, feat) / feat) * (up(p.J, size) / size);
@@ -350,36 +350,39 @@ int64_t steps_of(const TileProblem& p) {
 
 // `may_large`: not the epilogue of da in 32 bits, which does not fit the larger tile's registers.
 Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool few) {
-  const bool gate = epi == EPI_GATE, may_split = epi == EPI_STORE;
+  const bool gate = epi == EPI_GATE;
   int64_t steps = 0;
   double outs = 0;
   for (int i = 0; i < count; ++i) {
     steps = std::max(steps, steps_of(probs[i]));
     outs += (double)probs[i].I * probs[i].J;
   }
-  if (few && probs[0].J <= 64) {
-    const int64_t n = tiles_of(probs[0], 64, gate);
-    int splits = 1;
-    while (may_split && splits < 16 && n * splits * 2 <= 640 && steps >= 16 * splits) splits *= 2;
-    return {64, splits};
-  }
   Cut best;
   double least = 1e300;
+  const bool weights = few && probs[0].J <= 64;
   for (const Round& r : kRounds) {
     if (r.size == 256 && !may_large) continue;
+    if (r.size > 64 && weights) continue;
+    // tiles of 64 of two k-contiguous operands: two blocks a CU, more on their way (6.2 us at
+    // most half full)
+    const int full = r.size == 64 && few ? r.full / 2 : r.full;
+    const double fixed = full < r.full ? r.half_fixed : r.fixed;
+    const double slope = full < r.full ? r.half_slope : r.slope;
     int64_t tiles = 0;
     for (int i = 0; i < count; ++i) tiles += tiles_of(probs[i], r.size, gate);
     const double more = gate ? r.gate : epi == EPI_BACK ? r.back : 0;
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
-      if (splits > 1 && (!may_split || steps < 4 * splits)) break;
+      if (splits > 1 && (steps < 4 * splits || (r.size == 256 && epi != EPI_STORE))) break;
       const double k = (double)((steps + splits - 1) / splits) * kBK / 1024.0;
-      const int64_t whole = tiles * splits / r.full, rest = tiles * splits % r.full;
-      double t = (double)whole * (r.fixed + more + r.slope * k);
-      if (rest > r.full / 2)
-        t += r.fixed + more + r.slope * k;
+      const double epilogue = splits > 1 ? 0 : more;
+      const int64_t whole = tiles * splits / full, rest = tiles * splits % full;
+      double t = (double)whole * (fixed + epilogue + slope * k);
+      if (rest > full / 2)
+        t += fixed + epilogue + slope * k;
       else if (rest > 0)
-        t += r.half_fixed + more + r.half_slope * k;
-      if (splits > 1) t += 5 + outs * 4 * splits * 2 / 4e6;
+        t += r.half_fixed + epilogue + (full < r.full ? 6.2 : r.half_slope) * k;
+      if (splits > 1)
+        t += (epi == EPI_STORE ? 5 : 10) + more + outs * (gate ? 2 : 1) * 4 * splits * 2 / 4e6;
       if (t < least) {
         least = t;
         best.size = r.size;
@@ -393,10 +396,12 @@ Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool fe
 int64_t part_ld(int64_t I) { return up(I, 8); }
 
 // Room for the sums of products that are split.
-size_t part_room(const Cut& c, const TileProblem* probs, int count) {
+size_t part_bytes(const Cut& c, const TileProblem& p, int arrays) {
+  return c.splits > 1 ? up((size_t)c.splits * arrays * p.J * part_ld(p.I) * sizeof(float), 256) : 0;
+}
+size_t part_room(const Cut& c, const TileProblem* probs, int count, int arrays = 1) {
   size_t bytes = 0;
-  for (int i = 0; c.splits > 1 && i < count; ++i)
-    bytes += up((size_t)c.splits * probs[i].J * part_ld(probs[i].I) * sizeof(float), 256);
+  for (int i = 0; i < count; ++i) bytes += part_bytes(c, probs[i], arrays);
   return bytes;
 }
 
@@ -452,17 +457,32 @@ int tile_of_size(const char* name, TileArgs& t, const Cut& c, char* part, Joins*
     p.splits = c.splits;
     p.part = (float*)part;
     p.part_ld = part_ld(p.I);
-    part += up((size_t)c.splits * p.J * p.part_ld * sizeof(float), 256);
-    joins->add(p);
+    part += part_bytes(c, p, EPI == EPI_GATE ? 2 : 1);
+    if (EPI == EPI_STORE) joins->add(p);
   }
   if (c.size == 64) {
     // k-contiguous: for few tokens, where three more tiles on their way are worth their LDS
     constexpr int kAhead = !AKS && !BKS ? 3 : 1;
-    return launch_tile<T, AKS, BKS, EPI, KEEP, 64, 1, 4, kAhead>(name, t, st);
+    TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 64, 1, 4, kAhead>(name, t, st)));
+  } else if (c.size == 128) {
+    TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 128, 2, 2, 1>(name, t, st)));
+  } else {
+    if constexpr (!(Kind<T>::kParts == 3 && EPI == EPI_BACK))
+      TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 256, 2, 4, 1>(name, t, st)));
   }
-  if constexpr (!(Kind<T>::kParts == 3 && EPI == EPI_BACK))
-    if (c.size == 256) return launch_tile<T, AKS, BKS, EPI, KEEP, 256, 2, 4, 1>(name, t, st);
-  return launch_tile<T, AKS, BKS, EPI, KEEP, 128, 2, 2, 1>(name, t, st);
+  if constexpr (EPI != EPI_STORE) {
+    if (c.splits > 1) {
+      const TileProblem& p = t.prob[0];
+      const int64_t blocks = ((int64_t)p.J * groups_of(p.I) * 4 + 255) / 256;
+      if (blocks == 0) return LIRPA_OK;
+      if (blocks > 0x7fffffff)
+        return fail(LIRPA_EUNSUPPORTED, "ffn_finish: more than 2^42 values");
+      return launch_k("ffn_finish", st, [&] {
+        k_ffn_finish<T, EPI, KEEP><<<(unsigned)blocks, 256, 0, st>>>(t);
+      });
+    }
+  }
+  return LIRPA_OK;
 }
 
 template <bool AKS, bool BKS, int EPI>
@@ -524,10 +544,15 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
 
 struct ForwardRoom {
   Operand x, wg, wu, wd, a;
-  Cut cut_down;
-  void* part;
+  Cut cut_gate, cut_down;
+  void *part_gate, *part_down;
   size_t bytes;
 };
+TileProblem gate_problem(const FfnPlan& pl, const ForwardRoom& r) {
+  TileProblem p = problem(pl.F, pl.rows, pl.Dp, pl.Dp);
+  add_segs(pl, p, r.wg, r.x);
+  return p;
+}
 TileProblem down_problem(const FfnPlan& pl, const ForwardRoom& r) {
   TileProblem p = problem(pl.D, pl.rows, pl.Fp, pl.Fp);
   add_segs(pl, p, r.wd, r.a);
@@ -539,9 +564,11 @@ ForwardRoom forward_room(FfnPlan& pl) {
   if (!pl.in_in_place()) r.wg = pl.own(pl.F, pl.D), r.wu = pl.own(pl.F, pl.D);
   if (!pl.down_in_place()) r.wd = pl.own(pl.D, pl.F);
   r.a = pl.own(pl.rows, pl.F);
-  const TileProblem down = down_problem(pl, r);
+  const TileProblem gate = gate_problem(pl, r), down = down_problem(pl, r);
+  r.cut_gate = cut_of(&gate, 1, EPI_GATE, true, true);
+  r.part_gate = pl.ws.take(part_room(r.cut_gate, &gate, 1, 2));
   r.cut_down = cut_of(&down, 1, EPI_STORE, true, true);
-  r.part = pl.ws.take(part_room(r.cut_down, &down, 1));
+  r.part_down = pl.ws.take(part_room(r.cut_down, &down, 1));
   r.bytes = pl.ws.at;
   return r;
 }
@@ -567,8 +594,7 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
 
   TileArgs t = tile_args(pl, keep);
   TileProblem& p = t.prob[0];
-  p = problem(pl.F, rows, pl.Dp, pl.Dp);
-  add_segs(pl, p, r.wg, r.x);
+  p = gate_problem(pl, r);
   for (int s = 0; s < p.nseg; ++s) t.A2[s] = r.wu.p + (p.A[s] - r.wg.p);
   p.out = (void*)r.a.p;
   p.ldo = r.a.ld;
@@ -578,24 +604,29 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   t.u = u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, cut_of(&p, 1, EPI_GATE, true, true),
-                                          nullptr, nullptr, st)));
+  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, r.cut_gate, r.part_gate, nullptr,
+                                          st)));
 
   Joins joins;
   t = tile_args(pl, LIRPA_KEEP_NONE);
   t.prob[0] = down_problem(pl, r);
   t.prob[0].out = out;
   t.prob[0].ldo = ldo;
-  TRY((run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, r.cut_down, r.part, &joins, st)));
+  TRY((run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, r.cut_down, r.part_down, &joins, st)));
   return joins.run(pl, st);
 }
 
 struct BackwardRoom {
   Operand dout, x, wg, wu, wd, a, dg, du;
-  Cut cut_dx, cut_dw;
-  void *part_dx, *part_dw;
+  Cut cut_gate, cut_dx, cut_dw;
+  void *part_gate, *part_dx, *part_dw;
   size_t bytes;
 };
+TileProblem da_problem(const FfnPlan& pl, const BackwardRoom& r) {
+  TileProblem p = problem(pl.F, pl.rows, pl.D, pl.Dp);
+  add_segs(pl, p, r.wd, r.dout);
+  return p;
+}
 TileProblem dx_problem(const FfnPlan& pl, const BackwardRoom& r) {
   TileProblem p = problem(pl.D, pl.rows, pl.F, pl.Fp);
   add_segs(pl, p, r.wg, r.dg);
@@ -632,7 +663,9 @@ BackwardRoom backward_room(FfnPlan& pl, bool packed_x) {
   r.a = pl.own(pl.rows, pl.F);
   r.dg = pl.own(pl.rows, pl.F);
   r.du = pl.own(pl.rows, pl.F);
-  const TileProblem dx = dx_problem(pl, r);
+  const TileProblem da = da_problem(pl, r), dx = dx_problem(pl, r);
+  r.cut_gate = cut_of(&da, 1, EPI_BACK, !pl.f32, false);
+  r.part_gate = pl.ws.take(part_room(r.cut_gate, &da, 1));
   r.cut_dx = cut_of(&dx, 1, EPI_STORE, true, false);
   r.part_dx = pl.ws.take(part_room(r.cut_dx, &dx, 1));
   // cut as if all three were wanted: a gradient does not depend on which others are
@@ -669,8 +702,7 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
   // act(g) u, dg and du
   TileArgs t = tile_args(pl, keep);
   TileProblem& p = t.prob[0];
-  p = problem(pl.F, rows, pl.D, pl.Dp);
-  add_segs(pl, p, r.wd, r.dout);
+  p = da_problem(pl, r);
   p.out = dWd ? (void*)r.a.p : nullptr;
   p.ldo = r.a.ld;
   p.plane = r.a.plane;
@@ -681,8 +713,8 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
   t.u = (void*)u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, cut_of(&p, 1, EPI_BACK, !pl.f32, false),
-                                         nullptr, nullptr, st)));
+  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, r.cut_gate, r.part_gate, nullptr,
+                                         st)));
 
   Joins joins;
   if (dx) {

@@ -42,8 +42,9 @@ struct TileProblem {
   int I, J;            // output sizes
   int tiles_i, tiles_j;
   int first;           // block of its first tile
-  int splits;          // EPI_STORE: blocks that share a tile's k; over 1, their sums go to
-  float* part;         // part[split][J][part_ld] and are added by k_ffn_join
+  int splits;          // blocks that share a tile's k; over 1, their sums go to
+  float* part;         // part[split][J][part_ld] (EPI_GATE: [split][2][J][part_ld], g and u) and
+                       // are added by k_ffn_join or k_ffn_finish
   int64_t part_ld;
   void* out;           // the tensors' type (EPI_STORE), else an operand of a later product
   int64_t ldo;         // elements
@@ -364,6 +365,59 @@ struct Kept8<T, 8> {
   __device__ __forceinline__ void values(float (&v)[8]) const { unpack8(w, e, v); }
 };
 
+// The epilogues on eight consecutive features of a token.  Every lane of the wave comes here, `in`
+// where its token exists.
+
+// act(g) u and what is kept; x: g.
+template <typename T>
+__device__ __forceinline__ void finish_gate(const TileArgs& a, const TileProblem& p, int64_t row,
+                                            const Piece8& at, bool in, float (&x)[8],
+                                            float (&u)[8]) {
+  if (a.keep >= 0) {
+    keep8<T>(p, a.keep, a.g, a.ge, row, at, x);
+    keep8<T>(p, a.keep, a.u, a.ue, row, at, u);
+  }
+  if (!in || at.col >= p.pad_i) return;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    float act, slope;
+    gate_fn(a.gate, Kind<T>::kParts == 1, x[r], act, slope);
+    u[r] *= act;
+  }
+  put_operand<T>(p, p.out, row, at, u);
+}
+
+// act(g) u, dg and du; x: da.
+template <typename T, int KEEP>
+__device__ __forceinline__ void finish_back(const TileArgs& a, const TileProblem& p, int64_t row,
+                                            const Piece8& at, bool in, float (&x)[8],
+                                            const Kept8<T, KEEP>& kept_g,
+                                            const Kept8<T, KEEP>& kept_u) {
+  if (!in || at.col >= p.pad_i) return;
+  float g[8], u[8], v[8];
+  kept_g.values(g);
+  kept_u.values(u);
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    float act, slope;
+    gate_fn(a.gate, Kind<T>::kParts == 1, g[r], act, slope);
+    v[r] = act * u[r];
+    g[r] = x[r] * act;
+    x[r] *= u[r] * slope;
+  }
+  if (p.out) put_operand<T>(p, p.out, row, at, v);
+  if (a.dg) put_operand<T>(p, a.dg, row, at, x);
+  if (a.du) put_operand<T>(p, a.du, row, at, g);
+}
+
+// The sums of a block that shares its tile's k.  which: 0, or 1 for u of EPI_GATE.
+template <int ARRAYS>
+__device__ __forceinline__ void put_part(const TileProblem& p, int split, int which, int64_t row,
+                                         const Piece8& at, const float (&x)[8]) {
+  float* to = p.part + ((int64_t)(split * ARRAYS + which) * p.J + row) * p.part_ld;
+  store_row<float, 8>(to + (at.token * (uint32_t)p.part_ld + at.col), p.I - at.col, x);
+}
+
 // BI x BJ output tile, WI x WJ waves.  EPI_GATE: the tile's A rows are BI / 2 of Wg and the same
 // BI / 2 of Wu, and a wave owns both projections of its features.
 // KEEP: what was kept (EPI_BACK), 0 or 8.
@@ -390,8 +444,10 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     while (which + 1 < a.count && id >= a.prob[which + 1].first) ++which;
   const TileProblem& p = a.prob[which];
   id -= p.first;
+  // the larger tile's other epilogues leave no registers for it
+  constexpr bool kMaySplit = EPI == EPI_STORE || BI < 256;
   int split = 0;
-  if constexpr (EPI == EPI_STORE) {
+  if constexpr (kMaySplit) {
     split = id / (p.tiles_i * p.tiles_j);
     id -= split * (p.tiles_i * p.tiles_j);
   }
@@ -424,7 +480,7 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
   const int K = max(p.KA, p.KB);
   const int per_seg = (K + kBK - 1) / kBK;
   int steps = per_seg * p.nseg, first_seg = 0, first_k = 0;
-  if constexpr (EPI == EPI_STORE) {
+  if constexpr (kMaySplit) {
     if (p.splits > 1) {
       const int each = (steps + p.splits - 1) / p.splits, from = min(split * each, steps);
       steps = min(each, steps - from);
@@ -447,7 +503,7 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
           first};
   Next nb{first_seg, p.KB - first_k * kBK, p.B[first_seg] + corner_b + first_k * next_b,
           nullptr, first + kUnit};
-  if constexpr (EPI == EPI_GATE) na.p2 = a.A2[0] + corner_a;
+  if constexpr (EPI == EPI_GATE) na.p2 = a.A2[first_seg] + corner_a + first_k * next_a;
   constexpr int kCopiesA = (EPI == EPI_GATE ? 2 : 1) * decltype(bring_a)::kLoads;
   constexpr int kCopiesB = decltype(bring_b)::kLoads;
   auto bring_a_part = [&](int r) {
@@ -602,43 +658,26 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
         read8(turned + t * kRow + f, x);
         if constexpr (EPI == EPI_STORE) {
           if (!in) return;
-          if (p.splits > 1) {
-            float* to = p.part + ((int64_t)split * p.J + row) * p.part_ld;
-            store_row<float, 8>(to + (at.token * (uint32_t)p.part_ld + at.col), p.I - at.col, x);
-          } else {
+          if (p.splits > 1)
+            put_part<1>(p, split, 0, row, at, x);
+          else
             put_output<T>(p, p.out, p.ldo, row, at, x);
-          }
         } else if constexpr (EPI == EPI_GATE) {
           float u[8];
           read8(turned + t * kRow + kPieces * 8 + f, u);
-          if (a.keep >= 0) {
-            keep8<T>(p, a.keep, a.g, a.ge, row, at, x);
-            keep8<T>(p, a.keep, a.u, a.ue, row, at, u);
+          if (kMaySplit && p.splits > 1) {
+            if (!in) return;
+            put_part<2>(p, split, 0, row, at, x);
+            put_part<2>(p, split, 1, row, at, u);
+          } else {
+            finish_gate<T>(a, p, row, at, in, x, u);
           }
-          if (!in || at.col >= p.pad_i) return;
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            float act, slope;
-            gate_fn(a.gate, Kind<T>::kParts == 1, x[r], act, slope);
-            u[r] *= act;
-          }
-          put_operand<T>(p, p.out, row, at, u);
         } else {
-          if (!in || at.col >= p.pad_i) return;
-          float g[8], u[8], v[8];
-          kept_g.values(g);
-          kept_u.values(u);
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            float act, slope;
-            gate_fn(a.gate, Kind<T>::kParts == 1, g[r], act, slope);
-            v[r] = act * u[r];
-            g[r] = x[r] * act;
-            x[r] *= u[r] * slope;
+          if (kMaySplit && p.splits > 1) {
+            if (in) put_part<1>(p, split, 0, row, at, x);
+          } else {
+            finish_back<T, KEEP>(a, p, row, at, in, x, kept_g, kept_u);
           }
-          if (p.out) put_operand<T>(p, p.out, row, at, v);
-          if (a.dg) put_operand<T>(p, a.dg, row, at, x);
-          if (a.du) put_operand<T>(p, a.du, row, at, g);
         }
       };
       if constexpr (Kind<T>::kParts == 1) {
@@ -703,6 +742,53 @@ __global__ __launch_bounds__(256) void k_ffn_join(JoinJobs jobs) {
       }
   }
   store_row<W, 8>((W*)o.out + row * o.ldo + col, o.I - col, sum);
+}
+
+// The epilogue of a gate product whose tiles' k was shared.  Bound by bytes.
+template <typename T, int EPI, int KEEP>
+__global__ __launch_bounds__(256) void k_ffn_finish(TileArgs a) {
+  const TileProblem& p = a.prob[0];
+  constexpr int kArrays = EPI == EPI_GATE ? 2 : 1;
+  const int groups = groups_of(p.I), per_row = groups * 4;  // groups of lanes stay together
+  const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;
+  const uint32_t from = (uint32_t)(first - row0 * per_row) + threadIdx.x;
+  Piece8 at;
+  at.token = from / (uint32_t)per_row;
+  at.col = (int)(from - at.token * (uint32_t)per_row) * 8;
+  at.q = at.token * groups * kGroup + at.col;
+  at.e = at.token * groups + at.col / kGroup;
+  const bool in = row0 + at.token < p.J;
+  Kept8<T, KEEP> kg, ku;
+  if constexpr (EPI == EPI_BACK) {
+    kg.load(p, a.g, a.ge, row0, at);
+    ku.load(p, a.u, a.ue, row0, at);
+  }
+  float sum[kArrays][8] = {};
+  if (in && at.col < p.I) {
+    const float* part = p.part + (row0 + at.token) * p.part_ld + at.col;
+    const int64_t next = p.J * p.part_ld;
+    for (int s = 0; s < p.splits; s += 4) {  // four on their way; past the end the last one again
+      float x[4][kArrays][8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int w = 0; w < kArrays; ++w)
+          load_row<float, 8>(part + ((int64_t)min(s + i, p.splits - 1) * kArrays + w) * next,
+                             p.I - at.col, x[i][w]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (s + i < p.splits) {
+#pragma unroll
+          for (int w = 0; w < kArrays; ++w)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) sum[w][r] += x[i][w][r];
+        }
+    }
+  }
+  if constexpr (EPI == EPI_GATE)
+    finish_gate<T>(a, p, row0, at, in, sum[0], sum[1]);
+  else
+    finish_back<T, KEEP>(a, p, row0, at, in, sum[0], kg, ku);
 }
 
 // Copies [rows][n] into [rows][ld] 16-bit operands, columns from n to ld cleared; a 32-bit source
