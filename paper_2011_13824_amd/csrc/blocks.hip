@@ -507,7 +507,8 @@ int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, const Cut& cut, v
 // are copied.
 constexpr int kFewest = 8, kFewRows = 64;
 
-template <typename T, int TJ>
+// GATE: waves a block of the gate product (16 of the down product); UN: steps in flight.
+template <typename T, int TJ, int GATE, int UN>
 int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, void* out,
                 int64_t ldo, void* hidden, hipStream_t st) {
   FewArgs a{};
@@ -523,11 +524,8 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   a.gate = f->gate;
   a.out = hidden;
   a.ldo = f->n_hidden;
-  // waves a block and steps in flight, in us for 1 token of 4096 x 10944 in bf16: gate 16 waves
-  // 36.5, 8 39.5; both 16: 57.1, both 8: 62.6; with 64 tokens 4 and 16: 129, both 8: 166
-  constexpr int UN = TJ == 1 ? 4 : 2, kGate = TJ == 1 ? 16 : TJ == 2 ? 8 : 4;
   TRY(launch_k("ffn_few_gate", st, [&] {
-    k_ffn_few<T, true, TJ, kGate, UN><<<(a.I + 15) / 16, kGate * 64, 0, st>>>(a);
+    k_ffn_few<T, true, TJ, GATE, UN><<<(a.I + 15) / 16, GATE * 64, 0, st>>>(a);
   }));
   a.A = f->Wd;
   a.lda = f->ldd;
@@ -580,9 +578,17 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   if (keep == LIRPA_KEEP_NONE && rows <= (in && down ? kFewest : kFewRows))
     return by_type(f->dtype, [&](auto t) {
       using T = decltype(t);
-      if (rows <= 16) return few_forward<T, 1>(f, rows, x, ldx, out, ldo, ws, st);
-      if (rows <= 32) return few_forward<T, 2>(f, rows, x, ldx, out, ldo, ws, st);
-      return few_forward<T, 4>(f, rows, x, ldx, out, ldo, ws, st);
+      // Large weights keep the memory busy with more on the way, small ones are done sooner with
+      // fewer steps.  1 token, us with gate waves x steps in flight 8 x 2 / 8 x 4 / 16 x 4: 4096 x
+      // 10944 bf16 58.5 / - / 57.1, float 123 / 108 / 109; 1024 x 2752 bf16 10.4 / 11.2 / 13.6,
+      // float 18.2 / 19.4 / 23.0; 512 x 4400 float 17.9 / 23.1 / 27.8.
+      constexpr int kLargeGate = sizeof(T) == 2 ? 16 : 8;
+      const bool large = 3 * pl.D * pl.F * (int64_t)sizeof(T) >= (int64_t)64 << 20;
+      if (rows <= 16 && large)
+        return few_forward<T, 1, kLargeGate, 4>(f, rows, x, ldx, out, ldo, ws, st);
+      if (rows <= 16) return few_forward<T, 1, 8, 2>(f, rows, x, ldx, out, ldo, ws, st);
+      if (rows <= 32) return few_forward<T, 2, 8, 2>(f, rows, x, ldx, out, ldo, ws, st);
+      return few_forward<T, 4, 4, 2>(f, rows, x, ldx, out, ldo, ws, st);
     });
   ForwardRoom r = forward_room(pl);
   Copies copies;
