@@ -267,7 +267,10 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
  * - `dtype` is the type of every tensor of a call unless a parameter says otherwise.  Products
  *   of 16-bit types run on their matrix instructions with 32-bit sums; LIRPA_F32 operands are
  *   split into three bf16 parts each (24 bits), and the six products of the largest parts are
- *   summed in 32 bits.  Sums, norms and their reductions are held in 32 bits.
+ *   summed in 32 bits (an infinity then comes out as a NaN where its product with a smaller part
+ *   has the other sign); up to 64 tokens whose projections are not kept, they are multiplied in 32
+ *   bits.  Sums, norms and their reductions are held in 32 bits.
+ * - These calls take none of the inputs that LIRPA_VALIDATE checks, and report no findings.
  * - A matrix has contiguous rows; `ld` is the distance of two rows in elements (at least the
  *   row's length, less than 2^22).  Any alignment of the element type is taken; rows that start
  *   on 16 bytes and whose length is a multiple of 8 elements are read in place, others are
@@ -287,7 +290,8 @@ typedef enum { LIRPA_GATE_RELU = 0, LIRPA_GATE_SILU = 1, LIRPA_GATE_GELU = 2 } l
  * the least whole number in [-120, 121] with 127 * 2^e >= the group's largest magnitude, and a
  * value is held as the nearest whole multiple of it (ties to even); magnitudes over 127 * 2^121
  * are held as that.  The buffer is
- *     int8   [rows][groups * 32]   groups = ceil(n / 32); columns past n are 0
+ *     int8   [rows][groups * 32]   groups = ceil(n / 32); columns past n are 0 (any value in a
+ *                                  group without values)
  *     uint8  [rows][groups]        e + 127; 255 marks a group with an infinity or a NaN, all of
  *                                  which reads back as NaN
  * and starts on 16 bytes.  A multiple of at most 127 with a power-of-two scale is exact in bf16

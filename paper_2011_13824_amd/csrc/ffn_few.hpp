@@ -1,9 +1,14 @@
 // The feed-forward block for few tokens (a model that answers): every weight is read once.
 //
-// Bound by the weights' bytes.  A block takes 16 features; its waves take the k axis in turn, 32 k
-// a step, read the weights' rows straight into the registers of a 16-row matrix instruction
-// (nothing is shared between waves, so LDS would add a trip), and add their sums in LDS in order.
-// Tokens fill the other side of the instruction, 16 at a time; lanes past the last one repeat it.
+//   h = act(x Wg^T) * (x Wu^T),  out = h Wd^T
+//
+// Bound by the weights' bytes, and by latency where they are small.  A block takes 16 features; its
+// waves take the k axis in turn, 32 k a step, read the weights' rows straight into the registers of
+// a 16-row matrix instruction (nothing is shared between waves, so LDS would add a trip), and add
+// their sums in LDS in order.  Tokens fill the other side of the instruction, 16 at a time; lanes
+// past the last one repeat it.  Weights are read where they lie at any alignment, and in 32 bits
+// with the 32-bit instruction: three bf16 parts would be more bytes.  One token of 4096 x 10944 in
+// bf16: 57 us, 4.7 TB/s of the 5.1 that a large copy reaches.
 #pragma once
 
 #include "ffn_tile.hpp"

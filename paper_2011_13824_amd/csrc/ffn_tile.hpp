@@ -1,6 +1,9 @@
 // Matrix products of the gated feed-forward block on 16-bit matrix instructions.
 //
 //   C[j][i] = sum over segments s and k of A_s(i, k) * B_s(j, k),  32-bit sums
+//   out = (act(x Wg^T) * (x Wu^T)) Wd^T
+//   da = dout Wd, dg = da u act'(g), du = da act(g)
+//   dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x, dWd = dout^T (act(g) u)
 //
 // i runs over the contiguous dimension of the output (features), j over its rows (tokens).  An
 // operand is stored k-contiguous ([i][k]) or k-strided ([k][i]); the second kind is transposed on
@@ -11,11 +14,34 @@
 //   down          A = Wd (k-contiguous)          B = act(g) u              EPI_STORE
 //   da            A = Wd (k-strided)             B = dout                  EPI_BACK
 //   dx            A = Wg, Wu (k-strided)         B = dg, du                EPI_STORE, two segments
-//   dWg, dWu      A = x (k-strided)              B = dg, du (k-strided)    EPI_STORE, two batches
-//   dWd           A = act(g) u (k-strided)       B = dout (k-strided)      EPI_STORE
+//   dWg, dWu      A = x (k-strided)              B = dg, du (k-strided)    EPI_STORE, one launch
+//   dWd           A = act(g) u (k-strided)       B = dout (k-strided)      EPI_STORE, with them
 //
 // 32-bit operands are three bf16 parts (hi + mid + lo = 24 bits); a product is then six segments,
-// those of the largest parts, smallest first, and the error stays that of a 32-bit sum.
+// those of the largest parts, smallest first, and the error stays that of a 32-bit sum (4e-7 of
+// the result's norm against 64 bits, where a library's 32-bit product has 1.3e-6).  Their rate
+// counts a sixth: six bf16 products at 1.2 PFLOP/s, where the 32-bit matrix instruction ends at
+// 157 TFLOP/s.
+//
+// act(g) u, dg and du are rounded to the tensors' type between two products: they are operands of
+// 16-bit instructions.  That is one more rounding of 2^-9 (bf16) in each result, of random sign.
+//
+// How the loop is fed (8192^3 in bf16 on one MI355X, TFLOP/s; the matrix instructions alone reach
+// 1640 to 1930 there, a third less with random operands than with zeros, for power):
+//  - Two stages of 64 k, copied into LDS at once, fragments read when needed: 1109 (both operands
+//    k-contiguous), 1028 (both k-strided).
+//  - Copies go from memory straight into LDS.  Rows of 64 bytes a copy reach 17 to 22 TB/s over the
+//    chip, rows of 128 bytes and more 32 to 34: a tile is 64 k, 128 bytes of a row.
+//  - A copy that finds the address unit busy holds back everything its wave issues after it, so a
+//    burst of copies stops the matrix instructions.  They are issued one by one between them.
+//  - Fragments are read half a tile ahead into registers of their own, and a barrier a tile is
+//    left.  LDS holds five units (a tile of one operand each), A and B in turn, so that copies are
+//    one to one and a half tiles ahead: 1264 and 1366.
+//  - 8 waves of 128 x 64 rather than 4 of 128 x 128, which read a third less from LDS: two waves a
+//    SIMD hide each other's waits, and four waves' sums do not fit beside their fragments without
+//    moves (988 as built by the compiler).
+// A large library product reaches 1400 to 1445 with k-contiguous operands, 1088 to 1170 with
+// k-strided ones.
 #pragma once
 
 #include <type_traits>
@@ -28,8 +54,7 @@ enum Epi { EPI_STORE, EPI_GATE, EPI_BACK };
 enum Gate { RELU = 0, SILU = 1, GELU = 2 };
 
 constexpr int kMaxSegs = 12;
-constexpr int kBK = 64;    // k a tile: 128 bytes of a k-contiguous row, the width of a cache line
-
+constexpr int kBK = 64;  // k a tile: 128 bytes of a k-contiguous row, the width of a cache line
 constexpr int kMaxProblems = 3;
 
 // One product.
@@ -187,8 +212,9 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) s16x8 lds_s16x8;
 
 // Where an operand's tile (R rows of i or j, kBK of k) lies in LDS.
-//   k-contiguous: row r is 4 pieces of 16 bytes, piece p at p ^ (r / 2 % 4): the 16 rows that one
-//   read takes then start in 16 different 16-byte columns of the 256 bytes of banks.
+//   k-contiguous: row r is 8 pieces of 16 bytes, piece p at p ^ (r / 2 % 8): the 16 rows that one
+//   read takes then start in 16 different 16-byte columns of the 256 bytes of banks (without it a
+//   read takes 4 cycles more).
 //   k-strided: line k is R / 8 pieces, piece p at p ^ 2 f(k), f(k) = k % 4 + 4 (k / 8 % 2): a
 //   transposing read takes 32 bytes of 4 lines, from 2 groups of lanes at k and k + 8.  Two lines
 //   of 8 pieces fill the banks, and f(k) = k / 2 % 2 + 2 (k / 8 % 2) does.
@@ -420,9 +446,16 @@ __device__ __forceinline__ void put_part(const TileProblem& p, int split, int wh
 
 // BI x BJ output tile, WI x WJ waves.  EPI_GATE: the tile's A rows are BI / 2 of Wg and the same
 // BI / 2 of Wu, and a wave owns both projections of its features.
-// KEEP: what was kept (EPI_BACK), 0 or 8.
-template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ, int AHEAD>
-__global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 2) void k_ffn_tile(TileArgs a) {
+// KEEP: what was kept (EPI_BACK), 0 or 8.  AHEAD: whole tiles on their way.
+//
+// Bound by the matrix instructions (busy 62 to 74 % of the cycles at 8192 tokens, 4096 x 10944 in
+// bf16: gate and up 1.21 ms, 1218 TFLOP/s; down 0.54 ms, 1354; dx 1.03 ms, 1420; the three weight
+// gradients 1.77 ms, 1244), and, for da, by its epilogue (0.79 ms, 930 TFLOP/s, busy 47 %): there
+// all CUs come to read what was kept and to write three operands at the same time, 0.72 GB in all.
+// Few tokens are bound by the weights' bytes (64 tokens: 4.7 TB/s in gate and up).
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ,
+          int AHEAD>
+__global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_tile(TileArgs a) {
   constexpr int kThreads = WI * WJ * 64;
   constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;  // fragments of a wave
   constexpr int kTileA = Lay<AKS, BI>::kBytes, kTileB = Lay<BKS, BJ>::kBytes;
@@ -451,7 +484,7 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
     split = id / (p.tiles_i * p.tiles_j);
     id -= split * (p.tiles_i * p.tiles_j);
   }
-  constexpr int kBand = 8;
+  constexpr int kBand = 8;  // 4 and 16 within 1 %, 32 up to a quarter slower
   const int band = id / (kBand * p.tiles_i), in_band = id - band * kBand * p.tiles_i;
   const int height = min(kBand, p.tiles_j - band * kBand);
   const int ti = in_band / height, tj = band * kBand + in_band - ti * height;
@@ -701,7 +734,7 @@ __global__ __launch_bounds__(WI* WJ * 64, BI* BJ == 65536 && WI * WJ == 4 ? 1 : 
 }
 
 // Adds the sums of the blocks that shared a tile's k, in order, for all split products of a call.
-// Bound by bytes.
+// Bound by bytes (100 MB of sums and 40 MB out: 38 us).
 struct JoinJob {
   const float* part;
   void* out;
@@ -793,7 +826,8 @@ __global__ __launch_bounds__(256) void k_ffn_finish(TileArgs a) {
 
 // Copies [rows][n] into [rows][ld] 16-bit operands, columns from n to ld cleared; a 32-bit source
 // becomes three bf16 parts, a packed one (8 bits) is read back.  All operands of a call in one
-// launch: they are often small, and a launch then costs more than the copy.  Bound by bytes.
+// launch: they are often small, and a launch then costs more than the copy.  Bound by bytes (39 MB
+// of floats into 58 MB of parts: 23 us, 4.3 TB/s).
 struct OperandJob {
   const void* x;
   const uint8_t* exps;  // of a packed source (x: its int8 values), which one part holds
