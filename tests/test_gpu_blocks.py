@@ -432,6 +432,28 @@ def test_ffn_large_tiles(B, dtype, rows, D, F):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("keep", [8, 0])
+def test_ffn_largest_tiles(B, dtype, keep):
+    """Enough work for the largest tiles in every product, ragged on every side."""
+    g = gen_of(40)
+    rows, D, F = 4090, 4072, 4088
+    x, dout, W = rand(g, rows, D, dtype=dtype), rand(g, rows, D, dtype=dtype), weights(g, D, F,
+                                                                                     dtype)
+    ffn = B.FeedForward(*W, "gelu")
+    out, tol, *_ = forward64(x, W, "gelu", UNIT[dtype])
+    got, kept = ffn.forward(x, keep=keep)
+    tiny = TINY[dtype] * 100
+    check(got, out, tol + tiny, "out")
+    del out, tol
+    vx, vg, vu = ((t.values() for t in (kept.x, kept.g, kept.u)) if keep == 8
+                  else (kept.x, kept.g, kept.u))
+    grads = ffn.backward(dout, kept)
+    want, tol = backward64(dout, vx, vg.double(), vu.double(), W, "gelu", UNIT[dtype])
+    for name in want:
+        check(grads[name], want[name], tol[name] + tiny * 100, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
 @pytest.mark.parametrize("rows", [3, 90])
 def test_ffn_weights_of_different_strides(B, dtype, rows):
     """Wg and Wu with row distances of their own, one of them unaligned, Wd a view of a wider one."""
