@@ -319,7 +319,7 @@ TileArgs tile_args(const FfnPlan& pl, int keep) {
 // number of blocks that share a tile's k, whose sums are then added by k_ffn_join.
 struct Cut {
   int size = 128;
-  int splits = 1;
+  int splits[kMaxProblems] = {1, 1, 1, 1};
 };
 
 // What a round of blocks over the 256 CUs takes: fixed + slope * k us for k in thousands, when it is
@@ -351,15 +351,14 @@ int64_t steps_of(const TileProblem& p) {
 // `may_large`: not the epilogue of da in 32 bits, which does not fit the larger tile's registers.
 Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool few) {
   const bool gate = epi == EPI_GATE;
-  int64_t steps = 0;
-  double outs = 0;
+  int64_t steps[kMaxProblems], longest = 1;
   for (int i = 0; i < count; ++i) {
-    steps = std::max(steps, steps_of(probs[i]));
-    outs += (double)probs[i].I * probs[i].J;
+    steps[i] = steps_of(probs[i]);
+    longest = std::max(longest, steps[i]);
   }
+  const bool weights = few && probs[0].J <= 64;
   Cut best;
   double least = 1e300;
-  const bool weights = few && probs[0].J <= 64;
   for (const Round& r : kRounds) {
     if (r.size == 256 && !may_large) continue;
     if (r.size > 64 && weights) continue;
@@ -368,25 +367,49 @@ Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool fe
     const int full = r.size == 64 && few ? r.full / 2 : r.full;
     const double fixed = full < r.full ? r.half_fixed : r.fixed;
     const double slope = full < r.full ? r.half_slope : r.slope;
-    int64_t tiles = 0;
-    for (int i = 0; i < count; ++i) tiles += tiles_of(probs[i], r.size, gate);
     const double more = gate ? r.gate : epi == EPI_BACK ? r.back : 0;
-    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
-      if (splits > 1 && (steps < 4 * splits || (r.size == 256 && epi != EPI_STORE))) break;
-      const double k = (double)((steps + splits - 1) / splits) * kBK / 1024.0;
-      const double epilogue = splits > 1 ? 0 : more;
-      const int64_t whole = tiles * splits / full, rest = tiles * splits % full;
-      double t = (double)whole * (fixed + epilogue + slope * k);
-      if (rest > full / 2)
-        t += fixed + epilogue + slope * k;
-      else if (rest > 0)
-        t += r.half_fixed + epilogue + (full < r.full ? 6.2 : r.half_slope) * k;
-      if (splits > 1)
-        t += (epi == EPI_STORE ? 5 : 10) + more + outs * (gate ? 2 : 1) * 4 * splits * 2 / 4e6;
+    int64_t tiles[kMaxProblems];
+    for (int i = 0; i < count; ++i) tiles[i] = tiles_of(probs[i], r.size, gate);
+    for (int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+      if (parts > 1 && (longest < 4 * parts || (r.size == 256 && epi != EPI_STORE))) break;
+      // blocks of about as many steps each, whichever product they are of
+      const int64_t target = (longest + parts - 1) / parts;
+      Cut c;
+      c.size = r.size;
+      int64_t blocks = 0;
+      double sums = 0, k[kMaxProblems], longest_k = 0, shortest_k = 1e9;
+      for (int i = 0; i < count; ++i) {
+        c.splits[i] = (int)std::max<int64_t>(1, (steps[i] + target - 1) / target);
+        k[i] = (double)((steps[i] + c.splits[i] - 1) / c.splits[i]) * kBK / 1024.0;
+        longest_k = std::max(longest_k, k[i]);
+        shortest_k = std::min(shortest_k, k[i]);
+        blocks += tiles[i] * c.splits[i];
+        if (c.splits[i] > 1)
+          sums += (double)probs[i].I * probs[i].J * (gate ? 2 : 1) * c.splits[i];
+      }
+      const double base = fixed + (sums > 0 ? 0 : more);
+      const double half = r.half_fixed + (sums > 0 ? 0 : more) +
+                          (full < r.full ? 6.2 : r.half_slope) * longest_k;
+      const int64_t whole = blocks / full, rest = blocks % full;
+      double t;
+      if (blocks <= full / 2) {
+        t = half;
+      } else if (longest_k == shortest_k || blocks <= full) {
+        t = (double)whole * (base + slope * longest_k);
+        if (rest > full / 2)
+          t += base + slope * longest_k;
+        else if (rest > 0)
+          t += half;
+      } else {  // blocks of several lengths, the shortest last: half of one is lost at the end
+        t = 0.5 * (base + slope * shortest_k);
+        for (int i = 0; i < count; ++i)
+          t += (double)(tiles[i] * c.splits[i]) / full * (base + slope * k[i]);
+        t = std::max(t, base + slope * longest_k);
+      }
+      if (sums > 0) t += (epi == EPI_STORE ? 5 : 10) + more + sums * 4 * 2 / 4e6;
       if (t < least) {
         least = t;
-        best.size = r.size;
-        best.splits = splits;
+        best = c;
       }
     }
   }
@@ -396,13 +419,22 @@ Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool fe
 int64_t part_ld(int64_t I) { return up(I, 8); }
 
 // Room for the sums of products that are split.
-size_t part_bytes(const Cut& c, const TileProblem& p, int arrays) {
-  return c.splits > 1 ? up((size_t)c.splits * arrays * p.J * part_ld(p.I) * sizeof(float), 256) : 0;
+size_t part_bytes(int splits, const TileProblem& p, int arrays) {
+  return splits > 1 ? up((size_t)splits * arrays * p.J * part_ld(p.I) * sizeof(float), 256) : 0;
 }
 size_t part_room(const Cut& c, const TileProblem* probs, int count, int arrays = 1) {
   size_t bytes = 0;
-  for (int i = 0; i < count; ++i) bytes += part_bytes(c, probs[i], arrays);
+  for (int i = 0; i < count; ++i) bytes += part_bytes(c.splits[i], probs[i], arrays);
   return bytes;
+}
+
+// Takes a product's split and its part of the room.
+void split(TileProblem& p, int splits, char*& part, int arrays = 1) {
+  p.splits = splits;
+  if (splits == 1) return;
+  p.part = (float*)part;
+  p.part_ld = part_ld(p.I);
+  part += part_bytes(splits, p, arrays);
 }
 
 // What the split products of a call leave to be added.
@@ -428,9 +460,10 @@ struct Joins {
   }
 };
 
-template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int SIZE, int WI, int WJ, int AHEAD>
-int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
-  int64_t total = 0;
+// Numbers the tiles; `total` blocks.
+template <int SIZE, int EPI>
+int lay_out(const char* name, TileArgs& t, int64_t& total) {
+  total = 0;
   for (int i = 0; i < t.count; ++i) {
     TileProblem& p = t.prob[i];
     const int64_t feat = EPI == EPI_GATE ? SIZE / 2 : SIZE;
@@ -439,12 +472,19 @@ int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
       return fail(LIRPA_EUNSUPPORTED, "%s: more than 2^31 tiles", name);
     p.tiles_i = (int)ti;
     p.tiles_j = (int)tj;
-    p.first = (int)total;
+    p.first = (unsigned)total;
     total += ti * tj * p.splits;
   }
+  return LIRPA_OK;
+}
+
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int SIZE, int WI, int WJ, int AHEAD>
+int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
+  int64_t total;
+  TRY((lay_out<SIZE, EPI>(name, t, total)));
   if (total == 0) return LIRPA_OK;
   return launch_k(name, st, [&] {
-    k_ffn_tile<T, AKS, BKS, EPI, KEEP, SIZE, SIZE, WI, WJ, AHEAD>
+    k_ffn_tile<T, AKS, BKS, EPI, KEEP, SIZE, WI, WJ, AHEAD>
         <<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);
   });
 }
@@ -452,14 +492,9 @@ int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
 template <typename T, bool AKS, bool BKS, int EPI, int KEEP>
 int tile_of_size(const char* name, TileArgs& t, const Cut& c, char* part, Joins* joins,
                  hipStream_t st) {
-  for (int i = 0; c.splits > 1 && i < t.count; ++i) {
-    TileProblem& p = t.prob[i];
-    p.splits = c.splits;
-    p.part = (float*)part;
-    p.part_ld = part_ld(p.I);
-    part += part_bytes(c, p, EPI == EPI_GATE ? 2 : 1);
-    if (EPI == EPI_STORE) joins->add(p);
-  }
+  TileProblem& p = t.prob[0];
+  split(p, c.splits[0], part, EPI == EPI_GATE ? 2 : 1);
+  if (EPI == EPI_STORE && p.splits > 1) joins->add(p);
   if (c.size == 64) {
     // k-contiguous: for few tokens, where three more tiles on their way are worth their LDS
     constexpr int kAhead = !AKS && !BKS ? 3 : 1;
@@ -471,8 +506,7 @@ int tile_of_size(const char* name, TileArgs& t, const Cut& c, char* part, Joins*
       TRY((launch_tile<T, AKS, BKS, EPI, KEEP, 256, 2, 4, 1>(name, t, st)));
   }
   if constexpr (EPI != EPI_STORE) {
-    if (c.splits > 1) {
-      const TileProblem& p = t.prob[0];
+    if (p.splits > 1) {
       const int64_t blocks = ((int64_t)p.J * groups_of(p.I) * 4 + 255) / 256;
       if (blocks == 0) return LIRPA_OK;
       if (blocks > 0x7fffffff)
@@ -483,6 +517,29 @@ int tile_of_size(const char* name, TileArgs& t, const Cut& c, char* part, Joins*
     }
   }
   return LIRPA_OK;
+}
+
+template <typename T, int SIZE, int WI, int WJ>
+int launch_grads(TileArgs& t, hipStream_t st) {
+  int64_t total;
+  TRY((lay_out<SIZE, EPI_STORE>("ffn_grads", t, total)));
+  if (total == 0) return LIRPA_OK;
+  return launch_k("ffn_grads", st, [&] {
+    k_ffn_grads<T, SIZE, WI, WJ><<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);
+  });
+}
+template <typename T>
+int grads_of_size(TileArgs& t, int size, hipStream_t st) {
+  if (size == 64) return launch_grads<T, 64, 1, 4>(t, st);
+  if (size == 128) return launch_grads<T, 128, 2, 2>(t, st);
+  return launch_grads<T, 256, 2, 4>(t, st);
+}
+int run_grads(const FfnPlan& pl, TileArgs& t, int size, hipStream_t st) {
+  switch (pl.f->dtype) {
+    case LIRPA_F32: return grads_of_size<Split>(t, size, st);
+    case LIRPA_BF16: return grads_of_size<bf16>(t, size, st);
+    default: return grads_of_size<f16>(t, size, st);
+  }
 }
 
 template <bool AKS, bool BKS, int EPI>
@@ -624,8 +681,8 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
 
 struct BackwardRoom {
   Operand dout, x, wg, wu, wd, a, dg, du;
-  Cut cut_gate, cut_dx, cut_dw;
-  void *part_gate, *part_dx, *part_dw;
+  Cut cut_gate, cut_grads;
+  void *part_gate, *part_grads;
   size_t bytes;
 };
 TileProblem da_problem(const FfnPlan& pl, const BackwardRoom& r) {
@@ -633,32 +690,17 @@ TileProblem da_problem(const FfnPlan& pl, const BackwardRoom& r) {
   add_segs(pl, p, r.wd, r.dout);
   return p;
 }
-TileProblem dx_problem(const FfnPlan& pl, const BackwardRoom& r) {
-  TileProblem p = problem(pl.D, pl.rows, pl.F, pl.Fp);
-  add_segs(pl, p, r.wg, r.dg);
-  add_segs(pl, p, r.wu, r.du);
-  return p;
-}
-// The wanted ones of dWg, dWu and dWd.
-int dw_problems(const FfnPlan& pl, const BackwardRoom& r, bool packed_x, void* dWg, void* dWu,
-                void* dWd, TileProblem* probs) {
-  int n = 0;
-  for (int b = 0; b < 2; ++b) {
-    if (!(b ? dWu : dWg)) continue;
-    TileProblem& p = probs[n++];
-    p = problem(pl.D, pl.F, pl.rows, pl.rows);
-    add_segs(pl, p, r.x, b ? r.du : r.dg, packed_x);
-    p.out = b ? dWu : dWg;
-    p.ldo = pl.D;
-  }
-  if (dWd) {
-    TileProblem& p = probs[n++];
-    p = problem(pl.F, pl.D, pl.rows, pl.rows);
-    add_segs(pl, p, r.a, r.dout);
-    p.out = dWd;
-    p.ldo = pl.F;
-  }
-  return n;
+// dx, dWg, dWu and dWd.
+void grad_problems(const FfnPlan& pl, const BackwardRoom& r, bool packed_x, TileProblem* p) {
+  p[0] = problem(pl.D, pl.rows, pl.F, pl.Fp);
+  add_segs(pl, p[0], r.wg, r.dg);
+  add_segs(pl, p[0], r.wu, r.du);
+  p[1] = p[2] = problem(pl.D, pl.F, pl.rows, pl.rows);
+  add_segs(pl, p[1], r.x, r.dg, packed_x);
+  add_segs(pl, p[2], r.x, r.du, packed_x);
+  p[3] = problem(pl.F, pl.D, pl.rows, pl.rows);
+  add_segs(pl, p[3], r.a, r.dout);
+  for (int i = 1; i < 4; ++i) p[i].b_strided = true;
 }
 BackwardRoom backward_room(FfnPlan& pl, bool packed_x) {
   BackwardRoom r;
@@ -669,17 +711,14 @@ BackwardRoom backward_room(FfnPlan& pl, bool packed_x) {
   r.a = pl.own(pl.rows, pl.F);
   r.dg = pl.own(pl.rows, pl.F);
   r.du = pl.own(pl.rows, pl.F);
-  const TileProblem da = da_problem(pl, r), dx = dx_problem(pl, r);
+  const TileProblem da = da_problem(pl, r);
   r.cut_gate = cut_of(&da, 1, EPI_BACK, !pl.f32, false);
   r.part_gate = pl.ws.take(part_room(r.cut_gate, &da, 1));
-  r.cut_dx = cut_of(&dx, 1, EPI_STORE, true, false);
-  r.part_dx = pl.ws.take(part_room(r.cut_dx, &dx, 1));
-  // cut as if all three were wanted: a gradient does not depend on which others are
-  char all;
-  TileProblem dw[3];
-  const int n = dw_problems(pl, r, packed_x, &all, &all, &all, dw);
-  r.cut_dw = cut_of(dw, n, EPI_STORE, true, false);
-  r.part_dw = pl.ws.take(part_room(r.cut_dw, dw, n));
+  // cut as if all four were wanted: a gradient does not depend on which others are
+  TileProblem grads[4];
+  grad_problems(pl, r, packed_x, grads);
+  r.cut_grads = cut_of(grads, 4, EPI_STORE, true, false);
+  r.part_grads = pl.ws.take(part_room(r.cut_grads, grads, 4));
   r.bytes = pl.ws.at;
   return r;
 }
@@ -723,18 +762,23 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
                                          st)));
 
   Joins joins;
-  if (dx) {
-    t = tile_args(pl, LIRPA_KEEP_NONE);
-    t.prob[0] = dx_problem(pl, r);
-    t.prob[0].out = dx;
-    t.prob[0].ldo = lddx;
-    TRY((run_tile<true, false, EPI_STORE>(pl, "ffn_dx", t, r.cut_dx, r.part_dx, &joins, st)));
+  t = tile_args(pl, LIRPA_KEEP_NONE);
+  t.count = 0;
+  TileProblem grads[4];
+  grad_problems(pl, r, packed, grads);
+  void* outs[4] = {dx, dWg, dWu, dWd};
+  const int64_t lds[4] = {lddx, pl.D, pl.D, pl.F};
+  char* part = (char*)r.part_grads;
+  for (int i = 0; i < 4; ++i) {
+    if (!outs[i]) continue;
+    TileProblem& q = t.prob[t.count++];
+    q = grads[i];
+    q.out = outs[i];
+    q.ldo = lds[i];
+    split(q, r.cut_grads.splits[i], part);
+    if (q.splits > 1) joins.add(q);
   }
-  if (dWg || dWu || dWd) {
-    t = tile_args(pl, LIRPA_KEEP_NONE);
-    t.count = dw_problems(pl, r, packed, dWg, dWu, dWd, t.prob);
-    TRY((run_tile<true, true, EPI_STORE>(pl, "ffn_dw", t, r.cut_dw, r.part_dw, &joins, st)));
-  }
+  TRY(run_grads(pl, t, r.cut_grads.size, st));
   return joins.run(pl, st);
 }
 

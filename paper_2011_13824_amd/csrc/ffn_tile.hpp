@@ -55,7 +55,7 @@ enum Gate { RELU = 0, SILU = 1, GELU = 2 };
 
 constexpr int kMaxSegs = 12;
 constexpr int kBK = 64;  // k a tile: 128 bytes of a k-contiguous row, the width of a cache line
-constexpr int kMaxProblems = 3;
+constexpr int kMaxProblems = 4;
 
 // One product.
 struct TileProblem {
@@ -64,9 +64,10 @@ struct TileProblem {
   int64_t lda, ldb;    // bytes between rows, the same for all segments
   int nseg;
   int KA, KB;          // k extents (equal up to the zero padding of a packed operand)
+  bool b_strided;      // gradients: B is k-strided too
   int I, J;            // output sizes
   int tiles_i, tiles_j;
-  int first;           // block of its first tile
+  unsigned first;      // block of its first tile
   int splits;          // blocks that share a tile's k; over 1, their sums go to
   float* part;         // part[split][J][part_ld] (EPI_GATE: [split][2][J][part_ld], g and u) and
                        // are added by k_ffn_join or k_ffn_finish
@@ -444,47 +445,44 @@ __device__ __forceinline__ void put_part(const TileProblem& p, int split, int wh
   store_row<float, 8>(to + (at.token * (uint32_t)p.part_ld + at.col), p.I - at.col, x);
 }
 
-// BI x BJ output tile, WI x WJ waves.  EPI_GATE: the tile's A rows are BI / 2 of Wg and the same
-// BI / 2 of Wu, and a wave owns both projections of its features.
-// KEEP: what was kept (EPI_BACK), 0 or 8.  AHEAD: whole tiles on their way.
-//
-// Bound by the matrix instructions (busy 62 to 74 % of the cycles at 8192 tokens, 4096 x 10944 in
-// bf16: gate and up 1.21 ms, 1218 TFLOP/s; down 0.54 ms, 1354; dx 1.03 ms, 1420; the three weight
-// gradients 1.77 ms, 1244), and, for da, by its epilogue (0.79 ms, 930 TFLOP/s, busy 47 %): there
-// all CUs come to read what was kept and to write three operands at the same time, 0.72 GB in all.
-// Few tokens are bound by the weights' bytes (64 tokens: 4.7 TB/s in gate and up).
+// LDS of a tile: units of one operand each.
+template <bool AKS, bool BKS, int BI, int BJ, int AHEAD>
+struct Units {
+  static constexpr int kA = Lay<AKS, BI>::kBytes, kB = Lay<BKS, BJ>::kBytes;
+  static constexpr int kUnit = kA > kB ? kA : kB;
+  static constexpr int kCount = 2 * AHEAD + 3;
+};
+
+// The tile of block b of a product's n: tiles come in an order that gives each of the 8 XCDs (blocks
+// are dealt to them in turn) a run of neighbouring ones, which share operands in its L2.
+__device__ __forceinline__ int tile_of_block(int b, int n) {
+  const int x = b & 7, per = n >> 3, more = n & 7;
+  return x * per + min(x, more) + (b >> 3);
+}
+
+// One tile of BI x BJ outputs, WI x WJ waves.  EPI_GATE: the tile's A rows are BI / 2 of Wg and the
+// same BI / 2 of Wu, and a wave owns both projections of its features.
+// KEEP: what was kept (EPI_BACK), 0 or 8.  AHEAD: whole tiles on their way.  id: of the problem's
+// tiles, times its splits.
 template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int BI, int BJ, int WI, int WJ,
           int AHEAD>
-__global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_tile(TileArgs a) {
+__device__ __forceinline__ void ffn_tile(const TileArgs& a, const TileProblem& p, int id,
+                                         char* lds) {
   constexpr int kThreads = WI * WJ * 64;
   constexpr int FI = BI / WI / 16, FJ = BJ / WJ / 16;  // fragments of a wave
-  constexpr int kTileA = Lay<AKS, BI>::kBytes, kTileB = Lay<BKS, BJ>::kBytes;
-  constexpr int kUnit = kTileA > kTileB ? kTileA : kTileB;
-  constexpr int kUnits = 2 * AHEAD + 3;  // tiles of one operand in LDS
+  using U = Units<AKS, BKS, BI, BJ, AHEAD>;
+  constexpr int kTileA = U::kA, kUnit = U::kUnit, kUnits = U::kCount;
   constexpr int kFeat = EPI == EPI_GATE ? BI / 2 : BI;  // features a tile
-  __shared__ __align__(256) char lds[kUnits * kUnit];
 
-  // tiles in an order that gives each of the 8 XCDs (blocks are dealt to them in turn) a run of
-  // neighbouring tiles, in columns of 8 token tiles: they share operands in its L2
-  const int total = gridDim.x;
-  int id;
-  {
-    const int x = blockIdx.x & 7, per = total >> 3, more = total & 7;
-    id = x * per + min(x, more) + (blockIdx.x >> 3);
-  }
-  int which = 0;
-  if constexpr (EPI == EPI_STORE)
-    while (which + 1 < a.count && id >= a.prob[which + 1].first) ++which;
-  const TileProblem& p = a.prob[which];
-  id -= p.first;
-  // the larger tile's other epilogues leave no registers for it
+  // the larger tile's other epilogues leave no registers for sums that are put down
   constexpr bool kMaySplit = EPI == EPI_STORE || BI < 256;
   int split = 0;
   if constexpr (kMaySplit) {
     split = id / (p.tiles_i * p.tiles_j);
     id -= split * (p.tiles_i * p.tiles_j);
   }
-  constexpr int kBand = 8;  // 4 and 16 within 1 %, 32 up to a quarter slower
+  // columns of 8 token tiles; 4 and 16 within 1 %, 32 up to a quarter slower
+  constexpr int kBand = 8;
   const int band = id / (kBand * p.tiles_i), in_band = id - band * kBand * p.tiles_i;
   const int height = min(kBand, p.tiles_j - band * kBand);
   const int ti = in_band / height, tj = band * kBand + in_band - ti * height;
@@ -733,6 +731,38 @@ __global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_tile(TileArgs a) {
   }
 }
 
+// One product with its epilogue.
+//
+// Bound by the matrix instructions (busy 62 to 74 % of the cycles at 8192 tokens, 4096 x 10944 in
+// bf16: gate and up 1.21 ms, 1218 TFLOP/s; down 0.54 ms, 1354), and, for da, by its epilogue (0.79
+// ms, 930 TFLOP/s, busy 47 %): there all CUs come to read what was kept and to write three operands
+// at the same time, 0.72 GB in all.  Few tokens are bound by the weights' bytes (64 tokens: 4.7
+// TB/s in gate and up).
+template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int SIZE, int WI, int WJ, int AHEAD>
+__global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_tile(TileArgs a) {
+  using U = Units<AKS, BKS, SIZE, SIZE, AHEAD>;
+  __shared__ __align__(256) char lds[U::kCount * U::kUnit];
+  ffn_tile<T, AKS, BKS, EPI, KEEP, SIZE, SIZE, WI, WJ, AHEAD>(
+      a, a.prob[0], tile_of_block(blockIdx.x, gridDim.x), lds);
+}
+
+// The gradients, which do not depend on one another: dx (long sums) before dWg, dWu and dWd, so
+// that the shorter ones fill what it leaves.
+template <typename T, int SIZE, int WI, int WJ>
+__global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_grads(TileArgs a) {
+  using U = Units<true, true, SIZE, SIZE, 1>;
+  __shared__ __align__(256) char lds[U::kCount * U::kUnit];
+  int which = 0;
+  while (which + 1 < a.count && blockIdx.x >= a.prob[which + 1].first) ++which;
+  const TileProblem& p = a.prob[which];
+  const int id =
+      tile_of_block(blockIdx.x - p.first, p.tiles_i * p.tiles_j * p.splits);
+  if (p.b_strided)
+    ffn_tile<T, true, true, EPI_STORE, 0, SIZE, SIZE, WI, WJ, 1>(a, p, id, lds);
+  else
+    ffn_tile<T, true, false, EPI_STORE, 0, SIZE, SIZE, WI, WJ, 1>(a, p, id, lds);
+}
+
 // Adds the sums of the blocks that shared a tile's k, in order, for all split products of a call.
 // Bound by bytes (100 MB of sums and 40 MB out: 38 us).
 struct JoinJob {
@@ -743,7 +773,7 @@ struct JoinJob {
   unsigned first;  // block
 };
 struct JoinJobs {
-  JoinJob job[kMaxProblems + 1];
+  JoinJob job[kMaxProblems];
   int count;
 };
 
