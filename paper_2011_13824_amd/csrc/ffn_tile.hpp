@@ -898,7 +898,7 @@ __global__ __launch_bounds__(256) void k_ffn_operands(OperandJobs jobs) {
     store_row<H, 8>((H*)o.out + row * o.ld + col, 8, v);
     return;
   }
-  load_row<W, 8>((const W*)o.x + row * o.ldx + col, o.n - col, v);
+  load_row_end<W, 8>((const W*)o.x + row * o.ldx + col, o.n - col, v);
 #pragma unroll
   for (int part = 0; part < Kind<T>::kParts; ++part) {
 #pragma unroll

@@ -43,6 +43,20 @@ __device__ __forceinline__ void load_row(const T* p, int valid, float (&out)[N])
   }
 }
 
+// The same where few registers are live: past the row's end its last element is read again, so that
+// no branch stands between the loads and the lane waits for them once.  Against load_row, bf16 rows
+// of 4095: the norm's forward pass 2048 rows 60 for 77 us, packing rows of 5165 28 for 31 us; the
+// norm's gradient, whose registers are all taken, 87 for 57 us, and it keeps load_row.
+template <typename T, int N>
+__device__ __forceinline__ void load_row_end(const T* p, int valid, float (&out)[N]) {
+  if (valid >= N || valid <= 0) return load_row<T, N>(p, valid, out);
+  T t[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) t[i] = load_global<T>(p + min(i, valid - 1));
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = i < valid ? (float)t[i] : 0.f;
+}
+
 template <typename T, int N>
 __device__ __forceinline__ void store_row(T* p, int valid, const float (&x)[N]) {
   Vec<T, N> t;

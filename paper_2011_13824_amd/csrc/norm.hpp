@@ -51,7 +51,7 @@ template <typename T>
 __device__ __forceinline__ void norm_piece(const NormFwd<T>& a, int64_t row, int col,
                                            const float (&h)[8], float rstd, bool with_sum) {
   float y[8], w[8];
-  load_row<T, 8>(a.w + col, a.n - col, w);
+  load_row_end<T, 8>(a.w + col, a.n - col, w);
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = h[i] * rstd * w[i];
   if (with_sum && col < a.n) store_row<T, 8>(a.sum + row * a.lds + col, a.n - col, h);
@@ -78,10 +78,10 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_norm_fwd(Norm
   const T* x = a.x + row * a.ldx;
   const T* res = a.res ? a.res + row * a.ldr : nullptr;
   auto read = [&](int col, float(&h)[8]) {
-    load_row<T, 8>(x + col, a.n - col, h);
+    load_row_end<T, 8>(x + col, a.n - col, h);
     if (res) {
       float r[8];
-      load_row<T, 8>(res + col, a.n - col, r);
+      load_row_end<T, 8>(res + col, a.n - col, r);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[i] += r[i];
     }

@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void k_q8_pack(const T* __restrict__ x, int64_
   Piece p = piece_of((int64_t)blockIdx.x * 256, groups * 4);
   if (p.row >= rows) return;  // whole groups of lanes leave together
   float v[8];
-  load_row<T, 8>(x + p.row * ldx + p.col, n - p.col, v);
+  load_row_end<T, 8>(x + p.row * ldx + p.col, n - p.col, v);
   const int e = group_exponent4(v);
   store_global(q + p.row * groups * kGroup + p.col, pack8(v, e));
   if ((threadIdx.x & 3) == 0)
