@@ -163,8 +163,11 @@ int norm_bwd(NormBwd<T> a, T* dw, float* part, hipStream_t st) {
   if (blocks > 0 && (a.dh || s.ch > 0)) {
     TRY(by_norm_shape(s, [&](auto th, auto ch) {
       return launch_k("norm_backward", st, [&] {
-        k_norm_bwd<T, th.value, ch.value>
-            <<<(unsigned)blocks, th.value == 64 ? 256 : th.value, 0, st>>>(a);
+        const unsigned threads = th.value == 64 ? 256 : th.value;
+        if (ch.value == 0 || a.n % 8)
+          k_norm_bwd<T, th.value, ch.value, true><<<(unsigned)blocks, threads, 0, st>>>(a);
+        else if constexpr (ch.value > 0)
+          k_norm_bwd<T, th.value, ch.value, false><<<(unsigned)blocks, threads, 0, st>>>(a);
       });
     }));
   }

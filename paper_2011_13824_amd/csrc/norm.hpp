@@ -128,10 +128,42 @@ struct NormBwd {
   float* part;  // [blocks][n] sums of dy * xhat over a block's rows; NULL: no dw
 };
 
+// Columns col .. col + 7 of a row, 0 past its end, for k_norm_bwd.  CUT = false: n % 8 == 0, so a
+// piece is whole or absent.  CUT = true: 32-bit elements one by one; of 16 bits the row's last eight
+// where the end cuts a piece, moved down in registers, so that no branch keeps a row's loads from
+// being on their way together (8192 bf16 rows of 4095 with dsum: 68 us, one by one 112; the 32-bit
+// kernel's registers are all taken, and 2999 rows of 1001 took 13 us so, 11 one by one).
+template <typename T, bool CUT>
+__device__ __forceinline__ void load_piece(const T* row, int col, int n, float (&out)[8]) {
+  const int valid = n - col;
+  if constexpr (CUT && sizeof(T) == 2) {
+    Vec<T, 8> t;
+    if (n >= 8) {
+      t = load_global<Vec<T, 8>>(row + min(col, n - 8));
+      const int down = 8 - valid;  // of 1 .. 7; where it is 8 or more, nothing of t is kept
+#pragma unroll
+      for (int s = 4; s; s >>= 1)
+#pragma unroll
+        for (int i = 0; i + s < 8; ++i) t[i] = down > 0 && (down & s) ? t[i + s] : t[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = load_global<T>(row + min(i, n - 1));
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = i < valid ? (float)t[i] : 0.f;
+  } else if constexpr (CUT) {
+    load_row<T, 8>(row + col, valid, out);
+  } else {
+    const Vec<T, 8> t = load_global<Vec<T, 8>>(row + min(col, n - 8));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] = valid > 0 ? (float)t[i] : 0.f;
+  }
+}
+
 // A block walks over rows (blockIdx.x, + gridDim.x, ...), keeps the sums of dy * xhat of its
 // columns in registers and writes them once: dw needs no atomics, and its order is fixed by the
 // sizes alone.  CH as above; CH = 0 takes rows of any width and leaves dw to k_norm_dw_wide.
-template <typename T, int THREADS, int CH>
+template <typename T, int THREADS, int CH, bool CUT>
 __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_norm_bwd(NormBwd<T> a) {
   __shared__ float part[THREADS / 64];
   constexpr int kRows = THREADS == 64 ? 4 : 1;
@@ -145,7 +177,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_norm_bwd(Norm
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = (c * THREADS + t) * 8;
-      load_row<T, 8>(a.w + col, a.n - col, w[c]);
+      load_piece<T, CUT>(a.w, col, a.n, w[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) dw[c][i] = 0.f;
     }
@@ -155,8 +187,8 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_norm_bwd(Norm
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const int col = (c * THREADS + t) * 8;
-        load_row<T, 8>(a.h + row * a.ldh + col, a.n - col, xhat[c]);
-        load_row<T, 8>(a.dy + row * a.lddy + col, a.n - col, dy[c]);
+        load_piece<T, CUT>(a.h + row * a.ldh, col, a.n, xhat[c]);
+        load_piece<T, CUT>(a.dy + row * a.lddy, col, a.n, dy[c]);
       }
 #pragma unroll
       for (int c = 0; c < CH; ++c)
@@ -177,7 +209,7 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_norm_bwd(Norm
           for (int i = 0; i < 8; ++i) d[i] = rstd * (dy[c][i] * w[c][i] - xhat[c][i] * dot);
           if (a.dsum) {
             float s[8];
-            load_row<T, 8>(a.dsum + row * a.ldds + col, a.n - col, s);
+            load_piece<T, CUT>(a.dsum + row * a.ldds, col, a.n, s);
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] += s[i];
           }
