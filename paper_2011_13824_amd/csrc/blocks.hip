@@ -652,8 +652,9 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
       // Large weights keep the memory busy with more on the way, small ones are done sooner with
       // fewer steps.  1 token, us with gate waves x steps in flight 8 x 2 / 8 x 4 / 16 x 4: 4096 x
       // 10944 bf16 58.5 / - / 57.1, float 123 / 108 / 109; 1024 x 2752 bf16 10.4 / 11.2 / 13.6,
-      // float 18.2 / 19.4 / 23.0; 512 x 4400 float 17.9 / 23.1 / 27.8.  Gate product of 62 tokens, 2816 x
-      // 616 float, 4 / 8 waves 52 / 44, of 64, 1024 x 2752, 24.5 / 21.6; 20 tokens, 8 / 16, 25 / 27.
+      // float 18.2 / 19.4 / 23.0; 512 x 4400 float 17.9 / 23.1 / 27.8.  Gate product of 62 tokens,
+      // 2816 x 616 float, 4 / 8 waves 52 / 44, of 64, 1024 x 2752, 24.5 / 21.6; 20 tokens, 8 / 16
+      // waves, 25 / 27.
       constexpr int kLargeGate = sizeof(T) == 2 ? 16 : 8;
       const bool large = 3 * pl.D * pl.F * (int64_t)sizeof(T) >= (int64_t)64 << 20;
       if (rows <= 16 && large)
