@@ -325,9 +325,9 @@ struct Cut {
   int splits[kMaxProblems] = {1, 1, 1, 1};
 };
 
-// What a round of blocks over the 256 CUs takes: fixed + slope * k us for k in thousands, when it is
-// full and when it is at most half full, and what the other epilogues add.  Measured at k = 64 to
-// 4096 in bf16; a full round computes 1, 2 and 4 tiles of 128 x 128 a CU.
+// What a round of blocks over the 256 CUs takes: fixed + slope * k us for k in thousands, when it
+// is full and when it is at most half full, and what the other epilogues add.  Measured at k = 64
+// to 4096 in bf16; a full round computes 1, 2 and 4 tiles of 128 x 128 a CU.
 struct Round {
   int size, full;  // tile, blocks
   double fixed, slope, half_fixed, half_slope, gate, back;
@@ -337,8 +337,9 @@ constexpr Round kRounds[3] = {{64, 1024, 6.0, 11.8, 4.5, 7.4, 1, 4},
                               {256, 256, 10.0, 23.5, 10.0, 23.5, 8.6, 30}};
 
 // The cut of least estimated time for the products of a launch.  Joining moves the sums twice at
-// 4 TB/s and costs a launch (5 us; 10 with an epilogue, which then reads memory cold).  So few tiles over a long k are split, and tiles that would leave a
-// round nearly empty, or most of its time to epilogues, are made smaller.
+// 4 TB/s and costs a launch (5 us; 10 with an epilogue, which then reads memory cold).  So few
+// tiles over a long k are split, and tiles that would leave a round nearly empty, or most of its
+// time to epilogues, are made smaller.
 //
 // Up to 64 tokens (`few`: both operands k-contiguous) it is the weights' bytes that count: tiles of
 // 64, three more on their way, two blocks a CU.  4096 x 10944 in bf16: gate and up 34 us against
