@@ -579,6 +579,26 @@ int run_tile(const FfnPlan& pl, const char* name, TileArgs& t, const Cut& cut, v
 // are copied.
 constexpr int kFewest = 8, kFewRows = 64;
 
+template <typename T, bool GATE, int TJ, int WAVES, int UN>
+int few_product(const char* name, const FewArgs& a, hipStream_t st) {
+  return launch_k(name, st, [&] {
+    const unsigned blocks = (a.I + 15) / 16;
+    if constexpr (sizeof(T) == 2) {
+      // Rows off 4 bytes are read by words; the tokens' rows decide where a step has more of them
+      // than of weights.  bf16, us, words / elements: 11 tokens, 3167 x 9543, 94 / 130, 50, 2047 x
+      // 5501, 72 / 130.  Tokens alone off 4 bytes, 2046 x 5502: 50 of them 61 / 69, 10 33 / 29.
+      const bool weights = (uintptr_t)a.A % 4 || a.lda % 2 ||
+                           (GATE && ((uintptr_t)a.A2 % 4 || a.lda2 % 2));
+      const bool words = weights || (TJ > 1 && ((uintptr_t)a.B % 4 || a.ldb % 2));
+      if (words) {
+        k_ffn_few<T, GATE, TJ, WAVES, UN, true><<<blocks, WAVES * 64, 0, st>>>(a);
+        return;
+      }
+    }
+    k_ffn_few<T, GATE, TJ, WAVES, UN, false><<<blocks, WAVES * 64, 0, st>>>(a);
+  });
+}
+
 // GATE: waves a block of the gate product (16 of the down product); UN: steps in flight.
 template <typename T, int TJ, int GATE, int UN>
 int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, void* out,
@@ -596,9 +616,7 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   a.gate = f->gate;
   a.out = hidden;
   a.ldo = f->n_hidden;
-  TRY(launch_k("ffn_few_gate", st, [&] {
-    k_ffn_few<T, true, TJ, GATE, UN><<<(a.I + 15) / 16, GATE * 64, 0, st>>>(a);
-  }));
+  TRY((few_product<T, true, TJ, GATE, UN>("ffn_few_gate", a, st)));
   a.A = f->Wd;
   a.lda = f->ldd;
   a.B = hidden;
@@ -607,9 +625,7 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   a.K = f->n_hidden;
   a.out = out;
   a.ldo = ldo;
-  return launch_k("ffn_few_down", st, [&] {
-    k_ffn_few<T, false, TJ, 16, UN><<<(a.I + 15) / 16, 16 * 64, 0, st>>>(a);
-  });
+  return few_product<T, false, TJ, 16, UN>("ffn_few_down", a, st);
 }
 
 struct ForwardRoom {

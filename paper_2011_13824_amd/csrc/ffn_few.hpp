@@ -6,9 +6,9 @@
 // waves take the k axis in turn, 32 k a step, read the weights' rows straight into the registers of
 // a 16-row matrix instruction (nothing is shared between waves, so LDS would add a trip), and add
 // their sums in LDS in order.  Tokens fill the other side of the instruction, 16 at a time; lanes
-// past the last one repeat it.  Weights are read where they lie at any alignment, and in 32 bits
-// with the 32-bit instruction: three bf16 parts would be more bytes.  One token of 4096 x 10944 in
-// bf16: 57 us, 4.7 TB/s of the 5.1 that a large copy reaches.
+// past the last one repeat it.  Weights are read where they lie at any alignment (by words and a
+// shift off 4 bytes), and in 32 bits with the 32-bit instruction: three bf16 parts would be more
+// bytes.  One token of 4096 x 10944 in bf16: 57 us, 4.7 TB/s of the 5.1 that a large copy reaches.
 #pragma once
 
 #include "ffn_tile.hpp"
@@ -33,6 +33,18 @@ struct Eight {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < valid ? load_global<T>(p + i) : (T)0.f;
   }
+  // From the words that hold the elements, each of which holds one at least.
+  __device__ __forceinline__ void load_words(const T* p) {
+    const int odd = (int)((uintptr_t)p >> 1) & 1;
+    const T* words = p - odd;
+    const Vec<uint32_t, 4> w = load_global<Vec<uint32_t, 4>>(words);
+    const uint32_t last = load_global<uint32_t>(words + (odd ? 8 : 6));
+    Vec<uint32_t, 4> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      r[i] = __builtin_amdgcn_alignbit(i < 3 ? w[i < 3 ? i + 1 : 3] : last, w[i], 16 * odd);
+    v = __builtin_bit_cast(typename Mfma<T>::x8, r);
+  }
   static __device__ __forceinline__ f32x4 mac(const Eight& a, const Eight& b, f32x4 c) {
     return Mfma<T>::mac(a.v, b.v, c);
   }
@@ -56,8 +68,9 @@ struct Eight<float> {
   }
 };
 
-// TJ: groups of 16 tokens; UN: steps whose loads are in flight together.
-template <typename T, bool GATE, int TJ, int WAVES, int UN>
+// TJ: groups of 16 tokens; UN: steps whose loads are in flight together; WORDS: rows of 16-bit
+// weights that begin inside a 32-bit word are read by words and shifted.
+template <typename T, bool GATE, int TJ, int WAVES, int UN, bool WORDS>
 __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(FewArgs a) {
   constexpr int kMats = GATE ? 2 : 1;
   __shared__ float part[WAVES][kMats][TJ][4][64];
@@ -85,9 +98,19 @@ __global__ __launch_bounds__(WAVES * 64) void k_ffn_few(FewArgs a) {
     for (int n = 0; n < UN; ++n) {
       const int k = min(s + n * WAVES, full - 1) * 32;  // past the end: loaded, not multiplied
 #pragma unroll
-      for (int c = 0; c < kMats; ++c) fw[n][c].load(w[c] + k);
+      for (int c = 0; c < kMats; ++c) {
+        if constexpr (WORDS)
+          fw[n][c].load_words(w[c] + k);
+        else
+          fw[n][c].load(w[c] + k);
+      }
 #pragma unroll
-      for (int t = 0; t < TJ; ++t) fx[n][t].load(x[t] + k);
+      for (int t = 0; t < TJ; ++t) {
+        if constexpr (WORDS)
+          fx[n][t].load_words(x[t] + k);
+        else
+          fx[n][t].load(x[t] + k);
+      }
     }
 #pragma unroll
     for (int n = 0; n < UN; ++n)

@@ -475,6 +475,23 @@ def test_ffn_weights_of_different_strides(B, dtype, rows):
             assert torch.equal(got[k], grads[k]), (pads, k)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=ids)
+@pytest.mark.parametrize("rows", [1, 16, 31, 50])
+@pytest.mark.parametrize("wpad,wshift,xpad,xshift", [(1, 0, 0, 0), (0, 1, 0, 0), (0, 0, 1, 0),
+                                                     (0, 0, 0, 1), (1, 1, 1, 1), (2, 3, 2, 5)])
+def test_ffn_few_rows_inside_words(B, dtype, rows, wpad, wshift, xpad, xshift):
+    """Weights and tokens whose rows begin inside 32-bit words, and not; sums that end inside a
+    step of 32."""
+    g = gen_of(rows)
+    D, F = 610, 1126
+    x = rand(g, rows, D, dtype=dtype, pad=xpad, shift=xshift)
+    W = weights(g, D, F, dtype, wpad, wshift)
+    u = UNIT[dtype]
+    out, tol, *_ = forward64(x, W, "silu", u)
+    got = B.FeedForward(*W, "silu").forward(x)
+    check(got, out, tol + TINY[dtype] * (1 + W[2].double().abs().sum(1)), "out")
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
 def test_ffn_no_rows(B, dtype):
     W = weights(gen_of(1), 24, 40, dtype)
