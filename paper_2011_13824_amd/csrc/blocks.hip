@@ -160,6 +160,11 @@ int norm_bwd(NormBwd<T> a, T* dw, float* part, hipStream_t st) {
   const NormShape s = norm_shape(a.n);
   const int64_t blocks = norm_bwd_blocks(a.rows, a.n);
   a.part = dw ? part : nullptr;
+  // dw of wide rows has a kernel of its own, which reads dy before dh may take its place
+  if (dw && blocks > 0 && s.ch == 0)
+    TRY(launch_k("norm_backward", st, [&] {
+      k_norm_dw_wide<T><<<dim3((a.n + 2047) / 2048, (unsigned)blocks), 256, 0, st>>>(a);
+    }));
   if (blocks > 0 && (a.dh || s.ch > 0)) {
     TRY(by_norm_shape(s, [&](auto th, auto ch) {
       return launch_k("norm_backward", st, [&] {
@@ -171,10 +176,6 @@ int norm_bwd(NormBwd<T> a, T* dw, float* part, hipStream_t st) {
       });
     }));
   }
-  if (dw && blocks > 0 && s.ch == 0)
-    TRY(launch_k("norm_backward", st, [&] {
-      k_norm_dw_wide<T><<<dim3((a.n + 2047) / 2048, (unsigned)blocks), 256, 0, st>>>(a);
-    }));
   if (dw)
     TRY(launch_k("norm_dw", st, [&] {
       k_norm_dw<T><<<(a.n + 31) / 32, 256, 0, st>>>(part, (int)blocks, a.n, dw);
