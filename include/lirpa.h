@@ -337,8 +337,8 @@ typedef enum {
   LIRPA_KEEP_8 = 8     /* two lirpa_q8 buffers of n_hidden columns */
 } lirpa_keep;
 
-/* Workspace of a call over up to `rows` rows: backward 0 for lirpa_ffn_forward, 1 for
- * lirpa_ffn_backward.  0 for invalid arguments. */
+/* Workspace of a call over up to `rows` rows (it never falls as rows grow): backward 0 for
+ * lirpa_ffn_forward, 1 for lirpa_ffn_backward.  0 for invalid arguments. */
 size_t lirpa_ffn_workspace_bytes(const lirpa_ffn* ffn, int64_t rows, int backward);
 
 /* out = (act(x Wg^T) * (x Wu^T)) Wd^T for x [rows][n_model].  The product act(g) * u is rounded

@@ -353,8 +353,38 @@ int64_t steps_of(const TileProblem& p) {
   return up(std::max(p.KA, p.KB), kBK) / kBK * p.nseg;
 }
 
+int64_t part_ld(int64_t I) { return up(I, 8); }
+
+// Room for the sums of products that are split.
+size_t part_bytes(int splits, const TileProblem& p, int arrays) {
+  return splits > 1 ? up((size_t)splits * arrays * p.J * part_ld(p.I) * sizeof(float), 256) : 0;
+}
+size_t part_room(const Cut& c, const TileProblem* probs, int count, int arrays = 1) {
+  size_t bytes = 0;
+  for (int i = 0; i < count; ++i) bytes += part_bytes(c.splits[i], probs[i], arrays);
+  return bytes;
+}
+
+// The room that a call keeps for such sums.  It never falls with the rows, so that a workspace for
+// many rows holds fewer too, and a cut that needs more is not taken: the most parts there can be, and
+// no more than kMostParts.  Of 60,000 products up to 8192 rows of 4096 x 10944, that limit changes no
+// cut of 16-bit types and 0.1 % of those of floats, whose estimated times grow by 1 % on average.
+constexpr size_t kMostParts = (size_t)128 << 20, kMostParts32 = (size_t)256 << 20;
+constexpr int kMaxSplits = 16;
+size_t most_part_room(const FfnPlan& pl, const TileProblem* probs, int count, int arrays = 1) {
+  int64_t longest = 1;
+  for (int i = 0; i < count; ++i) longest = std::max(longest, steps_of(probs[i]));
+  size_t bytes = 0;
+  for (int i = 0; i < count; ++i) {
+    const int64_t splits = std::min<int64_t>({kMaxSplits, longest / 4, steps_of(probs[i])});
+    bytes += part_bytes((int)splits, probs[i], arrays);
+  }
+  return std::min(bytes, pl.f32 ? kMostParts32 : kMostParts);
+}
+
 // `may_large`: not the epilogue of da in 32 bits, which does not fit the larger tile's registers.
-Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool few) {
+// `room`: for the sums of split products.
+Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool few, size_t room) {
   const bool gate = epi == EPI_GATE;
   int64_t steps[kMaxProblems], longest = 1;
   for (int i = 0; i < count; ++i) {
@@ -375,7 +405,7 @@ Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool fe
     const double more = gate ? r.gate : epi == EPI_BACK ? r.back : 0;
     int64_t tiles[kMaxProblems];
     for (int i = 0; i < count; ++i) tiles[i] = tiles_of(probs[i], r.size, gate);
-    for (int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+    for (int parts : {1, 2, 3, 4, 5, 6, 8, 10, 12, kMaxSplits}) {
       if (parts > 1 && (longest < 4 * parts || (r.size == 256 && epi != EPI_STORE))) break;
       // blocks of about as many steps each, whichever product they are of
       const int64_t target = (longest + parts - 1) / parts;
@@ -392,6 +422,7 @@ Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool fe
         if (c.splits[i] > 1)
           sums += (double)probs[i].I * probs[i].J * (gate ? 2 : 1) * c.splits[i];
       }
+      if (part_room(c, probs, count, gate ? 2 : 1) > room) continue;
       const double base = fixed + (sums > 0 ? 0 : more);
       const double half = r.half_fixed + (sums > 0 ? 0 : more) +
                           (full < r.full ? 6.2 : r.half_slope) * longest_k;
@@ -419,18 +450,6 @@ Cut cut_of(const TileProblem* probs, int count, int epi, bool may_large, bool fe
     }
   }
   return best;
-}
-
-int64_t part_ld(int64_t I) { return up(I, 8); }
-
-// Room for the sums of products that are split.
-size_t part_bytes(int splits, const TileProblem& p, int arrays) {
-  return splits > 1 ? up((size_t)splits * arrays * p.J * part_ld(p.I) * sizeof(float), 256) : 0;
-}
-size_t part_room(const Cut& c, const TileProblem* probs, int count, int arrays = 1) {
-  size_t bytes = 0;
-  for (int i = 0; i < count; ++i) bytes += part_bytes(c.splits[i], probs[i], arrays);
-  return bytes;
 }
 
 // Takes a product's split and its part of the room.
@@ -632,7 +651,7 @@ int few_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
 struct ForwardRoom {
   Operand x, wg, wu, wd, a;
   Cut cut_gate, cut_down;
-  void *part_gate, *part_down;
+  void* part;
   size_t bytes;
 };
 TileProblem gate_problem(const FfnPlan& pl, const ForwardRoom& r) {
@@ -652,10 +671,11 @@ ForwardRoom forward_room(FfnPlan& pl) {
   if (!pl.down_in_place()) r.wd = pl.own(pl.D, pl.F);
   r.a = pl.own(pl.rows, pl.F);
   const TileProblem gate = gate_problem(pl, r), down = down_problem(pl, r);
-  r.cut_gate = cut_of(&gate, 1, EPI_GATE, true, true);
-  r.part_gate = pl.ws.take(part_room(r.cut_gate, &gate, 1, 2));
-  r.cut_down = cut_of(&down, 1, EPI_STORE, true, true);
-  r.part_down = pl.ws.take(part_room(r.cut_down, &down, 1));
+  const size_t gate_room = most_part_room(pl, &gate, 1, 2), down_room = most_part_room(pl, &down, 1);
+  r.cut_gate = cut_of(&gate, 1, EPI_GATE, true, true, gate_room);
+  r.cut_down = cut_of(&down, 1, EPI_STORE, true, true, down_room);
+  // the gate product's sums are added before the down product's are written
+  r.part = pl.ws.take(std::max(gate_room, down_room));
   r.bytes = pl.ws.at;
   return r;
 }
@@ -701,7 +721,7 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   t.u = u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, r.cut_gate, r.part_gate, nullptr,
+  TRY((run_tile<false, false, EPI_GATE>(pl, "ffn_gate_up", t, r.cut_gate, r.part, nullptr,
                                           st)));
 
   Joins joins;
@@ -709,14 +729,14 @@ int ffn_forward(const lirpa_ffn* f, int64_t rows, const void* x, int64_t ldx, vo
   t.prob[0] = down_problem(pl, r);
   t.prob[0].out = out;
   t.prob[0].ldo = ldo;
-  TRY((run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, r.cut_down, r.part_down, &joins, st)));
+  TRY((run_tile<false, false, EPI_STORE>(pl, "ffn_down", t, r.cut_down, r.part, &joins, st)));
   return joins.run(pl, st);
 }
 
 struct BackwardRoom {
   Operand dout, x, wg, wu, wd, a, dg, du;
   Cut cut_gate, cut_grads;
-  void *part_gate, *part_grads;
+  void* part;
   size_t bytes;
 };
 TileProblem da_problem(const FfnPlan& pl, const BackwardRoom& r) {
@@ -746,13 +766,13 @@ BackwardRoom backward_room(FfnPlan& pl, bool packed_x) {
   r.dg = pl.own(pl.rows, pl.F);
   r.du = pl.own(pl.rows, pl.F);
   const TileProblem da = da_problem(pl, r);
-  r.cut_gate = cut_of(&da, 1, EPI_BACK, !pl.f32, false);
-  r.part_gate = pl.ws.take(part_room(r.cut_gate, &da, 1));
   // cut as if all four were wanted: a gradient does not depend on which others are
   TileProblem grads[4];
   grad_problems(pl, r, packed_x, grads);
-  r.cut_grads = cut_of(grads, 4, EPI_STORE, true, false);
-  r.part_grads = pl.ws.take(part_room(r.cut_grads, grads, 4));
+  const size_t da_room = most_part_room(pl, &da, 1), grads_room = most_part_room(pl, grads, 4);
+  r.cut_gate = cut_of(&da, 1, EPI_BACK, !pl.f32, false, da_room);
+  r.cut_grads = cut_of(grads, 4, EPI_STORE, true, false, grads_room);
+  r.part = pl.ws.take(std::max(da_room, grads_room));  // da's sums are added first
   r.bytes = pl.ws.at;
   return r;
 }
@@ -792,7 +812,7 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
   t.u = (void*)u;
   t.ge = (uint8_t*)g + q8_exps_at(rows, (int)pl.F);
   t.ue = (uint8_t*)u + q8_exps_at(rows, (int)pl.F);
-  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, r.cut_gate, r.part_gate, nullptr,
+  TRY((run_tile<true, false, EPI_BACK>(pl, "ffn_back_gate", t, r.cut_gate, r.part, nullptr,
                                          st)));
 
   Joins joins;
@@ -802,7 +822,7 @@ int ffn_backward(const lirpa_ffn* f, int64_t rows, const void* dout, int64_t ldd
   grad_problems(pl, r, packed, grads);
   void* outs[4] = {dx, dWg, dWu, dWd};
   const int64_t lds[4] = {lddx, pl.D, pl.D, pl.F};
-  char* part = (char*)r.part_grads;
+  char* part = (char*)r.part;
   for (int i = 0; i < 4; ++i) {
     if (!outs[i]) continue;
     TileProblem& q = t.prob[t.count++];

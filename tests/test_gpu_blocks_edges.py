@@ -49,3 +49,27 @@ def test_norm_gradient_in_place_with_weights(lirpa, B, dtype, n, where):
     lirpa.lirpa_norm_backward(dy, ds, h, w, rstd, to, dw2, ws, need)
     assert torch.equal(to, dh)
     assert torch.equal(dw2, dw)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("D,F", [(1024, 2752), (256, 4288)])
+def test_one_workspace_for_all_batches(lirpa, B, dtype, D, F):
+    """A workspace for the largest batch, full of NaN, serves every smaller one, and what a call
+    leaves there is not read by the next."""
+    most = 800
+    W = [rand(s, *shape, dtype=dtype, scale=0.05)
+         for s, shape in ((1, (F, D)), (2, (F, D)), (3, (D, F)))]
+    ffn = B.FeedForward(*W)
+    needs = [lirpa.lirpa_ffn_workspace_bytes(ffn.block, most, b) for b in (0, 1)]
+    ws = torch.full((max(needs) // 4 + 1,), float("nan"), device="cuda").view(torch.uint8)
+    for rows in (800, 769, 768, 357, 356, 129, 65, 9, 1):
+        x, dout = rand(rows, rows, D, dtype=dtype), rand(rows + 1, rows, D, dtype=dtype)
+        want, kept = ffn.forward(x, keep=0)
+        grads = ffn.backward(dout, kept)
+        out, g, u = torch.empty_like(x), torch.empty_like(kept.g), torch.empty_like(kept.u)
+        lirpa.lirpa_ffn_forward(ffn.block, x, out, lirpa.KEEP_FULL, g, u, ws, needs[0])
+        assert torch.equal(out, want) and torch.equal(g, kept.g) and torch.equal(u, kept.u), rows
+        got = [torch.empty_like(t) for t in (x, *W)]
+        lirpa.lirpa_ffn_backward(ffn.block, dout, lirpa.KEEP_FULL, x, g, u, *got, ws, needs[1])
+        for name, t in zip(("dx", "dWg", "dWu", "dWd"), got):
+            assert torch.equal(t, grads[name]), (rows, name)
