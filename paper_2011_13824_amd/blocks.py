@@ -32,6 +32,19 @@ def _type(t, what):
     return lirpa._dtype(t, what), DTYPES[t.dtype]
 
 
+def _of_matrix(t, rows, n, what):
+    """The buffer of a Q8 of a [rows, n] matrix, or a uint8 buffer of that size: where the scales
+    lie follows from rows and n, so another matrix's would be read as something else."""
+    if isinstance(t, Q8):
+        if (t.rows, t.n) != (rows, n):
+            raise ValueError(f"{what} must be of [{rows}, {n}], got [{t.rows}, {t.n}]")
+        return t.buf
+    need = rows * -(-n // 32) * 33
+    if isinstance(t, torch.Tensor) and t.numel() != need:
+        raise ValueError(f"{what} must have {need} bytes for [{rows}, {n}], got {t.numel()}")
+    return t
+
+
 class Q8:
     """A matrix [rows, n] in 8 bits with a power-of-two scale per 32 columns of a row."""
 
@@ -50,7 +63,7 @@ class Q8:
 
     def values(self, dtype=torch.float32):
         rows, n = self.rows, self.n
-        p = lirpa._packed(self.buf, rows, n, "buf")
+        p = lirpa._packed(_of_matrix(self.buf, rows, n, "buf"), rows, n, "buf")
         x = torch.empty((rows, n), dtype=dtype, device=self.buf.device)
         code = _type(x, "dtype")[1]
         _check(load().lirpa_q8_unpack(code, rows, n, p, x.data_ptr(), n, _stream(None)))
@@ -114,8 +127,15 @@ class Kept:
         self.keep, self.rows = keep, rows
         self.x, self.g, self.u = x, g, u
 
-    def raw(self):
-        return [t.buf if isinstance(t, Q8) else t for t in (self.x, self.g, self.u)]
+    def raw(self, rows, block):
+        """x, g and u as the library takes them, checked to be of `rows` rows of the block's."""
+        if self.rows != rows:
+            raise ValueError(f"{self.rows} rows were kept, not {rows}")
+        if self.keep != lirpa.KEEP_8:
+            return self.x, self.g, self.u
+        return (_of_matrix(self.x, rows, block.n_model, "x"),
+                _of_matrix(self.g, rows, block.n_hidden, "g"),
+                _of_matrix(self.u, rows, block.n_hidden, "u"))
 
 
 class FeedForward:
@@ -140,6 +160,8 @@ class FeedForward:
         """out; with ``keep`` (8 or 0) (out, Kept).  ``x8``: x in 8 bits where the caller has it
         (a norm's y8); it is packed here otherwise."""
         rows, dev, hidden = x.shape[0], x.device, self.block.n_hidden
+        if x8 is not None:
+            _of_matrix(x8, rows, self.block.n_model, "x8")
         out = torch.empty_like(x)
         ws, need = self._workspace(rows, 0)
         if keep is None:
@@ -151,17 +173,17 @@ class FeedForward:
         else:
             g, u = (torch.empty((rows, hidden), dtype=x.dtype, device=dev) for _ in range(2))
             kept = Kept(keep, rows, x, g, u)
-        lirpa.lirpa_ffn_forward(self.block, x, out, keep, *kept.raw()[1:], ws, need)
+        lirpa.lirpa_ffn_forward(self.block, x, out, keep, *kept.raw(rows, self.block)[1:], ws, need)
         return out, kept
 
     def backward(self, dout, kept, want=("dx", "dWg", "dWu", "dWd")):
         """{name: gradient} of the wanted ones."""
+        x, g, u = kept.raw(dout.shape[0], self.block)
         like = {"dx": dout, "dWg": self.weights[0], "dWu": self.weights[1],
                 "dWd": self.weights[2]}
         grads = {k: torch.empty(like[k].shape, dtype=dout.dtype, device=dout.device)
                  for k in want}
         ws, need = self._workspace(dout.shape[0], 1)
-        x, g, u = kept.raw()
         lirpa.lirpa_ffn_backward(self.block, dout, kept.keep, x, g, u, *(
             grads.get(k) for k in ("dx", "dWg", "dWu", "dWd")), ws, need)
         return grads

@@ -73,3 +73,35 @@ def test_one_workspace_for_all_batches(lirpa, B, dtype, D, F):
         lirpa.lirpa_ffn_backward(ffn.block, dout, lirpa.KEEP_FULL, x, g, u, *got, ws, needs[1])
         for name, t in zip(("dx", "dWg", "dWu", "dWd"), got):
             assert torch.equal(t, grads[name]), (rows, name)
+
+
+# ---------------------------------------------------------------------------------------------
+# What does not belong together
+# ---------------------------------------------------------------------------------------------
+def test_packed_activations_of_another_matrix_are_refused(B):
+    """Larger ones too: where the scales lie follows from the matrix."""
+    D, F = 64, 96
+    ffn = B.FeedForward(rand(1, F, D), rand(2, F, D), rand(3, D, F))
+    x, dout = rand(4, 40, D), rand(5, 40, D)
+    for x8 in (B.Q8.pack(rand(6, 41, D)), B.Q8.pack(rand(6, 39, D)), B.Q8.pack(rand(6, 40, D + 1)),
+               B.Q8.pack(rand(6, 41, D)).buf):
+        with pytest.raises(ValueError, match="x8"):
+            ffn.forward(x, keep=8, x8=x8)
+    for keep in (8, 0):
+        _, kept = ffn.forward(x, keep=keep)
+        for rows in (39, 41):
+            with pytest.raises(ValueError, match="40 rows were kept"):
+                ffn.backward(rand(7, rows, D), kept)
+        ffn.backward(dout, kept)
+    other = B.Q8.pack(rand(8, 41, F))
+    _, kept = ffn.forward(x, keep=8)
+    for x8, g, u in ((kept.x, other, kept.u), (kept.x, kept.g, other),
+                     (B.Q8.pack(rand(9, 41, D)), kept.g, kept.u),
+                     (kept.x, other.buf, kept.u), (kept.g, kept.g, kept.u)):
+        with pytest.raises(ValueError, match="must"):
+            ffn.backward(dout, B.Kept(8, 40, x8, g, u))
+    raw = ffn.backward(dout, B.Kept(8, 40, kept.x.buf, kept.g.buf, kept.u.buf))
+    want = ffn.backward(dout, kept)
+    assert all(torch.equal(raw[k], want[k]) for k in want)
+    with pytest.raises(ValueError, match="bytes"):
+        B.Q8(40, D, other.buf).values()
