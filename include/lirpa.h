@@ -294,8 +294,9 @@ typedef enum { LIRPA_GATE_RELU = 0, LIRPA_GATE_SILU = 1, LIRPA_GATE_GELU = 2 } l
  *                                  group without values)
  *     uint8  [rows][groups]        e + 127; 255 marks a group with an infinity or a NaN, all of
  *                                  which reads back as NaN
- * and starts on 16 bytes.  A multiple of at most 127 with a power-of-two scale is exact in bf16
- * (and in f16 in its range), so reading it back rounds nothing. */
+ * and starts on 16 bytes.  A multiple of at most 127 with a power-of-two scale is exact in bf16, so
+ * reading it back rounds nothing.  In f16 magnitudes past its range are read as its largest, 65504
+ * (from 65024 on a value is held as 65536), and those under it lose what f16 has no bits for. */
 size_t lirpa_q8_bytes(int64_t rows, int n); /* 0 for invalid arguments */
 int lirpa_q8_pack(int dtype, int64_t rows, int n, const void* x, int64_t ldx, void* q8,
                   hipStream_t stream);

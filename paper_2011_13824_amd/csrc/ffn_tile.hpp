@@ -890,8 +890,8 @@ __global__ __launch_bounds__(256) void k_ffn_operands(OperandJobs jobs) {
   float v[8], p[8];
   if (o.exps) {
     const int groups = groups_of(o.n);
-    unpack8(load_global<u32x2>((const int8_t*)o.x + row * groups * kGroup + col),
-            load_global<uint8_t>(o.exps + row * groups + col / kGroup), v);
+    unpack8_as<H>(load_global<u32x2>((const int8_t*)o.x + row * groups * kGroup + col),
+                  load_global<uint8_t>(o.exps + row * groups + col / kGroup), v);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (col + i >= o.n) v[i] = 0.f;

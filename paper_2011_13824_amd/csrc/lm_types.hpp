@@ -149,4 +149,18 @@ __device__ __forceinline__ void unpack8(u32x2 w, int biased, float (&x)[8]) {
   for (int i = 0; i < 8; ++i) x[i] = (float)(int8_t)(w[i >> 2] >> 8 * (i & 3)) * s;
 }
 
+// The same for values that are stored as T.  A finite value can pass f16's range: magnitudes from
+// 65024 on are held as 64 * 2^10.  They become its largest, which is the nearer one to what was
+// packed; a NaN stays one.
+template <typename T>
+__device__ __forceinline__ void unpack8_as(u32x2 w, int biased, float (&x)[8]) {
+  unpack8(w, biased, x);
+  if constexpr (__is_same(T, f16)) {
+    constexpr float kMost = 65504.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (fabsf(x[i]) > kMost) x[i] = copysignf(kMost, x[i]);
+  }
+}
+
 }  // namespace lm

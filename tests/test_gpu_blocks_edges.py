@@ -105,3 +105,49 @@ def test_packed_activations_of_another_matrix_are_refused(B):
     assert all(torch.equal(raw[k], want[k]) for k in want)
     with pytest.raises(ValueError, match="bytes"):
         B.Q8(40, D, other.buf).values()
+
+
+# ---------------------------------------------------------------------------------------------
+# Ends of the types' ranges
+# ---------------------------------------------------------------------------------------------
+def test_q8_f16_keeps_finite_values_finite(B):
+    """Magnitudes from 65024 on are 64 * 2^10 in 8 bits: past f16's range, read as its largest."""
+    f16 = torch.float16
+    for top in (64992.0, 65024.0, 65056.0, 65504.0):
+        for sign in (1, -1):
+            x = rand(1, 3, 70, dtype=f16)
+            x[1, 37] = sign * top
+            q = B.Q8.pack(x)
+            v = q.values(f16)
+            assert torch.isfinite(v).all()
+            assert abs(v[1, 37].item() - sign * top) <= 512  # half a step of 2^10
+            wide = q.values(torch.float32)
+            assert torch.equal(v, wide.clamp(-65504, 65504).to(f16))
+    x = rand(1, 3, 70, dtype=f16)
+    x[1, 37] = float("inf")
+    v = B.Q8.pack(x).values(f16)
+    assert torch.isnan(v[1, 32:64]).all() and torch.isfinite(v[1, :32]).all()
+
+
+def test_ffn_gradients_from_f16_activations_at_the_end_of_the_range(B):
+    """A finite x near 65504, kept in 8 bits, leaves finite weight gradients: those of its value."""
+    rows, D, F = 40, 72, 104
+    dt = torch.float16
+    W = [rand(s, *shape, dtype=dt, scale=1e-3)
+         for s, shape in ((1, (F, D)), (2, (F, D)), (3, (D, F)))]
+    x, dout = rand(4, rows, D, dtype=dt), rand(5, rows, D, dtype=dt, scale=1e-3)
+    x[3, 7], x[9, 70] = 65504.0, -65300.0
+    kept = B.Kept(8, rows, *(B.Q8.pack(t) for t in (x, rand(6, rows, F), rand(7, rows, F))))
+    got = B.FeedForward(*W, "silu").backward(dout, kept)
+    vx, g, u = (t.values().double() for t in (kept.x, kept.g, kept.u))
+    vx = vx.clamp(-65504, 65504)
+    p = torch.sigmoid(g)
+    da = dout.double() @ W[2].double()
+    dg, du = da * u * p * (1 + g * (1 - p)), da * g * p
+    unit = 2.0 ** -11
+    for name, d in (("dWg", dg), ("dWu", du)):
+        want = d.T @ vx
+        # dg and du are rounded to f16 (2^-25 at the least), as is the result; the rest is under that
+        tol = (2 * unit * d.abs() + 2.0 ** -24).T @ vx.abs() + unit * want.abs() + 2.0 ** -24
+        assert torch.isfinite(got[name]).all()
+        assert ((got[name].double() - want).abs() <= tol).all(), name
