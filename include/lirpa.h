@@ -266,10 +266,12 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
  * Conventions of these calls, besides those above:
  * - `dtype` is the type of every tensor of a call unless a parameter says otherwise.  Products
  *   of 16-bit types run on their matrix instructions with 32-bit sums; LIRPA_F32 operands are
- *   split into three bf16 parts each (24 bits), and the six products of the largest parts are
- *   summed in 32 bits (an infinity then comes out as a NaN where its product with a smaller part
- *   has the other sign); up to 64 tokens whose projections are not kept, they are multiplied in 32
- *   bits.  Sums, norms and their reductions are held in 32 bits.
+ *   split into three bf16 parts each (24 bits from magnitudes of 2^-109 on; what lies under
+ *   2^-126 may be lost), and the six products of the largest parts are summed in 32 bits.  An
+ *   infinity in such an operand comes out as an infinity or as a NaN, since its products with the
+ *   other operand's smaller parts may have any sign or be 0 * inf.  Up to 64 tokens whose projections
+ *   are not kept, operands of LIRPA_F32 are multiplied in 32 bits.  Sums, norms and their
+ *   reductions are held in 32 bits.
  * - These calls take none of the inputs that LIRPA_VALIDATE checks, and report no findings.
  * - A matrix has contiguous rows; `ld` is the distance of two rows in elements (at least the
  *   row's length, less than 2^22).  Any alignment of the element type is taken; rows that start

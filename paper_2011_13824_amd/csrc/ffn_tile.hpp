@@ -17,7 +17,8 @@
 //   dWg, dWu      A = x (k-strided)              B = dg, du (k-strided)    EPI_STORE, one launch
 //   dWd           A = act(g) u (k-strided)       B = dout (k-strided)      EPI_STORE, with them
 //
-// 32-bit operands are three bf16 parts (hi + mid + lo = 24 bits); a product is then six segments,
+// 32-bit operands are three bf16 parts (hi + mid + lo = 24 bits, from magnitudes of 2^-109 on: parts
+// under bf16's least normal number may be lost); a product is then six segments,
 // those of the largest parts, smallest first, and the error stays that of a 32-bit sum (4e-7 of
 // the result's norm against 64 bits, where a library's 32-bit product has 1.3e-6).  Their rate
 // counts a sixth: six bf16 products at 1.2 PFLOP/s, where the 32-bit matrix instruction ends at
@@ -102,6 +103,18 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // Operands of the tile kernel: bf16, f16, or three bf16 parts of a float (Split).
 struct Split {};
+
+// The next bf16 part of v, which keeps what is left.  A finite v over bf16's largest stays finite, as
+// that and a rest; an infinity or a NaN is its first part alone.
+__device__ __forceinline__ float take_part(float& v) {
+  constexpr float kMost = 3.38953139e38f;  // 255 * 2^120
+  float p = (float)(bf16)v;
+  if (fabsf(p) > kMost && fabsf(v) < INFINITY) p = copysignf(kMost, v);
+  v -= p;
+  if (!(fabsf(v) < INFINITY)) v = 0.f;
+  return p;
+}
+
 template <typename T>
 struct Kind {
   using Half = T;  // what the matrix instruction takes
@@ -320,11 +333,7 @@ __device__ __forceinline__ void put_operand(const TileProblem& p, void* base, in
     for (int part = 0; part < 3; ++part) {
       float x[8];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        x[r] = (float)(H)rest[r];
-        rest[r] -= x[r];
-        if (!(fabsf(rest[r]) < INFINITY)) rest[r] = 0.f;  // of an infinity or a NaN
-      }
+      for (int r = 0; r < 8; ++r) x[r] = take_part(rest[r]);
       store_row<H, 8>((H*)(to + part * p.plane * sizeof(H) + at), p.pad_i - l.col, x);
     }
   }
@@ -887,7 +896,7 @@ __global__ __launch_bounds__(256) void k_ffn_operands(OperandJobs jobs) {
   const int64_t row = row0 + down;
   const int col = (int)(at - down * (uint32_t)per_row) * 8;
   if (row >= o.rows) return;
-  float v[8], p[8];
+  float v[8], p[8];  // p: a part
   if (o.exps) {
     const int groups = groups_of(o.n);
     unpack8_as<H>(load_global<u32x2>((const int8_t*)o.x + row * groups * kGroup + col),
@@ -899,15 +908,15 @@ __global__ __launch_bounds__(256) void k_ffn_operands(OperandJobs jobs) {
     return;
   }
   load_row_end<W, 8>((const W*)o.x + row * o.ldx + col, o.n - col, v);
+  if constexpr (Kind<T>::kParts == 1) {
+    store_row<H, 8>((H*)o.out + row * o.ld + col, 8, v);
+  } else {
 #pragma unroll
-  for (int part = 0; part < Kind<T>::kParts; ++part) {
+    for (int part = 0; part < Kind<T>::kParts; ++part) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = (float)(H)v[i];
-      v[i] -= p[i];
-      if (!(fabsf(v[i]) < INFINITY)) v[i] = 0.f;
+      for (int i = 0; i < 8; ++i) p[i] = take_part(v[i]);
+      store_row<H, 8>((H*)o.out + part * o.plane + row * o.ld + col, 8, p);
     }
-    store_row<H, 8>((H*)o.out + part * o.plane + row * o.ld + col, 8, p);
   }
 }
 

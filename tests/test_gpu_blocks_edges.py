@@ -151,3 +151,66 @@ def test_ffn_gradients_from_f16_activations_at_the_end_of_the_range(B):
         tol = (2 * unit * d.abs() + 2.0 ** -24).T @ vx.abs() + unit * want.abs() + 2.0 ** -24
         assert torch.isfinite(got[name]).all()
         assert ((got[name].double() - want).abs() <= tol).all(), name
+
+
+E = 2.0 ** -24
+
+
+def test_ffn_f32_finite_at_the_end_of_the_range(B):
+    """Finite floats over bf16's largest, 3.3895e38, are summed as what they are."""
+    rows, D, F = 90, 72, 104
+    x, dout = rand(1, rows, D), rand(2, rows, D, scale=1e-25)
+    W = [rand(s, *shape, scale=0.1) for s, shape in ((3, (F, D)), (4, (F, D)), (5, (D, F)))]
+    for i, top in ((3, 3.4e38), (70, -3.4028e38)):
+        x[i, 5] = top
+    for w in W[:2]:
+        w[:, 5] *= 1e-30
+    ffn = B.FeedForward(*W, "relu")
+    out, kept = ffn.forward(x, keep=0)
+    x64 = x.double()
+    for got, w in ((kept.g, W[0]), (kept.u, W[1])):
+        want = x64 @ w.double().T
+        tol = (D + 8) * E * (x64.abs() @ w.double().abs().T) + E * want.abs()
+        assert ((got.double() - want).abs() <= tol).all()
+    assert torch.isfinite(out).all()
+    g, u = rand(6, rows, F), rand(7, rows, F)
+    got = ffn.backward(dout, B.Kept(0, rows, x, g, u))
+    d64, w64, g64, u64 = dout.double(), W[2].double(), g.double(), u.double()
+    da, tda = d64 @ w64, (D + 8) * E * (d64.abs() @ w64.abs())
+    for name, by in (("dWg", u64 * (g64 > 0)), ("dWu", g64.clamp(min=0))):
+        d, td = da * by, tda * by.abs() + 8 * E * (da * by).abs()
+        want = d.T @ x64
+        tol = (td + (rows + 8) * E * d.abs()).T @ x64.abs() + E * want.abs()
+        assert ((got[name].double() - want).abs() <= tol).all(), name
+
+
+def test_ffn_f32_at_the_other_end(B):
+    """Under 2^-109 the parts of a float under 2^-126 may be lost: that much of it, no more."""
+    rows, D, F = 90, 72, 104
+    W = [rand(s, *shape) for s, shape in ((3, (F, D)), (4, (F, D)), (5, (D, F)))]
+    for scale in (1e-30, 1e-34, 1e-37, 1e-39):
+        x = rand(1, rows, D, scale=scale)
+        kept = B.FeedForward(*W, "relu").forward(x, keep=0)[1]
+        x64, w64 = x.double(), W[0].double()
+        want, size = x64 @ w64.T, x64.abs() @ w64.abs().T
+        tol = (D + 8) * E * size + 2.0 ** -125 * (w64.abs().sum(1) + 1)
+        assert ((kept.g.double() - want).abs() <= tol).all(), scale
+
+
+@pytest.mark.parametrize("rows", [8, 64, 65])
+def test_ffn_f32_infinities_stay_infinite_or_nan(B, rows):
+    W = [rand(s, *shape, scale=0.1) for s, shape in ((3, (104, 72)), (4, (104, 72)), (5, (72, 104)))]
+    W[0][7], W[1][9] = 1.0, 0.5  # one part alone
+    x = rand(1, rows, 72)
+    ffn = B.FeedForward(*W, "silu")
+    clean, kept0 = ffn.forward(x, keep=0)
+    x[5, 11] = float("inf")
+    for keep in (None, 0):
+        out = ffn.forward(x, keep=keep)
+        out, kept = out if keep == 0 else (out, None)
+        others = [r for r in range(rows) if r != 5]
+        assert not torch.isfinite(out[5]).any()
+        if keep == 0:
+            assert torch.equal(out[others], clean[others])
+            assert not torch.isfinite(kept.g[5]).any() and not torch.isfinite(kept.u[5]).any()
+            assert torch.equal(kept.g[others], kept0.g[others])
