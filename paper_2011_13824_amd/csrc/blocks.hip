@@ -558,18 +558,10 @@ int grads_of_size(TileArgs& t, int size, hipStream_t st) {
   if (size == 128) return launch_grads<T, 128, 2, 2>(t, st);
   return launch_grads<T, 256, 2, 4>(t, st);
 }
-// One launch, but dx of two and more whole rounds by itself: there is no idle CU to fill, and the
-// two kinds of tiles disturb each other's operands in the L2s (8192 tokens of 4096 x 10944 in bf16:
-// 2.83 ms, together 2.91).
+// All in one launch.  dx by itself gains 1 to 2 % where its tiles are whole rounds of the CUs (12,288
+// and 16,384 tokens of 4096 x 10944 in bf16: 4.42 and 5.99 ms, 4.46 and 6.05 together; 8192 the same)
+// and loses up to 12 % where they are not (8448: 3.31 ms, 2.96).
 int run_grads(const FfnPlan& pl, TileArgs& t, int size, hipStream_t st) {
-  if (t.count > 1 && !t.prob[0].b_strided && size == 256 &&
-      tiles_of(t.prob[0], 256, false) >= 2 * 256) {
-    TileArgs one = t;
-    one.count = 1;
-    TRY(run_grads(pl, one, size, st));
-    for (int i = 1; i < t.count; ++i) t.prob[i - 1] = t.prob[i];
-    --t.count;
-  }
   switch (pl.f->dtype) {
     case LIRPA_F32: return grads_of_size<Split>(t, size, st);
     case LIRPA_BF16: return grads_of_size<bf16>(t, size, st);

@@ -214,3 +214,19 @@ def test_ffn_f32_infinities_stay_infinite_or_nan(B, rows):
             assert torch.equal(out[others], clean[others])
             assert not torch.isfinite(kept.g[5]).any() and not torch.isfinite(kept.u[5]).any()
             assert torch.equal(kept.g[others], kept0.g[others])
+
+
+# ---------------------------------------------------------------------------------------------
+# Launches
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows", [8192, 8193])
+def test_ffn_gradients_share_a_launch(lirpa, B, rows):
+    """Also where dx's tiles fill the CUs twice and leave a few over: by itself those would leave
+    the rest idle."""
+    D, F, dt = 4096, 1024, torch.bfloat16
+    ffn = B.FeedForward(rand(1, F, D, dtype=dt), rand(2, F, D, dtype=dt), rand(3, D, F, dtype=dt))
+    x = rand(4, rows, D, dtype=dt)
+    _, kept = ffn.forward(x, keep=8)
+    lirpa.lirpa_timing_begin()
+    ffn.backward(x, kept)
+    assert lirpa.lirpa_timing_end()["ffn_grads"][1] == 1
