@@ -143,9 +143,18 @@ class FeedForward:
     relu, silu, gelu."""
 
     def __init__(self, Wg, Wu, Wd, gate="silu"):
-        self.weights = (Wg, Wu, Wd)
+        self.weights, self.gate = (Wg, Wu, Wd), gate
         self.block = lirpa.lirpa_ffn_block(Wg, Wu, Wd, gate)
-        self._need = {}  # workspace bytes by (rows, backward): they follow from the sizes
+        self._need = {}  # workspace bytes by (rows, backward) of this block
+
+    def _current(self):
+        """The block of the weights as they are now: a tensor's ``data`` may have been given another
+        storage, type or layout since the last call."""
+        block = lirpa.lirpa_ffn_block(*self.weights, self.gate)
+        if bytes(block) != bytes(self.block):
+            self.block = block
+            self._need.clear()
+        return self.block
 
     def _workspace(self, rows, backward):
         need = self._need.get((rows, backward))
@@ -159,13 +168,14 @@ class FeedForward:
     def forward(self, x, keep=None, x8=None):
         """out; with ``keep`` (8 or 0) (out, Kept).  ``x8``: x in 8 bits where the caller has it
         (a norm's y8); it is packed here otherwise."""
-        rows, dev, hidden = x.shape[0], x.device, self.block.n_hidden
+        block = self._current()
+        rows, dev, hidden = x.shape[0], x.device, block.n_hidden
         if x8 is not None:
-            _of_matrix(x8, rows, self.block.n_model, "x8")
+            _of_matrix(x8, rows, block.n_model, "x8")
         out = torch.empty_like(x)
         ws, need = self._workspace(rows, 0)
         if keep is None:
-            lirpa.lirpa_ffn_forward(self.block, x, out, lirpa.KEEP_NONE, None, None, ws, need)
+            lirpa.lirpa_ffn_forward(block, x, out, lirpa.KEEP_NONE, None, None, ws, need)
             return out
         if keep == 8:
             g, u = Q8(rows, hidden, device=dev), Q8(rows, hidden, device=dev)
@@ -173,17 +183,18 @@ class FeedForward:
         else:
             g, u = (torch.empty((rows, hidden), dtype=x.dtype, device=dev) for _ in range(2))
             kept = Kept(keep, rows, x, g, u)
-        lirpa.lirpa_ffn_forward(self.block, x, out, keep, *kept.raw(rows, self.block)[1:], ws, need)
+        lirpa.lirpa_ffn_forward(block, x, out, keep, *kept.raw(rows, block)[1:], ws, need)
         return out, kept
 
     def backward(self, dout, kept, want=("dx", "dWg", "dWu", "dWd")):
         """{name: gradient} of the wanted ones."""
-        x, g, u = kept.raw(dout.shape[0], self.block)
+        block = self._current()
+        x, g, u = kept.raw(dout.shape[0], block)
         like = {"dx": dout, "dWg": self.weights[0], "dWu": self.weights[1],
                 "dWd": self.weights[2]}
         grads = {k: torch.empty(like[k].shape, dtype=dout.dtype, device=dout.device)
                  for k in want}
         ws, need = self._workspace(dout.shape[0], 1)
-        lirpa.lirpa_ffn_backward(self.block, dout, kept.keep, x, g, u, *(
+        lirpa.lirpa_ffn_backward(block, dout, kept.keep, x, g, u, *(
             grads.get(k) for k in ("dx", "dWg", "dWu", "dWd")), ws, need)
         return grads

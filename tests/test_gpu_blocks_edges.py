@@ -230,3 +230,28 @@ def test_ffn_gradients_share_a_launch(lirpa, B, rows):
     lirpa.lirpa_timing_begin()
     ffn.backward(x, kept)
     assert lirpa.lirpa_timing_end()["ffn_grads"][1] == 1
+
+
+# ---------------------------------------------------------------------------------------------
+# Weights that move
+# ---------------------------------------------------------------------------------------------
+def test_ffn_reads_the_weights_as_they_are(B):
+    """After ``w.data = other``, of any layout or type, a call is that of a block made anew."""
+    D, F, rows = 72, 104, 90
+    W = [rand(s, *shape, scale=0.1) for s, shape in ((1, (F, D)), (2, (F, D)), (3, (D, F)))]
+    ffn = B.FeedForward(*W, "gelu")
+    x, dout = rand(4, rows, D), rand(5, rows, D)
+    ffn.backward(dout, ffn.forward(x, keep=8)[1])
+    held = [w.data for w in W]  # the old storage stays alive
+    for k, (pad, dtype) in enumerate([(0, torch.float32), (3, torch.float32), (0, torch.bfloat16),
+                                      (5, torch.bfloat16), (8, torch.float16)]):
+        for i, w in enumerate(W):
+            r, n = held[i].shape
+            w.data = rand(10 * k + i, r, n + pad, dtype=dtype, scale=0.1)[:, :n]
+        new = B.FeedForward(*(w.data for w in W), "gelu")
+        xt, dt = x.to(dtype), dout.to(dtype)
+        assert torch.equal(ffn.forward(xt[:3]), new.forward(xt[:3])), k
+        (out, kept), (want, nkept) = ffn.forward(xt, keep=8), new.forward(xt, keep=8)
+        assert torch.equal(out, want), k
+        got, grads = ffn.backward(dt, kept), new.backward(dt, nkept)
+        assert all(torch.equal(got[n], grads[n]) for n in grads), k
