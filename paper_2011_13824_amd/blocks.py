@@ -9,10 +9,14 @@ torch's current stream, where the calls run, and leave every computation to the 
     ...
     grads = ffn.backward(dout, kept)                  # dx, dWg, dWu, dWd
     dh, dw = norm.backward(grads["dx"], n.sum, n.rstd, dsum)
+
+Autograd records none of this: gradients are what the backward methods return.  A forward call whose
+inputs require gradients while autograd records warns of that.
 """
 from __future__ import annotations
 
 import collections
+import warnings
 
 import torch
 
@@ -30,6 +34,16 @@ def _bytes(n, device):
 def _type(t, what):
     """(dtype, its code in the library)"""
     return lirpa._dtype(t, what), DTYPES[t.dtype]
+
+
+def _no_tape(*tensors):
+    """Warns where a gradient would be lost."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            warnings.warn("autograd does not record the calls of paper_2011_13824_amd.blocks: their "
+                          "gradients come from the backward methods (call them under "
+                          "torch.no_grad(), or with detached tensors)", stacklevel=3)
+            return
 
 
 def _of_matrix(t, rows, n, what):
@@ -84,6 +98,7 @@ class Norm:
         wanted, else None; rstd is float32 [rows]."""
         rows, n = x.shape
         dt, code = _type(x, "x")
+        _no_tape(x, res, self.w)
         px, ldx = _matrix(x, rows, n, dt, "x")
         pr, ldr = _matrix(res, rows, n, dt, "res")
         pw = _vector(self.w, n, dt, "w")
@@ -169,6 +184,7 @@ class FeedForward:
         """out; with ``keep`` (8 or 0) (out, Kept).  ``x8``: x in 8 bits where the caller has it
         (a norm's y8); it is packed here otherwise."""
         block = self._current()
+        _no_tape(x, *self.weights)
         rows, dev, hidden = x.shape[0], x.device, block.n_hidden
         if x8 is not None:
             _of_matrix(x8, rows, block.n_model, "x8")

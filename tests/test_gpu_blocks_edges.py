@@ -1,5 +1,7 @@
 """The feed-forward block's calls where their contract is easily broken: buffers that are shared,
 ends of the types' ranges, batches that do not belong together, many rows."""
+import warnings
+
 import pytest
 import torch
 
@@ -255,3 +257,31 @@ def test_ffn_reads_the_weights_as_they_are(B):
         assert torch.equal(out, want), k
         got, grads = ffn.backward(dt, kept), new.backward(dt, nkept)
         assert all(torch.equal(got[n], grads[n]) for n in grads), k
+
+
+# ---------------------------------------------------------------------------------------------
+# Autograd
+# ---------------------------------------------------------------------------------------------
+def test_a_lost_gradient_is_warned_of(B):
+    D, F = 24, 40
+    x, w = rand(1, 5, D), rand(2, D)
+    W = [rand(s, *shape) for s, shape in ((3, (F, D)), (4, (F, D)), (5, (D, F)))]
+
+    def forward():
+        return B.Norm(w).forward(x, x), B.FeedForward(*W).forward(x)
+
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        forward()
+        for t in (x, w, W[1]):
+            t.requires_grad_()
+            with torch.no_grad():
+                forward()
+            t.requires_grad_(False)
+    for t, call in ((x, lambda: B.Norm(w).forward(x)), (w, lambda: B.Norm(w).forward(x)),
+                    (x, lambda: B.FeedForward(*W).forward(x)),
+                    (W[2], lambda: B.FeedForward(*W).forward(x, keep=8))):
+        t.requires_grad_()
+        with pytest.warns(UserWarning, match="autograd does not record"):
+            call()
+        t.requires_grad_(False)
