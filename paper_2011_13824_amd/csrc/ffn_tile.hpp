@@ -211,7 +211,7 @@ __device__ __forceinline__ u32x4 descriptor(const char* p, uint32_t bytes) {
 __device__ __forceinline__ void bring16(u32x4 desc, uint32_t offset, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds),
                "v"(offset), "s"(desc)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void wait_all() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
