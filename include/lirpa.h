@@ -276,8 +276,8 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
  * - A matrix has contiguous rows; `ld` is the distance of two rows in elements (at least the
  *   row's length, less than 2^22).  Any alignment of the element type is taken; rows that start
  *   on 16 bytes and whose length is a multiple of 8 elements are read in place, others are
- *   copied once per call into the workspace.  Outputs must not overlap inputs unless a
- *   parameter says so.
+ *   copied once per call into the workspace.  Outputs must not overlap inputs; where a parameter
+ *   may be the buffer of an input, it has the input's address and row distance.
  * - `rows` may be 0: nothing is read, sums over rows come out as 0.  Widths are 1 to 2^20,
  *   rows up to 2^31 - 1.
  * - Every call is deterministic: the order of its sums depends on sizes alone.

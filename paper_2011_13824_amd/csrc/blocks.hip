@@ -67,6 +67,15 @@ int check_rows(const char* who, const char* what, int dtype, const void* p, int6
   return LIRPA_OK;
 }
 
+// An output in an input's buffer: its rows lie where the input's do, or they would be written over
+// rows that are still to be read.
+int check_in_place(const char* who, const char* out, const void* po, int64_t ldo, const char* in,
+                   const void* pi, int64_t ldi, int64_t rows) {
+  if (!po || po != pi || ldo == ldi || rows == 1) return LIRPA_OK;
+  return fail(LIRPA_EINVAL, "%s: %s is the buffer of %s, with a row distance of %lld, not %lld", who,
+              out, in, (long long)ldo, (long long)ldi);
+}
+
 #define TRY(x)                     \
   do {                             \
     int rc_ = (x);                 \
@@ -889,6 +898,8 @@ int lirpa_norm_forward(int dtype, int64_t rows, int n, const void* x, int64_t ld
     if (sum) TRY(check_rows(who, "sum", dtype, sum, lds, n));
     if (y) TRY(check_rows(who, "y", dtype, y, ldy, n));
     if (y8) TRY(check_q8(who, "y8", y8));
+    TRY(check_in_place(who, "sum", sum, lds, "x", x, ldx, rows));
+    TRY(check_in_place(who, "sum", sum, lds, "res", res, ldr, rows));
     return by_type(dtype, [&](auto t) {
       using T = decltype(t);
       NormFwd<T> a{};
@@ -932,6 +943,8 @@ int lirpa_norm_backward(int dtype, int64_t rows, int n, const void* dy, int64_t 
       TRY(check_rows(who, "w", dtype, w, n, n));
       if (!rstd) return fail(LIRPA_EINVAL, "%s: rstd is null", who);
       if (dh) TRY(check_rows(who, "dh", dtype, dh, lddh, n));
+      TRY(check_in_place(who, "dh", dh, lddh, "dy", dy, lddy, rows));
+      TRY(check_in_place(who, "dh", dh, lddh, "dsum", dsum, ldds, rows));
     }
     if (dw) {
       TRY(check_rows(who, "dw", dtype, dw, n, n));
