@@ -334,10 +334,10 @@ def _matrix(t, rows, n, dtype, what):
     ld, step = t.stride()
     if step != 1 and n > 1:
         raise ValueError(f"{what} must have contiguous rows")
-    if ld < n:
-        if rows > 1:
-            raise ValueError(f"rows of {what} overlap")
+    if rows <= 1:  # no second row: its distance is of no account, and may be any
         ld = n
+    elif ld < n:
+        raise ValueError(f"rows of {what} overlap")
     return t.data_ptr(), ld
 
 

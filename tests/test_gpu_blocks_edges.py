@@ -285,3 +285,25 @@ def test_a_lost_gradient_is_warned_of(B):
         with pytest.warns(UserWarning, match="autograd does not record"):
             call()
         t.requires_grad_(False)
+
+
+# ---------------------------------------------------------------------------------------------
+# Rows
+# ---------------------------------------------------------------------------------------------
+def test_one_row_has_no_row_distance(B):
+    """The last token of a long sequence: a row whose tensor's stride passes 2^22."""
+    D, F, dt = 64, 96, torch.bfloat16
+    seq = rand(1, 1, (1 << 22) // D + 3, D, dtype=dt)
+    x = seq[:, -1]
+    assert x.shape == (1, D) and x.stride(0) >= 1 << 22
+    same = x.clone(memory_format=torch.contiguous_format)
+    ffn = B.FeedForward(rand(2, F, D, dtype=dt), rand(3, F, D, dtype=dt), rand(4, D, F, dtype=dt))
+    norm = B.Norm(rand(5, D, dtype=dt))
+    assert torch.equal(ffn.forward(x), ffn.forward(same))
+    n, want = norm.forward(x, x, want8=True), norm.forward(same, same, want8=True)
+    assert torch.equal(n.y, want.y) and torch.equal(n.sum, want.sum)
+    assert torch.equal(n.y8.buf, want.y8.buf)
+    assert torch.equal(B.Q8.pack(x).buf, B.Q8.pack(same).buf)
+    (_, kept), (_, nkept) = ffn.forward(x, keep=0), ffn.forward(same, keep=0)
+    got, grads = ffn.backward(x, kept), ffn.backward(same, nkept)
+    assert all(torch.equal(got[k], grads[k]) for k in grads)
