@@ -279,7 +279,8 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
  *   copied once per call into the workspace.  Outputs must not overlap inputs; where a parameter
  *   may be the buffer of an input, it has the input's address and row distance.
  * - `rows` may be 0: nothing is read, sums over rows come out as 0.  Widths are 1 to 2^20,
- *   rows up to 2^31 - 1.
+ *   rows up to 2^30; lirpa_ffn_* returns LIRPA_EUNSUPPORTED where a matrix of the call has more than
+ *   2^35 values.
  * - Every call is deterministic: the order of its sums depends on sizes alone.
  * ============================================================================================= */
 typedef enum { LIRPA_F32 = 0, LIRPA_BF16 = 1, LIRPA_F16 = 2 } lirpa_dtype;

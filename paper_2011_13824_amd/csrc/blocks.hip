@@ -28,6 +28,9 @@ bool is_dtype(int t) { return t == LIRPA_F32 || t == LIRPA_BF16 || t == LIRPA_F1
 size_t bytes_of(int dtype) { return dtype == LIRPA_F32 ? 4 : 2; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// A launch has fewer than 2^32 threads.  The most blocks of `threads`:
+constexpr int64_t max_blocks(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+
 // No C++ exception leaves a C entry.
 template <typename F>
 int guarded(F&& f) {
@@ -94,24 +97,35 @@ int check_q8(const char* who, const char* what, const void* p) {
   return LIRPA_OK;
 }
 
+// Rows of groups that one launch takes, a thread for 8 columns; more go out in several.
+int64_t q8_launch_rows(int n) { return max_blocks(256) * 256 / (groups_of(n) * 4); }
+
 template <typename T>
 int q8_pack(int64_t rows, int n, const T* x, int64_t ldx, void* q8, hipStream_t st) {
-  const int64_t blocks = (rows * groups_of(n) * 4 + 255) / 256;
-  if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "q8_pack: more than 2^42 values");
-  return launch_k("q8_pack", st, [&] {
-    k_q8_pack<T><<<(unsigned)blocks, 256, 0, st>>>(x, ldx, rows, n, (int8_t*)q8,
-                                                   (uint8_t*)q8 + q8_exps_at(rows, n));
-  });
+  const int64_t each = q8_launch_rows(n), groups = groups_of(n);
+  for (int64_t r0 = 0; r0 < rows; r0 += each) {
+    const int64_t r = std::min(each, rows - r0), blocks = (r * groups * 4 + 255) / 256;
+    TRY(launch_k("q8_pack", st, [&] {
+      k_q8_pack<T><<<(unsigned)blocks, 256, 0, st>>>(
+          x + r0 * ldx, ldx, r, n, (int8_t*)q8 + r0 * groups * kGroup,
+          (uint8_t*)q8 + q8_exps_at(rows, n) + r0 * groups);
+    }));
+  }
+  return LIRPA_OK;
 }
 
 template <typename T>
 int q8_unpack(int64_t rows, int n, const void* q8, T* x, int64_t ldx, hipStream_t st) {
-  const int64_t blocks = (rows * groups_of(n) * 4 + 255) / 256;
-  if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "q8_unpack: more than 2^42 values");
-  return launch_k("q8_unpack", st, [&] {
-    k_q8_unpack<T><<<(unsigned)blocks, 256, 0, st>>>(
-        (const int8_t*)q8, (const uint8_t*)q8 + q8_exps_at(rows, n), rows, n, x, ldx);
-  });
+  const int64_t each = q8_launch_rows(n), groups = groups_of(n);
+  for (int64_t r0 = 0; r0 < rows; r0 += each) {
+    const int64_t r = std::min(each, rows - r0), blocks = (r * groups * 4 + 255) / 256;
+    TRY(launch_k("q8_unpack", st, [&] {
+      k_q8_unpack<T><<<(unsigned)blocks, 256, 0, st>>>(
+          (const int8_t*)q8 + r0 * groups * kGroup,
+          (const uint8_t*)q8 + q8_exps_at(rows, n) + r0 * groups, r, n, x + r0 * ldx, ldx);
+    }));
+  }
+  return LIRPA_OK;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -146,15 +160,29 @@ int by_norm_shape(NormShape s, F&& f) {
 }
 
 template <typename T>
-int norm_fwd(const NormFwd<T>& a, hipStream_t st) {
+int norm_fwd(NormFwd<T> a, hipStream_t st) {
   const NormShape s = norm_shape(a.n);
-  const int64_t blocks = s.threads == 64 ? (a.rows + 3) / 4 : a.rows;
-  return by_norm_shape(s, [&](auto th, auto ch) {
-    return launch_k("norm_forward", st, [&] {
-      k_norm_fwd<T, th.value, ch.value>
-          <<<(unsigned)blocks, th.value == 64 ? 256 : th.value, 0, st>>>(a);
-    });
-  });
+  const int per_block = s.threads == 64 ? 4 : 1, threads = s.threads == 64 ? 256 : s.threads;
+  const int64_t each = max_blocks(threads) * per_block;  // rows a launch
+  for (int64_t left = a.rows; left > 0; left -= each) {
+    a.rows = std::min(each, left);
+    const int64_t blocks = (a.rows + per_block - 1) / per_block;
+    TRY(by_norm_shape(s, [&](auto th, auto ch) {
+      return launch_k("norm_forward", st, [&] {
+        k_norm_fwd<T, th.value, ch.value><<<(unsigned)blocks, threads, 0, st>>>(a);
+      });
+    }));
+    a.x += a.rows * a.ldx;
+    if (a.res) a.res += a.rows * a.ldr;
+    if (a.sum) a.sum += a.rows * a.lds;
+    if (a.y) a.y += a.rows * a.ldy;
+    if (a.q) {
+      a.q += a.rows * groups_of(a.n) * kGroup;
+      a.exps += a.rows * groups_of(a.n);
+    }
+    if (a.rstd) a.rstd += a.rows;
+  }
+  return LIRPA_OK;
 }
 
 // Blocks of the backward pass, and so partial sums of dw: enough to fill the chip.
@@ -281,7 +309,8 @@ struct Copies {
   }
   int run(const FfnPlan& pl, hipStream_t st) const {
     if (blocks == 0) return LIRPA_OK;
-    if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "ffn_operands: more than 2^42 values");
+    if (blocks > max_blocks(256))
+      return fail(LIRPA_EUNSUPPORTED, "ffn_operands: more than 2^35 values");
     return launch_k("ffn_operands", st, [&] {
       switch (pl.f->dtype) {
         case LIRPA_F32: k_ffn_operands<Split><<<(unsigned)blocks, 256, 0, st>>>(jobs); break;
@@ -482,7 +511,8 @@ struct Joins {
   }
   int run(const FfnPlan& pl, hipStream_t st) const {
     if (blocks == 0) return LIRPA_OK;
-    if (blocks > 0x7fffffff) return fail(LIRPA_EUNSUPPORTED, "ffn_join: more than 2^42 values");
+    if (blocks > max_blocks(256))
+      return fail(LIRPA_EUNSUPPORTED, "ffn_join: more than 2^35 values");
     return launch_k("ffn_join", st, [&] {
       switch (pl.f->dtype) {
         case LIRPA_F32: k_ffn_join<float><<<(unsigned)blocks, 256, 0, st>>>(jobs); break;
@@ -493,16 +523,17 @@ struct Joins {
   }
 };
 
-// Numbers the tiles; `total` blocks.
+// Numbers the tiles; `total` blocks of `threads`.
 template <int SIZE, int EPI>
-int lay_out(const char* name, TileArgs& t, int64_t& total) {
+int lay_out(const char* name, TileArgs& t, int threads, int64_t& total) {
   total = 0;
   for (int i = 0; i < t.count; ++i) {
     TileProblem& p = t.prob[i];
     const int64_t feat = EPI == EPI_GATE ? SIZE / 2 : SIZE;
     const int64_t ti = up(p.I, feat) / feat, tj = up(p.J, SIZE) / SIZE;
-    if (total + ti * tj * p.splits > 0x7fffffff)
-      return fail(LIRPA_EUNSUPPORTED, "%s: more than 2^31 tiles", name);
+    if (total + ti * tj * p.splits > max_blocks(threads))
+      return fail(LIRPA_EUNSUPPORTED, "%s: more than %lld tiles", name,
+                  (long long)max_blocks(threads));
     p.tiles_i = (int)ti;
     p.tiles_j = (int)tj;
     p.first = (unsigned)total;
@@ -514,7 +545,7 @@ int lay_out(const char* name, TileArgs& t, int64_t& total) {
 template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int SIZE, int WI, int WJ, int AHEAD>
 int launch_tile(const char* name, TileArgs& t, hipStream_t st) {
   int64_t total;
-  TRY((lay_out<SIZE, EPI>(name, t, total)));
+  TRY((lay_out<SIZE, EPI>(name, t, WI * WJ * 64, total)));
   if (total == 0) return LIRPA_OK;
   return launch_k(name, st, [&] {
     k_ffn_tile<T, AKS, BKS, EPI, KEEP, SIZE, WI, WJ, AHEAD>
@@ -542,8 +573,8 @@ int tile_of_size(const char* name, TileArgs& t, const Cut& c, char* part, Joins*
     if (p.splits > 1) {
       const int64_t blocks = ((int64_t)p.J * groups_of(p.I) * 4 + 255) / 256;
       if (blocks == 0) return LIRPA_OK;
-      if (blocks > 0x7fffffff)
-        return fail(LIRPA_EUNSUPPORTED, "ffn_finish: more than 2^42 values");
+      if (blocks > max_blocks(256))
+        return fail(LIRPA_EUNSUPPORTED, "ffn_finish: more than 2^35 values");
       return launch_k("ffn_finish", st, [&] {
         k_ffn_finish<T, EPI, KEEP><<<(unsigned)blocks, 256, 0, st>>>(t);
       });
@@ -555,7 +586,7 @@ int tile_of_size(const char* name, TileArgs& t, const Cut& c, char* part, Joins*
 template <typename T, int SIZE, int WI, int WJ>
 int launch_grads(TileArgs& t, hipStream_t st) {
   int64_t total;
-  TRY((lay_out<SIZE, EPI_STORE>("ffn_grads", t, total)));
+  TRY((lay_out<SIZE, EPI_STORE>("ffn_grads", t, WI * WJ * 64, total)));
   if (total == 0) return LIRPA_OK;
   return launch_k("ffn_grads", st, [&] {
     k_ffn_grads<T, SIZE, WI, WJ><<<(unsigned)total, WI * WJ * 64, 0, st>>>(t);

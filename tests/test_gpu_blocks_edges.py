@@ -307,3 +307,33 @@ def test_one_row_has_no_row_distance(B):
     (_, kept), (_, nkept) = ffn.forward(x, keep=0), ffn.forward(same, keep=0)
     got, grads = ffn.backward(x, kept), ffn.backward(same, nkept)
     assert all(torch.equal(got[k], grads[k]) for k in grads)
+
+
+def test_norm_of_more_rows_than_a_launch_takes(B):
+    """2^26 rows of a wave each are 2^32 threads."""
+    rows = (1 << 26) + 5
+    x = rand(1, rows, 1, dtype=torch.bfloat16)
+    w = torch.full((1,), 1.5, dtype=torch.bfloat16, device="cuda")
+    got = B.Norm(w).forward(x, x, want8=True)
+    h = 2 * x.float()
+    rstd = torch.rsqrt(h[:, 0].square() + 1e-5)
+    assert ((got.rstd - rstd).abs() <= 16 * E * rstd).all()
+    assert torch.equal(got.sum, h.to(x.dtype))
+    del rstd
+    y = h * got.rstd[:, None] * 1.5
+    assert ((got.y.float() - y).abs() <= 2.0 ** -7 * y.abs()).all()
+    # the packed y is within half a step, its scale the least one
+    v = got.y8.values()
+    assert ((v - y).abs() <= y.abs() / 126).all()
+    dh, dw = B.Norm(w).backward(x, got.sum, got.rstd)
+    assert torch.isfinite(dh[-9:]).all() and torch.isfinite(dw).all()
+
+
+def test_q8_of_the_most_rows(B):
+    """2^30 rows of one group each are 2^32 threads; the scales lie 2^35 bytes into the buffer."""
+    rows = 1 << 30
+    x = torch.arange(rows, dtype=torch.int32, device="cuda").remainder_(251).sub_(125)
+    x = x.to(torch.bfloat16).view(rows, 1)  # one value a group: exact in 8 bits
+    q = B.Q8.pack(x)
+    assert q.buf.numel() == rows * 33
+    assert torch.equal(q.values(torch.bfloat16), x)
