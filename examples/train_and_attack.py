@@ -4,7 +4,8 @@ The blocks run on ``paper_2011_13824_amd.blocks``: each adds its input to the re
 norms it, and keeps what its backward pass needs in 8 bits.  Training fits a synthetic function
 with Adam; the search is projected gradient descent on a margin of the trained net over an l_inf
 box, and ends with an upper bound on the margin's minimum there: the least value it has met (a
-point with a negative margin violates the property margin >= 0).
+point with a negative margin violates the property margin >= 0).  The points it tries are values of
+the net's type inside the box.
 
     python examples/train_and_attack.py [--steps 60] [--width 256] [--hidden 704] [--rows 2048]
 """
@@ -97,14 +98,34 @@ def train(net, steps, rows, width, outputs, dtype, lr=2e-3):
     return [float(x) for x in losses]
 
 
+def box(x0, eps, dtype):
+    """(lowest, highest) values of `dtype` with |v - x0| <= eps in every place, in 64 bits."""
+    ends = []
+    for sign in (-1, 1):
+        end = x0.double() + sign * eps
+        v = end.to(dtype).double()
+        # one past the end by rounding: the next value inwards is at most two units of v away
+        unit = v.abs().clamp(min=torch.finfo(dtype).tiny) * torch.finfo(dtype).eps
+        for part in (0.25, 0.5, 1.0):
+            v = torch.where(sign * (v - end) > 0, (v - sign * part * unit).to(dtype).double(), v)
+        ends.append(v)
+    lo, hi = ends
+    if (lo > hi).any():
+        raise ValueError(f"{dtype} has no value within {eps} of x0 in some places")
+    return lo, hi
+
+
 def attack(net, x0, eps, c, steps=20, starts=64):
     """The least c . f(x) met over ||x - x0||_inf <= eps, from `starts` random points."""
     gen = torch.Generator(device="cuda")
     gen.manual_seed(2)
+    dtype = net.params["out"].dtype
+    lo, hi = box(x0, eps, dtype)
     x = x0 + eps * (2 * torch.rand(starts, x0.numel(), generator=gen, device="cuda") - 1)
     least = float("inf")
     for t in range(steps + 1):
-        y, tape = net.forward(x.to(net.params["out"].dtype), keep=t < steps)
+        at = torch.clamp(x.to(dtype).double(), lo, hi).to(dtype)  # clamp rounds nothing
+        y, tape = net.forward(at, keep=t < steps)
         least = min(least, float((y @ c).min()))
         if t < steps:
             _, dx = net.backward(c.expand(starts, -1).contiguous(), tape, weights=False)
