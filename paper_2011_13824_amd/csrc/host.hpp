@@ -15,13 +15,19 @@ namespace lirpa_host {
 
 inline thread_local std::string g_err;
 
-inline int fail(int code, const char* fmt, ...) {
+// Never throws: it ends the C entries, the one for sizes too.  Without memory for it the message is
+// left out.
+inline int fail(int code, const char* fmt, ...) noexcept {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  g_err = buf;
+  try {
+    g_err = buf;
+  } catch (...) {
+    g_err.clear();
+  }
   return code;
 }
 
