@@ -104,14 +104,14 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 // Operands of the tile kernel: bf16, f16, or three bf16 parts of a float (Split).
 struct Split {};
 
-// The next bf16 part of v, which keeps what is left.  A finite v over bf16's largest stays finite, as
-// that and a rest; an infinity or a NaN is its first part alone.
-__device__ __forceinline__ float take_part(float& v) {
+// The next bf16 part of v, which keeps what is left.  The first part of a finite v over bf16's largest
+// is that, and the second holds the rest; an infinity or a NaN is its first part alone.
+__device__ __forceinline__ float take_part(float& v, bool first) {
   constexpr float kMost = 3.38953139e38f;  // 255 * 2^120
-  float p = (float)(bf16)v;
-  if (fabsf(p) > kMost && fabsf(v) < INFINITY) p = copysignf(kMost, v);
+  const float whole = v;
+  float p = (float)(bf16)(first ? __builtin_amdgcn_fmed3f(v, -kMost, kMost) : v);
   v -= p;
-  if (!(fabsf(v) < INFINITY)) v = 0.f;
+  if (first && !(fabsf(v) < INFINITY)) p = whole, v = 0.f;
   return p;
 }
 
@@ -333,7 +333,7 @@ __device__ __forceinline__ void put_operand(const TileProblem& p, void* base, in
     for (int part = 0; part < 3; ++part) {
       float x[8];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) x[r] = take_part(rest[r]);
+      for (int r = 0; r < 8; ++r) x[r] = take_part(rest[r], part == 0);
       store_row<H, 8>((H*)(to + part * p.plane * sizeof(H) + at), p.pad_i - l.col, x);
     }
   }
@@ -914,7 +914,7 @@ __global__ __launch_bounds__(256) void k_ffn_operands(OperandJobs jobs) {
 #pragma unroll
     for (int part = 0; part < Kind<T>::kParts; ++part) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = take_part(v[i]);
+      for (int i = 0; i < 8; ++i) p[i] = take_part(v[i], part == 0);
       store_row<H, 8>((H*)o.out + part * o.plane + row * o.ld + col, 8, p);
     }
   }
