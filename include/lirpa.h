@@ -257,8 +257,10 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
 /* =============================================================================================
  * The feed-forward block of a language model
  *
- * The passes of the networks whose answers are bounded: what a user runs to train such a block,
- * to search its input box for a violating point (the gradient of the input), and to serve it.
+ * What a user runs to train such a block, to search its input box for a violating point (the
+ * gradient of the input), and to serve it.  These calls stand beside the bounds: lirpa_net
+ * describes LINEAR and CONV2D layers with ReLU between them, and no bound covers a gated block or a
+ * norm.
  * A block is a root-mean-square norm that adds the residual, then
  *     out = (act(x Wg^T) * (x Wu^T)) Wd^T
  * and its backward pass reads activations that the forward pass kept in 8 bits.
@@ -269,9 +271,9 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
  *   split into three bf16 parts each (24 bits from magnitudes of 2^-109 on; what lies under
  *   2^-126 may be lost), and the six products of the largest parts are summed in 32 bits.  An
  *   infinity in such an operand comes out as an infinity or as a NaN, since its products with the
- *   other operand's smaller parts may have any sign or be 0 * inf.  Up to 64 tokens whose projections
- *   are not kept, operands of LIRPA_F32 are multiplied in 32 bits.  Sums, norms and their
- *   reductions are held in 32 bits.
+ *   other operand's smaller parts may have any sign or be 0 * inf.  Up to 64 tokens whose
+ *   projections are not kept, operands of LIRPA_F32 are multiplied in 32 bits.  Sums, norms and
+ *   their reductions are held in 32 bits.
  * - These calls take none of the inputs that LIRPA_VALIDATE checks, and report no findings.
  * - A matrix has contiguous rows; `ld` is the distance of two rows in elements (at least the
  *   row's length, less than 2^22).  Any alignment of the element type is taken; rows that start
@@ -279,9 +281,10 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
  *   copied once per call into the workspace.  Outputs must not overlap inputs; where a parameter
  *   may be the buffer of an input, it has the input's address and row distance.
  * - `rows` may be 0: nothing is read, sums over rows come out as 0.  Widths are 1 to 2^20,
- *   rows up to 2^30; lirpa_ffn_* returns LIRPA_EUNSUPPORTED where a matrix of the call has more than
- *   2^35 values.
- * - Every call is deterministic: the order of its sums depends on sizes alone.
+ *   rows up to 2^30; lirpa_ffn_* returns LIRPA_EUNSUPPORTED where a matrix of the call has more
+ *   than 2^35 values.
+ * - Every call is deterministic: the order of its sums depends on sizes and types, and for 9 to 64
+ *   tokens whose projections are not kept on whether the weights are read in place.
  * ============================================================================================= */
 typedef enum { LIRPA_F32 = 0, LIRPA_BF16 = 1, LIRPA_F16 = 2 } lirpa_dtype;
 

@@ -404,9 +404,10 @@ size_t part_room(const Cut& c, const TileProblem* probs, int count, int arrays =
 }
 
 // The room that a call keeps for such sums.  It never falls with the rows, so that a workspace for
-// many rows holds fewer too, and a cut that needs more is not taken: the most parts there can be, and
-// no more than kMostParts.  Of 60,000 products up to 8192 rows of 4096 x 10944, that limit changes no
-// cut of 16-bit types and 0.1 % of those of floats, whose estimated times grow by 1 % on average.
+// many rows holds fewer too, and a cut that needs more is not taken: the most parts there can be,
+// and no more than kMostParts.  Of 60,000 products up to 8192 rows of 4096 x 10944, that limit
+// changes no cut of 16-bit types and 0.1 % of those of floats, whose estimated times grow by 1 % on
+// average.
 constexpr size_t kMostParts = (size_t)128 << 20, kMostParts32 = (size_t)256 << 20;
 constexpr int kMaxSplits = 16;
 size_t most_part_room(const FfnPlan& pl, const TileProblem* probs, int count, int arrays = 1) {
@@ -598,9 +599,9 @@ int grads_of_size(TileArgs& t, int size, hipStream_t st) {
   if (size == 128) return launch_grads<T, 128, 2, 2>(t, st);
   return launch_grads<T, 256, 2, 4>(t, st);
 }
-// All in one launch.  dx by itself gains 1 to 2 % where its tiles are whole rounds of the CUs (12,288
-// and 16,384 tokens of 4096 x 10944 in bf16: 4.42 and 5.99 ms, 4.46 and 6.05 together; 8192 the same)
-// and loses up to 12 % where they are not (8448: 3.31 ms, 2.96).
+// All in one launch.  dx by itself gains 1 to 2 % where its tiles are whole rounds of the CUs
+// (12,288 and 16,384 tokens of 4096 x 10944 in bf16: 4.42 and 5.99 ms, 4.46 and 6.05 together; 8192
+// the same) and loses up to 12 % where they are not (8448: 3.31 ms, 2.96).
 int run_grads(const FfnPlan& pl, TileArgs& t, int size, hipStream_t st) {
   switch (pl.f->dtype) {
     case LIRPA_F32: return grads_of_size<Split>(t, size, st);

@@ -19,13 +19,15 @@
 //
 // 32-bit operands are three bf16 parts (hi + mid + lo = 24 bits, from magnitudes of 2^-109 on: parts
 // under bf16's least normal number may be lost); a product is then six segments,
-// those of the largest parts, smallest first, and the error stays that of a 32-bit sum (4e-7 of
+// those of the largest parts, smallest first, and the error stays that of a 32-bit sum (6e-7 of
 // the result's norm against 64 bits, where a library's 32-bit product has 1.3e-6).  Their rate
 // counts a sixth: six bf16 products at 1.2 PFLOP/s, where the 32-bit matrix instruction ends at
 // 157 TFLOP/s.
 //
 // act(g) u, dg and du are rounded to the tensors' type between two products: they are operands of
-// 16-bit instructions.  That is one more rounding of 2^-9 (bf16) in each result, of random sign.
+// 16-bit instructions.  That is one more rounding of up to 2^-8 (bf16) or 2^-11 (f16) of every term,
+// of random sign: a bf16 result is off by 0.0023 of its norm, where operands of 32 bits leave
+// 0.0017.
 //
 // How the loop is fed (8192^3 in bf16 on one MI355X, TFLOP/s; the matrix instructions alone reach
 // 1640 to 1930 there, a third less with random operands than with zeros, for power):
@@ -104,8 +106,8 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 // Operands of the tile kernel: bf16, f16, or three bf16 parts of a float (Split).
 struct Split {};
 
-// The next bf16 part of v, which keeps what is left.  The first part of a finite v over bf16's largest
-// is that, and the second holds the rest; an infinity or a NaN is its first part alone.
+// The next bf16 part of v, which keeps what is left.  The first part of a finite v over bf16's
+// largest is that, and the second holds the rest; an infinity or a NaN is its first part alone.
 __device__ __forceinline__ float take_part(float& v, bool first) {
   constexpr float kMost = 3.38953139e38f;  // 255 * 2^120
   const float whole = v;
@@ -742,11 +744,11 @@ __device__ __forceinline__ void ffn_tile(const TileArgs& a, const TileProblem& p
 
 // One product with its epilogue.
 //
-// Bound by the matrix instructions (busy 62 to 74 % of the cycles at 8192 tokens, 4096 x 10944 in
-// bf16: gate and up 1.21 ms, 1218 TFLOP/s; down 0.54 ms, 1354), and, for da, by its epilogue (0.79
-// ms, 930 TFLOP/s, busy 47 %): there all CUs come to read what was kept and to write three operands
-// at the same time, 0.72 GB in all.  Few tokens are bound by the weights' bytes (64 tokens: 4.7
-// TB/s in gate and up).
+// Bound by the matrix instructions (busy 61 to 70 % of the cycles at 8192 tokens, 4096 x 10944 in
+// bf16: gate and up 1.22 ms, 1200 TFLOP/s; down 0.54 ms, 1360; loops of 30 calls), and, for da, by
+// its epilogue (0.80 ms, 920 TFLOP/s, busy 46 %): there all CUs come to read what was kept and to
+// write three operands at the same time, 0.72 GB in all.  Few tokens are bound by the weights' bytes
+// (24 tokens of 2048 x 5504: 3.1 TB/s in gate and up, 4.1 in down).
 template <typename T, bool AKS, bool BKS, int EPI, int KEEP, int SIZE, int WI, int WJ, int AHEAD>
 __global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_tile(TileArgs a) {
   using U = Units<AKS, BKS, SIZE, SIZE, AHEAD>;
@@ -757,7 +759,7 @@ __global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_tile(TileArgs a) {
 
 // The gradients, which do not depend on one another: dx (long sums) before dWg, dWu and dWd, so
 // that the shorter ones fill what it leaves.  Bound by the matrix instructions at 8192 tokens (4096
-// x 10944 in bf16: 2.83 ms, 1300 TFLOP/s); 777 x 1001 x 2731 in f16 34 us, 45 in three launches.
+// x 10944 in bf16: 2.84 ms, 1290 TFLOP/s); 777 x 1001 x 2731 in f16 34 us, 45 in three launches.
 template <typename T, int SIZE, int WI, int WJ>
 __global__ __launch_bounds__(WI* WJ * 64, 2) void k_ffn_grads(TileArgs a) {
   using U = Units<true, true, SIZE, SIZE, 1>;

@@ -2,9 +2,10 @@
 //
 // q = rint(x * 2^-e), e the least with 127 * 2^e >= max |x| of the group: the scale is a power of
 // two, so neither the product nor reading back rounds (127 multiples fit the 8-bit significand of
-// bf16; in f16 magnitudes past its range are read as its largest).  Both kernels are bound by the bytes that they move: a thread takes 8 columns (16 bytes of
-// a 16-bit type, 8 of the packed values), four neighbouring lanes make a group and find its largest
-// magnitude with two lane exchanges.  8192 x 10944 in bf16, packed and read back: 93 us for 549 MB,
+// bf16; in f16 magnitudes past its range are read as its largest).  Both kernels are bound by the
+// bytes that they move: a thread takes 8 columns (16 bytes of a 16-bit type, 8 of the packed
+// values), four neighbouring lanes make a group and find its largest magnitude with two lane
+// exchanges.  8192 x 10944 in bf16, packed and read back: 93 us for 549 MB,
 // 5.9 TB/s (part of it out of the last-level cache).
 #pragma once
 
