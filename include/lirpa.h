@@ -281,8 +281,8 @@ int lirpa_bab(lirpa_net* net, const float* x0, float eps, const float* c,
  *   copied once per call into the workspace.  Outputs must not overlap inputs; where a parameter
  *   may be the buffer of an input, it has the input's address and row distance.
  * - `rows` may be 0: nothing is read, sums over rows come out as 0.  Widths are 1 to 2^20,
- *   rows up to 2^30; lirpa_ffn_* returns LIRPA_EUNSUPPORTED where a matrix of the call has more
- *   than 2^35 values.
+ *   rows up to 2^30; lirpa_ffn_* returns LIRPA_EUNSUPPORTED where one of its launches would pass
+ *   2^32 threads (some 2^35 values in a matrix).
  * - Every call is deterministic: the order of its sums depends on sizes and types, and for 9 to 64
  *   tokens whose projections are not kept on whether the weights are read in place.
  * ============================================================================================= */
