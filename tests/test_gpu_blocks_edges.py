@@ -5,6 +5,8 @@ import warnings
 import pytest
 import torch
 
+from .test_gpu_blocks import UNIT, backward64, check, forward64
+
 pytestmark = pytest.mark.gpu
 
 TYPES = [torch.float32, torch.bfloat16, torch.float16]
@@ -337,3 +339,31 @@ def test_q8_of_the_most_rows(B):
     q = B.Q8.pack(x)
     assert q.buf.numel() == rows * 33
     assert torch.equal(q.values(torch.bfloat16), x)
+
+
+@pytest.mark.parametrize("keep", [8, 0])
+def test_ffn_of_more_values_than_32_bits_count(B, keep):
+    """Projections of 2^31 and more values: the last rows, and the weights' gradients, to which they
+    alone contribute, against 64 bits."""
+    D, F, rows, last, dt = 64, 2112, 1 << 20, 90, torch.bfloat16
+    W = [rand(s, *shape, dtype=dt, scale=0.1)
+         for s, shape in ((1, (F, D)), (2, (F, D)), (3, (D, F)))]
+    ffn = B.FeedForward(*W)
+    x, dout = rand(4, rows, D, dtype=dt), torch.zeros(rows, D, dtype=dt, device="cuda")
+    dout[-last:] = rand(5, last, D, dtype=dt)
+    got, kept = ffn.forward(x, keep=keep)
+    out, tol, g, tg, u, tu = forward64(x[-last:], W, "silu", UNIT[dt])
+    check(got[-last:], out, tol + 1e-30, "out")
+    if keep == 0:
+        ends = [t[-last:] for t in (x, kept.g, kept.u)]
+        check(ends[1], g, tg + UNIT[dt] * g.abs(), "g")
+        check(ends[2], u, tu + UNIT[dt] * u.abs(), "u")
+    else:
+        ends = [t.values()[-last:] for t in (kept.x, kept.g, kept.u)]
+    grads = ffn.backward(dout, kept)
+    assert (grads["dx"][:-last] == 0).all()
+    grads["dx"] = grads["dx"][-last:]
+    want, tol = backward64(dout[-last:], ends[0], ends[1].double(), ends[2].double(), W, "silu",
+                           UNIT[dt])
+    for name in want:
+        check(grads[name], want[name], tol[name] + 1e-30, name)
