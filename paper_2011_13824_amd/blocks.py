@@ -39,7 +39,7 @@ def _type(t, what):
 def _no_tape(*tensors):
     """Warns where a gradient would be lost."""
     for t in tensors:
-        if t is not None and t.requires_grad and torch.is_grad_enabled():
+        if getattr(t, "requires_grad", False) and torch.is_grad_enabled():
             warnings.warn("autograd does not record the calls of paper_2011_13824_amd.blocks: their "
                           "gradients come from the backward methods (call them under "
                           "torch.no_grad(), or with detached tensors)", stacklevel=3)

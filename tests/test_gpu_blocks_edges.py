@@ -289,6 +289,17 @@ def test_a_lost_gradient_is_warned_of(B):
         t.requires_grad_(False)
 
 
+def test_what_is_no_tensor_is_a_type_error(B):
+    x = rand(1, 5, 24)
+    ffn = B.FeedForward(rand(2, 40, 24), rand(3, 40, 24), rand(4, 24, 40))
+    for call in (lambda: B.Norm([1.0] * 24).forward(x),
+                 lambda: B.Norm(rand(5, 24)).forward(x, x.tolist()),
+                 lambda: B.Norm(rand(5, 24)).forward(x.cpu().numpy()),
+                 lambda: ffn.forward(x.cpu().numpy())):
+        with pytest.raises(TypeError):
+            call()
+
+
 # ---------------------------------------------------------------------------------------------
 # Rows
 # ---------------------------------------------------------------------------------------------
