@@ -369,6 +369,52 @@ int lirpa_ffn_backward(const lirpa_ffn* ffn, int64_t rows, const void* dout, int
                        void* dx, int64_t lddx, void* dWg, void* dWu, void* dWd, void* ws,
                        size_t ws_bytes, hipStream_t stream);
 
+/* =============================================================================================
+ * The ends of a language model: tokens into rows, rows of logits into log probabilities
+ *
+ * Conventions as for the feed-forward block.  Tokens are int64; one outside [0, vocab) (-1, say) is
+ * padding wherever tokens are read.
+ * ============================================================================================= */
+
+/* out = scale * table[token], a row of 0 for padding.  table is [vocab][n], vocab up to 2^20. */
+int lirpa_embed_forward(int dtype, int64_t rows, int n, int vocab, const int64_t* tokens,
+                        const void* table, int64_t ldt, float scale, void* out, int64_t ldo,
+                        hipStream_t stream);
+
+/* The table's gradient: dtable_v = base_v + scale * (sum of dout over the positions of token v, in
+ * their order, in 32 bits).  base [vocab][n] may be NULL (zeros) or dtable itself: then only rows
+ * that a token names are read and written.  EUNSUPPORTED where a launch would pass 2^32 threads. */
+size_t lirpa_embed_workspace_bytes(int64_t rows, int n); /* 0 for invalid arguments */
+int lirpa_embed_backward(int dtype, int64_t rows, int n, int vocab, const int64_t* tokens,
+                         const void* dout, int64_t lddo, float scale, const void* base, int64_t ldb,
+                         void* dtable, int64_t ldd, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* Of each row of logits l [n] (n is the vocabulary), scaled by scale > 0 (one over a temperature):
+ *     lse = log(sum e^(scale l)),   logp = scale l_token - lse (0 for padding),
+ *     entropy = -sum p log p with p = e^(scale l - lse),
+ *     top_logp, top_tokens [rows][top]: the `top` (0 to 32) most likely tokens, the largest first,
+ *     the lowest token first among equal logits.
+ * Outputs are float, each NULL where it is not wanted (tokens may be NULL where logp is).  A logit
+ * of -inf is a token that cannot come: it is no alternative, and places that are left over hold
+ * token -1 and log probability -inf.  A row of -inf alone has lse and logp -inf and entropy 0.  A row
+ * with a NaN or +inf has NaN everywhere and alternatives -1.  logp, entropy and top_logp are taken
+ * from the differences to the row's largest logit, not from lse. */
+size_t lirpa_logprob_workspace_bytes(int64_t rows, int n, int top); /* 0 for invalid arguments */
+int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
+                          float scale, const int64_t* tokens, float* logp, float* lse,
+                          float* entropy, int top, float* top_logp, int64_t* top_tokens, void* ws,
+                          size_t ws_bytes, hipStream_t stream);
+
+/* The gradient of the logits from those of logp and entropy (float [rows], either may be NULL) and
+ * the lse and entropy (NULL where dentropy is) that the forward call returned:
+ *     dl_j = scale (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)).
+ * dlogp is not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer
+ * of logits. */
+int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
+                           float scale, const int64_t* tokens, const float* lse,
+                           const float* entropy, const float* dlogp, const float* dentropy,
+                           void* dlogits, int64_t ldd, hipStream_t stream);
+
 /* Kernel timing, for profiling harnesses.  Between lirpa_timing_begin() and
  * lirpa_timing_end() every kernel the calls of this thread enqueue is bracketed by a pair of
  * hipEvents recorded on the call's own stream.  lirpa_timing_end() waits for those events and

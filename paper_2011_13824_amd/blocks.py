@@ -214,3 +214,84 @@ class FeedForward:
         lirpa.lirpa_ffn_backward(block, dout, kept.keep, x, g, u, *(
             grads.get(k) for k in ("dx", "dWg", "dWu", "dWd")), ws, need)
         return grads
+
+
+class Embedding:
+    """out = scale * table[token]; a token outside the table (-1, say) is padding, a row of 0."""
+
+    def __init__(self, table, scale=1.0):
+        self.table, self.scale = table, float(scale)
+
+    def forward(self, tokens):
+        """[rows, n] of the int64 tokens [rows]."""
+        table = self.table
+        _no_tape(table)
+        vocab, n = lirpa._2d(table, "table")
+        dt, code = _type(table, "table")
+        lirpa._here(table, "table")
+        p, ld = _matrix(table, vocab, n, dt, "table")
+        rows = len(tokens)
+        ptok = lirpa._tokens(tokens, rows)
+        out = torch.empty((rows, n), dtype=dt, device=table.device)
+        _check(load().lirpa_embed_forward(code, rows, n, vocab, ptok, p, ld, self.scale,
+                                          out.data_ptr(), n, _stream(None)))
+        return out
+
+    def backward(self, tokens, dout, base=None, out=None):
+        """The table's gradient, with ``base`` added where it is given.  It is written to ``out``:
+        a new tensor, or one of the caller's, which may be base itself (then the rows that no
+        token names are not touched)."""
+        vocab, n = lirpa._2d(self.table, "table")
+        if out is None:
+            out = torch.empty((vocab, n), dtype=self.table.dtype, device=self.table.device)
+        elif lirpa._2d(out, "out") != (vocab, n):
+            raise ValueError(f"out must be [{vocab}, {n}], got {list(out.shape)}")
+        need = lirpa.lirpa_embed_workspace_bytes(len(tokens), n)
+        lirpa.lirpa_embed_backward(tokens, dout, self.scale, base, out, _bytes(need, out.device),
+                                   need)
+        return out
+
+
+LogP = collections.namedtuple("LogP", "logp lse entropy top_logp top_tokens")
+
+
+class LogProbs:
+    """Of rows of logits, times ``scale`` (one over a temperature): the log probabilities of given
+    tokens, the entropies and the ``top`` most likely tokens."""
+
+    def __init__(self, scale=1.0, top=0):
+        self.scale, self.top = float(scale), int(top)
+
+    def forward(self, logits, tokens=None):
+        """LogP; logp is None without tokens, top_logp and top_tokens [rows, top] without top.  A
+        token outside the vocabulary is padding: its logp is 0."""
+        rows, n = lirpa._2d(logits, "logits")
+        dt, code = _type(logits, "logits")
+        _no_tape(logits)
+        lirpa._here(logits, "logits")
+        p, ld = _matrix(logits, rows, n, dt, "logits")
+        ptok = lirpa._tokens(tokens, rows)
+        top = self.top
+        own = torch.empty((2 if tokens is None else 3, rows), dtype=torch.float32,
+                          device=logits.device)
+        lse, entropy = own[0], own[1]
+        logp = None if tokens is None else own[2]
+        top_logp = top_tokens = None
+        if top:
+            top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device)
+            top_tokens = torch.empty((rows, top), dtype=torch.int64, device=logits.device)
+        need = load().lirpa_logprob_workspace_bytes(rows, n, top)
+        ws = _bytes(need, logits.device)
+        _check(load().lirpa_logprob_forward(
+            code, rows, n, p, ld, self.scale, ptok, None if logp is None else logp.data_ptr(),
+            lse.data_ptr(), entropy.data_ptr(), top, top_logp.data_ptr() if top else None,
+            top_tokens.data_ptr() if top else None, ws.data_ptr(), need, _stream(None)))
+        return LogP(logp, lse, entropy, top_logp, top_tokens)
+
+    def backward(self, logits, tokens, lse, entropy=None, dlogp=None, dentropy=None, out=None):
+        """The gradient of the logits from those of logp and entropy, and what forward returned of
+        the same logits and tokens.  ``out`` may be the logits, whose place it then takes."""
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        lirpa.lirpa_logprob_backward(logits, self.scale, tokens, lse, entropy, dlogp, dentropy, out)
+        return out

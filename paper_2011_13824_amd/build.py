@@ -22,6 +22,7 @@ UNITS = {
     # MFMA results in ordinary VGPRs (no accumulator-register copies before the VALU reads them)
     "lirpa.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
     "blocks.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
+    "ends.hip": [],
 }
 
 

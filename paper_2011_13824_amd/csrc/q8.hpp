@@ -13,19 +13,6 @@
 
 namespace lm {
 
-// The 8 columns that thread `id` of a matrix with `per_row` pieces a row takes.  The block's first
-// piece is divided in 64 bits once (uniform), the thread's offset from it in 32.
-struct Piece {
-  int64_t row;
-  int col;
-};
-__device__ __forceinline__ Piece piece_of(int64_t first, int per_row) {
-  int64_t row0 = first / per_row;
-  uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x;
-  uint32_t down = at / (uint32_t)per_row;
-  return {row0 + down, (int)(at - down * (uint32_t)per_row) * 8};
-}
-
 template <typename T>
 __global__ __launch_bounds__(256) void k_q8_pack(const T* __restrict__ x, int64_t ldx,
                                                  int64_t rows, int n, int8_t* __restrict__ q,

@@ -74,6 +74,8 @@ SYMBOLS = ("lirpa_net_create", "lirpa_net_destroy", "lirpa_net_num_relu",
            "lirpa_q8_bytes", "lirpa_q8_pack", "lirpa_q8_unpack",
            "lirpa_norm_forward", "lirpa_norm_workspace_bytes", "lirpa_norm_backward",
            "lirpa_ffn_workspace_bytes", "lirpa_ffn_forward", "lirpa_ffn_backward",
+           "lirpa_embed_forward", "lirpa_embed_workspace_bytes", "lirpa_embed_backward",
+           "lirpa_logprob_workspace_bytes", "lirpa_logprob_forward", "lirpa_logprob_backward",
            "lirpa_timing_begin", "lirpa_timing_end", "lirpa_last_error")
 
 _lib = None
@@ -137,6 +139,18 @@ def load() -> ctypes.CDLL:
     L.lirpa_ffn_forward.restype = i
     L.lirpa_ffn_backward.argtypes = [block, q, P, q, i, P, q, P, P, P, q, P, P, P, P, sz, P]
     L.lirpa_ffn_backward.restype = i
+    L.lirpa_embed_forward.argtypes = [i, q, i, i, P, P, q, f, P, q, P]
+    L.lirpa_embed_forward.restype = i
+    L.lirpa_embed_workspace_bytes.argtypes = [q, i]
+    L.lirpa_embed_workspace_bytes.restype = sz
+    L.lirpa_embed_backward.argtypes = [i, q, i, i, P, P, q, f, P, q, P, q, P, sz, P]
+    L.lirpa_embed_backward.restype = i
+    L.lirpa_logprob_workspace_bytes.argtypes = [q, i, i]
+    L.lirpa_logprob_workspace_bytes.restype = sz
+    L.lirpa_logprob_forward.argtypes = [i, q, i, P, q, f, P, P, P, P, i, P, P, P, sz, P]
+    L.lirpa_logprob_forward.restype = i
+    L.lirpa_logprob_backward.argtypes = [i, q, i, P, q, f, P, P, P, P, P, P, q, P]
+    L.lirpa_logprob_backward.restype = i
     L.lirpa_timing_begin.argtypes = []
     L.lirpa_timing_begin.restype = i
     L.lirpa_timing_end.argtypes = [ctypes.POINTER(lirpa_kernel_time), i, ctypes.POINTER(i)]
@@ -458,6 +472,84 @@ def lirpa_ffn_backward(ffn, dout, keep, x, g, u, dx, dWg, dWu, dWd, ws, ws_bytes
         *_matrix(dx, rows, D, dt, "dx"), _vector(dWg, F * D, dt, "dWg"),
         _vector(dWu, F * D, dt, "dWu"), _vector(dWd, D * F, dt, "dWd"), _dev(ws, None, "ws"),
         int(ws_bytes), _stream(stream)))
+
+
+def _here(t, what):
+    """Refuses a tensor of another device than the current one, whose stream the calls run on."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} lies on {t.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+def _2d(t, what):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a CUDA tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{what} must have two dimensions, got {t.dim()}")
+    return t.shape
+
+
+def _tokens(t, rows):
+    if t is not None and isinstance(t, torch.Tensor) and t.dim() != 1:
+        raise ValueError(f"tokens must have one dimension, got {t.dim()}")
+    return _vector(t, rows, torch.int64, "tokens")
+
+
+def lirpa_embed_forward(tokens, table, scale, out, stream=None):
+    vocab, n = _2d(table, "table")
+    rows = _2d(out, "out")[0]
+    dt = _dtype(table, "table")
+    _here(table, "table")
+    _check(load().lirpa_embed_forward(
+        DTYPES[dt], rows, n, vocab, _tokens(tokens, rows), *_matrix(table, vocab, n, dt, "table"),
+        float(scale), *_matrix(out, rows, n, dt, "out"), _stream(stream)))
+
+
+def lirpa_embed_workspace_bytes(rows, n) -> int:
+    return int(load().lirpa_embed_workspace_bytes(int(rows), int(n)))
+
+
+def lirpa_embed_backward(tokens, dout, scale, base, dtable, ws, ws_bytes, stream=None):
+    rows, n = _2d(dout, "dout")
+    vocab = _2d(dtable, "dtable")[0]
+    dt = _dtype(dout, "dout")
+    _here(dout, "dout")
+    _check(load().lirpa_embed_backward(
+        DTYPES[dt], rows, n, vocab, _tokens(tokens, rows), *_matrix(dout, rows, n, dt, "dout"),
+        float(scale), *_matrix(base, vocab, n, dt, "base"),
+        *_matrix(dtable, vocab, n, dt, "dtable"), _dev(ws, None, "ws"), int(ws_bytes),
+        _stream(stream)))
+
+
+def lirpa_logprob_workspace_bytes(rows, n, top) -> int:
+    return int(load().lirpa_logprob_workspace_bytes(int(rows), int(n), int(top)))
+
+
+def lirpa_logprob_forward(logits, scale, tokens, logp, lse, entropy, top, top_logp, top_tokens, ws,
+                          ws_bytes, stream=None):
+    rows, n = _2d(logits, "logits")
+    dt, f32 = _dtype(logits, "logits"), torch.float32
+    _here(logits, "logits")
+    _check(load().lirpa_logprob_forward(
+        DTYPES[dt], rows, n, *_matrix(logits, rows, n, dt, "logits"), float(scale),
+        _tokens(tokens, rows), _vector(logp, rows, f32, "logp"), _vector(lse, rows, f32, "lse"),
+        _vector(entropy, rows, f32, "entropy"), int(top),
+        _vector(top_logp, rows * top, f32, "top_logp"),
+        _vector(top_tokens, rows * top, torch.int64, "top_tokens"), _dev(ws, None, "ws"),
+        int(ws_bytes), _stream(stream)))
+
+
+def lirpa_logprob_backward(logits, scale, tokens, lse, entropy, dlogp, dentropy, dlogits,
+                           stream=None):
+    rows, n = _2d(logits, "logits")
+    dt, f32 = _dtype(logits, "logits"), torch.float32
+    _here(logits, "logits")
+    _check(load().lirpa_logprob_backward(
+        DTYPES[dt], rows, n, *_matrix(logits, rows, n, dt, "logits"), float(scale),
+        _tokens(tokens, rows), _vector(lse, rows, f32, "lse"),
+        _vector(entropy, rows, f32, "entropy"), _vector(dlogp, rows, f32, "dlogp"),
+        _vector(dentropy, rows, f32, "dentropy"), *_matrix(dlogits, rows, n, dt, "dlogits"),
+        _stream(stream)))
 
 
 class Network:
