@@ -415,6 +415,75 @@ int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, i
                            const float* entropy, const float* dlogp, const float* dentropy,
                            void* dlogits, int64_t ldd, hipStream_t stream);
 
+/* =============================================================================================
+ * What mixes the rows of a sequence: a short causal convolution and a selective state space scan
+ *
+ * Conventions as for the feed-forward block, and:
+ * - Sequences lie behind each other in the rows.  seq (int32 [rows], on the device) names the
+ *   sequence of every row, and the slot of its state; rows of one sequence are neighbours, so a
+ *   sequence begins and ends where the number changes.  seq = NULL: all rows are sequence 0.  A number
+ *   outside [0, slots) is padding: outputs and gradients of its rows are 0, its inputs are of no
+ *   account.  slots >= 1; without states any bound will do.
+ * - state holds what stands in front of a sequence's first row, by slot, and state_out receives what
+ *   the next row will need; either may be NULL (zeros; not wanted), and state_out may be state.
+ *   Slots that no row names are not touched.  A slot is named by one sequence of a call; if it is
+ *   named by more, its state is one of theirs, or parts of several.
+ * - *_step takes one row of every sequence: row t is that of slot seq[t] (slot t without seq).
+ * - The backward passes are those of sequences that begin with states of 0.
+ * ============================================================================================= */
+typedef enum { LIRPA_CONV_LINEAR = 0, LIRPA_CONV_SILU = 1 } lirpa_conv_act;
+
+/* y_t = act(bias + sum_{k < taps} w_k x_{t - taps + 1 + k}) for every column; w [taps][n], bias [n]
+ * or NULL, taps 1 to 8.  state [slots][taps - 1][n] of dtype: the last inputs, oldest first.
+ * EUNSUPPORTED where a launch would pass 2^32 threads. */
+int lirpa_conv_forward(int dtype, int64_t rows, int n, int taps, const void* x, int64_t ldx,
+                       const void* w, const void* bias, int act, const int32_t* seq, int slots,
+                       const void* state, void* state_out, void* y, int64_t ldy,
+                       hipStream_t stream);
+int lirpa_conv_step(int dtype, int64_t rows, int n, int taps, const void* x, int64_t ldx,
+                    const void* w, const void* bias, int act, const int32_t* seq, int slots,
+                    const void* state, void* state_out, void* y, int64_t ldy, hipStream_t stream);
+
+/* Gradients of x, w [taps][n] and bias (dbias may be NULL). */
+size_t lirpa_conv_workspace_bytes(int64_t rows, int n, int taps); /* 0 for invalid arguments */
+int lirpa_conv_backward(int dtype, int64_t rows, int n, int taps, const void* dy, int64_t lddy,
+                        const void* x, int64_t ldx, const void* w, const void* bias, int act,
+                        const int32_t* seq, int slots, void* dx, int64_t lddx, void* dw,
+                        void* dbias, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* A scan's inputs (device pointers, read during a call's enqueued work only).  u, dt, z [rows][n]
+ * and B, C [rows][states] of dtype; A [n][states], D [n], bias [n] of float.  z (no gate), D and bias
+ * may be NULL.  states 1 to 64. */
+typedef struct {
+  int dtype;
+  int64_t rows;
+  int n, states;
+  const void *u, *dt, *z, *B, *C;
+  int64_t ldu, lddt, ldz, ldB, ldC;
+  const float *A, *D, *bias;
+  const int32_t* seq;
+  int slots;
+} lirpa_scan;
+
+/* For every column, with states h [states] of its own:
+ *     delta = log(1 + e^(dt + bias)),  h_t = e^(delta A) * h_{t-1} + delta u B_t,
+ *     y = (C_t . h_t + D u) z / (1 + e^-z).
+ * state [slots][n][states] of float.  kept (lirpa_scan_kept_bytes, on 16 bytes) receives what the
+ * backward pass needs, NULL where it is not wanted; with it state is NULL. */
+size_t lirpa_scan_workspace_bytes(int64_t rows, int n, int states, int backward); /* 0: invalid */
+size_t lirpa_scan_kept_bytes(int64_t rows, int n, int states);                    /* 0: invalid */
+int lirpa_scan_forward(const lirpa_scan* scan, const float* state, float* state_out, void* y,
+                       int64_t ldy, void* kept, void* ws, size_t ws_bytes, hipStream_t stream);
+int lirpa_scan_step(const lirpa_scan* scan, const float* state, float* state_out, void* y,
+                    int64_t ldy, hipStream_t stream);
+
+/* Gradients from what was kept, for the same inputs: du, ddt, dz (NULL without z) [rows][n], dB, dC
+ * [rows][states] of dtype; dA [n][states], dD, dbias [n] of float, each NULL where it is not wanted. */
+int lirpa_scan_backward(const lirpa_scan* scan, const void* dy, int64_t lddy, const void* kept,
+                        void* du, int64_t lddu, void* ddt, int64_t ldddt, void* dz, int64_t lddz,
+                        void* dB, int64_t lddB, void* dC, int64_t lddC, float* dA, float* dD,
+                        float* dbias, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* Kernel timing, for profiling harnesses.  Between lirpa_timing_begin() and
  * lirpa_timing_end() every kernel the calls of this thread enqueue is bracketed by a pair of
  * hipEvents recorded on the call's own stream.  lirpa_timing_end() waits for those events and

@@ -216,6 +216,120 @@ class FeedForward:
         return grads
 
 
+def sequences(lengths, rows=None, slots=None, device="cuda"):
+    """seq, the int32 [rows] that the calls over sequences take: sequences of the given lengths
+    behind each other, those of 0 left out; ``slots`` are the slots of their states (0, 1, ... by
+    default).  Rows behind the last one are padding."""
+    lengths = [int(n) for n in lengths]
+    if any(n < 0 for n in lengths):
+        raise ValueError("a sequence has a negative length")
+    slots = list(range(len(lengths))) if slots is None else [int(s) for s in slots]
+    if len(slots) != len(lengths) or len(set(slots)) != len(slots) or min(slots, default=0) < 0:
+        raise ValueError("every sequence needs a slot of its own")
+    rows = sum(lengths) if rows is None else int(rows)
+    if rows < sum(lengths):
+        raise ValueError(f"{sum(lengths)} rows do not fit {rows}")
+    slots, lengths = slots + [-1], lengths + [rows - sum(lengths)]
+    return torch.repeat_interleave(torch.tensor(slots, dtype=torch.int32),
+                                   torch.tensor(lengths)).to(device)
+
+
+class CausalConv:
+    """y_t = act(bias + sum_k w_k x_{t - taps + 1 + k}) of every column; w [taps, n], bias [n] or
+    None, act "silu" or "linear".
+
+    ``seq`` (see ``sequences``; None: one sequence) says which rows belong together, ``state``
+    [slots, taps - 1, n] holds a sequence's last inputs, oldest first, and ``state_out`` (it may be
+    state) receives them."""
+
+    def __init__(self, w, bias=None, act="silu"):
+        if act not in lirpa.CONV_ACTS:
+            raise ValueError(f"act must be one of {sorted(lirpa.CONV_ACTS)}, got {act!r}")
+        self.w, self.bias, self.act = w, bias, act
+
+    def forward(self, x, seq=None, state=None, state_out=None):
+        _no_tape(x, self.w, self.bias, state)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        lirpa.lirpa_conv_forward(x, self.w, self.bias, self.act, seq, state, state_out, y)
+        return y
+
+    def step(self, x, state, seq=None, state_out=None):
+        """One row of every sequence: row t is that of slot seq[t], of slot t without seq."""
+        _no_tape(x, self.w, self.bias, state)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        lirpa.lirpa_conv_step(x, self.w, self.bias, self.act, seq, state, state_out, y)
+        return y
+
+    def backward(self, dy, x, seq=None):
+        """{"dx", "dw", "dbias"} (dbias where there is a bias), for sequences without a state."""
+        lirpa._2d(x, "x")
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        grads = {"dx": dx, "dw": torch.empty(self.w.shape, dtype=x.dtype, device=x.device)}
+        if self.bias is not None:
+            grads["dbias"] = torch.empty(self.bias.shape, dtype=x.dtype, device=x.device)
+        need = lirpa.lirpa_conv_workspace_bytes(*x.shape, self.w.shape[0])
+        lirpa.lirpa_conv_backward(dy, x, self.w, self.bias, self.act, seq, dx, grads["dw"],
+                                  grads.get("dbias"), _bytes(need, x.device), need)
+        return grads
+
+
+class KeptScan:
+    """What SelectiveScan.forward kept for its backward pass: the inputs, and states of the walk."""
+
+    def __init__(self, u, dt, B, C, z, seq, states):
+        self.inputs, self.seq, self.states = (u, dt, B, C, z), seq, states
+
+
+class SelectiveScan:
+    """h_t = exp(delta A) h_{t-1} + delta u B_t, y = (C_t . h_t + D u) silu(z) of every column, with
+    delta = log(1 + exp(dt + bias)); A [n, states], D and bias [n] or None, all float32.
+
+    u, dt, z [rows, n] (z may be None: no gate), B, C [rows, states].  ``seq`` as for CausalConv;
+    ``state`` [slots, n, states], float32."""
+
+    def __init__(self, A, D=None, bias=None):
+        self.A, self.D, self.bias = A, D, bias
+
+    def _inputs(self, u, dt, B, C, z, seq):
+        return lirpa.lirpa_scan_inputs(u, dt, B, C, z, self.A, self.D, self.bias, seq)
+
+    def forward(self, u, dt, B, C, z=None, seq=None, state=None, state_out=None, keep=False):
+        """y; with ``keep`` (y, KeptScan), for sequences that begin with states of 0."""
+        _no_tape(u, dt, B, C, z, state, self.A, self.D, self.bias)
+        scan = self._inputs(u, dt, B, C, z, seq)
+        if keep and state is not None:
+            raise ValueError("the backward pass starts from states of 0: keep and state exclude "
+                             "each other")
+        size = (scan.rows, scan.n, scan.states)
+        y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+        kept = _bytes(lirpa.lirpa_scan_kept_bytes(*size), u.device) if keep else None
+        need = lirpa.lirpa_scan_workspace_bytes(*size, 0)
+        lirpa.lirpa_scan_forward(scan, state, state_out, y, kept, _bytes(need, u.device), need)
+        return (y, KeptScan(u, dt, B, C, z, seq, kept)) if keep else y
+
+    def step(self, u, dt, B, C, z=None, state=None, seq=None, state_out=None):
+        """One row of every sequence: row t is that of slot seq[t], of slot t without seq."""
+        _no_tape(u, dt, B, C, z, state, self.A, self.D, self.bias)
+        scan = self._inputs(u, dt, B, C, z, seq)
+        y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+        lirpa.lirpa_scan_step(scan, state, state_out, y)
+        return y
+
+    def backward(self, dy, kept):
+        """The gradients of what the forward pass took: du, ddt, dB, dC, dA, and dz, dD, dbias where
+        there are z, D and bias."""
+        u, dt, B, C, z = kept.inputs
+        scan = self._inputs(u, dt, B, C, z, kept.seq)
+        like = {"du": u, "ddt": dt, "dz": z, "dB": B, "dC": C, "dA": self.A, "dD": self.D,
+                "dbias": self.bias}
+        grads = {k: torch.empty(t.shape, dtype=t.dtype, device=t.device)
+                 for k, t in like.items() if t is not None}
+        need = lirpa.lirpa_scan_workspace_bytes(scan.rows, scan.n, scan.states, 1)
+        lirpa.lirpa_scan_backward(scan, dy, kept.states, *(grads.get(k) for k in like),
+                                  _bytes(need, u.device), need)
+        return grads
+
+
 class Embedding:
     """out = scale * table[token]; a token outside the table (-1, say) is padding, a row of 0."""
 

@@ -23,6 +23,7 @@ UNITS = {
     "lirpa.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
     "blocks.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=true"],
     "ends.hip": [],
+    "mixer.hip": [],
 }
 
 

@@ -58,6 +58,19 @@ class lirpa_ffn(ctypes.Structure):
                 ("ldd", ctypes.c_int64)]
 
 
+class lirpa_scan(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("rows", ctypes.c_int64), ("n", ctypes.c_int),
+                ("states", ctypes.c_int), ("u", ctypes.c_void_p), ("dt", ctypes.c_void_p),
+                ("z", ctypes.c_void_p), ("B", ctypes.c_void_p), ("C", ctypes.c_void_p),
+                ("ldu", ctypes.c_int64), ("lddt", ctypes.c_int64), ("ldz", ctypes.c_int64),
+                ("ldB", ctypes.c_int64), ("ldC", ctypes.c_int64), ("A", ctypes.c_void_p),
+                ("D", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("seq", ctypes.c_void_p),
+                ("slots", ctypes.c_int)]
+
+
+CONV_ACTS = {"linear": 0, "silu": 1}
+ANY_SLOT = 2 ** 31 - 1  # where no states come with the sequences
+
 BAB_VERIFIED, BAB_VIOLATED, BAB_UNKNOWN_STUCK, BAB_UNKNOWN_LIMIT = 1, 2, 3, 4
 
 
@@ -76,6 +89,9 @@ SYMBOLS = ("lirpa_net_create", "lirpa_net_destroy", "lirpa_net_num_relu",
            "lirpa_ffn_workspace_bytes", "lirpa_ffn_forward", "lirpa_ffn_backward",
            "lirpa_embed_forward", "lirpa_embed_workspace_bytes", "lirpa_embed_backward",
            "lirpa_logprob_workspace_bytes", "lirpa_logprob_forward", "lirpa_logprob_backward",
+           "lirpa_conv_forward", "lirpa_conv_step", "lirpa_conv_workspace_bytes",
+           "lirpa_conv_backward", "lirpa_scan_workspace_bytes", "lirpa_scan_kept_bytes",
+           "lirpa_scan_forward", "lirpa_scan_step", "lirpa_scan_backward",
            "lirpa_timing_begin", "lirpa_timing_end", "lirpa_last_error")
 
 _lib = None
@@ -151,6 +167,24 @@ def load() -> ctypes.CDLL:
     L.lirpa_logprob_forward.restype = i
     L.lirpa_logprob_backward.argtypes = [i, q, i, P, q, f, P, P, P, P, P, P, q, P]
     L.lirpa_logprob_backward.restype = i
+    conv = [i, q, i, i, P, q, P, P, i, P, i, P, P, P, q, P]
+    L.lirpa_conv_forward.argtypes = L.lirpa_conv_step.argtypes = conv
+    L.lirpa_conv_forward.restype = L.lirpa_conv_step.restype = i
+    L.lirpa_conv_workspace_bytes.argtypes = [q, i, i]
+    L.lirpa_conv_workspace_bytes.restype = sz
+    L.lirpa_conv_backward.argtypes = [i, q, i, i, P, q, P, q, P, P, i, P, i, P, q, P, P, P, sz, P]
+    L.lirpa_conv_backward.restype = i
+    scan = ctypes.POINTER(lirpa_scan)
+    L.lirpa_scan_workspace_bytes.argtypes = [q, i, i, i]
+    L.lirpa_scan_workspace_bytes.restype = sz
+    L.lirpa_scan_kept_bytes.argtypes = [q, i, i]
+    L.lirpa_scan_kept_bytes.restype = sz
+    L.lirpa_scan_forward.argtypes = [scan, P, P, P, q, P, P, sz, P]
+    L.lirpa_scan_forward.restype = i
+    L.lirpa_scan_step.argtypes = [scan, P, P, P, q, P]
+    L.lirpa_scan_step.restype = i
+    L.lirpa_scan_backward.argtypes = [scan, P, q, P, *[P, q] * 5, P, P, P, P, sz, P]
+    L.lirpa_scan_backward.restype = i
     L.lirpa_timing_begin.argtypes = []
     L.lirpa_timing_begin.restype = i
     L.lirpa_timing_end.argtypes = [ctypes.POINTER(lirpa_kernel_time), i, ctypes.POINTER(i)]
@@ -550,6 +584,131 @@ def lirpa_logprob_backward(logits, scale, tokens, lse, entropy, dlogp, dentropy,
         _vector(entropy, rows, f32, "entropy"), _vector(dlogp, rows, f32, "dlogp"),
         _vector(dentropy, rows, f32, "dentropy"), *_matrix(dlogits, rows, n, dt, "dlogits"),
         _stream(stream)))
+
+
+def _seq(seq, rows):
+    return _vector(seq, rows, torch.int32, "seq")
+
+
+def _slots(state, state_out, tail, dtype):
+    """(slots, pointers of state and state_out) of [slots, *tail] tensors."""
+    slots, out = None, []
+    for t, what in ((state, "state"), (state_out, "state_out")):
+        if t is not None:
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{what} must be a CUDA tensor")
+            if tuple(t.shape[1:]) != tail or t.dim() != len(tail) + 1 or t.shape[0] < 1:
+                raise ValueError(f"{what} must be [slots, {', '.join(map(str, tail))}], got "
+                                 f"{list(t.shape)}")
+            if slots is not None and t.shape[0] != slots:
+                raise ValueError(f"state has {slots} slots, state_out {t.shape[0]}")
+            slots = t.shape[0]
+        out.append(_dev(t, dtype, what))
+    return (ANY_SLOT if slots is None else slots), *out
+
+
+def _conv(call, x, w, bias, act, seq, state, state_out, y, stream):
+    rows, n = _2d(x, "x")
+    taps = _2d(w, "w")[0]
+    dt = _dtype(x, "x")
+    _here(x, "x")
+    if act not in CONV_ACTS:
+        raise ValueError(f"act must be one of {sorted(CONV_ACTS)}, got {act!r}")
+    slots, s_in, s_out = _slots(state, state_out, (taps - 1, n), dt)
+    _check(call(DTYPES[dt], rows, n, taps, *_matrix(x, rows, n, dt, "x"),
+                _vector(w, taps * n, dt, "w"), _vector(bias, n, dt, "bias"), CONV_ACTS[act],
+                _seq(seq, rows), slots, s_in, s_out, *_matrix(y, rows, n, dt, "y"),
+                _stream(stream)))
+
+
+def lirpa_conv_forward(x, w, bias, act, seq, state, state_out, y, stream=None):
+    _conv(load().lirpa_conv_forward, x, w, bias, act, seq, state, state_out, y, stream)
+
+
+def lirpa_conv_step(x, w, bias, act, seq, state, state_out, y, stream=None):
+    _conv(load().lirpa_conv_step, x, w, bias, act, seq, state, state_out, y, stream)
+
+
+def lirpa_conv_workspace_bytes(rows, n, taps) -> int:
+    return int(load().lirpa_conv_workspace_bytes(int(rows), int(n), int(taps)))
+
+
+def lirpa_conv_backward(dy, x, w, bias, act, seq, dx, dw, dbias, ws, ws_bytes, stream=None):
+    rows, n = _2d(x, "x")
+    taps = _2d(w, "w")[0]
+    dt = _dtype(x, "x")
+    _here(x, "x")
+    if act not in CONV_ACTS:
+        raise ValueError(f"act must be one of {sorted(CONV_ACTS)}, got {act!r}")
+    _check(load().lirpa_conv_backward(
+        DTYPES[dt], rows, n, taps, *_matrix(dy, rows, n, dt, "dy"), *_matrix(x, rows, n, dt, "x"),
+        _vector(w, taps * n, dt, "w"), _vector(bias, n, dt, "bias"), CONV_ACTS[act],
+        _seq(seq, rows), ANY_SLOT, *_matrix(dx, rows, n, dt, "dx"), _vector(dw, taps * n, dt, "dw"),
+        _vector(dbias, n, dt, "dbias"), _dev(ws, None, "ws"), int(ws_bytes), _stream(stream)))
+
+
+def lirpa_scan_inputs(u, dt, B, C, z, A, D, bias, seq, slots=ANY_SLOT):
+    """The lirpa_scan of device tensors, which have to outlive the calls that take it."""
+    rows, n = _2d(u, "u")
+    states = _2d(A, "A")[1]
+    kind, f32 = _dtype(u, "u"), torch.float32
+    _here(u, "u")
+    pu, ldu = _matrix(u, rows, n, kind, "u")
+    pdt, lddt = _matrix(dt, rows, n, kind, "dt")
+    pz, ldz = _matrix(z, rows, n, kind, "z")
+    pB, ldB = _matrix(B, rows, states, kind, "B")
+    pC, ldC = _matrix(C, rows, states, kind, "C")
+    return lirpa_scan(DTYPES[kind], rows, n, states, pu, pdt, pz, pB, pC, ldu, lddt, ldz, ldB, ldC,
+                      _vector(A, n * states, f32, "A"), _vector(D, n, f32, "D"),
+                      _vector(bias, n, f32, "bias"), _seq(seq, rows), slots)
+
+
+def lirpa_scan_workspace_bytes(rows, n, states, backward) -> int:
+    return int(load().lirpa_scan_workspace_bytes(int(rows), int(n), int(states), int(backward)))
+
+
+def lirpa_scan_kept_bytes(rows, n, states) -> int:
+    return int(load().lirpa_scan_kept_bytes(int(rows), int(n), int(states)))
+
+
+def _of_scan(scan):
+    return scan.rows, scan.n, scan.states, {v: k for k, v in DTYPES.items()}[scan.dtype]
+
+
+def _kept_states(kept, scan):
+    need = lirpa_scan_kept_bytes(scan.rows, scan.n, scan.states)
+    if isinstance(kept, torch.Tensor) and kept.numel() * kept.element_size() < need:
+        raise ValueError(f"kept must have {need} bytes")
+    return _dev(kept, None, "kept")
+
+
+def lirpa_scan_forward(scan, state, state_out, y, kept, ws, ws_bytes, stream=None):
+    """``scan`` is what lirpa_scan_inputs returned; its slots become those of the states."""
+    rows, n, states, dt = _of_scan(scan)
+    scan.slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32)
+    _check(load().lirpa_scan_forward(
+        ctypes.byref(scan), s_in, s_out, *_matrix(y, rows, n, dt, "y"), _kept_states(kept, scan),
+        _dev(ws, None, "ws"), int(ws_bytes), _stream(stream)))
+
+
+def lirpa_scan_step(scan, state, state_out, y, stream=None):
+    rows, n, states, dt = _of_scan(scan)
+    scan.slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32)
+    _check(load().lirpa_scan_step(ctypes.byref(scan), s_in, s_out, *_matrix(y, rows, n, dt, "y"),
+                                  _stream(stream)))
+
+
+def lirpa_scan_backward(scan, dy, kept, du, ddt, dz, dB, dC, dA, dD, dbias, ws, ws_bytes,
+                        stream=None):
+    rows, n, states, dt = _of_scan(scan)
+    f32 = torch.float32
+    _check(load().lirpa_scan_backward(
+        ctypes.byref(scan), *_matrix(dy, rows, n, dt, "dy"), _kept_states(kept, scan),
+        *_matrix(du, rows, n, dt, "du"), *_matrix(ddt, rows, n, dt, "ddt"),
+        *_matrix(dz, rows, n, dt, "dz"), *_matrix(dB, rows, states, dt, "dB"),
+        *_matrix(dC, rows, states, dt, "dC"), _vector(dA, n * states, f32, "dA"),
+        _vector(dD, n, f32, "dD"), _vector(dbias, n, f32, "dbias"), _dev(ws, None, "ws"),
+        int(ws_bytes), _stream(stream)))
 
 
 class Network:
