@@ -71,6 +71,44 @@ __device__ __forceinline__ void store_row(T* p, int valid, const float (&x)[N]) 
   }
 }
 
+// N columns of a row, for threads that stand side by side at multiples of N: the last piece of a row
+// that does not end with one is moved back to the row's end, so that every load is whole and without
+// a branch, and many can be on their way.  The columns that it shares with its neighbour are read by
+// both, and only the neighbour's are stored (`skip`: how many that are), so that an output may lie
+// in an input's place.  A row shorter than N is one piece, read one by one.
+template <int N>
+struct Columns {
+  int at, skip, count;
+  __device__ __forceinline__ Columns(int col, int n)
+      : at(n >= N ? min(col, n - N) : 0), skip(col - at), count(min(n, N)) {}
+};
+template <typename T, int N>
+__device__ __forceinline__ Vec<T, N> load_columns(const T* row, const Columns<N>& c) {
+  if (c.count == N) return load_global<Vec<T, N>>(row + c.at);
+  Vec<T, N> v;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = load_global<T>(row + min(i, c.count - 1));
+  return v;
+}
+template <typename T, int N>
+__device__ __forceinline__ void store_columns(T* row, const Columns<N>& c, const float (&x)[N]) {
+  Vec<T, N> v;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = (T)x[i];
+  if (c.skip == 0 && c.count == N) {
+    store_global(row + c.at, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i >= c.skip && i < c.count) store_global<T>(row + c.at + i, v[i]);
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void floats(const Vec<T, N>& v, float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = (float)v[i];
+}
+
 // The 8 columns that thread `id` of a matrix with `per_row` pieces a row takes.  The block's first
 // piece is divided in 64 bits once (uniform), the thread's offset from it in 32.
 struct Piece {

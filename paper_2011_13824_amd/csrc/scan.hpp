@@ -90,84 +90,122 @@ __device__ __forceinline__ float column_sum(float v) {
   return v;
 }
 
-// N values of a row of floats that may end in between.
-template <int N, typename T>
-__device__ __forceinline__ void load_some(const T* p, int valid, float (&v)[N]) {
-  if constexpr (N == 1) {
-    v[0] = valid > 0 ? (float)load_global<T>(p) : 0.f;
-  } else {
-    load_row_end<T, N>(p, valid, v);
-  }
-}
-template <int N, typename T>
-__device__ __forceinline__ void store_some(T* p, int valid, const float (&v)[N]) {
-  if constexpr (N == 1) {
-    if (valid > 0) store_global<T>(p, (T)v[0]);
-  } else {
-    store_row<T, N>(p, valid, v);
-  }
-}
-
 // The columns and rows of a block and its threads.
 template <int LANES>
 struct ScanPlace {
   static constexpr int kColumns = 256 / LANES;
   static constexpr int kWide = kSpan / LANES;  // columns that a thread prepares of one row
-  int first_col, col, lane;                    // of the walk
-  int own_row, own_col;                        // of what the thread prepares
-  __device__ __forceinline__ explicit ScanPlace(int group) {
-    first_col = group * kColumns;
-    col = first_col + (int)threadIdx.x / LANES;
-    lane = threadIdx.x % LANES;
-    own_row = (int)threadIdx.x / (kColumns / kWide);
-    own_col = (int)threadIdx.x % (kColumns / kWide) * kWide;
+  int col, lane;                               // of the walk
+  int own_row, own_at;                         // of what the thread prepares: its first column,
+  int own_slot;                                // and where that stands in LDS
+  Columns<kWide> own;
+  __device__ __forceinline__ ScanPlace(int group, int n)
+      : col(group * kColumns + (int)threadIdx.x / LANES),
+        lane(threadIdx.x % LANES),
+        own_row((int)threadIdx.x / (kColumns / kWide)),
+        own_at(group * kColumns + (int)threadIdx.x % (kColumns / kWide) * kWide),
+        own_slot(kWide),
+        own(own_at, n) {
+    // a piece that is moved back may begin in front of the block's columns: kWide places are there
+    own_slot += max(own.at - group * kColumns, -kWide);
   }
 };
 
 template <int LANES>
 struct ScanShared {
-  static constexpr int kColumns = 256 / LANES, kStates = 4 * LANES;
-  float delta[kSpan][kColumns], du[kSpan][kColumns];
+  static constexpr int kColumns = 256 / LANES + kSpan / LANES, kStates = 4 * LANES;
+  float2 step[kSpan][kColumns];  // delta, delta u; column j of the block stands at kWide + j
   __attribute__((aligned(16))) float B[kSpan][kStates];
   __attribute__((aligned(16))) float C[kSpan][kStates];
-  float v[kSpan][kColumns];
   int flags[kSpan], slot[kSpan], plain;  // plain: 16 rows inside one sequence
 };
 
-// Flags and slots of the rows t0 .. t0 + 15, by the first 16 threads.
+// What a thread reads for a step, ahead of it.
 template <typename T, int LANES>
-__device__ __forceinline__ void scan_rows(const Scan<T>& a, int64_t t0, ScanShared<LANES>& sh) {
-  if (threadIdx.x >= 64) return;
-  const int64_t t = t0 + threadIdx.x;
-  int flags = 0;
-  if (threadIdx.x < kSpan) {
-    const int slot = a.s.slot(t);
-    if (slot >= 0) {
-      flags = kInside;
-      if (t == 0 || a.s.slot(t - 1) != slot) flags |= kBegins;
-      if (a.s.slot(t + 1) != slot) flags |= kEnds;
-    }
-    sh.flags[threadIdx.x] = flags;
-    sh.slot[threadIdx.x] = slot;
-  }
-  const uint64_t plain = __ballot(flags == kInside);
-  if (threadIdx.x == 0) sh.plain = (plain & 0xffff) == 0xffff;
-}
+struct ScanNext {
+  static constexpr int W = ScanPlace<LANES>::kWide;
+  static constexpr int kEach = (kSpan * 4 * LANES + 255) / 256;
+  Vec<T, W> u, dt, z, dy;
+  T B[kEach], C[kEach];
+  int slot[3];  // of the row, the one before and the one behind; by the first threads
 
-// B and C of 16 rows as floats, 0 behind the last state and the last row.
-template <typename T, int LANES>
-__device__ __forceinline__ void scan_vectors(const Scan<T>& a, int64_t t0, const T* p, int64_t ld,
-                                             float (&out)[kSpan][4 * LANES]) {
-  for (int i = threadIdx.x; i < kSpan * 4 * LANES; i += 256) {
-    const int r = i / (4 * LANES), k = i % (4 * LANES);
-    float v = 0.f;
-    if (t0 + r < a.s.rows && k < a.states) v = (float)load_global<T>(p + (t0 + r) * ld + k);
-    out[r][k] = v;
+  // What: 1 u and dt, 2 z, 4 dy, 8 B, 16 C, 32 slots.
+  template <int WHAT>
+  __device__ __forceinline__ void read(const Scan<T>& a, const ScanPlace<LANES>& at, int64_t t0) {
+    const int64_t t = min(max(t0, (int64_t)0) + at.own_row, a.s.rows - 1);
+    if constexpr (WHAT & 1) {
+      u = load_columns<T, W>(a.u + t * a.ldu, at.own);
+      dt = load_columns<T, W>(a.dt + t * a.lddt, at.own);
+    }
+    if constexpr (WHAT & 2)
+      if (a.z) z = load_columns<T, W>(a.z + t * a.ldz, at.own);
+    if constexpr (WHAT & 4) dy = load_columns<T, W>(a.dy + t * a.lddy, at.own);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = e * 256 + threadIdx.x;
+      const int64_t row = min(max(t0, (int64_t)0) + i / (4 * LANES), a.s.rows - 1);
+      const int k = min(i % (4 * LANES), a.states - 1);
+      if constexpr (WHAT & 8) B[e] = load_global<T>(a.B + row * a.ldB + k);
+      if constexpr (WHAT & 16) C[e] = load_global<T>(a.C + row * a.ldC + k);
+    }
+    if constexpr (WHAT & 32)
+      if (threadIdx.x < kSpan) {
+        const int64_t row = t0 + threadIdx.x;
+        slot[0] = a.s.slot(row);
+        slot[1] = a.s.slot(row - 1);
+        slot[2] = a.s.slot(row + 1);
+      }
   }
+
+  // B or C of 16 rows as floats, 0 behind the last state.
+  __device__ __forceinline__ void put(const Scan<T>& a, const T (&v)[kEach],
+                                      float (&out)[kSpan][4 * LANES]) const {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = e * 256 + threadIdx.x, k = i % (4 * LANES);
+      if (i < kSpan * 4 * LANES) out[i / (4 * LANES)][k] = k < a.states ? (float)v[e] : 0.f;
+    }
+  }
+
+  __device__ __forceinline__ void put_rows(const Scan<T>& a, int64_t t0,
+                                           ScanShared<LANES>& sh) const {
+    if (threadIdx.x >= 64) return;
+    int flags = 0;
+    if (threadIdx.x < kSpan) {
+      if (slot[0] >= 0) {
+        flags = kInside;
+        if (t0 + threadIdx.x == 0 || slot[1] != slot[0]) flags |= kBegins;
+        if (slot[2] != slot[0]) flags |= kEnds;
+      }
+      sh.flags[threadIdx.x] = flags;
+      sh.slot[threadIdx.x] = slot[0];
+    }
+    const uint64_t plain = __ballot(flags == kInside);
+    if (threadIdx.x == 0) sh.plain = (plain & 0xffff) == 0xffff;
+  }
+
+  __device__ __forceinline__ void put_steps(const ScanPlace<LANES>& at, const float (&bias)[W],
+                                            ScanShared<LANES>& sh) const {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      float v;
+      const float delta = softplus((float)dt[i] + bias[i], v);
+      sh.step[at.own_row][at.own_slot + i] = make_float2(delta, delta * (float)u[i]);
+    }
+  }
+};
+
+// Floats of the thread's own columns, 0 without p.
+template <int LANES>
+__device__ __forceinline__ void own_floats(const float* p, const ScanPlace<LANES>& at,
+                                           float (&v)[ScanPlace<LANES>::kWide]) {
+  constexpr int W = ScanPlace<LANES>::kWide;
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = 0.f;
+  if (p) floats<float, W>(load_columns<float, W>(p, at.own), v);
 }
 
 // Four states of a column out of [n][states] (padded: [n][4 * LANES]), 0 behind the last.
-template <int LANES>
 __device__ __forceinline__ void load_states(const float* p, int col, int lane, int states, int n,
                                             float (&h)[4]) {
   load_row_end<float, 4>(p + (int64_t)min(col, n - 1) * states + min(lane * 4, states - 1),
@@ -184,40 +222,22 @@ __device__ __forceinline__ void store_padded(float* p, int64_t at, int n, int co
   if (col < n) store_row<float, 4>(p + (at * n + col) * (4 * LANES) + lane * 4, 4, h);
 }
 
-// A in powers of two a unit of delta.
-template <typename T, int LANES>
-__device__ __forceinline__ void load_A(const Scan<T>& a, int col, int lane, float (&A)[4]) {
-  load_states<LANES>(a.A, col, lane, a.states, a.n, A);
-}
-
-// What a thread holds of a row's inputs.
-template <int W>
-struct ScanOwn {
-  float u[W], dt[W];
-};
-
-template <typename T, int LANES>
-__device__ __forceinline__ ScanOwn<ScanPlace<LANES>::kWide> scan_own(
-    const Scan<T>& a, const ScanPlace<LANES>& at, int64_t t0) {
-  constexpr int W = ScanPlace<LANES>::kWide;
-  ScanOwn<W> o;
-  const int64_t t = min(t0 + at.own_row, a.s.rows - 1);
-  const int col = at.first_col + at.own_col, c = min(col, a.n - 1);
-  load_some<W>(a.u + t * a.ldu + c, a.n - col, o.u);
-  load_some<W>(a.dt + t * a.lddt + c, a.n - col, o.dt);
-  return o;
-}
-
-template <int LANES, int W>
-__device__ __forceinline__ void scan_prepare(const ScanPlace<LANES>& at, const ScanOwn<W>& o,
-                                             const float (&bias)[W], ScanShared<LANES>& sh) {
+// A, and A in powers of two.
+template <typename T>
+__device__ __forceinline__ void load_A(const Scan<T>& a, int col, int lane, float (&A)[4],
+                                       float (&A2)[4]) {
+  load_states(a.A, col, lane, a.states, a.n, A);
 #pragma unroll
-  for (int i = 0; i < W; ++i) {
-    float v;
-    const float delta = softplus(o.dt[i] + bias[i], v);
-    sh.delta[at.own_row][at.own_col + i] = delta;
-    sh.du[at.own_row][at.own_col + i] = delta * o.u[i];
-  }
+  for (int i = 0; i < 4; ++i) A2[i] = A[i] * 1.44269504f;
+}
+
+// A row's step of four states.
+__device__ __forceinline__ void advance(float (&h)[4], float2 step, const float (&A2)[4],
+                                        const float* B) {
+  const f32x4 b = *(const f32x4*)B;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    h[i] = fmaf(__builtin_amdgcn_exp2f(step.x * A2[i]), h[i], step.y * b[i]);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -231,7 +251,7 @@ __global__ __launch_bounds__(256) void k_scan_local(Scan<T> a, int groups) {
   __shared__ ScanShared<LANES> sh;
   __shared__ int begins;
   const int chunk = blockIdx.x / groups, group = blockIdx.x % groups;
-  const ScanPlace<LANES> at(group);
+  const ScanPlace<LANES> at(group, a.n);
   const int64_t first = (int64_t)chunk * a.chunk, end = first + a.chunk;  // not the last chunk
   const int slot = a.s.slot(end - 1);
   const bool goes_on = slot >= 0 && a.s.slot(end) == slot;
@@ -246,46 +266,36 @@ __global__ __launch_bounds__(256) void k_scan_local(Scan<T> a, int groups) {
   if (group == 0 && threadIdx.x == 0)
     a.links[chunk] = goes_on ? kGoesOn | (from < 0 ? kWhole : 0) : 0;
   if (!goes_on) return;
-  float A[4], h[4] = {}, bias[W] = {};
-  load_A<T, LANES>(a, at.col, at.lane, A);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) A[i] *= 1.44269504f;
-  if (a.bias)
-    load_some<W>(a.bias + min(at.first_col + at.own_col, a.n - 1),
-                 a.n - at.first_col - at.own_col, bias);
+  float A[4], A2[4], h[4] = {}, bias[W];
+  load_A(a, at.col, at.lane, A, A2);
+  own_floats<LANES>(a.bias, at, bias);
   if (from >= 0 && a.state) {
-    load_states<LANES>(a.state + (int64_t)slot * a.n * a.states, at.col, at.lane, a.states, a.n, h);
+    load_states(a.state + (int64_t)slot * a.n * a.states, at.col, at.lane, a.states, a.n, h);
     store_padded<LANES>(a.begin, chunk, a.n, at.col, at.lane, h);
   }
   float sum = 0.f;
   const int64_t start = first + max(from, 0);
   int64_t t0 = start / kSpan * kSpan;
-  ScanOwn<W> own = scan_own<T, LANES>(a, at, t0);
+  const int column = W + (int)threadIdx.x / LANES;
+  ScanNext<T, LANES> next;
+  next.template read<1 | 8>(a, at, t0);
   for (; t0 < end; t0 += kSpan) {
     __syncthreads();
-    scan_prepare<LANES>(at, own, bias, sh);
-    scan_vectors<T, LANES>(a, t0, a.B, a.ldB, sh.B);
+    next.put_steps(at, bias, sh);
+    next.put(a, next.B, sh.B);
     __syncthreads();
-    own = scan_own<T, LANES>(a, at, t0 + kSpan);
-    const int column = threadIdx.x / LANES;
+    next.template read<1 | 8>(a, at, t0 + kSpan);
     const int skip = (int)max((int64_t)0, start - t0);
+    auto row = [&](int r) {
+      const float2 step = sh.step[r][column];
+      sum += step.x;
+      advance(h, step, A2, sh.B[r] + at.lane * 4);
+    };
     if (skip == 0) {
 #pragma unroll
-      for (int r = 0; r < kSpan; ++r) {
-        const float delta = sh.delta[r][column], du = sh.du[r][column];
-        sum += delta;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          h[i] = fmaf(__builtin_amdgcn_exp2f(delta * A[i]), h[i], du * sh.B[r][at.lane * 4 + i]);
-      }
+      for (int r = 0; r < kSpan; ++r) row(r);
     } else {
-      for (int r = skip; r < kSpan; ++r) {
-        const float delta = sh.delta[r][column], du = sh.du[r][column];
-        sum += delta;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          h[i] = fmaf(__builtin_amdgcn_exp2f(delta * A[i]), h[i], du * sh.B[r][at.lane * 4 + i]);
-      }
+      for (int r = skip; r < kSpan; ++r) row(r);
     }
   }
   store_padded<LANES>(a.local, chunk, a.n, at.col, at.lane, h);
@@ -299,10 +309,8 @@ __global__ __launch_bounds__(256) void k_scan_link(Scan<T> a) {
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int col = (int)(id / LANES), lane = (int)(id % LANES);
   if (col >= a.n) return;
-  float A[4], h[4] = {};
-  load_A<T, LANES>(a, col, lane, A);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) A[i] *= 1.44269504f;
+  float A[4], A2[4], h[4] = {};
+  load_A(a, col, lane, A, A2);
   for (int i = 0; i + 1 < a.chunks; ++i) {
     const int c = BACK ? a.chunks - 1 - i : i;
     const int link = a.links[c];
@@ -315,7 +323,7 @@ __global__ __launch_bounds__(256) void k_scan_link(Scan<T> a) {
     const float sum = a.deltas[(int64_t)c * a.n + col];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      h[k] = link & kWhole ? fmaf(__builtin_amdgcn_exp2f(sum * A[k]), h[k], add[k]) : add[k];
+      h[k] = link & kWhole ? fmaf(__builtin_amdgcn_exp2f(sum * A2[k]), h[k], add[k]) : add[k];
     store_padded<LANES>(a.local, c, a.n, col, lane, h);
   }
 }
@@ -324,57 +332,48 @@ template <typename T, int LANES>
 __global__ __launch_bounds__(256) void k_scan_fwd(Scan<T> a, int groups) {
   constexpr int W = ScanPlace<LANES>::kWide, kOwn = kSpan / LANES;
   __shared__ ScanShared<LANES> sh;
+  __shared__ float shv[kSpan][ScanShared<LANES>::kColumns];  // sum_n C h
   const int chunk = blockIdx.x / groups;
-  const ScanPlace<LANES> at(blockIdx.x % groups);
+  const ScanPlace<LANES> at(blockIdx.x % groups, a.n);
   const int64_t first = (int64_t)chunk * a.chunk, end = min(first + a.chunk, a.s.rows);
-  const int column = threadIdx.x / LANES;
-  const int own_at = at.first_col + at.own_col, own_safe = min(own_at, a.n - 1);
-  const int own_valid = a.n - own_at;
-  float A[4], h[4] = {}, bias[W] = {}, D[W] = {};
-  load_A<T, LANES>(a, at.col, at.lane, A);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) A[i] *= 1.44269504f;
-  if (a.bias) load_some<W>(a.bias + own_safe, own_valid, bias);
-  if (a.D) load_some<W>(a.D + own_safe, own_valid, D);
+  const int column = W + (int)threadIdx.x / LANES;
+  float A[4], A2[4], h[4] = {}, bias[W], D[W];
+  load_A(a, at.col, at.lane, A, A2);
+  own_floats<LANES>(a.bias, at, bias);
+  own_floats<LANES>(a.D, at, D);
   if (chunk > 0 && a.links[chunk - 1] & kGoesOn)
     load_padded<LANES>(a.local, chunk - 1, a.n, at.col, at.lane, h);
   // the state of the sequence that goes on behind the chunk may have been replaced in the meantime,
   // where it goes to the place that it came from
   const bool goes_on = chunk + 1 < a.chunks && a.links[chunk] & kGoesOn;
   const int last_slot = goes_on ? a.s.slot(end - 1) : -1;
-  ScanOwn<W> own = scan_own<T, LANES>(a, at, first);
+  ScanNext<T, LANES> next;
+  next.template read<1 | 2 | 8 | 16 | 32>(a, at, first);
   for (int64_t t0 = first; t0 < end; t0 += kSpan) {
     const int64_t mine = t0 + at.own_row;
-    float z[W];
-    if (a.z) load_some<W>(a.z + min(mine, a.s.rows - 1) * a.ldz + own_safe, own_valid, z);
-    scan_prepare<LANES>(at, own, bias, sh);
-    scan_vectors<T, LANES>(a, t0, a.B, a.ldB, sh.B);
-    scan_vectors<T, LANES>(a, t0, a.C, a.ldC, sh.C);
-    scan_rows<T, LANES>(a, t0, sh);
-    float u[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) u[i] = own.u[i];
+    next.put_steps(at, bias, sh);
+    next.put(a, next.B, sh.B);
+    next.put(a, next.C, sh.C);
+    next.put_rows(a, t0, sh);
+    const Vec<T, W> u = next.u, z = next.z;
     __syncthreads();
-    own = scan_own<T, LANES>(a, at, t0 + kSpan);
+    next.template read<1 | 2 | 8 | 16 | 32>(a, at, t0 + kSpan);
     const bool inside = sh.flags[at.own_row] & kInside;
     if (a.kept) store_padded<LANES>(a.kept, t0 / kSpan, a.n, at.col, at.lane, h);
     float v[kOwn];
     auto row = [&](int r) {
-      const float delta = sh.delta[r][column], du = sh.du[r][column];
-      float sum = 0.f;
+      advance(h, sh.step[r][column], A2, sh.B[r] + at.lane * 4);
+      const f32x4 c = *(const f32x4*)(sh.C[r] + at.lane * 4);
+      float sum = c[0] * h[0];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        h[i] = fmaf(__builtin_amdgcn_exp2f(delta * A[i]), h[i], du * sh.B[r][at.lane * 4 + i]);
-        sum = fmaf(sh.C[r][at.lane * 4 + i], h[i], sum);
-      }
+      for (int i = 1; i < 4; ++i) sum = fmaf(c[i], h[i], sum);
       return column_sum<LANES>(sum);
     };
     if (sh.plain) {
 #pragma unroll
       for (int r = 0; r < kSpan; ++r) {
         const float sum = row(r);
-        if (r % LANES == 0) v[r / LANES] = sum;
-        v[r / LANES] = at.lane == r % LANES ? sum : v[r / LANES];
+        v[r / LANES] = r % LANES == 0 || at.lane == r % LANES ? sum : v[r / LANES];
       }
     } else {
 #pragma unroll
@@ -387,30 +386,29 @@ __global__ __launch_bounds__(256) void k_scan_fwd(Scan<T> a, int groups) {
             if (slot == last_slot)
               load_padded<LANES>(a.begin, chunk, a.n, at.col, at.lane, h);
             else
-              load_states<LANES>(a.state + (int64_t)slot * a.n * a.states, at.col, at.lane,
-                                 a.states, a.n, h);
+              load_states(a.state + (int64_t)slot * a.n * a.states, at.col, at.lane, a.states, a.n,
+                          h);
           }
         }
         if (flags & kInside) sum = row(r);
         if (flags & kEnds && a.state_out && at.col < a.n)
           store_row<float, 4>(a.state_out + ((int64_t)slot * a.n + at.col) * a.states + at.lane * 4,
                               a.states - at.lane * 4, h);
-        if (r % LANES == 0) v[r / LANES] = sum;
-        v[r / LANES] = at.lane == r % LANES ? sum : v[r / LANES];
+        v[r / LANES] = r % LANES == 0 || at.lane == r % LANES ? sum : v[r / LANES];
       }
     }
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) sh.v[i * LANES + at.lane][column] = v[i];
+    for (int i = 0; i < kOwn; ++i) shv[i * LANES + at.lane][column] = v[i];
     __syncthreads();
-    if (mine < end) {
+    if (mine < end && at.own_at < a.n) {
       float y[W];
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        y[i] = fmaf(D[i], u[i], sh.v[at.own_row][at.own_col + i]);
-        if (a.z) y[i] *= z[i] * sigmoid(z[i]);
+        y[i] = fmaf(D[i], (float)u[i], shv[at.own_row][at.own_slot + i]);
+        if (a.z) y[i] *= (float)z[i] * sigmoid((float)z[i]);
         if (!inside) y[i] = 0.f;
       }
-      store_some<W>(a.y + mine * a.ldy + own_safe, own_valid, y);
+      store_columns<T, W>(a.y + mine * a.ldy, at.own, y);
     }
   }
 }
@@ -423,8 +421,8 @@ __global__ __launch_bounds__(256) void k_scan_step(Scan<T> a, int groups) {
   const int col = (int)(blockIdx.x % groups) * (256 / LANES) + column;
   const int slot = a.s.seq ? a.s.slot(t) : t < a.s.slots ? (int)t : -1;
   if (col >= a.n) return;
-  float A[4], B[4], C[4], h[4] = {};
-  load_A<T, LANES>(a, col, lane, A);
+  float A[4], A2[4], B[4], C[4], h[4] = {};
+  load_A(a, col, lane, A, A2);
   const int k = min(lane * 4, a.states - 1);
   load_row_end<T, 4>(a.B + t * a.ldB + k, a.states - lane * 4, B);
   load_row_end<T, 4>(a.C + t * a.ldC + k, a.states - lane * 4, C);
@@ -437,7 +435,7 @@ __global__ __launch_bounds__(256) void k_scan_step(Scan<T> a, int groups) {
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    h[i] = fmaf(__builtin_amdgcn_exp2f(delta * (A[i] * 1.44269504f)), h[i], du * B[i]);
+    h[i] = fmaf(__builtin_amdgcn_exp2f(delta * A2[i]), h[i], du * B[i]);
     sum = fmaf(C[i], h[i], sum);
   }
   sum = column_sum<LANES>(sum);
@@ -455,30 +453,19 @@ __global__ __launch_bounds__(256) void k_scan_step(Scan<T> a, int groups) {
 // ---------------------------------------------------------------------------------------------
 // Backward
 // ---------------------------------------------------------------------------------------------
-template <int LANES>
-struct ScanBackShared {
-  static constexpr int kColumns = 256 / LANES;
-  ScanShared<LANES> s;  // s.v: sum_n C h
-  float p[kSpan][kColumns], gB[kSpan][kColumns], eA[kSpan][kColumns];
-  float dBC[4][kSpan][2][4 * LANES];  // of the four waves
-};
 
-// dy silu(z), and dy silu'(z), of a row's own values.
-template <typename T, int LANES>
-__device__ __forceinline__ void scan_gate(const Scan<T>& a, int64_t t, int safe, int valid,
-                                          float (&p)[ScanPlace<LANES>::kWide],
-                                          float (&q)[ScanPlace<LANES>::kWide]) {
-  constexpr int W = ScanPlace<LANES>::kWide;
-  const int64_t row = min(t, a.s.rows - 1);
-  load_some<W>(a.dy + row * a.lddy + safe, valid, p);
-  if (!a.z) return;
-  float z[W];
-  load_some<W>(a.z + row * a.ldz + safe, valid, z);
+// p = dy silu(z) and q = dy silu'(z) of a row's own values.
+template <typename T, int W>
+__device__ __forceinline__ void scan_gate(bool gate, const Vec<T, W>& dy, const Vec<T, W>& z,
+                                          float (&p)[W], float (&q)[W]) {
 #pragma unroll
   for (int i = 0; i < W; ++i) {
-    const float s = sigmoid(z[i]);
-    q[i] = p[i] * s * fmaf(z[i], 1.f - s, 1.f);
-    p[i] *= z[i] * s;
+    p[i] = (float)dy[i];
+    if (gate) {
+      const float x = (float)z[i], s = sigmoid(x);
+      q[i] = p[i] * s * fmaf(x, 1.f - s, 1.f);
+      p[i] *= x * s;
+    }
   }
 }
 
@@ -486,10 +473,11 @@ __device__ __forceinline__ void scan_gate(const Scan<T>& a, int64_t t, int safe,
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void k_scan_back_local(Scan<T> a, int groups) {
   constexpr int W = ScanPlace<LANES>::kWide;
-  __shared__ ScanShared<LANES> sh;  // v: p
+  __shared__ ScanShared<LANES> sh;
+  __shared__ float shp[kSpan][ScanShared<LANES>::kColumns];  // p
   __shared__ int ends;
   const int chunk = blockIdx.x / groups + 1, group = blockIdx.x % groups;  // not the first chunk
-  const ScanPlace<LANES> at(group);
+  const ScanPlace<LANES> at(group, a.n);
   const int64_t first = (int64_t)chunk * a.chunk, end = min(first + a.chunk, a.s.rows);
   const int slot = a.s.slot(first);
   const bool goes_on = slot >= 0 && a.s.slot(first - 1) == slot;
@@ -504,31 +492,31 @@ __global__ __launch_bounds__(256) void k_scan_back_local(Scan<T> a, int groups) 
     a.links[chunk] = goes_on ? kGoesOn | (whole ? kWhole : 0) : 0;
   if (!goes_on) return;
   const int64_t stop = whole ? end : first + ends + 1;  // behind the sequence's last row here
-  const int column = threadIdx.x / LANES;
-  const int own_at = at.first_col + at.own_col, own_safe = min(own_at, a.n - 1);
-  const int own_valid = a.n - own_at;
-  float A[4], g[4] = {}, bias[W] = {}, sum = 0.f;
-  load_A<T, LANES>(a, at.col, at.lane, A);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) A[i] *= 1.44269504f;
-  if (a.bias) load_some<W>(a.bias + own_safe, own_valid, bias);
-  for (int64_t t0 = (stop - 1) / kSpan * kSpan; t0 >= first; t0 -= kSpan) {
-    const ScanOwn<W> own = scan_own<T, LANES>(a, at, t0);
+  const int column = W + (int)threadIdx.x / LANES;
+  float A[4], A2[4], g[4] = {}, bias[W], sum = 0.f;
+  load_A(a, at.col, at.lane, A, A2);
+  own_floats<LANES>(a.bias, at, bias);
+  int64_t t0 = (stop - 1) / kSpan * kSpan;
+  ScanNext<T, LANES> next;
+  next.template read<1 | 2 | 4 | 16>(a, at, t0);
+  for (; t0 >= first; t0 -= kSpan) {
     float p[W], q[W];
-    scan_gate<T, LANES>(a, t0 + at.own_row, own_safe, own_valid, p, q);
+    scan_gate<T, W>(a.z, next.dy, next.z, p, q);
     __syncthreads();
-    scan_prepare<LANES>(at, own, bias, sh);
-    scan_vectors<T, LANES>(a, t0, a.C, a.ldC, sh.C);
+    next.put_steps(at, bias, sh);
+    next.put(a, next.C, sh.C);
 #pragma unroll
-    for (int i = 0; i < W; ++i) sh.v[at.own_row][at.own_col + i] = p[i];
+    for (int i = 0; i < W; ++i) shp[at.own_row][at.own_slot + i] = p[i];
     __syncthreads();
+    next.template read<1 | 2 | 4 | 16>(a, at, t0 - kSpan);
     const int rows = (int)min((int64_t)kSpan, stop - t0);
     auto row = [&](int r) {
-      const float delta = sh.delta[r][column], pr = sh.v[r][column];
+      const float delta = sh.step[r][column].x, pr = shp[r][column];
+      const f32x4 c = *(const f32x4*)(sh.C[r] + at.lane * 4);
       sum += delta;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        g[i] = __builtin_amdgcn_exp2f(delta * A[i]) * fmaf(sh.C[r][at.lane * 4 + i], pr, g[i]);
+        g[i] = __builtin_amdgcn_exp2f(delta * A2[i]) * fmaf(c[i], pr, g[i]);
     };
     if (rows == kSpan) {
 #pragma unroll
@@ -572,153 +560,165 @@ __device__ __forceinline__ void wave_sums(const float (&v)[8], float (&out)[2]) 
   }
 }
 
+// The 16 rows of a step are taken in two halves, so that the states and decays of a half stay in
+// registers between the walk to its end and the walk back; the state between the halves is computed
+// first.
 template <typename T, int LANES>
 __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
-  constexpr int W = ScanPlace<LANES>::kWide, kOwn = kSpan / LANES, kStates = 4 * LANES;
-  __shared__ ScanBackShared<LANES> sh;
+  constexpr int W = ScanPlace<LANES>::kWide, kStates = 4 * LANES, kHalf = kSpan / 2;
+  constexpr int kColumns = ScanShared<LANES>::kColumns;
+  __shared__ ScanShared<LANES> sh;
+  __shared__ float shp[kSpan][kColumns];       // p
+  __shared__ f32x4 sums[kSpan][kColumns];      // over the states: C h, g B, e A
+  __shared__ float dBC[4][kSpan][2][kStates];  // of the four waves
   const int chunk = blockIdx.x / groups, group = blockIdx.x % groups;
-  const ScanPlace<LANES> at(group);
+  const ScanPlace<LANES> at(group, a.n);
   const int64_t first = (int64_t)chunk * a.chunk, end = min(first + a.chunk, a.s.rows);
-  const int column = threadIdx.x / LANES, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int own_at = at.first_col + at.own_col, own_safe = min(own_at, a.n - 1);
-  const int own_valid = a.n - own_at;
-  float A[4], A2[4], g[4] = {}, dA[4] = {}, bias[W] = {}, D[W] = {}, dD[W] = {}, dbias[W] = {};
-  load_A<T, LANES>(a, at.col, at.lane, A);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) A2[i] = A[i] * 1.44269504f;
-  if (a.bias) load_some<W>(a.bias + own_safe, own_valid, bias);
-  if (a.D) load_some<W>(a.D + own_safe, own_valid, D);
+  const int column = W + (int)threadIdx.x / LANES, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float A[4], A2[4], g[4] = {}, dA[4] = {}, bias[W], D[W], dD[W] = {}, dbias[W] = {};
+  load_A(a, at.col, at.lane, A, A2);
+  own_floats<LANES>(a.bias, at, bias);
+  own_floats<LANES>(a.D, at, D);
   // g: e^(delta A) g of the row behind
   if (chunk + 1 < a.chunks && a.links[chunk + 1] & kGoesOn)
     load_padded<LANES>(a.local, chunk + 1, a.n, at.col, at.lane, g);
-  for (int64_t t0 = (end - 1) / kSpan * kSpan; t0 >= first; t0 -= kSpan) {
+  int64_t t0 = (end - 1) / kSpan * kSpan;
+  ScanNext<T, LANES> next;
+  next.template read<1 | 2 | 4 | 8 | 16 | 32>(a, at, t0);
+  float kept[4];
+  load_padded<LANES>(a.kept, t0 / kSpan, a.n, at.col, at.lane, kept);
+  for (; t0 >= first; t0 -= kSpan) {
     const int64_t mine = t0 + at.own_row;
-    const ScanOwn<W> own = scan_own<T, LANES>(a, at, t0);
-    float p[W], q[W];
-    scan_gate<T, LANES>(a, mine, own_safe, own_valid, p, q);
-    float h0[4];
-    load_padded<LANES>(a.kept, t0 / kSpan, a.n, at.col, at.lane, h0);
-    scan_prepare<LANES>(at, own, bias, sh.s);
-    scan_vectors<T, LANES>(a, t0, a.B, a.ldB, sh.s.B);
-    scan_vectors<T, LANES>(a, t0, a.C, a.ldC, sh.s.C);
-    scan_rows<T, LANES>(a, t0, sh.s);
+    const Vec<T, W> u = next.u, dt = next.dt;
+    float p[W], q[W], half_state[2][4];
+    scan_gate<T, W>(a.z, next.dy, next.z, p, q);
+    next.put_steps(at, bias, sh);
+    next.put(a, next.B, sh.B);
+    next.put(a, next.C, sh.C);
+    next.put_rows(a, t0, sh);
 #pragma unroll
-    for (int i = 0; i < W; ++i) sh.p[at.own_row][at.own_col + i] = p[i];
+    for (int i = 0; i < W; ++i) shp[at.own_row][at.own_slot + i] = p[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) half_state[0][i] = half_state[1][i] = kept[i];
     __syncthreads();
-    // the 16 rows' states again
-    float h[kSpan][4], e[kSpan][4];  // h_t; e^(delta A)
-    const bool plain = sh.s.plain;
+    next.template read<1 | 2 | 4 | 8 | 16 | 32>(a, at, t0 - kSpan);
+    load_padded<LANES>(a.kept, max(t0 / kSpan - 1, (int64_t)0), a.n, at.col, at.lane, kept);
+    const bool plain = sh.plain;
 #pragma unroll
-    for (int r = 0; r < kSpan; ++r) {
-      const float delta = sh.s.delta[r][column], du = sh.s.du[r][column];
-      if (!plain && sh.s.flags[r] & kBegins) h0[0] = h0[1] = h0[2] = h0[3] = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        e[r][i] = __builtin_amdgcn_exp2f(delta * A2[i]);
-        h0[i] = fmaf(e[r][i], h0[i], du * sh.s.B[r][at.lane * 4 + i]);
-        h[r][i] = h0[i];
-      }
+    for (int r = 0; r < kHalf; ++r) {
+      if (!plain && sh.flags[r] & kBegins)
+        half_state[1][0] = half_state[1][1] = half_state[1][2] = half_state[1][3] = 0.f;
+      advance(half_state[1], sh.step[r][column], A2, sh.B[r] + at.lane * 4);
     }
-    load_padded<LANES>(a.kept, t0 / kSpan, a.n, at.col, at.lane, h0);
-    float v[kOwn], gB[kOwn], eA[kOwn];
+#pragma unroll 1
+    for (int half = 1; half >= 0; --half) {
+      const int row0 = half * kHalf;
+      float h[kHalf + 1][4], e[kHalf][4];  // the state in front of the half and behind its rows
 #pragma unroll
-    for (int r = kSpan - 1; r >= 0; --r) {
-      const int flags = plain ? kInside : sh.s.flags[r];
-      float cs = 0.f, bs = 0.f, es = 0.f, out[8] = {};
-      if (flags & kInside) {
-        const float delta = sh.s.delta[r][column], du = sh.s.du[r][column];
-        const float pr = sh.p[r][column];
-        const bool begins = flags & kBegins;
-        if (flags & kEnds) g[0] = g[1] = g[2] = g[3] = 0.f;
+      for (int i = 0; i < 4; ++i) h[0][i] = half ? half_state[1][i] : half_state[0][i];
+#pragma unroll
+      for (int r = 0; r < kHalf; ++r) {
+        const float2 step = sh.step[row0 + r][column];
+        const f32x4 b = *(const f32x4*)(sh.B[row0 + r] + at.lane * 4);
+        // what is left of the state in front of a sequence's first row: nothing
+        const bool begins = !plain && sh.flags[row0 + r] & kBegins;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float C = sh.s.C[r][at.lane * 4 + i], B = sh.s.B[r][at.lane * 4 + i];
-          g[i] = fmaf(C, pr, g[i]);
-          cs = fmaf(C, h[r][i], cs);
-          out[i] = g[i] * du;
-          out[4 + i] = pr * h[r][i];
-          bs = fmaf(g[i], B, bs);
-          g[i] *= e[r][i];
-          const float before = begins ? 0.f : r ? h[r ? r - 1 : 0][i] : h0[i];
-          const float t = g[i] * before;
-          es = fmaf(t, A[i], es);
-          dA[i] = fmaf(t, delta, dA[i]);
-        }
-        if (at.col >= a.n)  // columns past the matrix have no part in the sums over columns
-#pragma unroll
-          for (int i = 0; i < 8; ++i) out[i] = 0.f;
-      }
-      cs = column_sum<LANES>(cs);
-      bs = column_sum<LANES>(bs);
-      es = column_sum<LANES>(es);
-      const bool keep = at.lane == r % LANES;
-      v[r / LANES] = keep || r % LANES == LANES - 1 ? cs : v[r / LANES];
-      gB[r / LANES] = keep || r % LANES == LANES - 1 ? bs : gB[r / LANES];
-      eA[r / LANES] = keep || r % LANES == LANES - 1 ? es : eA[r / LANES];
-      float two[2];
-      wave_sums<LANES>(out, two);
-      if (lane % 16 < LANES) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int value = lane / 16 * 2 + i;
-          sh.dBC[wave][r][value / 4][at.lane * 4 + value % 4] = two[i];
+          e[r][i] = begins ? 0.f : __builtin_amdgcn_exp2f(step.x * A2[i]);
+          h[r + 1][i] = fmaf(e[r][i], begins ? 0.f : h[r][i], step.y * b[i]);
         }
       }
-    }
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      sh.s.v[i * LANES + at.lane][column] = v[i];
-      sh.gB[i * LANES + at.lane][column] = gB[i];
-      sh.eA[i * LANES + at.lane][column] = eA[i];
+      for (int r = kHalf - 1; r >= 0; --r) {
+        const int flags = plain ? kInside : sh.flags[row0 + r];
+        float cs = 0.f, bs = 0.f, es = 0.f, out[8] = {};
+        if (flags & kInside) {
+          const float2 step = sh.step[row0 + r][column];
+          const float pr = shp[row0 + r][column];
+          const f32x4 b = *(const f32x4*)(sh.B[row0 + r] + at.lane * 4);
+          const f32x4 c = *(const f32x4*)(sh.C[row0 + r] + at.lane * 4);
+          const bool begins = flags & kBegins;
+          if (flags & kEnds) g[0] = g[1] = g[2] = g[3] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            g[i] = fmaf(c[i], pr, g[i]);
+            cs = fmaf(c[i], h[r + 1][i], cs);
+            out[i] = g[i] * step.y;
+            out[4 + i] = pr * h[r + 1][i];
+            bs = fmaf(g[i], b[i], bs);
+            g[i] *= e[r][i];
+            const float t = begins ? 0.f : g[i] * h[r][i];
+            es = fmaf(t, A[i], es);
+            dA[i] = fmaf(t, step.x, dA[i]);
+          }
+          if (at.col >= a.n)  // columns past the matrix have no part in the sums over columns
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[i] = 0.f;
+        }
+        cs = column_sum<LANES>(cs);
+        bs = column_sum<LANES>(bs);
+        es = column_sum<LANES>(es);
+        if (at.lane == 0) sums[row0 + r][column] = f32x4{cs, bs, es, 0.f};
+        float two[2];
+        wave_sums<LANES>(out, two);
+        if (lane % 16 < LANES) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int value = lane / 16 * 2 + i;
+            dBC[wave][row0 + r][value / 4][at.lane * 4 + value % 4] = two[i];
+          }
+        }
+      }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < kSpan * 2 * kStates; i += 256) {
       const int r = i / (2 * kStates), k = i % (2 * kStates);
-      const float* w = &sh.dBC[0][r][0][0] + k;
+      const float* w = &dBC[0][r][0][0] + k;
       constexpr int kWave = kSpan * 2 * kStates;
       if (t0 + r < end)
         a.dBC[((int64_t)group * a.s.rows + t0 + r) * (2 * kStates) + k] =
             (w[0] + w[kWave]) + (w[2 * kWave] + w[3 * kWave]);
     }
-    if (mine < end) {
-      const bool inside = sh.s.flags[at.own_row] & kInside;
+    if (mine < end && at.own_at < a.n) {
+      const bool inside = sh.flags[at.own_row] & kInside;
       float du[W], ddt[W], dz[W];
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        float w;
-        const float x = own.dt[i] + bias[i], delta = softplus(x, w);
-        const float sum_gB = sh.gB[at.own_row][at.own_col + i];
-        du[i] = fmaf(delta, sum_gB, D[i] * p[i]);
-        ddt[i] = fmaf(own.u[i], sum_gB, sh.eA[at.own_row][at.own_col + i]) * softplus_slope(x, w);
-        dz[i] = q[i] * fmaf(D[i], own.u[i], sh.s.v[at.own_row][at.own_col + i]);
+        const float x = (float)dt[i] + bias[i], ui = (float)u[i];
+        const float v = __builtin_amdgcn_exp2f(fabsf(x) * -1.44269504f);
+        const f32x4 s = sums[at.own_row][at.own_slot + i];
+        du[i] = fmaf(sh.step[at.own_row][at.own_slot + i].x, s[1], D[i] * p[i]);
+        ddt[i] = fmaf(ui, s[1], s[2]) * softplus_slope(x, v);
+        dz[i] = q[i] * fmaf(D[i], ui, s[0]);
         if (!inside) du[i] = ddt[i] = dz[i] = 0.f;
-        dD[i] += inside ? p[i] * own.u[i] : 0.f;
+        dD[i] += inside ? p[i] * ui : 0.f;
         dbias[i] += ddt[i];
       }
-      store_some<W>(a.du + mine * a.lddu + own_safe, own_valid, du);
-      store_some<W>(a.ddt + mine * a.ldddt + own_safe, own_valid, ddt);
-      if (a.z) store_some<W>(a.dz + mine * a.lddz + own_safe, own_valid, dz);
+      store_columns<T, W>(a.du + mine * a.lddu, at.own, du);
+      store_columns<T, W>(a.ddt + mine * a.ldddt, at.own, ddt);
+      if (a.z) store_columns<T, W>(a.dz + mine * a.lddz, at.own, dz);
     }
     __syncthreads();
   }
   store_padded<LANES>(a.dA, chunk, a.n, at.col, at.lane, dA);
   // dD and dbias over the 16 rows of a step, in order
+  if (at.own_at < a.n)
 #pragma unroll
-  for (int i = 0; i < W; ++i) {
-    sh.gB[at.own_row][at.own_col + i] = dD[i];
-    sh.eA[at.own_row][at.own_col + i] = dbias[i];
-  }
+    for (int i = 0; i < W; ++i)
+      sh.step[at.own_row][at.own_slot + i] = make_float2(dD[i], dbias[i]);
   __syncthreads();
   for (int i = threadIdx.x; i < ScanPlace<LANES>::kColumns; i += 256) {
-    if (at.first_col + i >= a.n) continue;
+    const int col = group * ScanPlace<LANES>::kColumns + i;
+    if (col >= a.n) continue;
     float d = 0.f, b = 0.f;
 #pragma unroll
     for (int r = 0; r < kSpan; ++r) {
-      d += sh.gB[r][i];
-      b += sh.eA[r][i];
+      const float2 s = sh.step[r][W + i];
+      d += s.x;
+      b += s.y;
     }
-    a.dD[(int64_t)chunk * a.n + at.first_col + i] = d;
-    a.dbias[(int64_t)chunk * a.n + at.first_col + i] = b;
+    a.dD[(int64_t)chunk * a.n + col] = d;
+    a.dbias[(int64_t)chunk * a.n + col] = b;
   }
 }
 
