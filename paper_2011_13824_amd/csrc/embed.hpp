@@ -26,13 +26,14 @@ __global__ __launch_bounds__(256) void k_embed_fwd(const int64_t* __restrict__ t
   const Piece p = piece_of((int64_t)blockIdx.x * 256, (n + 7) / 8);
   if (p.row >= rows) return;
   const int64_t t = load_global<int64_t>(tokens + p.row);
+  const Columns<8> c(p.col, n);
   float v[8] = {};
   if (t >= 0 && t < vocab) {
-    load_row_end<T, 8>(table + t * ldt + p.col, n - p.col, v);
+    floats<T, 8>(load_columns<T, 8>(table + t * ldt, c), v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= scale;
   }
-  store_row<T, 8>(out + p.row * ldo + p.col, n - p.col, v);
+  store_columns<T, 8>(out + p.row * ldo, c, v);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -64,14 +65,28 @@ constexpr int kFillPieces = 256 * 8;
 template <typename T>
 __device__ __forceinline__ void embed_fill(const EmbedFill<T>& f, int64_t block) {
   const int per_row = (f.n + 7) / 8;
-#pragma unroll 4
-  for (int i = 0; i < kFillPieces / 256; ++i) {
-    const int64_t start = f.first + block * kFillPieces + i * 256;
-    if (start + threadIdx.x >= f.end) return;
-    const Piece p = piece_of(start, per_row);
-    float v[8] = {};
-    if (f.base) load_row_end<T, 8>(f.base + p.row * f.ldb + p.col, f.n - p.col, v);
-    store_row<T, 8>(f.dtable + p.row * f.ldd + p.col, f.n - p.col, v);
+  constexpr int kAhead = 4;
+  for (int i0 = 0; i0 < kFillPieces / 256; i0 += kAhead) {
+    Vec<T, 8> v[kAhead];
+    if (f.base)
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int64_t start = f.first + block * kFillPieces + (i0 + i) * 256;
+        if (start >= f.end) break;
+        const Piece p = piece_of(start, per_row);
+        // behind the end of the matrix the last row again
+        const int64_t last = (f.end - 1) / per_row;
+        v[i] = load_columns<T, 8>(f.base + min(p.row, last) * f.ldb, Columns<8>(p.col, f.n));
+      }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t start = f.first + block * kFillPieces + (i0 + i) * 256;
+      if (start + threadIdx.x >= f.end) break;
+      const Piece p = piece_of(start, per_row);
+      float x[8] = {};
+      if (f.base) floats<T, 8>(v[i], x);  // and back: exact
+      store_columns<T, 8>(f.dtable + p.row * f.ldd, Columns<8>(p.col, f.n), x);
+    }
   }
 }
 
@@ -211,59 +226,69 @@ struct EmbedSum {
 };
 
 template <typename T>
-__device__ __forceinline__ void embed_write(const EmbedSum<T>& a, uint32_t token, int col,
-                                            const float (&sum)[8]) {
+__device__ __forceinline__ void embed_write(const EmbedSum<T>& a, uint32_t token,
+                                            const Columns<8>& c, const float (&sum)[8]) {
   float v[8] = {};
-  if (a.base) load_row_end<T, 8>(a.base + token * a.ldb + col, a.n - col, v);
+  if (a.base) floats<T, 8>(load_columns<T, 8>(a.base + token * a.ldb, c), v);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = fmaf(sum[i], a.scale, v[i]);
-  store_row<T, 8>(a.dtable + token * a.ldd + col, a.n - col, v);
+  store_columns<T, 8>(a.dtable + token * a.ldd, c, v);
 }
 
 // TX threads, 8 columns each, take a piece of a.each entries; 256 / TX pieces a block.  Eight rows
 // are on their way at a time.
 template <typename T, int TX>
 __global__ __launch_bounds__(256) void k_embed_sum(EmbedSum<T> a, int slabs) {
-  const int piece = (int)(blockIdx.x / slabs) * (256 / TX) + threadIdx.x / TX;
+  // a wave's threads have one piece: its tokens are the wave's, and so are the branches on them
+  auto uniform = [](auto v) {
+    return TX >= 64 ? (decltype(v))__builtin_amdgcn_readfirstlane((int)v) : v;
+  };
+  const int piece = uniform((int)(blockIdx.x / slabs) * (256 / TX) + (int)threadIdx.x / TX);
   const int col = (int)(blockIdx.x % slabs) * (TX * 8) + threadIdx.x % TX * 8;
   if (piece >= a.pieces || col >= a.n) return;
+  const Columns<8> c(col, a.n);
   const int64_t first = (int64_t)piece * a.each, end = min(first + a.each, a.rows);
-  uint32_t token = load_named(a.named + first).token;
-  bool began = first == 0 || load_named(a.named + first - 1).token != token;
-  float sum[8] = {};
   constexpr int kAhead = 8;
-  for (int64_t i0 = first; i0 < end; i0 += kAhead) {
-    Named e[kAhead];
-    float x[kAhead][8];
+  Named e[kAhead];
+  auto names = [&](int64_t i0) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)  // past the end the last one again
-      e[j] = load_named(a.named + min(i0 + j, end - 1));
+    for (int j = 0; j < kAhead; ++j) {  // past the end the last one again
+      const Named v = load_named(a.named + min(i0 + j, end - 1));
+      e[j] = Named{uniform(v.token), uniform(v.at)};
+    }
+  };
+  const uint32_t before = uniform(load_named(a.named + max(first - 1, (int64_t)0)).token);
+  uint32_t token = uniform(load_named(a.named + first).token);
+  bool began = first == 0 || before != token;
+  float sum[8] = {};
+  for (int64_t i0 = first; i0 < end; i0 += kAhead) {
+    Vec<T, 8> x[kAhead];
+    names(i0);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
-      load_row_end<T, 8>(a.dout + (int64_t)e[j].at * a.lddo + col, a.n - col, x[j]);
+      x[j] = load_columns<T, 8>(a.dout + (int64_t)e[j].at * a.lddo, c);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       if (i0 + j >= end) break;
       if (e[j].token != token) {
         if (!began)
-          store_row<float, 8>(a.part + (int64_t)piece * 2 * a.n + col, a.n - col, sum);
+          store_columns<float, 8>(a.part + (int64_t)piece * 2 * a.n, c, sum);
         else if (token < (uint32_t)a.vocab)
-          embed_write(a, token, col, sum);
+          embed_write(a, token, c, sum);
         began = true;
         token = e[j].token;
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum[k] = 0.f;
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sum[k] += x[j][k];
+      for (int k = 0; k < 8; ++k) sum[k] += (float)x[j][k];
     }
   }
-  const bool goes_on = end < a.rows && load_named(a.named + end).token == token;
+  const bool goes_on = end < a.rows && uniform(load_named(a.named + end).token) == token;
   if (!began || goes_on)
-    store_row<float, 8>(a.part + ((int64_t)piece * 2 + (began ? 1 : 0)) * a.n + col, a.n - col,
-                        sum);
+    store_columns<float, 8>(a.part + ((int64_t)piece * 2 + (began ? 1 : 0)) * a.n, c, sum);
   else if (token < (uint32_t)a.vocab)
-    embed_write(a, token, col, sum);
+    embed_write(a, token, c, sum);
 }
 
 // Joins a token that begins in `piece` and goes on behind it: 64 threads take 512 columns, four such
@@ -296,15 +321,15 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSum<T> a, int slabs) {
   }
   const int lane = threadIdx.x & 63, group = threadIdx.x >> 6;
   const int col = (int)(blockIdx.x % slabs) * 512 + lane * 8;
+  const Columns<8> c(min(col, a.n - 1) / 8 * 8, a.n);
   __shared__ float all[3][64][8];
   float sum[8] = {};
   if (col < a.n) {
     if (group == 0)
-      load_row<float, 8>(a.part + ((int64_t)piece * 2 + 1) * a.n + col, a.n - col, sum);
+      floats<float, 8>(load_columns<float, 8>(a.part + ((int64_t)piece * 2 + 1) * a.n, c), sum);
 #pragma unroll 4
     for (int p = piece + 1 + group; p <= last; p += 4) {
-      float x[8];
-      load_row_end<float, 8>(a.part + (int64_t)p * 2 * a.n + col, a.n - col, x);
+      const Vec<float, 8> x = load_columns<float, 8>(a.part + (int64_t)p * 2 * a.n, c);
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[i] += x[i];
     }
@@ -318,7 +343,7 @@ __global__ __launch_bounds__(256) void k_embed_join(EmbedSum<T> a, int slabs) {
   for (int g = 0; g < 3; ++g)
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] += all[g][lane][i];
-  embed_write(a, token, col, sum);
+  embed_write(a, token, c, sum);
 }
 
 }  // namespace lm

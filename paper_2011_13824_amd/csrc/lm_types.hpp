@@ -109,17 +109,18 @@ __device__ __forceinline__ void floats(const Vec<T, N>& v, float (&x)[N]) {
   for (int i = 0; i < N; ++i) x[i] = (float)v[i];
 }
 
-// The 8 columns that thread `id` of a matrix with `per_row` pieces a row takes.  The block's first
+// The 8 (N) columns that thread `id` of a matrix with `per_row` pieces a row takes.  The block's first
 // piece is divided in 64 bits once (uniform), the thread's offset from it in 32.
 struct Piece {
   int64_t row;
   int col;
 };
+template <int N = 8>
 __device__ __forceinline__ Piece piece_of(int64_t first, int per_row) {
   int64_t row0 = first / per_row;
   uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x;
   uint32_t down = at / (uint32_t)per_row;
-  return {row0 + down, (int)(at - down * (uint32_t)per_row) * 8};
+  return {row0 + down, (int)(at - down * (uint32_t)per_row) * N};
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -92,22 +92,28 @@ __device__ __forceinline__ Sums block_sums(Sums s, float scale, Sums* shared) {
   return s;
 }
 
-// What a row's sums say of it; by one thread.
+// The given token's logit, for thread 0: it is on its way while the row is read.
 template <typename T>
-__device__ __forceinline__ float finish_row(const LogProb<T>& a, int64_t row, const Sums& s) {
+__device__ __forceinline__ float given_logit(const LogProb<T>& a, int64_t row, bool& named) {
+  named = false;
+  if (!a.logp || threadIdx.x) return 0.f;
+  const int64_t t = load_global<int64_t>(a.tokens + row);
+  named = t >= 0 && t < a.n;
+  return named ? (float)load_global<T>(a.logits + row * a.ldl + t) : 0.f;
+}
+
+// What a row's sums say of it; by thread 0.
+template <typename T>
+__device__ __forceinline__ float finish_row(const LogProb<T>& a, int64_t row, const Sums& s,
+                                            float given, bool named) {
   const float log_total = logf(s.total);
   if (a.lse) a.lse[row] = fmaf(s.most, a.scale, log_total);
   const bool empty = s.total == 0.f;  // no logit over -inf
   if (a.entropy) a.entropy[row] = empty ? 0.f : log_total - s.moment / s.total;
-  if (a.logp) {
-    const int64_t t = a.tokens[row];
-    float v = 0.f;
-    if (t >= 0 && t < a.n) {
-      const float l = (float)a.logits[row * a.ldl + t];
-      v = empty ? -__builtin_inff() : (l - s.most) * a.scale - log_total;
-    }
-    a.logp[row] = v;
-  }
+  if (a.logp)
+    a.logp[row] = !named  ? 0.f
+                  : empty ? -__builtin_inff()
+                          : (given - s.most) * a.scale - log_total;
   return log_total;
 }
 
@@ -123,76 +129,92 @@ __device__ __forceinline__ void write_top(const LogProb<T>& a, int64_t row, int 
                                        : (key_value(key) - s.most) * a.scale - log_total;
 }
 
-// The number of keys over `key` among `count` in shared memory (0 .. count; keys differ, apart from
-// the zeros that stand for none).
+// The number of keys over `key` among the first `count`, which stand on 16 bytes and whose number is
+// made even by a 0 behind them.
 __device__ __forceinline__ int keys_over(const uint64_t* keys, int count, uint64_t key) {
+  typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
   int over = 0;
 #pragma unroll 8
-  for (int i = 0; i < count; ++i) over += keys[i] > key;
+  for (int i = 0; i < count; i += 2) {
+    const u64x2 k = *(const u64x2*)(keys + i);
+    over += (k[0] > key) + (k[1] > key);
+  }
   return over;
 }
 
 // The `top` largest of the keys that 256 threads hold, in `steps` steps of at most kStepKeys each;
-// best: the thread's largest, 0 for none.  offer(bound, step, put) calls put(key) for the keys of
-// that step that reach the bound; emit(i, key) is called once for every place, with 0 where there is
-// no key.  Where more keys reach the bound than there is room for, they are taken in turns of a few
-// steps, each of which raises the bound.
+// best: the thread's largest, 0 for none.  offer(thread, step, bound, put) calls put(key) for the keys
+// of a thread's step that reach the bound; emit(i, key) is called once for every place, with 0 where
+// there is no key.  The steps of the `top` threads that matter are shared out among all.  Where more
+// keys reach the bound than there is room for, they are taken in turns of a few steps, each of which
+// raises the bound.
 constexpr int kStepKeys = 8, kRoom = 2048;
 struct TopShared {
-  uint64_t best[256], room[kRoom], held[kTop], bound;
-  int count;
+  __attribute__((aligned(16))) uint64_t best[256], room[kRoom + 2], held[kTop], bound;
+  int who[kTop], offers, count;
 };
 template <typename Offer, typename Emit>
 __device__ __forceinline__ void block_top(TopShared& sh, int top, uint64_t best, int steps,
                                           Offer&& offer, Emit&& emit) {
-  if (threadIdx.x == 0) sh.bound = 1, sh.count = 0;  // every key, if fewer threads have one
-  sh.best[threadIdx.x] = best;
+  const int t = threadIdx.x;
+  if (t == 0) sh.bound = 1, sh.count = 0, sh.offers = 0;  // every key, if fewer threads have one
+  sh.best[t] = best;
   __syncthreads();
   const int over = keys_over(sh.best, 256, best);
-  if (best != 0 && over == top - 1) sh.bound = best;
+  if (best != 0 && over < top) {  // keys differ: places do too
+    sh.who[over] = t;
+    atomicMax(&sh.offers, over + 1);
+    if (over == top - 1) sh.bound = best;
+  }
   __syncthreads();
   const uint64_t bound = sh.bound;
-  const bool offers = best != 0 && over < top;
-  if (offers)
-    for (int step = 0; step < steps; ++step)
-      offer(bound, step, [&](uint64_t key) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < kRoom) sh.room[at] = key;
-      });
+  const int offers = sh.offers;
+  // the steps from step0 on, `turn` of them
+  auto all = [&](int step0, int turn, auto&& put) {
+    turn = min(turn, steps - step0);
+    for (int i = t; i < offers * turn; i += 256)
+      offer(sh.who[i / turn], step0 + i % turn, bound, put);
+  };
+  all(0, steps, [&](uint64_t key) {
+    const int at = atomicAdd(&sh.count, 1);
+    if (at < kRoom) sh.room[at] = key;
+  });
   __syncthreads();
   int count = sh.count;
   if (count > kRoom) {  // the first keys that came are dropped, and all are offered again
     constexpr int kTurn = (kRoom - kTop) / (kTop * kStepKeys);
-    if (threadIdx.x < kTop) sh.held[threadIdx.x] = 0;
+    if (t < kTop) sh.held[t] = 0;
     for (int step0 = 0; step0 < steps; step0 += kTurn) {
       __syncthreads();
-      if (threadIdx.x == 0) sh.count = top;
-      if ((int)threadIdx.x < top) sh.room[threadIdx.x] = sh.held[threadIdx.x];
+      if (t == 0) sh.count = top;
+      if (t < top) sh.room[t] = sh.held[t];
       __syncthreads();
       const uint64_t last = sh.room[top - 1];
-      if (offers)
-        for (int step = step0; step < min(step0 + kTurn, steps); ++step)
-          offer(bound, step, [&](uint64_t key) {
-            if (key > last) sh.room[atomicAdd(&sh.count, 1)] = key;
-          });
+      all(step0, kTurn, [&](uint64_t key) {
+        if (key > last) sh.room[atomicAdd(&sh.count, 1)] = key;
+      });
       __syncthreads();
       count = sh.count;
-      for (int i = threadIdx.x; i < count; i += 256) {
+      if (t == 0) sh.room[count] = 0;
+      __syncthreads();
+      for (int i = t; i < count; i += 256) {
         const uint64_t key = sh.room[i];
         const int place = keys_over(sh.room, count, key);
         if (key != 0 && place < top) sh.held[place] = key;
       }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < top; i += 256) emit(i, sh.held[i]);
+    for (int i = t; i < top; i += 256) emit(i, sh.held[i]);
     return;
   }
-  for (int i = threadIdx.x; i < count; i += 256) {
+  if (t == 0) sh.room[count] = 0;
+  __syncthreads();
+  for (int i = t; i < count; i += 256) {
     const uint64_t key = sh.room[i];
     const int place = keys_over(sh.room, count, key);
     if (place < top) emit(place, key);
   }
-  for (int i = count + threadIdx.x; i < top; i += 256) emit(i, (uint64_t)0);
+  for (int i = count + t; i < top; i += 256) emit(i, (uint64_t)0);
 }
 
 // A block takes part blockIdx.x % parts of a row.  TOP: the most likely tokens are wanted.
@@ -205,6 +227,9 @@ __global__ __launch_bounds__(256) void k_logprob(LogProb<T> a) {
   const int first = part * a.part_columns, end = min(first + a.part_columns, a.n);
   const T* l = a.logits + row * a.ldl;
   const float to2 = a.scale * 1.44269504f;  // powers of two from here on, joined in powers of e
+  const bool whole = a.parts == 1;
+  bool named = false;
+  const float given = whole ? given_logit(a, row, named) : 0.f;
   Sums s = no_sums();
   int best_at = -1;
   float best_value = -__builtin_inff();
@@ -255,11 +280,10 @@ __global__ __launch_bounds__(256) void k_logprob(LogProb<T> a) {
   }
   s.moment *= 0.693147181f;
   s = block_sums(s, a.scale, shared);
-  const bool whole = a.parts == 1;
   float log_total = 0.f;
   if (threadIdx.x == 0) {
     if (whole)
-      log_total = finish_row(a, row, s);
+      log_total = finish_row(a, row, s, given, named);
     else
       a.part_sums[row * a.parts + part] = s;
   }
@@ -269,8 +293,8 @@ __global__ __launch_bounds__(256) void k_logprob(LogProb<T> a) {
     block_top(
         top, a.top, best_at < 0 ? 0 : rank_key(best_value, best_at),
         (end - first + kStep - 1) / kStep,
-        [&](uint64_t bound, int step, auto&& put) {
-          const int c = first + step * kStep + threadIdx.x * 8;
+        [&](int thread, int step, uint64_t bound, auto&& put) {
+          const int c = first + step * kStep + thread * 8;
           float v[8];
           load_row_end<T, 8>(l + min(c, end - 1), end - c, v);
 #pragma unroll
@@ -293,21 +317,23 @@ __global__ __launch_bounds__(256) void k_logprob_join(LogProb<T> a) {
   __shared__ Sums shared[4];
   __shared__ float row_log, row_most, row_total;
   const int64_t row = blockIdx.x;
+  bool named;
+  const float given = given_logit(a, row, named);
   Sums s = no_sums();
   if ((int)threadIdx.x < a.parts) s = a.part_sums[row * a.parts + threadIdx.x];
   s = block_sums(s, a.scale, shared);
   if (threadIdx.x == 0) {
-    row_log = finish_row(a, row, s);
+    row_log = finish_row(a, row, s, given, named);
     row_most = s.most;
     row_total = s.total;
   }
   if constexpr (TOP) {
     __shared__ TopShared top;
-    const uint64_t* keys = a.part_keys + (row * a.parts + threadIdx.x) * a.top;
+    const uint64_t* keys = a.part_keys + row * a.parts * a.top;  // a thread's are a part's
     block_top(
-        top, a.top, (int)threadIdx.x < a.parts ? keys[0] : 0, a.top,
-        [&](uint64_t bound, int step, auto&& put) {
-          const uint64_t key = keys[step];
+        top, a.top, (int)threadIdx.x < a.parts ? keys[threadIdx.x * a.top] : 0, a.top,
+        [&](int thread, int step, uint64_t bound, auto&& put) {
+          const uint64_t key = keys[thread * a.top + step];
           if (key >= bound && key != 0) put(key);
         },
         [&](int i, uint64_t key) {

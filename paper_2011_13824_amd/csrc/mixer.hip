@@ -62,24 +62,25 @@ int by_taps(int taps, F&& f) {
   }
 }
 
-int64_t pieces8(int n) { return (n + 7) / 8; }
+int64_t pieces(int n, int wide) { return (n + wide - 1) / wide; }
 
-// Rows of a strip: as many as leave 2^18 threads, and no more than `most`.
-int conv_strip(int64_t rows, int n, int most) {
-  const int64_t each = rows * pieces8(n) >> 18;
-  return (int)std::clamp<int64_t>(up(each, 4), 4, most);
+// Rows of a strip, at least `least`: with those in front of it and, in the gradient, behind it (`more`)
+// a multiple of what is on its way at a time; the fewest of some sizes that leave no more than
+// kConvThreads threads.
+constexpr int64_t kConvThreads = (int64_t)1 << 18;
+constexpr int kConvLeast = 4, kConvBackLeast = 8;  // a strip of the gradient writes a part of dw
+int conv_strip(int64_t rows, int n, int wide, int ahead, int more, int least) {
+  int strip = 0;
+  for (int m : {2, 3, 4, 5, 6, 8}) {
+    strip = m * ahead - more;
+    if (strip >= least && (rows + strip - 1) / strip * pieces(n, wide) <= kConvThreads) break;
+  }
+  return strip;
 }
-constexpr int kStripFwd = 16, kStripBwd = 32;
 
-int64_t conv_strips(int64_t rows, int n) {
-  const int strip = conv_strip(rows, n, kStripBwd);
-  return (rows + strip - 1) / strip;
-}
-
-// At most this many strips for up to `rows` rows: it does not fall as rows grow.
+// For any type and up to `rows` rows: it does not fall as rows grow.
 size_t conv_bytes(int64_t rows, int n, int taps) {
-  const int64_t few = ((int64_t)1 << 18) / pieces8(n) + 1;
-  const int64_t strips = std::min((rows + 3) / 4, few) + (rows + kStripBwd - 1) / kStripBwd;
+  const int64_t strips = (rows + kConvBackLeast - 1) / kConvBackLeast;
   return std::max<size_t>(256, (size_t)strips * (taps + 1) * n * sizeof(float));
 }
 
@@ -304,10 +305,11 @@ int lirpa_conv_forward(int dtype, int64_t rows, int n, int taps, const void* x, 
       a.state_out = (T*)state_out;
       a.y = (T*)y;
       a.ldy = ldy;
-      a.strip = conv_strip(rows, n, kStripFwd);
+      constexpr int wide = kConvWide<T>;
+      a.strip = conv_strip(rows, n, wide, kConvAhead, taps - 1, kConvLeast);
       const int64_t strips = (rows + a.strip - 1) / a.strip;
-      const int64_t blocks = (strips * pieces8(n) + 255) / 256;
-      const int64_t slabs = (pieces8(n) + 255) / 256, ends = (rows + 63) / 64 * slabs;
+      const int64_t blocks = (strips * pieces(n, wide) + 255) / 256;
+      const int64_t slabs = (pieces(n, wide) + 255) / 256, ends = (rows + 63) / 64 * slabs;
       if (std::max(blocks, ends) > max_blocks(256)) return too_large(who);
       return by_taps(taps, [&](auto k) {
         TRY(launch_k("conv_forward", stream, [&] {
@@ -340,7 +342,7 @@ int lirpa_conv_step(int dtype, int64_t rows, int n, int taps, const void* x, int
       a.state_out = (T*)state_out;
       a.y = (T*)y;
       a.ldy = ldy;
-      const int64_t blocks = (rows * pieces8(n) + 255) / 256;
+      const int64_t blocks = (rows * pieces(n, kConvWide<T>) + 255) / 256;
       if (blocks > max_blocks(256)) return too_large(who);
       return by_taps(taps, [&](auto k) {
         return launch_k("conv_step", stream, [&] {
@@ -379,10 +381,12 @@ int lirpa_conv_backward(int dtype, int64_t rows, int n, int taps, const void* dy
       a.lddy = lddy;
       a.dx = (T*)dx;
       a.lddx = lddx;
-      a.strip = conv_strip(rows, n, kStripBwd);
+      constexpr int wide = kConvBackWide<T>;
+      a.strip = conv_strip(rows, n, wide, kConvAhead, 2 * (taps - 1),
+                           kConvBackLeast);
       a.part = (float*)ws;
-      const int64_t strips = conv_strips(rows, n), ld = (int64_t)(taps + 1) * n;
-      const int64_t blocks = (strips * pieces8(n) + 255) / 256;
+      const int64_t strips = (rows + a.strip - 1) / a.strip, ld = (int64_t)(taps + 1) * n;
+      const int64_t blocks = (strips * pieces(n, wide) + 255) / 256;
       if (blocks > max_blocks(256)) return too_large(who);
       if (rows > 0)
         TRY(by_taps(taps, [&](auto k) {
@@ -390,14 +394,10 @@ int lirpa_conv_backward(int dtype, int64_t rows, int n, int taps, const void* dy
             k_conv_bwd<T, k.value><<<(unsigned)blocks, 256, 0, stream>>>(a);
           });
         }));
-      TRY(launch_k("conv_dw", stream, [&] {
-        k_sum_parts<T><<<(unsigned)(((int64_t)taps * n + 31) / 32), 256, 0, stream>>>(
-            a.part, strips, ld, (int64_t)taps * n, (T*)dw);
-      }));
-      if (!dbias) return (int)LIRPA_OK;
       return launch_k("conv_dw", stream, [&] {
-        k_sum_parts<T><<<(unsigned)((n + 31) / 32), 256, 0, stream>>>(
-            a.part + (int64_t)taps * n, strips, ld, n, (T*)dbias);
+        const int64_t values = dbias ? ld : (int64_t)taps * n;
+        k_sum_parts<T><<<(unsigned)((values + 31) / 32), 256, 0, stream>>>(
+            a.part, strips, ld, values, (int64_t)taps * n, (T*)dw, (T*)dbias);
       });
     });
   });

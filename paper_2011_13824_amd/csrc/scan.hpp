@@ -129,28 +129,32 @@ struct ScanNext {
   T B[kEach], C[kEach];
   int slot[3];  // of the row, the one before and the one behind; by the first threads
 
-  // What: 1 u and dt, 2 z, 4 dy, 8 B, 16 C, 32 slots.
+  // WHAT: 1 u and dt, 2 z, 4 dy, 8 B, 16 C, 32 slots.  The step's first row is the block's, so that a
+  // thread's place in it is a 32-bit offset.  Rows behind the last are the last, steps in front of
+  // the first the first.
   template <int WHAT>
-  __device__ __forceinline__ void read(const Scan<T>& a, const ScanPlace<LANES>& at, int64_t t0) {
-    const int64_t t = min(max(t0, (int64_t)0) + at.own_row, a.s.rows - 1);
+  __device__ __forceinline__ void read(const Scan<T>& a, const ScanPlace<LANES>& at, int64_t t) {
+    const int64_t t0 = min(max(t, (int64_t)0), a.s.rows - 1);
+    const int most = (int)min(a.s.rows - 1 - t0, (int64_t)(kSpan - 1));
+    const int r = min(at.own_row, most);
+    auto place = [](int row, int64_t ld) { return __umul24(row, (int)ld); };  // under 2^4, 2^22
     if constexpr (WHAT & 1) {
-      u = load_columns<T, W>(a.u + t * a.ldu, at.own);
-      dt = load_columns<T, W>(a.dt + t * a.lddt, at.own);
+      u = load_columns<T, W>(a.u + t0 * a.ldu + place(r, a.ldu), at.own);
+      dt = load_columns<T, W>(a.dt + t0 * a.lddt + place(r, a.lddt), at.own);
     }
     if constexpr (WHAT & 2)
-      if (a.z) z = load_columns<T, W>(a.z + t * a.ldz, at.own);
-    if constexpr (WHAT & 4) dy = load_columns<T, W>(a.dy + t * a.lddy, at.own);
+      if (a.z) z = load_columns<T, W>(a.z + t0 * a.ldz + place(r, a.ldz), at.own);
+    if constexpr (WHAT & 4) dy = load_columns<T, W>(a.dy + t0 * a.lddy + place(r, a.lddy), at.own);
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int i = e * 256 + threadIdx.x;
-      const int64_t row = min(max(t0, (int64_t)0) + i / (4 * LANES), a.s.rows - 1);
-      const int k = min(i % (4 * LANES), a.states - 1);
-      if constexpr (WHAT & 8) B[e] = load_global<T>(a.B + row * a.ldB + k);
-      if constexpr (WHAT & 16) C[e] = load_global<T>(a.C + row * a.ldC + k);
+      const int row = min(i / (4 * LANES), most), k = min(i % (4 * LANES), a.states - 1);
+      if constexpr (WHAT & 8) B[e] = load_global<T>(a.B + t0 * a.ldB + place(row, a.ldB) + k);
+      if constexpr (WHAT & 16) C[e] = load_global<T>(a.C + t0 * a.ldC + place(row, a.ldC) + k);
     }
     if constexpr (WHAT & 32)
       if (threadIdx.x < kSpan) {
-        const int64_t row = t0 + threadIdx.x;
+        const int64_t row = t + threadIdx.x;
         slot[0] = a.s.slot(row);
         slot[1] = a.s.slot(row - 1);
         slot[2] = a.s.slot(row + 1);
@@ -186,14 +190,40 @@ struct ScanNext {
 
   __device__ __forceinline__ void put_steps(const ScanPlace<LANES>& at, const float (&bias)[W],
                                             ScanShared<LANES>& sh) const {
+    float sum[W];
+    put_steps(at, bias, sh, false, sum);
+  }
+  // `counts`: the steps are added to sum.
+  __device__ __forceinline__ void put_steps(const ScanPlace<LANES>& at, const float (&bias)[W],
+                                            ScanShared<LANES>& sh, bool counts,
+                                            float (&sum)[W]) const {
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       float v;
       const float delta = softplus((float)dt[i] + bias[i], v);
       sh.step[at.own_row][at.own_slot + i] = make_float2(delta, delta * (float)u[i]);
+      if (counts) sum[i] += delta;
     }
   }
 };
+
+// The sums of delta over a chunk, from those of the 16 rows of its steps, in order.
+template <typename T, int LANES>
+__device__ __forceinline__ void put_deltas(const Scan<T>& a, const ScanPlace<LANES>& at, int chunk,
+                                           int group, const float (&sum)[ScanPlace<LANES>::kWide],
+                                           ScanShared<LANES>& sh) {
+  constexpr int W = ScanPlace<LANES>::kWide, kColumns = ScanPlace<LANES>::kColumns;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < W; ++i) sh.step[at.own_row][at.own_slot + i].x = sum[i];
+  __syncthreads();
+  const int col = group * kColumns + (int)threadIdx.x;
+  if (threadIdx.x >= kColumns || col >= a.n) return;
+  float d = 0.f;
+#pragma unroll
+  for (int r = 0; r < kSpan; ++r) d += sh.step[r][W + threadIdx.x].x;
+  a.deltas[(int64_t)chunk * a.n + col] = d;
+}
 
 // Floats of the thread's own columns, 0 without p.
 template <int LANES>
@@ -273,24 +303,20 @@ __global__ __launch_bounds__(256) void k_scan_local(Scan<T> a, int groups) {
     load_states(a.state + (int64_t)slot * a.n * a.states, at.col, at.lane, a.states, a.n, h);
     store_padded<LANES>(a.begin, chunk, a.n, at.col, at.lane, h);
   }
-  float sum = 0.f;
+  float sum[W] = {};
   const int64_t start = first + max(from, 0);
   int64_t t0 = start / kSpan * kSpan;
   const int column = W + (int)threadIdx.x / LANES;
   ScanNext<T, LANES> next;
   next.template read<1 | 8>(a, at, t0);
   for (; t0 < end; t0 += kSpan) {
+    const int skip = (int)max((int64_t)0, start - t0);
     __syncthreads();
-    next.put_steps(at, bias, sh);
+    next.put_steps(at, bias, sh, at.own_row >= skip, sum);
     next.put(a, next.B, sh.B);
     __syncthreads();
     next.template read<1 | 8>(a, at, t0 + kSpan);
-    const int skip = (int)max((int64_t)0, start - t0);
-    auto row = [&](int r) {
-      const float2 step = sh.step[r][column];
-      sum += step.x;
-      advance(h, step, A2, sh.B[r] + at.lane * 4);
-    };
+    auto row = [&](int r) { advance(h, sh.step[r][column], A2, sh.B[r] + at.lane * 4); };
     if (skip == 0) {
 #pragma unroll
       for (int r = 0; r < kSpan; ++r) row(r);
@@ -299,7 +325,7 @@ __global__ __launch_bounds__(256) void k_scan_local(Scan<T> a, int groups) {
     }
   }
   store_padded<LANES>(a.local, chunk, a.n, at.col, at.lane, h);
-  if (at.lane == 0 && at.col < a.n) a.deltas[(int64_t)chunk * a.n + at.col] = sum;
+  put_deltas(a, at, chunk, group, sum, sh);
 }
 
 // The states that enter the chunks, in the place of what the chunks add: that of chunk c + 1 stands
@@ -493,7 +519,7 @@ __global__ __launch_bounds__(256) void k_scan_back_local(Scan<T> a, int groups) 
   if (!goes_on) return;
   const int64_t stop = whole ? end : first + ends + 1;  // behind the sequence's last row here
   const int column = W + (int)threadIdx.x / LANES;
-  float A[4], A2[4], g[4] = {}, bias[W], sum = 0.f;
+  float A[4], A2[4], g[4] = {}, bias[W], sum[W] = {};
   load_A(a, at.col, at.lane, A, A2);
   own_floats<LANES>(a.bias, at, bias);
   int64_t t0 = (stop - 1) / kSpan * kSpan;
@@ -502,18 +528,17 @@ __global__ __launch_bounds__(256) void k_scan_back_local(Scan<T> a, int groups) 
   for (; t0 >= first; t0 -= kSpan) {
     float p[W], q[W];
     scan_gate<T, W>(a.z, next.dy, next.z, p, q);
+    const int rows = (int)min((int64_t)kSpan, stop - t0);
     __syncthreads();
-    next.put_steps(at, bias, sh);
+    next.put_steps(at, bias, sh, at.own_row < rows, sum);
     next.put(a, next.C, sh.C);
 #pragma unroll
     for (int i = 0; i < W; ++i) shp[at.own_row][at.own_slot + i] = p[i];
     __syncthreads();
     next.template read<1 | 2 | 4 | 16>(a, at, t0 - kSpan);
-    const int rows = (int)min((int64_t)kSpan, stop - t0);
     auto row = [&](int r) {
       const float delta = sh.step[r][column].x, pr = shp[r][column];
       const f32x4 c = *(const f32x4*)(sh.C[r] + at.lane * 4);
-      sum += delta;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         g[i] = __builtin_amdgcn_exp2f(delta * A2[i]) * fmaf(c[i], pr, g[i]);
@@ -526,7 +551,7 @@ __global__ __launch_bounds__(256) void k_scan_back_local(Scan<T> a, int groups) 
     }
   }
   store_padded<LANES>(a.local, chunk, a.n, at.col, at.lane, g);
-  if (at.lane == 0 && at.col < a.n) a.deltas[(int64_t)chunk * a.n + at.col] = sum;
+  put_deltas(a, at, chunk, group, sum, sh);
 }
 
 // Sums of 8 values over the lanes of a wave that hold the same states of its columns: halves of the
@@ -603,73 +628,78 @@ __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
     __syncthreads();
     next.template read<1 | 2 | 4 | 8 | 16 | 32>(a, at, t0 - kSpan);
     load_padded<LANES>(a.kept, max(t0 / kSpan - 1, (int64_t)0), a.n, at.col, at.lane, kept);
-    const bool plain = sh.plain;
-#pragma unroll
-    for (int r = 0; r < kHalf; ++r) {
-      if (!plain && sh.flags[r] & kBegins)
-        half_state[1][0] = half_state[1][1] = half_state[1][2] = half_state[1][3] = 0.f;
-      advance(half_state[1], sh.step[r][column], A2, sh.B[r] + at.lane * 4);
-    }
-#pragma unroll 1
-    for (int half = 1; half >= 0; --half) {
-      const int row0 = half * kHalf;
-      float h[kHalf + 1][4], e[kHalf][4];  // the state in front of the half and behind its rows
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[0][i] = half ? half_state[1][i] : half_state[0][i];
+    auto walk = [&](auto plain) {
 #pragma unroll
       for (int r = 0; r < kHalf; ++r) {
-        const float2 step = sh.step[row0 + r][column];
-        const f32x4 b = *(const f32x4*)(sh.B[row0 + r] + at.lane * 4);
-        // what is left of the state in front of a sequence's first row: nothing
-        const bool begins = !plain && sh.flags[row0 + r] & kBegins;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          e[r][i] = begins ? 0.f : __builtin_amdgcn_exp2f(step.x * A2[i]);
-          h[r + 1][i] = fmaf(e[r][i], begins ? 0.f : h[r][i], step.y * b[i]);
-        }
+        if (!plain.value && sh.flags[r] & kBegins)
+          half_state[1][0] = half_state[1][1] = half_state[1][2] = half_state[1][3] = 0.f;
+        advance(half_state[1], sh.step[r][column], A2, sh.B[r] + at.lane * 4);
       }
+#pragma unroll 1
+      for (int half = 1; half >= 0; --half) {
+        const int row0 = half * kHalf;
+        float h[kHalf + 1][4], e[kHalf][4];  // the state in front of the half and behind its rows
 #pragma unroll
-      for (int r = kHalf - 1; r >= 0; --r) {
-        const int flags = plain ? kInside : sh.flags[row0 + r];
-        float cs = 0.f, bs = 0.f, es = 0.f, out[8] = {};
-        if (flags & kInside) {
+        for (int i = 0; i < 4; ++i) h[0][i] = half ? half_state[1][i] : half_state[0][i];
+#pragma unroll
+        for (int r = 0; r < kHalf; ++r) {
           const float2 step = sh.step[row0 + r][column];
-          const float pr = shp[row0 + r][column];
           const f32x4 b = *(const f32x4*)(sh.B[row0 + r] + at.lane * 4);
-          const f32x4 c = *(const f32x4*)(sh.C[row0 + r] + at.lane * 4);
-          const bool begins = flags & kBegins;
-          if (flags & kEnds) g[0] = g[1] = g[2] = g[3] = 0.f;
+          // what is left of the state in front of a sequence's first row: nothing
+          const bool begins = !plain.value && sh.flags[row0 + r] & kBegins;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            g[i] = fmaf(c[i], pr, g[i]);
-            cs = fmaf(c[i], h[r + 1][i], cs);
-            out[i] = g[i] * step.y;
-            out[4 + i] = pr * h[r + 1][i];
-            bs = fmaf(g[i], b[i], bs);
-            g[i] *= e[r][i];
-            const float t = begins ? 0.f : g[i] * h[r][i];
-            es = fmaf(t, A[i], es);
-            dA[i] = fmaf(t, step.x, dA[i]);
+            e[r][i] = begins ? 0.f : __builtin_amdgcn_exp2f(step.x * A2[i]);
+            h[r + 1][i] = fmaf(e[r][i], begins ? 0.f : h[r][i], step.y * b[i]);
           }
-          if (at.col >= a.n)  // columns past the matrix have no part in the sums over columns
-#pragma unroll
-            for (int i = 0; i < 8; ++i) out[i] = 0.f;
         }
-        cs = column_sum<LANES>(cs);
-        bs = column_sum<LANES>(bs);
-        es = column_sum<LANES>(es);
-        if (at.lane == 0) sums[row0 + r][column] = f32x4{cs, bs, es, 0.f};
-        float two[2];
-        wave_sums<LANES>(out, two);
-        if (lane % 16 < LANES) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int value = lane / 16 * 2 + i;
-            dBC[wave][row0 + r][value / 4][at.lane * 4 + value % 4] = two[i];
+        for (int r = kHalf - 1; r >= 0; --r) {
+          const int flags = plain.value ? kInside : sh.flags[row0 + r];
+          float cs = 0.f, bs = 0.f, es = 0.f, out[8] = {};
+          if (flags & kInside) {
+            const float2 step = sh.step[row0 + r][column];
+            const float pr = shp[row0 + r][column];
+            const f32x4 b = *(const f32x4*)(sh.B[row0 + r] + at.lane * 4);
+            const f32x4 c = *(const f32x4*)(sh.C[row0 + r] + at.lane * 4);
+            const bool begins = flags & kBegins;
+            if (flags & kEnds) g[0] = g[1] = g[2] = g[3] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              g[i] = fmaf(c[i], pr, g[i]);
+              cs = fmaf(c[i], h[r + 1][i], cs);
+              out[i] = g[i] * step.y;
+              out[4 + i] = pr * h[r + 1][i];
+              bs = fmaf(g[i], b[i], bs);
+              g[i] *= e[r][i];
+              const float t = begins ? 0.f : g[i] * h[r][i];
+              es = fmaf(t, A[i], es);
+              dA[i] = fmaf(t, step.x, dA[i]);
+            }
+            if (at.col >= a.n)  // columns past the matrix have no part in the sums over columns
+#pragma unroll
+              for (int i = 0; i < 8; ++i) out[i] = 0.f;
+          }
+          cs = column_sum<LANES>(cs);
+          bs = column_sum<LANES>(bs);
+          es = column_sum<LANES>(es);
+          if (at.lane == 0) sums[row0 + r][column] = f32x4{cs, bs, es, 0.f};
+          float two[2];
+          wave_sums<LANES>(out, two);
+          if (lane % 16 < LANES) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int value = lane / 16 * 2 + i;
+              dBC[wave][row0 + r][value / 4][at.lane * 4 + value % 4] = two[i];
+            }
           }
         }
       }
-    }
+    };
+    if (sh.plain)
+      walk(std::true_type{});
+    else
+      walk(std::false_type{});
     __syncthreads();
     for (int i = threadIdx.x; i < kSpan * 2 * kStates; i += 256) {
       const int r = i / (2 * kStates), k = i % (2 * kStates);

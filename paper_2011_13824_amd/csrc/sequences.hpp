@@ -28,12 +28,14 @@ __device__ __forceinline__ float sigmoid(float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f));
 }
 
-// out[i] = sum over b of part[b][i], b < blocks, rows ld apart: a block takes 32 columns, each of
-// its 32 groups of 8 threads every 32nd row, eight of them on their way at a time; the groups' sums
-// are joined in order.  Bound by the latency of a few loads.
+// out[i] = sum over b of part[b][i], b < blocks, rows ld apart; from column `split` on they are
+// other's.  A block takes 32 columns, each of its 32 groups of 8 threads every 32nd row, eight of
+// them on their way at a time; the groups' sums are joined in order.  Bound by the latency of a few
+// loads.
 template <typename T>
 __global__ __launch_bounds__(256) void k_sum_parts(const float* __restrict__ part, int64_t blocks,
-                                                   int64_t ld, int64_t n, T* __restrict__ out) {
+                                                   int64_t ld, int64_t n, int64_t split,
+                                                   T* __restrict__ out, T* __restrict__ other) {
   __shared__ float all[32][33];
   const int c = threadIdx.x & 7, g = threadIdx.x >> 3;
   const int64_t col = (int64_t)blockIdx.x * 32 + c * 4;
@@ -63,7 +65,7 @@ __global__ __launch_bounds__(256) void k_sum_parts(const float* __restrict__ par
   float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) sum += all[i][threadIdx.x];
-  out[at] = (T)sum;
+  (at < split ? out : other - split)[at] = (T)sum;
 }
 
 }  // namespace lm
