@@ -81,7 +81,7 @@ template <int LANES>
 __device__ __forceinline__ float column_sum(float v) {
   auto dpp = [](float x, auto ctrl) {
     return __int_as_float(
-        __builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl.value, 0xf, 0xf, true));
+        __builtin_amdgcn_mov_dpp(__float_as_int(x), ctrl.value, 0xf, 0xf, true));
   };
   v += dpp(v, std::integral_constant<int, 0xb1>{});  // quad_perm 1 0 3 2
   if constexpr (LANES > 2) v += dpp(v, std::integral_constant<int, 0x4e>{});   // 2 3 0 1
@@ -201,7 +201,8 @@ struct ScanNext {
     for (int i = 0; i < W; ++i) {
       float v;
       const float delta = softplus((float)dt[i] + bias[i], v);
-      sh.step[at.own_row][at.own_slot + i] = make_float2(delta, delta * (float)u[i]);
+      if (i < at.own.count)
+        sh.step[at.own_row][at.own_slot + i] = make_float2(delta, delta * (float)u[i]);
       if (counts) sum[i] += delta;
     }
   }
@@ -533,7 +534,8 @@ __global__ __launch_bounds__(256) void k_scan_back_local(Scan<T> a, int groups) 
     next.put_steps(at, bias, sh, at.own_row < rows, sum);
     next.put(a, next.C, sh.C);
 #pragma unroll
-    for (int i = 0; i < W; ++i) shp[at.own_row][at.own_slot + i] = p[i];
+    for (int i = 0; i < W; ++i)
+      if (i < at.own.count) shp[at.own_row][at.own_slot + i] = p[i];
     __syncthreads();
     next.template read<1 | 2 | 4 | 16>(a, at, t0 - kSpan);
     auto row = [&](int r) {
@@ -574,7 +576,7 @@ __device__ __forceinline__ void wave_sums(const float (&v)[8], float (&out)[2]) 
   }
   auto ror = [](float x, auto ctrl) {
     return __int_as_float(
-        __builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl.value, 0xf, 0xf, true));
+        __builtin_amdgcn_mov_dpp(__float_as_int(x), ctrl.value, 0xf, 0xf, true));
   };
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -607,6 +609,12 @@ __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
   // g: e^(delta A) g of the row behind
   if (chunk + 1 < a.chunks && a.links[chunk + 1] & kGoesOn)
     load_padded<LANES>(a.local, chunk + 1, a.n, at.col, at.lane, g);
+  // Columns past the matrix have no part in the sums over columns: their delta u and p stay 0.
+  for (int i = threadIdx.x; i < kSpan * kColumns; i += 256) {
+    sh.step[0][i] = make_float2(0.f, 0.f);
+    shp[0][i] = 0.f;
+  }
+  __syncthreads();
   int64_t t0 = (end - 1) / kSpan * kSpan;
   ScanNext<T, LANES> next;
   next.template read<1 | 2 | 4 | 8 | 16 | 32>(a, at, t0);
@@ -622,7 +630,8 @@ __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
     next.put(a, next.C, sh.C);
     next.put_rows(a, t0, sh);
 #pragma unroll
-    for (int i = 0; i < W; ++i) shp[at.own_row][at.own_slot + i] = p[i];
+    for (int i = 0; i < W; ++i)
+      if (i < at.own.count) shp[at.own_row][at.own_slot + i] = p[i];
 #pragma unroll
     for (int i = 0; i < 4; ++i) half_state[0][i] = half_state[1][i] = kept[i];
     __syncthreads();
@@ -676,9 +685,6 @@ __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
               es = fmaf(t, A[i], es);
               dA[i] = fmaf(t, step.x, dA[i]);
             }
-            if (at.col >= a.n)  // columns past the matrix have no part in the sums over columns
-#pragma unroll
-              for (int i = 0; i < 8; ++i) out[i] = 0.f;
           }
           cs = column_sum<LANES>(cs);
           bs = column_sum<LANES>(bs);
