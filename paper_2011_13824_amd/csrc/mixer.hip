@@ -142,7 +142,7 @@ int64_t scan_groups(int n, int states) {
 }
 
 // Rows are cut into chunks of at least kChunkLeast, until there are kScanBlocks blocks.
-constexpr int kChunkLeast = 64, kScanBlocks = 1024;
+constexpr int kChunkLeast = 64, kScanBlocks = 2048;
 int64_t scan_most_chunks(int n, int states) {
   const int64_t groups = scan_groups(n, states);
   return std::max<int64_t>(1, (kScanBlocks + groups - 1) / groups);

@@ -338,20 +338,30 @@ __global__ __launch_bounds__(256) void k_scan_link(Scan<T> a) {
   if (col >= a.n) return;
   float A[4], A2[4], h[4] = {};
   load_A(a, col, lane, A, A2);
-  for (int i = 0; i + 1 < a.chunks; ++i) {
-    const int c = BACK ? a.chunks - 1 - i : i;
-    const int link = a.links[c];
-    if (!(link & kGoesOn)) {
-      h[0] = h[1] = h[2] = h[3] = 0.f;
-      continue;
-    }
-    float add[4];
-    load_padded<LANES>(a.local, c, a.n, col, lane, add);
-    const float sum = a.deltas[(int64_t)c * a.n + col];
+  constexpr int kAhead = 8;  // chunks whose values are on their way at a time
+  for (int i0 = 0; i0 + 1 < a.chunks; i0 += kAhead) {
+    float add[kAhead][4], sum[kAhead];
+    int link[kAhead];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      h[k] = link & kWhole ? fmaf(__builtin_amdgcn_exp2f(sum * A2[k]), h[k], add[k]) : add[k];
-    store_padded<LANES>(a.local, c, a.n, col, lane, h);
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = min(i0 + j, a.chunks - 2), c = BACK ? a.chunks - 1 - i : i;
+      link[j] = load_global<int>(a.links + c);
+      load_padded<LANES>(a.local, c, a.n, col, lane, add[j]);
+      sum[j] = load_global<float>(a.deltas + (int64_t)c * a.n + col);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (i0 + j + 1 >= a.chunks) break;
+      const int c = BACK ? a.chunks - 1 - (i0 + j) : i0 + j;
+      const bool goes_on = link[j] & kGoesOn, whole = link[j] & kWhole;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // what a chunk without a link holds was never written
+        const float left = whole ? __builtin_amdgcn_exp2f(sum[j] * A2[k]) * h[k] : 0.f;
+        h[k] = goes_on ? left + add[j][k] : 0.f;
+      }
+      if (goes_on) store_padded<LANES>(a.local, c, a.n, col, lane, h);
+    }
   }
 }
 
