@@ -342,13 +342,13 @@ class Embedding:
         _no_tape(table)
         vocab, n = lirpa._2d(table, "table")
         dt, code = _type(table, "table")
-        lirpa._here(table, "table")
+        stream = lirpa._here(None, table, tokens)
         p, ld = _matrix(table, vocab, n, dt, "table")
         rows = len(tokens)
         ptok = lirpa._tokens(tokens, rows)
         out = torch.empty((rows, n), dtype=dt, device=table.device)
         _check(load().lirpa_embed_forward(code, rows, n, vocab, ptok, p, ld, self.scale,
-                                          out.data_ptr(), n, _stream(None)))
+                                          out.data_ptr(), n, stream))
         return out
 
     def backward(self, tokens, dout, base=None, out=None):
@@ -382,14 +382,14 @@ class LogProbs:
         rows, n = lirpa._2d(logits, "logits")
         dt, code = _type(logits, "logits")
         _no_tape(logits)
-        lirpa._here(logits, "logits")
+        stream = lirpa._here(None, logits, tokens)
         p, ld = _matrix(logits, rows, n, dt, "logits")
         ptok = lirpa._tokens(tokens, rows)
         top = self.top
         own = torch.empty((2 if tokens is None else 3, rows), dtype=torch.float32,
                           device=logits.device)
-        lse, entropy = own[0], own[1]
-        logp = None if tokens is None else own[2]
+        lse, entropy, *logp = own.unbind(0)
+        logp = logp[0] if logp else None
         top_logp = top_tokens = None
         if top:
             top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device)
@@ -399,7 +399,7 @@ class LogProbs:
         _check(load().lirpa_logprob_forward(
             code, rows, n, p, ld, self.scale, ptok, None if logp is None else logp.data_ptr(),
             lse.data_ptr(), entropy.data_ptr(), top, top_logp.data_ptr() if top else None,
-            top_tokens.data_ptr() if top else None, ws.data_ptr(), need, _stream(None)))
+            top_tokens.data_ptr() if top else None, ws.data_ptr(), need, stream))
         return LogP(logp, lse, entropy, top_logp, top_tokens)
 
     def backward(self, logits, tokens, lse, entropy=None, dlogp=None, dentropy=None, out=None):

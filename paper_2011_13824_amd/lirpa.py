@@ -508,11 +508,24 @@ def lirpa_ffn_backward(ffn, dout, keep, x, g, u, dx, dWg, dWu, dWd, ws, ws_bytes
         int(ws_bytes), _stream(stream)))
 
 
-def _here(t, what):
-    """Refuses a tensor of another device than the current one, whose stream the calls run on."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what} lies on {t.device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
+_TORCH_TYPES = {code: t for t, code in DTYPES.items()}
+
+
+def _here(stream, *tensors):
+    """The stream's handle (None: torch's current one).  Refuses tensors of another device than the
+    current one, whose streams the calls run on; what is no CUDA tensor is refused where its pointer
+    is taken."""
+    device = -1
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            if device < 0:
+                device = torch._C._cuda_getDevice()
+            if t.get_device() != device:
+                raise ValueError(f"a tensor lies on {t.device}, the current device is "
+                                 f"cuda:{device}")
+    if stream is not None or device < 0:
+        return None if stream is None else _stream(stream)
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _2d(t, what):
@@ -533,10 +546,10 @@ def lirpa_embed_forward(tokens, table, scale, out, stream=None):
     vocab, n = _2d(table, "table")
     rows = _2d(out, "out")[0]
     dt = _dtype(table, "table")
-    _here(table, "table")
+    st = _here(stream, tokens, table, out)
     _check(load().lirpa_embed_forward(
         DTYPES[dt], rows, n, vocab, _tokens(tokens, rows), *_matrix(table, vocab, n, dt, "table"),
-        float(scale), *_matrix(out, rows, n, dt, "out"), _stream(stream)))
+        float(scale), *_matrix(out, rows, n, dt, "out"), st))
 
 
 def lirpa_embed_workspace_bytes(rows, n) -> int:
@@ -547,12 +560,12 @@ def lirpa_embed_backward(tokens, dout, scale, base, dtable, ws, ws_bytes, stream
     rows, n = _2d(dout, "dout")
     vocab = _2d(dtable, "dtable")[0]
     dt = _dtype(dout, "dout")
-    _here(dout, "dout")
+    st = _here(stream, tokens, dout, base, dtable, ws)
     _check(load().lirpa_embed_backward(
         DTYPES[dt], rows, n, vocab, _tokens(tokens, rows), *_matrix(dout, rows, n, dt, "dout"),
         float(scale), *_matrix(base, vocab, n, dt, "base"),
         *_matrix(dtable, vocab, n, dt, "dtable"), _dev(ws, None, "ws"), int(ws_bytes),
-        _stream(stream)))
+        st))
 
 
 def lirpa_logprob_workspace_bytes(rows, n, top) -> int:
@@ -563,62 +576,67 @@ def lirpa_logprob_forward(logits, scale, tokens, logp, lse, entropy, top, top_lo
                           ws_bytes, stream=None):
     rows, n = _2d(logits, "logits")
     dt, f32 = _dtype(logits, "logits"), torch.float32
-    _here(logits, "logits")
+    st = _here(stream, logits, tokens, logp, lse, entropy, top_logp, top_tokens, ws)
     _check(load().lirpa_logprob_forward(
         DTYPES[dt], rows, n, *_matrix(logits, rows, n, dt, "logits"), float(scale),
         _tokens(tokens, rows), _vector(logp, rows, f32, "logp"), _vector(lse, rows, f32, "lse"),
         _vector(entropy, rows, f32, "entropy"), int(top),
         _vector(top_logp, rows * top, f32, "top_logp"),
         _vector(top_tokens, rows * top, torch.int64, "top_tokens"), _dev(ws, None, "ws"),
-        int(ws_bytes), _stream(stream)))
+        int(ws_bytes), st))
 
 
 def lirpa_logprob_backward(logits, scale, tokens, lse, entropy, dlogp, dentropy, dlogits,
                            stream=None):
     rows, n = _2d(logits, "logits")
     dt, f32 = _dtype(logits, "logits"), torch.float32
-    _here(logits, "logits")
+    st = _here(stream, logits, tokens, lse, entropy, dlogp, dentropy, dlogits)
     _check(load().lirpa_logprob_backward(
         DTYPES[dt], rows, n, *_matrix(logits, rows, n, dt, "logits"), float(scale),
         _tokens(tokens, rows), _vector(lse, rows, f32, "lse"),
         _vector(entropy, rows, f32, "entropy"), _vector(dlogp, rows, f32, "dlogp"),
         _vector(dentropy, rows, f32, "dentropy"), *_matrix(dlogits, rows, n, dt, "dlogits"),
-        _stream(stream)))
+        st))
 
 
 def _seq(seq, rows):
     return _vector(seq, rows, torch.int32, "seq")
 
 
-def _slots(state, state_out, tail, dtype):
-    """(slots, pointers of state and state_out) of [slots, *tail] tensors."""
-    slots, out = None, []
-    for t, what in ((state, "state"), (state_out, "state_out")):
-        if t is not None:
-            if not isinstance(t, torch.Tensor):
-                raise TypeError(f"{what} must be a CUDA tensor")
-            if tuple(t.shape[1:]) != tail or t.dim() != len(tail) + 1 or t.shape[0] < 1:
-                raise ValueError(f"{what} must be [slots, {', '.join(map(str, tail))}], got "
-                                 f"{list(t.shape)}")
-            if slots is not None and t.shape[0] != slots:
-                raise ValueError(f"state has {slots} slots, state_out {t.shape[0]}")
-            slots = t.shape[0]
-        out.append(_dev(t, dtype, what))
-    return (ANY_SLOT if slots is None else slots), *out
+def _state(t, rest, dtype, what):
+    """(slots, device pointer) of a [slots, *rest] tensor; (None, NULL) of None."""
+    if t is None:
+        return None, None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{what} must be a CUDA tensor")
+    shape = t.shape
+    if len(shape) != 3 or shape[1:] != rest or shape[0] < 1:
+        raise ValueError(f"{what} must be [slots, {rest[0]}, {rest[1]}], got {list(shape)}")
+    return shape[0], _dev(t, dtype, what)
+
+
+def _slots(state, state_out, rest, dtype):
+    """(slots, pointers of state and state_out) of [slots, *rest] tensors."""
+    n_in, p_in = _state(state, rest, dtype, "state")
+    n_out, p_out = _state(state_out, rest, dtype, "state_out")
+    if n_in is not None and n_out is not None and n_in != n_out:
+        raise ValueError(f"state has {n_in} slots, state_out {n_out}")
+    slots = n_out if n_in is None else n_in
+    return ANY_SLOT if slots is None else slots, p_in, p_out
 
 
 def _conv(call, x, w, bias, act, seq, state, state_out, y, stream):
     rows, n = _2d(x, "x")
     taps = _2d(w, "w")[0]
     dt = _dtype(x, "x")
-    _here(x, "x")
+    st = _here(stream, x, w, bias, seq, state, state_out, y)
     if act not in CONV_ACTS:
         raise ValueError(f"act must be one of {sorted(CONV_ACTS)}, got {act!r}")
     slots, s_in, s_out = _slots(state, state_out, (taps - 1, n), dt)
     _check(call(DTYPES[dt], rows, n, taps, *_matrix(x, rows, n, dt, "x"),
                 _vector(w, taps * n, dt, "w"), _vector(bias, n, dt, "bias"), CONV_ACTS[act],
                 _seq(seq, rows), slots, s_in, s_out, *_matrix(y, rows, n, dt, "y"),
-                _stream(stream)))
+                st))
 
 
 def lirpa_conv_forward(x, w, bias, act, seq, state, state_out, y, stream=None):
@@ -637,14 +655,14 @@ def lirpa_conv_backward(dy, x, w, bias, act, seq, dx, dw, dbias, ws, ws_bytes, s
     rows, n = _2d(x, "x")
     taps = _2d(w, "w")[0]
     dt = _dtype(x, "x")
-    _here(x, "x")
+    st = _here(stream, dy, x, w, bias, seq, dx, dw, dbias, ws)
     if act not in CONV_ACTS:
         raise ValueError(f"act must be one of {sorted(CONV_ACTS)}, got {act!r}")
     _check(load().lirpa_conv_backward(
         DTYPES[dt], rows, n, taps, *_matrix(dy, rows, n, dt, "dy"), *_matrix(x, rows, n, dt, "x"),
         _vector(w, taps * n, dt, "w"), _vector(bias, n, dt, "bias"), CONV_ACTS[act],
         _seq(seq, rows), ANY_SLOT, *_matrix(dx, rows, n, dt, "dx"), _vector(dw, taps * n, dt, "dw"),
-        _vector(dbias, n, dt, "dbias"), _dev(ws, None, "ws"), int(ws_bytes), _stream(stream)))
+        _vector(dbias, n, dt, "dbias"), _dev(ws, None, "ws"), int(ws_bytes), st))
 
 
 def lirpa_scan_inputs(u, dt, B, C, z, A, D, bias, seq, slots=ANY_SLOT):
@@ -652,7 +670,7 @@ def lirpa_scan_inputs(u, dt, B, C, z, A, D, bias, seq, slots=ANY_SLOT):
     rows, n = _2d(u, "u")
     states = _2d(A, "A")[1]
     kind, f32 = _dtype(u, "u"), torch.float32
-    _here(u, "u")
+    _here(None, u, dt, B, C, z, A, D, bias, seq)
     pu, ldu = _matrix(u, rows, n, kind, "u")
     pdt, lddt = _matrix(dt, rows, n, kind, "dt")
     pz, ldz = _matrix(z, rows, n, kind, "z")
@@ -672,7 +690,7 @@ def lirpa_scan_kept_bytes(rows, n, states) -> int:
 
 
 def _of_scan(scan):
-    return scan.rows, scan.n, scan.states, {v: k for k, v in DTYPES.items()}[scan.dtype]
+    return scan.rows, scan.n, scan.states, _TORCH_TYPES[scan.dtype]
 
 
 def _kept_states(kept, scan):
@@ -685,30 +703,33 @@ def _kept_states(kept, scan):
 def lirpa_scan_forward(scan, state, state_out, y, kept, ws, ws_bytes, stream=None):
     """``scan`` is what lirpa_scan_inputs returned; its slots become those of the states."""
     rows, n, states, dt = _of_scan(scan)
+    st = _here(stream, state, state_out, y, kept, ws)
     scan.slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32)
     _check(load().lirpa_scan_forward(
         ctypes.byref(scan), s_in, s_out, *_matrix(y, rows, n, dt, "y"), _kept_states(kept, scan),
-        _dev(ws, None, "ws"), int(ws_bytes), _stream(stream)))
+        _dev(ws, None, "ws"), int(ws_bytes), st))
 
 
 def lirpa_scan_step(scan, state, state_out, y, stream=None):
     rows, n, states, dt = _of_scan(scan)
+    st = _here(stream, state, state_out, y)
     scan.slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32)
     _check(load().lirpa_scan_step(ctypes.byref(scan), s_in, s_out, *_matrix(y, rows, n, dt, "y"),
-                                  _stream(stream)))
+                                  st))
 
 
 def lirpa_scan_backward(scan, dy, kept, du, ddt, dz, dB, dC, dA, dD, dbias, ws, ws_bytes,
                         stream=None):
     rows, n, states, dt = _of_scan(scan)
     f32 = torch.float32
+    st = _here(stream, dy, kept, du, ddt, dz, dB, dC, dA, dD, dbias, ws)
     _check(load().lirpa_scan_backward(
         ctypes.byref(scan), *_matrix(dy, rows, n, dt, "dy"), _kept_states(kept, scan),
         *_matrix(du, rows, n, dt, "du"), *_matrix(ddt, rows, n, dt, "ddt"),
         *_matrix(dz, rows, n, dt, "dz"), *_matrix(dB, rows, states, dt, "dB"),
         *_matrix(dC, rows, states, dt, "dC"), _vector(dA, n * states, f32, "dA"),
         _vector(dD, n, f32, "dD"), _vector(dbias, n, f32, "dbias"), _dev(ws, None, "ws"),
-        int(ws_bytes), _stream(stream)))
+        int(ws_bytes), st))
 
 
 class Network:
