@@ -1,0 +1,197 @@
+"""The embedding's, the log probabilities', the convolution's and the scan's calls read and write
+their tensors alone: every input lies among NaN and every output among a mark that has to stay.  And
+what one sequence holds does not reach another."""
+import pytest
+import torch
+
+from .test_gpu_blocks_bounds import TYPES, Frame, ids
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lirpa():
+    from paper_2011_13824_amd import lirpa
+    return lirpa
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2011_13824_amd import blocks
+    return blocks
+
+
+SHAPES = [(1, 1, 0, 1), (5, 7, 1, 0), (9, 33, 5, 3), (70, 511, 0, 0), (33, 8, 3, 1), (17, 4, 0, 0),
+          (66, 3, 1, 2), (6, 2049, 1, 1), (130, 66, 8, 8), (3, 5, 0, 3), (40, 2, 5, 1)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,pad,shift", SHAPES + [(4200, 9, 2, 1)])
+def test_embedding(lirpa, dtype, rows, n, pad, shift):
+    f = Frame(dtype, rows + n)
+    vocab = 21
+    tokens = torch.randint(-1, vocab, (rows,), device="cuda")
+    table, base = f.input(vocab, n, pad, shift), f.input(vocab, n, pad + 1, shift)
+    out, dout = f.output(rows, n, pad, shift), f.input(rows, n, pad + 2, shift)
+    lirpa.lirpa_embed_forward(tokens, table, 1.5, out)
+    need = lirpa.lirpa_embed_workspace_bytes(rows, n)
+    for b in (None, base):
+        ws = f.output(1, need, dtype=torch.uint8)[0]
+        d = f.output(vocab, n, pad + 3, shift)
+        lirpa.lirpa_embed_backward(tokens, dout, 1.5, b, d, ws, need)
+        assert torch.isfinite(d).all()
+    same = f.output(vocab, n, pad + 1, shift)
+    same.copy_(base)
+    ws = f.output(1, need, dtype=torch.uint8)[0]
+    lirpa.lirpa_embed_backward(tokens, dout, 1.5, same, same, ws, need)
+    assert torch.isfinite(out).all() and torch.equal(same, d)
+    f.check("embedding")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,pad,shift", SHAPES + [(1, 9001, 0, 3), (1100, 2051, 1, 1)])
+@pytest.mark.parametrize("top", [0, 3])
+def test_log_probabilities(lirpa, dtype, rows, n, pad, shift, top):
+    f = Frame(dtype, rows + n)
+    f32 = torch.float32
+    logits = f.input(rows, n, pad, shift)
+    tokens = torch.randint(-1, n, (rows,), device="cuda")
+    logp, lse, entropy = (f.output(1, rows, dtype=f32)[0] for _ in range(3))
+    top_logp = f.output(1, rows * top, dtype=f32)[0] if top else None
+    top_tokens = f.output(1, rows * top, dtype=torch.int64)[0] if top else None
+    need = lirpa.lirpa_logprob_workspace_bytes(rows, n, top)
+    ws = f.output(1, need, dtype=torch.uint8)[0]
+    lirpa.lirpa_logprob_forward(logits, 1.1, tokens, logp, lse, entropy, top, top_logp, top_tokens,
+                                ws, need)
+    d = f.output(rows, n, pad + 1, shift)
+    lirpa.lirpa_logprob_backward(logits, 1.1, tokens, lse, entropy, logp, entropy, d)
+    for t in (logp, lse, entropy, d):
+        assert torch.isfinite(t).all()
+    if top:
+        assert ((top_tokens >= -1) & (top_tokens < n)).all()
+    f.check("log probabilities")
+
+
+def some_sequences(rows, g):
+    cuts = (torch.rand(rows, generator=g, device="cuda") < 0.1).int().cumsum(0)
+    seq = cuts * 3 % 7 + cuts // 7 * 7  # every number once, some out of order
+    return torch.where(torch.rand(rows, generator=g, device="cuda") < 0.02, -1, seq).int()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,pad,shift", SHAPES + [(300, 17, 3, 0)])
+@pytest.mark.parametrize("taps", [1, 2, 4, 7])
+def test_convolution(lirpa, dtype, rows, n, pad, shift, taps):
+    f = Frame(dtype, rows + n + taps)
+    x, dy = f.input(rows, n, pad, shift), f.input(rows, n, pad + 1, shift)
+    w, b = f.input(taps, n, 0, shift), f.input(1, n, 0, shift)[0]
+    slots = rows + 9
+    for seq in (None, some_sequences(rows, f.gen)):
+        state = f.input(slots, (taps - 1) * n, 0, shift).view(slots, taps - 1, n)
+        out = f.output(slots, (taps - 1) * n, 0, shift).view(slots, taps - 1, n)
+        y = f.output(rows, n, pad + 2, shift)
+        lirpa.lirpa_conv_forward(x, w, b, "silu", seq, state, out, y)
+        y1 = f.output(rows, n, pad, shift + 1)
+        lirpa.lirpa_conv_step(x, w, b, "silu", None, state, out, y1)
+        need = lirpa.lirpa_conv_workspace_bytes(rows, n, taps)
+        ws = f.output(1, need, dtype=torch.uint8)[0]
+        dx, dw = f.output(rows, n, pad, shift), f.output(taps, n, 0, shift)
+        db = f.output(1, n, 0, shift)[0]
+        lirpa.lirpa_conv_backward(dy, x, w, b, "silu", seq, dx, dw, db, ws, need)
+        for t in (y, y1, dx, dw, db):
+            assert torch.isfinite(t).all()
+        assert torch.isfinite(out).all()
+    f.check("convolution")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,pad,shift", SHAPES + [(300, 17, 3, 0), (200, 131, 0, 1)])
+@pytest.mark.parametrize("N", [1, 6, 8, 16, 19, 64])
+def test_scan(lirpa, dtype, rows, n, pad, shift, N):
+    if rows * n * N > 1 << 20:
+        N = 5
+    f = Frame(dtype, rows + n + N)
+    f32 = torch.float32
+    u, dt, z = (f.input(rows, n, pad + i, shift) for i in range(3))
+    Bm, Cm = f.input(rows, N, pad, shift), f.input(rows, N, pad + 1, shift)
+    small = Frame(f32, n)
+    A = small.input(n, N)
+    A.copy_(-A.abs())
+    D, bias = small.input(1, n)[0], small.input(1, n)[0]
+    slots = rows + 9
+    state = small.input(slots, n * N).view(slots, n, N)
+    dy = f.input(rows, n, pad + 3, shift)
+    for seq in (None, some_sequences(rows, f.gen)):
+        out = f.output(slots, n * N, dtype=f32).view(slots, n, N)
+        y = f.output(rows, n, pad + 1, shift)
+        scan = lirpa.lirpa_scan_inputs(u, dt, Bm, Cm, z, A, D, bias, seq)
+        need = lirpa.lirpa_scan_workspace_bytes(rows, n, N, 0)
+        ws = f.output(1, need, dtype=torch.uint8)[0]
+        lirpa.lirpa_scan_forward(scan, state, out, y, None, ws, need)
+        y1 = f.output(rows, n, pad, shift + 1)
+        alone = lirpa.lirpa_scan_inputs(u, dt, Bm, Cm, z, A, D, bias, None)
+        lirpa.lirpa_scan_step(alone, state, out, y1)
+        kept = f.output(1, lirpa.lirpa_scan_kept_bytes(rows, n, N), dtype=torch.uint8)[0]
+        y2 = f.output(rows, n, pad, shift)
+        lirpa.lirpa_scan_forward(scan, None, None, y2, kept, ws, need)
+        need = lirpa.lirpa_scan_workspace_bytes(rows, n, N, 1)
+        ws = f.output(1, need, dtype=torch.uint8)[0]
+        grads = [f.output(rows, n, pad + i, shift) for i in range(3)]
+        grads += [f.output(rows, N, pad, shift), f.output(rows, N, pad + 2, shift)]
+        sums = [f.output(1, n * N, dtype=f32)[0]] + [f.output(1, n, dtype=f32)[0] for _ in "ab"]
+        lirpa.lirpa_scan_backward(scan, dy, kept, *grads, *sums, ws, need)
+        for t in (y, y1, y2, out, *grads, *sums):
+            assert torch.isfinite(t).all()
+    f.check("scan")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+def test_a_sequence_that_is_not_finite_stays_alone(B, dtype):
+    """NaN and infinities in one sequence's inputs and gradients: all others are what they were."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    rows, n, N = 400, 70, 16
+    lengths = [40, 3, 100, 1, 16, 150, 90]
+
+    def new(*shape):
+        return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+    seq = B.sequences(lengths, rows)
+    x = dict(u=new(rows, n), dt=new(rows, n), B=new(rows, N), C=new(rows, N), z=new(rows, n))
+    dy = new(rows, n)
+    scan = B.SelectiveScan(-torch.rand(n, N, generator=g, device="cuda"))
+    conv = B.CausalConv(new(4, n))
+
+    def run(x, dy):
+        y, kept = scan.forward(*x.values(), seq, keep=True)
+        grads = scan.backward(dy, kept)
+        c = conv.forward(x["u"], seq)
+        return [y, c, conv.backward(dy, x["u"], seq)["dx"]] + [grads["d" + k] for k in x]
+
+    want = run(x, dy)
+    for bad in (2, 3, 5):
+        first = sum(lengths[:bad])
+        here = torch.zeros(rows, dtype=torch.bool, device="cuda")
+        here[first:first + lengths[bad]] = True
+        for value in (float("nan"), float("inf")):
+            spoilt = {k: t.clone() for k, t in x.items()}
+            for t in spoilt.values():
+                t[here] = value
+            d = dy.clone()
+            d[here] = value
+            for a, b in zip(run(spoilt, d), want):
+                assert torch.equal(a[~here], b[~here])
+
+
+def test_tensors_of_another_device_are_refused(lirpa, B, monkeypatch):
+    """As if the current device were another than the tensors'."""
+    x, t = torch.randn(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    w = torch.randn(4, 8, device="cuda")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    for call in (lambda: B.Embedding(x).forward(t), lambda: B.Embedding(x).backward(t, x),
+                 lambda: B.LogProbs().forward(x, t), lambda: B.LogProbs().backward(x, t, x[:, 0]),
+                 lambda: B.CausalConv(w).forward(x), lambda: B.CausalConv(w).step(x, None),
+                 lambda: B.CausalConv(w).backward(x, x),
+                 lambda: B.SelectiveScan(w.t().contiguous()).forward(x, x, x[:, :4], x[:, :4])):
+        with pytest.raises(ValueError, match="current device"):
+            call()
