@@ -397,7 +397,7 @@ int lirpa_embed_backward(int dtype, int64_t rows, int n, int vocab, const int64_
  * Outputs are float, each NULL where it is not wanted (tokens may be NULL where logp is).  A logit
  * of -inf is a token that cannot come: it is no alternative, and places that are left over hold
  * token -1 and log probability -inf.  A row of -inf alone has lse and logp -inf and entropy 0.  A row
- * with a NaN or +inf has NaN everywhere and alternatives -1.  logp, entropy and top_logp are taken
+ * with a NaN or +inf has NaN everywhere (but for padding's logp) and alternatives -1.  logp, entropy and top_logp are taken
  * from the differences to the row's largest logit, not from lse. */
 size_t lirpa_logprob_workspace_bytes(int64_t rows, int n, int top); /* 0 for invalid arguments */
 int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
@@ -408,8 +408,8 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
 /* The gradient of the logits from those of logp and entropy (float [rows], either may be NULL) and
  * the lse and entropy (NULL where dentropy is) that the forward call returned:
  *     dl_j = scale (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)).
- * dlogp is not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer
- * of logits. */
+ * p comes from lse, whose rounding (2^-24 of its magnitude) is a relative error of it.  dlogp is not
+ * read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer of logits. */
 int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                            float scale, const int64_t* tokens, const float* lse,
                            const float* entropy, const float* dlogp, const float* dentropy,

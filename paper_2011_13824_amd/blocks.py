@@ -1,4 +1,5 @@
-"""The feed-forward block of a language model over ``liblirpa.so``: norm, gated block, 8 bits.
+"""The blocks of a language model over ``liblirpa.so``: norm, gated feed-forward block, 8 bits;
+embedding, causal convolution, selective scan, log probabilities.
 
 Convenience owners in the manner of ``lirpa.Network``: they allocate outputs and workspaces on
 torch's current stream, where the calls run, and leave every computation to the library.
@@ -9,6 +10,19 @@ torch's current stream, where the calls run, and leave every computation to the 
     ...
     grads = ffn.backward(dout, kept)                  # dx, dWg, dWu, dWd
     dh, dw = norm.backward(grads["dx"], n.sum, n.rstd, dsum)
+
+    embed, conv = Embedding(table), CausalConv(w, bias)
+    scan, loss = SelectiveScan(A, D, dt_bias), LogProbs(top=5)
+    seq = sequences([300, 12, 700])                   # three texts behind each other
+    x = embed.forward(tokens)
+    c = conv.forward(x, seq)
+    y, kept = scan.forward(c, dt, B, C, z, seq, keep=True)
+    p = loss.forward(logits, targets)                 # p.logp, p.lse, p.entropy, p.top_tokens
+    ...
+    dlogits = loss.backward(logits, targets, p.lse, dlogp=dlogp, out=logits)
+    grads = scan.backward(dy, kept)                   # du, ddt, dB, dC, dz, dA, dD, dbias
+    grads = conv.backward(grads["du"], x, seq)        # dx, dw, dbias
+    dtable = embed.backward(tokens, grads["dx"])
 
 Autograd records none of this: gradients are what the backward methods return.  A forward call whose
 inputs require gradients while autograd records warns of that.
@@ -249,24 +263,24 @@ class CausalConv:
 
     def forward(self, x, seq=None, state=None, state_out=None):
         _no_tape(x, self.w, self.bias, state)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x)
         lirpa.lirpa_conv_forward(x, self.w, self.bias, self.act, seq, state, state_out, y)
         return y
 
     def step(self, x, state, seq=None, state_out=None):
         """One row of every sequence: row t is that of slot seq[t], of slot t without seq."""
         _no_tape(x, self.w, self.bias, state)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        y = torch.empty_like(x)
         lirpa.lirpa_conv_step(x, self.w, self.bias, self.act, seq, state, state_out, y)
         return y
 
     def backward(self, dy, x, seq=None):
         """{"dx", "dw", "dbias"} (dbias where there is a bias), for sequences without a state."""
         lirpa._2d(x, "x")
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        grads = {"dx": dx, "dw": torch.empty(self.w.shape, dtype=x.dtype, device=x.device)}
+        dx = torch.empty_like(x)
+        grads = {"dx": dx, "dw": torch.empty_like(self.w)}
         if self.bias is not None:
-            grads["dbias"] = torch.empty(self.bias.shape, dtype=x.dtype, device=x.device)
+            grads["dbias"] = torch.empty_like(self.bias)
         need = lirpa.lirpa_conv_workspace_bytes(*x.shape, self.w.shape[0])
         lirpa.lirpa_conv_backward(dy, x, self.w, self.bias, self.act, seq, dx, grads["dw"],
                                   grads.get("dbias"), _bytes(need, x.device), need)
@@ -301,7 +315,7 @@ class SelectiveScan:
             raise ValueError("the backward pass starts from states of 0: keep and state exclude "
                              "each other")
         size = (scan.rows, scan.n, scan.states)
-        y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+        y = torch.empty_like(u)
         kept = _bytes(lirpa.lirpa_scan_kept_bytes(*size), u.device) if keep else None
         need = lirpa.lirpa_scan_workspace_bytes(*size, 0)
         lirpa.lirpa_scan_forward(scan, state, state_out, y, kept, _bytes(need, u.device), need)
@@ -311,7 +325,7 @@ class SelectiveScan:
         """One row of every sequence: row t is that of slot seq[t], of slot t without seq."""
         _no_tape(u, dt, B, C, z, state, self.A, self.D, self.bias)
         scan = self._inputs(u, dt, B, C, z, seq)
-        y = torch.empty(u.shape, dtype=u.dtype, device=u.device)
+        y = torch.empty_like(u)
         lirpa.lirpa_scan_step(scan, state, state_out, y)
         return y
 
@@ -322,8 +336,7 @@ class SelectiveScan:
         scan = self._inputs(u, dt, B, C, z, kept.seq)
         like = {"du": u, "ddt": dt, "dz": z, "dB": B, "dC": C, "dA": self.A, "dD": self.D,
                 "dbias": self.bias}
-        grads = {k: torch.empty(t.shape, dtype=t.dtype, device=t.device)
-                 for k, t in like.items() if t is not None}
+        grads = {k: torch.empty_like(t) for k, t in like.items() if t is not None}
         need = lirpa.lirpa_scan_workspace_bytes(scan.rows, scan.n, scan.states, 1)
         lirpa.lirpa_scan_backward(scan, dy, kept.states, *(grads.get(k) for k in like),
                                   _bytes(need, u.device), need)
@@ -375,6 +388,8 @@ class LogProbs:
 
     def __init__(self, scale=1.0, top=0):
         self.scale, self.top = float(scale), int(top)
+        if not 0 <= self.top <= 32:
+            raise ValueError(f"top must be 0 to 32, got {top}")
 
     def forward(self, logits, tokens=None):
         """LogP; logp is None without tokens, top_logp and top_tokens [rows, top] without top.  A
@@ -406,6 +421,6 @@ class LogProbs:
         """The gradient of the logits from those of logp and entropy, and what forward returned of
         the same logits and tokens.  ``out`` may be the logits, whose place it then takes."""
         if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            out = torch.empty_like(logits)
         lirpa.lirpa_logprob_backward(logits, self.scale, tokens, lse, entropy, dlogp, dentropy, out)
         return out

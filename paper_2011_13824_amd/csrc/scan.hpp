@@ -568,7 +568,8 @@ __global__ __launch_bounds__(256) void k_scan_back_local(Scan<T> a, int groups) 
 
 // Sums of 8 values over the lanes of a wave that hold the same states of its columns: halves of the
 // wave, then of the halves, exchange one of two values each.  Row k (of 16 lanes) ends up with
-// values 2k and 2k + 1, in all its columns.
+// values 2k and 2k + 1, in all its columns.  (Products of the matrix units with ones, which add four
+// lanes each, took the gradient of 8192 rows of 4096 columns from 0.60 to 0.79 ms.)
 template <int LANES>
 __device__ __forceinline__ void wave_sums(const float (&v)[8], float (&out)[2]) {
   float a[4], b[2];

@@ -115,3 +115,9 @@ def test_binding_refuses():
         blocks.LogProbs().forward(x[0], t)
     with pytest.raises(TypeError, match="CUDA"):
         blocks.LogProbs().backward(x, t, torch.zeros(4), dlogp=torch.zeros(4))
+
+
+@pytest.mark.parametrize("top", [-1, 33])
+def test_more_alternatives_than_there_are_places(top):
+    with pytest.raises(ValueError, match="top"):
+        blocks.LogProbs(top=top)
