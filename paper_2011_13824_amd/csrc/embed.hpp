@@ -105,17 +105,37 @@ __global__ __launch_bounds__(256) void k_embed_rank(const int64_t* __restrict__ 
   __shared__ __attribute__((aligned(16))) uint32_t keys[kRankRows];
   __shared__ int below[4][64];
   const int padded = (rows + 15) / 16 * 16;
-  for (int i = threadIdx.x; i < padded; i += 256)
-    keys[i] = i < rows ? token_key(tokens, i, vocab) : 0xffffffffu;
-  __syncthreads();
-  const int lane = threadIdx.x & 63, part = threadIdx.x >> 6, me = blockIdx.x * 64 + lane;
-  const uint32_t key = me < rows ? keys[me] : 0u;
-  int count = 0;
-  for (int i = part * (padded / 4); i < (part + 1) * (padded / 4); i += 4) {
-    const u32x4 k = *(const u32x4*)(keys + i);
+  constexpr int kAhead = 8;
+  for (int i0 = 0; i0 < padded; i0 += 256 * kAhead) {
+    uint32_t key[kAhead];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) count += k[j] < key || (k[j] == key && i + j < me);
+    for (int j = 0; j < kAhead; ++j)
+      key[j] = token_key(tokens, min(i0 + j * 256 + (int)threadIdx.x, rows - 1), vocab);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + j * 256 + threadIdx.x;
+      if (i < padded) keys[i] = i < rows ? key[j] : 0xffffffffu;
+    }
   }
+  __syncthreads();
+  const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+  const int first = blockIdx.x * 64, me = first + lane;
+  const uint32_t key = me < rows ? keys[me] : 0u;
+  const int from = part * (padded / 4), to = from + padded / 4;
+  int count = 0;
+  // in front of the block's own tokens equal ones count, behind them they do not
+  auto take = [&](int i, int end, auto&& in_front) {
+#pragma unroll 4
+    for (; i < end; i += 4) {
+      const u32x4 k = *(const u32x4*)(keys + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) count += in_front(k[j], i + j);
+    }
+  };
+  take(from, min(to, first), [&](uint32_t k, int) { return k <= key; });
+  take(max(from, first), min(to, first + 64),
+       [&](uint32_t k, int i) { return k < key || (k == key && i < me); });
+  take(max(from, first + 64), to, [&](uint32_t k, int) { return k < key; });
   below[part][lane] = count;
   __syncthreads();
   if (part == 0 && me < rows)

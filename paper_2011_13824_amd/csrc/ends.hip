@@ -48,11 +48,13 @@ int check_vocab(const char* who, int vocab) {
 // ---------------------------------------------------------------------------------------------
 int64_t pieces8(int n) { return (n + 7) / 8; }
 
-// Entries that a block of the sums takes: few where there is little to share out.
-constexpr int64_t kManyPieces = (int64_t)1 << 21;
-int sum_entries(int64_t rows, int n) { return rows * pieces8(n) >= kManyPieces ? 32 : 8; }
+// Entries of a piece of the sums: few where there are few rows, more where a frequent token's pieces,
+// which one block joins, would be many.
+int sum_entries(int64_t rows) { return (int)std::clamp<int64_t>(rows >> 10 & ~7, 8, 32); }
 
 constexpr int kRadixBlocks = 256, kRadixLeast = 1024;
+
+constexpr int kNarrow = 128;  // columns of rows that share a block of the sums, 16 at a time
 
 struct EmbedRoom {
   Named *a, *b;
@@ -66,8 +68,8 @@ EmbedRoom embed_room(int64_t rows, int n, void* base) {
   r.a = (Named*)ws.take((size_t)rows * sizeof(Named));
   r.b = (Named*)ws.take((size_t)rows * sizeof(Named));
   r.counts = (uint32_t*)ws.take(((size_t)kRadixBlocks << kMaxDigit) * sizeof(uint32_t));
-  // sum_entries' two cases: neither term falls as rows grow
-  const int64_t pieces = (rows + 31) / 32 + std::min((rows + 7) / 8, kManyPieces / pieces8(n) / 8 + 1);
+  // no less than sum_entries asks for with fewer rows: 8 entries a piece up to 2^14
+  const int64_t pieces = (rows + 31) / 32 + std::min<int64_t>((rows + 7) / 8, 1 << 11);
   r.part = (float*)ws.take((size_t)pieces * 2 * n * sizeof(float));
   r.bytes = std::max<size_t>(256, ws.at);
   return r;
@@ -127,12 +129,12 @@ int embed_backward(int64_t rows, int n, int vocab, const int64_t* tokens, const 
   sum.ldb = ldb;
   sum.ldd = ldd;
   sum.rows = rows;
-  sum.each = sum_entries(rows, n);
+  sum.each = sum_entries(rows);
   sum.pieces = (int)((rows + sum.each - 1) / sum.each);
   sum.n = n;
   sum.vocab = vocab;
   sum.scale = scale;
-  const int tx = n <= 128 ? 16 : n <= 512 ? 64 : 256;
+  const int tx = n <= kNarrow ? 16 : 256;
   const int64_t slabs = (n + tx * 8 - 1) / (tx * 8), join_slabs = (n + 511) / 512;
   const int64_t sum_blocks = (sum.pieces + 256 / tx - 1) / (256 / tx) * slabs;
   const int64_t join_blocks = (int64_t)(sum.pieces - 1) * join_slabs;
@@ -177,8 +179,6 @@ int embed_backward(int64_t rows, int n, int vocab, const int64_t* tokens, const 
   TRY(launch_k("embed_sum", st, [&] {
     if (tx == 16)
       k_embed_sum<T, 16><<<(unsigned)sum_blocks, 256, 0, st>>>(sum, (int)slabs);
-    else if (tx == 64)
-      k_embed_sum<T, 64><<<(unsigned)sum_blocks, 256, 0, st>>>(sum, (int)slabs);
     else
       k_embed_sum<T, 256><<<(unsigned)sum_blocks, 256, 0, st>>>(sum, (int)slabs);
   }));
@@ -192,7 +192,7 @@ int embed_backward(int64_t rows, int n, int vocab, const int64_t* tokens, const 
 // Log probabilities
 // ---------------------------------------------------------------------------------------------
 // Few rows are split, so that about kFewBlocks blocks have work: rows * parts < 2 * kFewBlocks.
-constexpr int kFewBlocks = 1024;
+constexpr int kFewBlocks = 256;
 void logprob_parts(int64_t rows, int n, int& parts, int& columns) {
   const int64_t most = std::min<int64_t>(kMaxParts, (n + kPartColumns - 1) / kPartColumns);
   const int64_t want = std::clamp<int64_t>((kFewBlocks + rows - 1) / rows, 1, most);

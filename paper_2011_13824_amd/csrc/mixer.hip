@@ -141,15 +141,16 @@ int64_t scan_groups(int n, int states) {
   return (n + columns - 1) / columns;
 }
 
-// Rows are cut into chunks of at least kChunkLeast, until there are kScanBlocks blocks.
-constexpr int kChunkLeast = 64, kScanBlocks = 2048;
+// Rows are cut into chunks until there are kScanBlocks blocks, or kMostChunks chunks: their states
+// are linked one after the other.
+constexpr int kScanBlocks = 2048, kMostChunks = 64;
 int64_t scan_most_chunks(int n, int states) {
   const int64_t groups = scan_groups(n, states);
-  return std::max<int64_t>(1, (kScanBlocks + groups - 1) / groups);
+  return std::clamp<int64_t>((kScanBlocks + groups - 1) / groups, 1, kMostChunks);
 }
 int64_t scan_chunk(int64_t rows, int n, int states) {
   const int64_t want = scan_most_chunks(n, states);
-  return std::max<int64_t>(kChunkLeast, up((rows + want - 1) / want, kSpan));
+  return std::max<int64_t>(kSpan, up((rows + want - 1) / want, kSpan));
 }
 
 struct ScanRoom {
@@ -163,7 +164,7 @@ ScanRoom scan_room(int64_t rows, int n, int states, bool backward, void* base) {
   ScanRoom r{};
   const int padded = 4 * scan_lanes(states);
   const int64_t chunks =
-      std::min((rows + kChunkLeast - 1) / kChunkLeast, scan_most_chunks(n, states));
+      std::min((rows + kSpan - 1) / kSpan, scan_most_chunks(n, states));
   const size_t column = (size_t)chunks * n * sizeof(float);
   if (chunks > 1) {
     r.local = (float*)ws.take(column * padded);
