@@ -396,9 +396,9 @@ int lirpa_embed_backward(int dtype, int64_t rows, int n, int vocab, const int64_
  *     the lowest token first among equal logits.
  * Outputs are float, each NULL where it is not wanted (tokens may be NULL where logp is).  A logit
  * of -inf is a token that cannot come: it is no alternative, and places that are left over hold
- * token -1 and log probability -inf.  A row of -inf alone has lse and logp -inf and entropy 0.  A row
- * with a NaN or +inf has NaN everywhere (but for padding's logp) and alternatives -1.  logp, entropy and top_logp are taken
- * from the differences to the row's largest logit, not from lse. */
+ * token -1 and log probability -inf.  A row of -inf alone has lse and logp -inf and entropy 0.  A
+ * row with a NaN or +inf has NaN everywhere (but for padding's logp) and alternatives -1.  logp,
+ * entropy and top_logp are taken from the differences to the row's largest logit, not from lse. */
 size_t lirpa_logprob_workspace_bytes(int64_t rows, int n, int top); /* 0 for invalid arguments */
 int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                           float scale, const int64_t* tokens, float* logp, float* lse,
@@ -408,8 +408,9 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
 /* The gradient of the logits from those of logp and entropy (float [rows], either may be NULL) and
  * the lse and entropy (NULL where dentropy is) that the forward call returned:
  *     dl_j = scale (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)).
- * p comes from lse, whose rounding (2^-24 of its magnitude) is a relative error of it.  dlogp is not
- * read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer of logits. */
+ * p comes from lse, whose rounding (2^-24 of its magnitude) is a relative error of it.  dlogp is
+ * not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer of
+ * logits. */
 int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                            float scale, const int64_t* tokens, const float* lse,
                            const float* entropy, const float* dlogp, const float* dentropy,
@@ -421,11 +422,11 @@ int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, i
  * Conventions as for the feed-forward block, and:
  * - Sequences lie behind each other in the rows.  seq (int32 [rows], on the device) names the
  *   sequence of every row, and the slot of its state; rows of one sequence are neighbours, so a
- *   sequence begins and ends where the number changes.  seq = NULL: all rows are sequence 0.  A number
- *   outside [0, slots) is padding: outputs and gradients of its rows are 0, its inputs are of no
- *   account.  slots >= 1; without states any bound will do.
- * - state holds what stands in front of a sequence's first row, by slot, and state_out receives what
- *   the next row will need; either may be NULL (zeros; not wanted), and state_out may be state.
+ *   sequence begins and ends where the number changes.  seq = NULL: all rows are sequence 0.  A
+ *   number outside [0, slots) is padding: outputs and gradients of its rows are 0, its inputs are of
+ *   no account.  slots >= 1; without states any bound will do.
+ * - state holds what stands in front of a sequence's first row, by slot, and state_out receives
+ *   what the next row will need; either may be NULL (zeros; not wanted), and state_out may be state.
  *   Slots that no row names are not touched.  A slot is named by one sequence of a call; if it is
  *   named by more, its state is one of theirs, or parts of several.
  * - *_step takes one row of every sequence: row t is that of slot seq[t] (slot t without seq).
@@ -452,8 +453,8 @@ int lirpa_conv_backward(int dtype, int64_t rows, int n, int taps, const void* dy
                         void* dbias, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /* A scan's inputs (device pointers, read during a call's enqueued work only).  u, dt, z [rows][n]
- * and B, C [rows][states] of dtype; A [n][states], D [n], bias [n] of float.  z (no gate), D and bias
- * may be NULL.  states 1 to 64. */
+ * and B, C [rows][states] of dtype; A [n][states], D [n], bias [n] of float.  z (no gate), D and
+ * bias may be NULL.  states 1 to 64. */
 typedef struct {
   int dtype;
   int64_t rows;
@@ -478,7 +479,8 @@ int lirpa_scan_step(const lirpa_scan* scan, const float* state, float* state_out
                     int64_t ldy, hipStream_t stream);
 
 /* Gradients from what was kept, for the same inputs: du, ddt, dz (NULL without z) [rows][n], dB, dC
- * [rows][states] of dtype; dA [n][states], dD, dbias [n] of float, each NULL where it is not wanted. */
+ * [rows][states] of dtype; dA [n][states], dD, dbias [n] of float, each NULL where it is not
+ * wanted. */
 int lirpa_scan_backward(const lirpa_scan* scan, const void* dy, int64_t lddy, const void* kept,
                         void* du, int64_t lddu, void* ddt, int64_t ldddt, void* dz, int64_t lddz,
                         void* dB, int64_t lddB, void* dC, int64_t lddC, float* dA, float* dD,

@@ -7,11 +7,17 @@
 // In front of a sequence's first row stand the taps - 1 inputs of its state, or zeros.
 //
 // Bound by bytes.  A thread takes 16 bytes of columns (8 in the gradient) and walks over a strip of
-// rows with the last taps - 1 inputs in registers, so that a row is read once, but for those in front
-// of the strip, which its neighbour reads too and which come out of a cache.  The walk begins taps - 1 rows in front of the
-// strip; a sequence that begins on the way replaces what the walk has met by its state.  The
-// gradient walks on behind the strip's end, for the outputs that its last inputs reach, and adds a
-// strip's part of dw and dbias in registers; the strips' parts are joined in order by k_sum_parts.
+// rows with the last taps - 1 inputs in registers, so that a row is read once, but for those in
+// front of the strip, which its neighbour reads too and which come out of a cache.  The walk begins
+// taps - 1 rows in front of the strip; a sequence that begins on the way replaces what the walk has
+// met by its state.  The gradient walks on behind the strip's end, for the outputs that its last
+// inputs reach, and adds a strip's part of dw and dbias in registers; the strips' parts are joined
+// in order by k_sum_parts.
+//
+// 4 taps with silu: 8192 x 4096 bf16 33 us for 147 MB (4.4 TB/s, vector units 75 % busy); 4099 x
+// 1001 f16 12 us forward, 23 + 5 backward: some 1600 waves of 16 rows each, twice the latency of
+// their loads and as much arithmetic.  With 8 columns a thread the gradient's registers left two
+// waves a SIMD (34 us); with 8 rows ahead instead of 4 the forward pass took 52 us for 33.
 #pragma once
 
 #include "sequences.hpp"

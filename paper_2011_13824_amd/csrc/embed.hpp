@@ -1,17 +1,18 @@
 // Embedding: rows of a table by token, scaled, and the table's gradient.
 //
-//   out_i = scale * table[token_i],   dtable_v = base_v + scale * sum over {i : token_i = v} of dout_i
+//   out_i = scale * table[token_i]
+//   dtable_v = base_v + scale * sum over {i : token_i = v} of dout_i
 //
 // A token outside [0, vocab) is padding: its row is 0, and it takes no part in the gradient.
 //
 // The gradient adds rows in the order of their positions, so the tokens are sorted first, stably.
-// Up to kRankRows tokens every token counts those in front of it; more go through a radix sort.  Both
-// keep a few blocks busy, and the blocks behind them in the same launches write what no token names:
-// zeros, or a copy of base.  The sorted tokens are then cut into pieces of equal length, whatever
-// tokens they hold: a block sums the rows of each token of its piece and writes the sums of tokens
-// that lie inside it, and those that cross an end go to the workspace and are joined in order by a
-// second kernel.  So one token in all positions costs no more than all of them different, and no sum
-// depends on the order in which blocks run.
+// Up to kRankRows tokens every token counts those in front of it; more go through a radix sort.
+// Both keep a few blocks busy, and the blocks behind them in the same launches write what no token
+// names: zeros, or a copy of base.  The sorted tokens are then cut into pieces of equal length,
+// whatever tokens they hold: a block sums the rows of each token of its piece and writes the sums
+// of tokens that lie inside it, and those that cross an end go to the workspace and are joined in
+// order by a second kernel.  So one token in all positions costs no more than all of them
+// different, and no sum depends on the order in which blocks run.
 #pragma once
 
 #include "lm_types.hpp"
@@ -47,15 +48,21 @@ __device__ __forceinline__ Named load_named(const Named* p) {
   return Named{v[0], v[1]};
 }
 
+// Counting grows with the square: 4000 tokens 14 us in one launch, where the four launches of a
+// radix sort take 16 to 20; 8000 would take some 45 us, the radix sort 18.
 constexpr int kRankRows = 4096;
 constexpr int kMaxDigit = 9;  // bits of a radix pass
 
-// The part of a launch that fills the table's gradient: pieces [first, end) of 8 columns.
+// The part of a launch that fills the table's gradient: pieces [first, end) of 8 columns.  Rows
+// that lie behind each other are one row (n = 0) of `values` values: a piece's place then takes no
+// division, and odd widths no cut pieces (32003 rows of 1001 floats, copied: 45 us for 55).  Its
+// stores pass the caches by, which the sums need: with 128000 x 4096 bf16 the fill takes 194 us for
+// 175, and the sums behind it 34 for 68.
 template <typename T>
 struct EmbedFill {
   T* dtable;
   const T* base;  // NULL: zeros
-  int64_t ldd, ldb, first, end;
+  int64_t ldd, ldb, first, end, values;
   int n;
 };
 
@@ -63,7 +70,30 @@ struct EmbedFill {
 constexpr int kFillPieces = 256 * 8;
 
 template <typename T>
+__device__ __forceinline__ void embed_fill_flat(const EmbedFill<T>& f, int64_t block) {
+  const int64_t p0 = f.first + block * kFillPieces + threadIdx.x;
+  Vec<T, 8> v[kFillPieces / 256];
+#pragma unroll
+  for (int i = 0; i < kFillPieces / 256; ++i) {
+    // behind the last whole piece the values before it again
+    const int64_t at = min((p0 + i * 256) * 8, f.values - 8);
+    if (f.base)
+      v[i] = load_global<Vec<T, 8>>(f.base + at);
+    else
+      v[i] = Vec<T, 8>{};
+  }
+#pragma unroll
+  for (int i = 0; i < kFillPieces / 256; ++i) {
+    const int64_t at = min((p0 + i * 256) * 8, f.values - 8);
+    if (p0 + i * 256 < f.end)
+      __builtin_nontemporal_store(v[i],
+                                  (__attribute__((address_space(1))) Vec<T, 8>*)(f.dtable + at));
+  }
+}
+
+template <typename T>
 __device__ __forceinline__ void embed_fill(const EmbedFill<T>& f, int64_t block) {
+  if (f.n == 0) return embed_fill_flat(f, block);
   const int per_row = (f.n + 7) / 8;
   constexpr int kAhead = 4;
   for (int i0 = 0; i0 < kFillPieces / 256; i0 += kAhead) {
@@ -139,7 +169,8 @@ __global__ __launch_bounds__(256) void k_embed_rank(const int64_t* __restrict__ 
   below[part][lane] = count;
   __syncthreads();
   if (part == 0 && me < rows)
-    out[below[0][lane] + below[1][lane] + below[2][lane] + below[3][lane]] = Named{key, (uint32_t)me};
+    out[below[0][lane] + below[1][lane] + below[2][lane] + below[3][lane]] =
+        Named{key, (uint32_t)me};
 }
 
 // One radix pass, over `bits` bits from `shift` on: block b takes the `each` entries from b * each
@@ -311,8 +342,8 @@ __global__ __launch_bounds__(256) void k_embed_sum(EmbedSum<T> a, int slabs) {
     embed_write(a, token, c, sum);
 }
 
-// Joins a token that begins in `piece` and goes on behind it: 64 threads take 512 columns, four such
-// groups every fourth of the pieces that follow, and the groups' sums are added in order.
+// Joins a token that begins in `piece` and goes on behind it: 64 threads take 512 columns, four
+// such groups every fourth of the pieces that follow, and the groups' sums are added in order.
 template <typename T>
 __global__ __launch_bounds__(256) void k_embed_join(EmbedSum<T> a, int slabs) {
   const int piece = (int)(blockIdx.x / slabs);

@@ -1,5 +1,5 @@
-// The ends of a language model: host side of lirpa_embed_* and lirpa_logprob_*.  Kernels: embed.hpp,
-// logprob.hpp.
+// The ends of a language model: host side of lirpa_embed_* and lirpa_logprob_*.  Kernels:
+// embed.hpp, logprob.hpp.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -48,13 +48,18 @@ int check_vocab(const char* who, int vocab) {
 // ---------------------------------------------------------------------------------------------
 int64_t pieces8(int n) { return (n + 7) / 8; }
 
-// Entries of a piece of the sums: few where there are few rows, more where a frequent token's pieces,
-// which one block joins, would be many.
+// Entries of a piece of the sums: few where there are few rows, more where a frequent token's
+// pieces, which one block joins, would be many.  Sums and join of bf16 rows, us: 3000 x 1000 9 + 10
+// with 8, 21 + 9 with 32; 16384 x 4096 34 + 15 with 16, 34 + 25 with 8; 60000 x 400 27 + 17 with
+// 32, 20 + 43 with 8.
 int sum_entries(int64_t rows) { return (int)std::clamp<int64_t>(rows >> 10 & ~7, 8, 32); }
 
 constexpr int kRadixBlocks = 256, kRadixLeast = 1024;
 
-constexpr int kNarrow = 128;  // columns of rows that share a block of the sums, 16 at a time
+// Up to so many columns 16 pieces share a block of the sums, 16 threads each; a block a piece
+// otherwise (4000 x 100: 11 us, 25 with a block a piece; 60000 x 400 takes 27 either way with 64
+// threads a piece).
+constexpr int kNarrow = 128;
 
 struct EmbedRoom {
   Named *a, *b;
@@ -96,8 +101,9 @@ struct Fills {
   int64_t total = 0, each = 0;
 
   Fills(T* dtable, int64_t ldd, const T* base, int64_t ldb, int vocab, int n, int launches) {
-    fill = {dtable, base, ldd, ldb, 0, 0, n};
-    if (base != dtable) total = vocab * pieces8(n);
+    const bool flat = ldd == n && (!base || ldb == n) && (int64_t)vocab * n >= 8;
+    fill = {dtable, base, ldd, ldb, 0, 0, (int64_t)vocab * n, flat ? 0 : n};
+    if (base != dtable) total = flat ? (fill.values + 7) / 8 : vocab * pieces8(n);
     each = up((total + launches - 1) / launches, kFillPieces);
   }
   // The next part: the blocks that it takes.
@@ -191,7 +197,11 @@ int embed_backward(int64_t rows, int n, int vocab, const int64_t* tokens, const 
 // ---------------------------------------------------------------------------------------------
 // Log probabilities
 // ---------------------------------------------------------------------------------------------
-// Few rows are split, so that about kFewBlocks blocks have work: rows * parts < 2 * kFewBlocks.
+// Few rows are split, so that about kFewBlocks blocks have work: rows * parts < 2 * kFewBlocks.  A
+// part costs a launch that joins (6 us, 10 with alternatives) and, with alternatives, its own
+// search (4 us): 61 rows of 50000 bf16 logits with 5 alternatives take 22 us in parts of about 256
+// blocks, 24 of 1024 and 26 of 4096; 300 rows 19 us whole and 30 in four parts, 8000 logits without
+// alternatives 8 and 13.
 constexpr int kFewBlocks = 256;
 void logprob_parts(int64_t rows, int n, int& parts, int& columns) {
   const int64_t most = std::min<int64_t>(kMaxParts, (n + kPartColumns - 1) / kPartColumns);
@@ -339,7 +349,8 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
     if (top < 0 || top > kTop)
       return fail(LIRPA_EINVAL, "%s: top = %d is outside [0, %d]", who, top, kTop);
     if (rows == 0) return (int)LIRPA_OK;
-    if (!logp && !lse && !entropy && !top) return fail(LIRPA_EINVAL, "%s: no output is wanted", who);
+    if (!logp && !lse && !entropy && !top)
+      return fail(LIRPA_EINVAL, "%s: no output is wanted", who);
     TRY(check_rows(who, "logits", dtype, logits, ldl, n));
     if (logp) TRY(check_tokens(who, tokens));
     TRY(check_floats(who, "logp", logp));

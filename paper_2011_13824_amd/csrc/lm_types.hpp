@@ -71,11 +71,11 @@ __device__ __forceinline__ void store_row(T* p, int valid, const float (&x)[N]) 
   }
 }
 
-// N columns of a row, for threads that stand side by side at multiples of N: the last piece of a row
-// that does not end with one is moved back to the row's end, so that every load is whole and without
-// a branch, and many can be on their way.  The columns that it shares with its neighbour are read by
-// both, and only the neighbour's are stored (`skip`: how many that are), so that an output may lie
-// in an input's place.  A row shorter than N is one piece, read one by one.
+// N columns of a row, for threads that stand side by side at multiples of N: the last piece of a
+// row that does not end with one is moved back to the row's end, so that every load is whole and
+// without a branch, and many can be on their way.  The columns that it shares with its neighbour
+// are read by both, and only the neighbour's are stored (`skip`: how many that are), so that an
+// output may lie in an input's place.  A row shorter than N is one piece, read one by one.
 template <int N>
 struct Columns {
   int at, skip, count;
@@ -109,8 +109,8 @@ __device__ __forceinline__ void floats(const Vec<T, N>& v, float (&x)[N]) {
   for (int i = 0; i < N; ++i) x[i] = (float)v[i];
 }
 
-// The 8 (N) columns that thread `id` of a matrix with `per_row` pieces a row takes.  The block's first
-// piece is divided in 64 bits once (uniform), the thread's offset from it in 32.
+// The 8 (N) columns that thread `id` of a matrix with `per_row` pieces a row takes.  The block's
+// first piece is divided in 64 bits once (uniform), the thread's offset from it in 32.
 struct Piece {
   int64_t row;
   int col;

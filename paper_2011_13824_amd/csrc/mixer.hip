@@ -1,5 +1,5 @@
-// What mixes the rows of a sequence: host side of lirpa_conv_* and lirpa_scan_*.  Kernels: conv.hpp,
-// scan.hpp.
+// What mixes the rows of a sequence: host side of lirpa_conv_* and lirpa_scan_*.  Kernels:
+// conv.hpp, scan.hpp.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -64,9 +64,10 @@ int by_taps(int taps, F&& f) {
 
 int64_t pieces(int n, int wide) { return (n + wide - 1) / wide; }
 
-// Rows of a strip, at least `least`: with those in front of it and, in the gradient, behind it (`more`)
-// a multiple of what is on its way at a time; the fewest of some sizes that leave no more than
-// kConvThreads threads.
+// Rows of a strip, at least `least`: with those in front of it and, in the gradient, behind it
+// (`more`) a multiple of what is on its way at a time; the fewest of some sizes that leave no more
+// than kConvThreads threads.  Forward, 8192 x 4096 bf16: 34 us with 2^18, 44 with 2^17 (strips of
+// 32), 37 with 2^19 (of 8); 4099 x 1001 f16: strips of 5 14 us, of 8 16.
 constexpr int64_t kConvThreads = (int64_t)1 << 18;
 constexpr int kConvLeast = 4, kConvBackLeast = 8;  // a strip of the gradient writes a part of dw
 int conv_strip(int64_t rows, int n, int wide, int ahead, int more, int least) {
@@ -142,7 +143,10 @@ int64_t scan_groups(int n, int states) {
 }
 
 // Rows are cut into chunks until there are kScanBlocks blocks, or kMostChunks chunks: their states
-// are linked one after the other.
+// are linked one after the other.  16 states, bf16, first walk, link and real walk, us: 8192 x 4096
+// 131 + 10 + 244 with 512 blocks, 115 + 14 + 183 with 1024, 105 + 11 + 178 with 2048; 512 x 1024
+// with chunks of 16 rows 8 + 9 + 11, of 64 11 + 6 + 18, of 256 29 + 6 + 51; 8192 x 256 with 64
+// chunks 18 + 15 + 29, with 512 14 + 97 + 19.
 constexpr int kScanBlocks = 2048, kMostChunks = 64;
 int64_t scan_most_chunks(int n, int states) {
   const int64_t groups = scan_groups(n, states);
@@ -355,7 +359,8 @@ int lirpa_conv_step(int dtype, int64_t rows, int n, int taps, const void* x, int
 }
 
 size_t lirpa_conv_workspace_bytes(int64_t rows, int n, int taps) {
-  if (rows < 0 || rows > kMaxRows || n < 1 || n > kMaxWidth || taps < 1 || taps > kMaxTaps) return 0;
+  if (rows < 0 || rows > kMaxRows || n < 1 || n > kMaxWidth || taps < 1 || taps > kMaxTaps)
+    return 0;
   return conv_bytes(rows, n, taps);
 }
 
