@@ -22,21 +22,6 @@ int check_tokens(const char* who, const void* p) {
   return LIRPA_OK;
 }
 
-int check_floats(const char* who, const char* what, const void* p) {
-  if ((uintptr_t)p % 4) return fail(LIRPA_EINVAL, "%s: %s is not aligned to its type", who, what);
-  return LIRPA_OK;
-}
-
-int check_ws(const char* who, const void* ws, size_t ws_bytes, size_t need) {
-  if (!ws) return fail(LIRPA_EINVAL, "%s: the workspace is null", who);
-  if (!aligned16(ws))
-    return fail(LIRPA_EINVAL, "%s: the workspace does not start on 16 bytes", who);
-  if (ws_bytes < need)
-    return fail(LIRPA_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes,
-                need);
-  return LIRPA_OK;
-}
-
 int check_vocab(const char* who, int vocab) {
   if (vocab < 1 || vocab > kMaxWidth)
     return fail(LIRPA_EINVAL, "%s: vocab %d is outside [1, 2^20]", who, vocab);

@@ -74,6 +74,22 @@ inline int check_in_place(const char* who, const char* out, const void* po, int6
               out, in, (long long)ldo, (long long)ldi);
 }
 
+inline int check_floats(const char* who, const char* what, const void* p, bool needed = false) {
+  if (needed && !p) return fail(LIRPA_EINVAL, "%s: %s is null", who, what);
+  if ((uintptr_t)p % 4) return fail(LIRPA_EINVAL, "%s: %s is not aligned to its type", who, what);
+  return LIRPA_OK;
+}
+
+inline int check_ws(const char* who, const void* ws, size_t ws_bytes, size_t need) {
+  if (!ws) return fail(LIRPA_EINVAL, "%s: the workspace is null", who);
+  if (!aligned16(ws))
+    return fail(LIRPA_EINVAL, "%s: the workspace does not start on 16 bytes", who);
+  if (ws_bytes < need)
+    return fail(LIRPA_ENOMEM, "%s: the workspace has %zu bytes, %zu are needed", who, ws_bytes,
+                need);
+  return LIRPA_OK;
+}
+
 #define TRY(x)                     \
   do {                             \
     int rc_ = (x);                 \
