@@ -389,7 +389,8 @@ int lirpa_embed_backward(int dtype, int64_t rows, int n, int vocab, const int64_
                          const void* dout, int64_t lddo, float scale, const void* base, int64_t ldb,
                          void* dtable, int64_t ldd, void* ws, size_t ws_bytes, hipStream_t stream);
 
-/* Of each row of logits l [n] (n is the vocabulary), scaled by scale > 0 (one over a temperature):
+/* Of each row of logits l [n] (n is the vocabulary), scaled by scale (one over a temperature; over 0,
+ * at most 2^100):
  *     lse = log(sum e^(scale l)),   logp = scale l_token - lse (0 for padding),
  *     entropy = -sum p log p with p = e^(scale l - lse),
  *     top_logp, top_tokens [rows][top]: the `top` (0 to 32) most likely tokens, the largest first,

@@ -233,7 +233,7 @@ __global__ __launch_bounds__(256) void k_embed_place(RadixPass r, EmbedFill<T> f
   const uint32_t lower = t ? sum[t - 1] : 0u;
   if (2 * t < bins) next[2 * t] = lower + before[0];
   if (2 * t + 1 < bins) next[2 * t + 1] = lower + all[0] + before[1];
-  for (int i = t; i < 4 * (1 << kMaxDigit); i += 256) mine[0][i] = 0;
+  for (int i = t; i < 1 << kMaxDigit; i += 256) mine[0][i] = mine[1][i] = mine[2][i] = mine[3][i] = 0;
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * r.each, end = min(first + r.each, r.rows);
   for (int64_t i0 = first; i0 < end; i0 += 256) {

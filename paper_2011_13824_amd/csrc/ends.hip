@@ -258,9 +258,15 @@ int logprob_backward(LogProbBack<T> a, hipStream_t st) {
   return LIRPA_OK;
 }
 
-int check_scale(const char* who, float scale, bool positive) {
-  if (!std::isfinite(scale) || (positive && !(scale > 0.f)))
-    return fail(LIRPA_EINVAL, "%s: scale must be finite%s", who, positive ? " and > 0" : "");
+int check_scale(const char* who, float scale) {
+  if (!std::isfinite(scale)) return fail(LIRPA_EINVAL, "%s: scale must be finite", who);
+  return LIRPA_OK;
+}
+
+// Of logits: its product with 1 / log 2 is a float too.
+int check_factor(const char* who, float scale) {
+  if (!(scale > 0.f) || scale > 0x1p100f)
+    return fail(LIRPA_EINVAL, "%s: scale must be over 0 and at most 2^100", who);
   return LIRPA_OK;
 }
 
@@ -275,7 +281,7 @@ int lirpa_embed_forward(int dtype, int64_t rows, int n, int vocab, const int64_t
     const char* who = "lirpa_embed_forward";
     TRY(check_shape(who, dtype, rows, n));
     TRY(check_vocab(who, vocab));
-    TRY(check_scale(who, scale, false));
+    TRY(check_scale(who, scale));
     if (rows == 0) return (int)LIRPA_OK;
     TRY(check_tokens(who, tokens));
     TRY(check_rows(who, "table", dtype, table, ldt, n));
@@ -301,7 +307,7 @@ int lirpa_embed_backward(int dtype, int64_t rows, int n, int vocab, const int64_
     const char* who = "lirpa_embed_backward";
     TRY(check_shape(who, dtype, rows, n));
     TRY(check_vocab(who, vocab));
-    TRY(check_scale(who, scale, false));
+    TRY(check_scale(who, scale));
     if (rows > 0) {
       TRY(check_tokens(who, tokens));
       TRY(check_rows(who, "dout", dtype, dout, lddo, n));
@@ -330,7 +336,7 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
   return guarded([&] {
     const char* who = "lirpa_logprob_forward";
     TRY(check_shape(who, dtype, rows, n));
-    TRY(check_scale(who, scale, true));
+    TRY(check_factor(who, scale));
     if (top < 0 || top > kTop)
       return fail(LIRPA_EINVAL, "%s: top = %d is outside [0, %d]", who, top, kTop);
     if (rows == 0) return (int)LIRPA_OK;
@@ -376,7 +382,7 @@ int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, i
   return guarded([&] {
     const char* who = "lirpa_logprob_backward";
     TRY(check_shape(who, dtype, rows, n));
-    TRY(check_scale(who, scale, true));
+    TRY(check_factor(who, scale));
     if (rows == 0) return (int)LIRPA_OK;
     if (!dlogp && !dentropy) return fail(LIRPA_EINVAL, "%s: no gradient comes in", who);
     TRY(check_rows(who, "logits", dtype, logits, ldl, n));

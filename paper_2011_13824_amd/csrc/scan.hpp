@@ -628,8 +628,8 @@ __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
     load_padded<LANES>(a.local, chunk + 1, a.n, at.col, at.lane, g);
   // Columns past the matrix have no part in the sums over columns: their delta u and p stay 0.
   for (int i = threadIdx.x; i < kSpan * kColumns; i += 256) {
-    sh.step[0][i] = make_float2(0.f, 0.f);
-    shp[0][i] = 0.f;
+    sh.step[i / kColumns][i % kColumns] = make_float2(0.f, 0.f);
+    shp[i / kColumns][i % kColumns] = 0.f;
   }
   __syncthreads();
   int64_t t0 = (end - 1) / kSpan * kSpan;
@@ -726,11 +726,11 @@ __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
     __syncthreads();
     for (int i = threadIdx.x; i < kSpan * 2 * kStates; i += 256) {
       const int r = i / (2 * kStates), k = i % (2 * kStates);
-      const float* w = &dBC[0][r][0][0] + k;
-      constexpr int kWave = kSpan * 2 * kStates;
+      const int vec = k / kStates, state = k % kStates;
       if (t0 + r < end)
         a.dBC[((int64_t)group * a.s.rows + t0 + r) * (2 * kStates) + k] =
-            (w[0] + w[kWave]) + (w[2 * kWave] + w[3 * kWave]);
+            (dBC[0][r][vec][state] + dBC[1][r][vec][state]) +
+            (dBC[2][r][vec][state] + dBC[3][r][vec][state]);
     }
     if (mine < end && at.own_at < a.n) {
       const bool inside = sh.flags[at.own_row] & kInside;

@@ -47,7 +47,7 @@ def test_embed_backward_refusals(L, bad, code):
 
 @pytest.mark.parametrize("bad,code", [
     (dict(dtype=5), -1), (dict(rows=-1), -1), (dict(n=0), -1), (dict(scale=0.0), -1),
-    (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(top=-1), -1), (dict(top=33), -1),
+    (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=2.0 ** 101), -1), (dict(top=-1), -1), (dict(top=33), -1),
     (dict(logits=None), -1), (dict(logits=ODD), -1), (dict(ldl=7), -1), (dict(tokens=None), -1),
     (dict(tokens=P + 4), -1), (dict(logp=P + 2), -1), (dict(lse=P + 2), -1),
     (dict(entropy=P + 1), -1), (dict(top_logp=None), -1), (dict(top_tokens=None), -1),
@@ -61,7 +61,8 @@ def test_logprob_forward_refusals(L, bad, code):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(dtype=5), dict(rows=-1), dict(n=0), dict(scale=0.0), dict(logits=None), dict(ldl=7),
+    dict(dtype=5), dict(rows=-1), dict(n=0), dict(scale=0.0), dict(scale=float("inf")),
+    dict(logits=None), dict(ldl=7),
     dict(tokens=None), dict(lse=None), dict(lse=P + 2), dict(entropy=None), dict(entropy=P + 2),
     dict(dlogp=P + 2), dict(dentropy=ODD), dict(dlogp=None, dentropy=None), dict(dlogits=None),
     dict(ldd=7), dict(dlogits=P, ldd=9)])

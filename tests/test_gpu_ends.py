@@ -323,6 +323,18 @@ def test_logprob_large_logits(B):
         assert torch.equal(a[i], b[i])
 
 
+def test_logprob_ends_of_the_scale(B):
+    """From logits that all count alike to the largest alone; equal ones share."""
+    x = torch.tensor([[0.0, 1.0, -3.0, 1.0, 0.5]], device="cuda")
+    t = torch.tensor([3], device="cuda")
+    for scale, logp, entropy in ((2.0 ** 100, -math.log(2), math.log(2)),
+                                 (2.0 ** -140, -math.log(5), math.log(5))):
+        r = B.LogProbs(scale, 5).forward(x, t)
+        assert abs(float(r.logp) - logp) < 1e-6 and abs(float(r.entropy) - entropy) < 1e-6
+        assert r.top_tokens[0].tolist() == [1, 3, 4, 0, 2]
+        assert torch.isfinite(r.top_logp[0, :2]).all()
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=ids)
 @pytest.mark.parametrize("rows,n,pad,shift", LOGIT_SHAPES)
 @pytest.mark.parametrize("which", ["logp", "entropy", "both", "in place"])
