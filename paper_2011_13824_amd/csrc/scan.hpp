@@ -62,20 +62,14 @@ struct Scan {
 // before); it fills the whole chunk, so that the state that enters is not replaced in it.
 constexpr int kGoesOn = 1, kWhole = 2;
 
-// log(1 + e^x) and, for its slope, e^-|x|.  log(1 + v) = 2 artanh(v / (2 + v)), whose series in the
-// square of that (at most 1/9) is cut where a term is under 2^-25 of the sum.
+// log(1 + e^x) and, for its slope, v = e^-|x|.  The logarithm instruction is right to a unit in the
+// last place, next to 1 too; what 1 + v loses of v is added again, where it counts (a small v), as it
+// is.  Together at most 3.3 x 2^-24 of log(1 + v), for 2^22 values of v in each of eight octaves down
+// to 2^-40.  (A series for the inverse hyperbolic tangent took 8 instructions more.)
 __device__ __forceinline__ float softplus(float x, float& v) {
   v = __builtin_amdgcn_exp2f(fabsf(x) * -1.44269504f);
-  const float s = v * __builtin_amdgcn_rcpf(2.f + v), q = s * s;
-  float r = 2.f / 15.f;
-  r = fmaf(r, q, 2.f / 13.f);
-  r = fmaf(r, q, 2.f / 11.f);
-  r = fmaf(r, q, 2.f / 9.f);
-  r = fmaf(r, q, 2.f / 7.f);
-  r = fmaf(r, q, 2.f / 5.f);
-  r = fmaf(r, q, 2.f / 3.f);
-  r = fmaf(r, q, 2.f);
-  return fmaf(s, r, fmaxf(x, 0.f));
+  const float w = 1.f + v;
+  return fmaf(__builtin_amdgcn_logf(w), 0.693147181f, v - (w - 1.f)) + fmaxf(x, 0.f);
 }
 __device__ __forceinline__ float softplus_slope(float x, float v) {
   return (x >= 0.f ? 1.f : v) * __builtin_amdgcn_rcpf(1.f + v);
