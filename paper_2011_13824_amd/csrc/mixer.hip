@@ -107,7 +107,8 @@ Conv<T> conv_args(int64_t rows, int n, const void* x, int64_t ldx, const void* w
 // ---------------------------------------------------------------------------------------------
 constexpr int kMaxStates = 64;
 
-// Lanes that share a column, four states each.
+// Lanes that share a column, four states each.  With eight, half the lanes and twice the chunks the
+// real walk of 8192 x 4096 with 16 states gains 7 us of 174, the first one and the link lose 23.
 int scan_lanes(int states) { return states <= 8 ? 2 : states <= 16 ? 4 : states <= 32 ? 8 : 16; }
 
 template <typename F>
