@@ -238,16 +238,25 @@ __global__ __launch_bounds__(256) void k_conv_bwd(Conv<T> a) {
   auto put = [&](int64_t row, const float(&v)[W]) {
     if (row >= at.first && row < at.end) store_columns<T, W>(a.dx + row * a.lddx, at.c, v);
   };
+  Vec<T, W> next_x[kConvAhead], next_dy[kConvAhead];
+  int next_slot[kConvAhead];
+  auto read = [&](int64_t from) {
+#pragma unroll
+    for (int j = 0; j < kConvAhead; ++j) {
+      const int64_t row = min(from + j, past - 1);
+      next_slot[j] = a.s.slot(row);
+      next_x[j] = load_columns<T, W>(a.x + row * a.ldx, at.c);
+      next_dy[j] = load_columns<T, W>(a.dy + row * a.lddy, at.c);
+    }
+  };
+  read(t);
   for (; t < past; t += kConvAhead) {
     Vec<T, W> rows[kConvAhead], dy[kConvAhead];
     int slot[kConvAhead];
 #pragma unroll
-    for (int j = 0; j < kConvAhead; ++j) {
-      const int64_t row = min(t + j, past - 1);
-      slot[j] = a.s.slot(row);
-      rows[j] = load_columns<T, W>(a.x + row * a.ldx, at.c);
-      dy[j] = load_columns<T, W>(a.dy + row * a.lddy, at.c);
-    }
+    for (int j = 0; j < kConvAhead; ++j)
+      rows[j] = next_x[j], dy[j] = next_dy[j], slot[j] = next_slot[j];
+    if (t + kConvAhead < past) read(t + kConvAhead);
 #pragma unroll
     for (int j = 0; j < kConvAhead; ++j) {
       if (t + j >= past) break;
@@ -276,11 +285,18 @@ __global__ __launch_bounds__(256) void k_conv_bwd(Conv<T> a) {
             d[i] *= p * fmaf(pre[i], 1.f - p, 1.f);
           }
         }
+        auto reach = [&](int k) {
 #pragma unroll
-        for (int k = 0; k < TAPS; ++k)
-          if (k <= age)
+          for (int i = 0; i < W; ++i) dx[k][i] = fmaf(taps.w[TAPS - 1 - k][i], d[i], dx[k][i]);
+        };
+        if (age >= TAPS - 1) {
 #pragma unroll
-            for (int i = 0; i < W; ++i) dx[k][i] = fmaf(taps.w[TAPS - 1 - k][i], d[i], dx[k][i]);
+          for (int k = 0; k < TAPS; ++k) reach(k);
+        } else {
+#pragma unroll
+          for (int k = 0; k < TAPS; ++k)
+            if (k <= age) reach(k);
+        }
         if (t + j < at.end) {
 #pragma unroll
           for (int i = 0; i < W; ++i) db[i] += d[i];
