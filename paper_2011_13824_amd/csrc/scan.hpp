@@ -75,6 +75,13 @@ __device__ __forceinline__ float softplus_slope(float x, float v) {
   return (x >= 0.f ? 1.f : v) * __builtin_amdgcn_rcpf(1.f + v);
 }
 
+// The value as it is at this place: a last addition is else moved behind the branch that stores its
+// sum, away from the lane exchange that it can be one instruction with.
+__device__ __forceinline__ float here(float x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // The sum over the LANES neighbouring lanes of a column; each gets it.  The second half of the
 // steps mirrors, which exchanges groups that already hold one value.
 template <int LANES>
@@ -594,7 +601,7 @@ __device__ __forceinline__ void wave_sums(const float (&v)[8], float (&out)[2]) 
     if constexpr (LANES <= 8) b[i] += ror(b[i], std::integral_constant<int, 0x128>{});
     if constexpr (LANES <= 4) b[i] += ror(b[i], std::integral_constant<int, 0x124>{});
     if constexpr (LANES <= 2) b[i] += ror(b[i], std::integral_constant<int, 0x122>{});
-    out[i] = b[i];
+    out[i] = here(b[i]);
   }
 }
 
@@ -697,9 +704,9 @@ __global__ __launch_bounds__(256) void k_scan_bwd(Scan<T> a, int groups) {
               dA[i] = fmaf(t, step.x, dA[i]);
             }
           }
-          cs = column_sum<LANES>(cs);
-          bs = column_sum<LANES>(bs);
-          es = column_sum<LANES>(es);
+          cs = here(column_sum<LANES>(cs));
+          bs = here(column_sum<LANES>(bs));
+          es = here(column_sum<LANES>(es));
           if (at.lane == 0) sums[row0 + r][column] = f32x4{cs, bs, es, 0.f};
           float two[2];
           wave_sums<LANES>(out, two);
