@@ -195,3 +195,60 @@ def test_tensors_of_another_device_are_refused(lirpa, B, monkeypatch):
                  lambda: B.SelectiveScan(w.t().contiguous()).forward(x, x, x[:, :4], x[:, :4])):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+def test_two_graphs_share_a_workspace(lirpa):
+    """Captured calls of other sizes in one workspace, replayed in turns: a call leaves nothing
+    there that the next one's results depend on."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    N, vocab = 16, 5000
+    sizes = [(700, 70), (260, 40)]
+    need = max(max(lirpa.lirpa_scan_workspace_bytes(r, n, N, 1),
+                   lirpa.lirpa_embed_workspace_bytes(r, n),
+                   lirpa.lirpa_conv_workspace_bytes(r, n, 4),
+                   lirpa.lirpa_logprob_workspace_bytes(r, vocab, 4)) for r, n in sizes)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+
+    def new(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+
+    def job(rows, n):
+        """(what to run, what it writes)"""
+        u, dt, z, dy, Bm, Cm = (new(rows, w) for w in (n, n, n, n, N, N))
+        A, w, tokens = -new(n, N).abs(), new(4, n), torch.randint(-1, vocab, (rows,), device="cuda")
+        seq = some_sequences(rows, g)
+        scan = lirpa.lirpa_scan_inputs(u, dt, Bm, Cm, z, A, None, None, seq)
+        kept = torch.empty(lirpa.lirpa_scan_kept_bytes(rows, n, N), dtype=torch.uint8,
+                           device="cuda")
+        logits = new(8, vocab)
+        out = [torch.empty_like(t) for t in (u, u, dt, z, Bm, Cm, A, u, w)]
+        out += [new(vocab, n), new(8), new(8), new(8, 4),
+                torch.empty(8, 4, dtype=torch.int64, device="cuda")]
+        y, du, ddt, dz, dB, dC, dA, dx, dw, dtable, lse, entropy, top, top_tokens = out
+
+        def run():
+            lirpa.lirpa_scan_forward(scan, None, None, y, kept, ws, need)
+            lirpa.lirpa_scan_backward(scan, dy, kept, du, ddt, dz, dB, dC, dA, None, None, ws, need)
+            lirpa.lirpa_conv_backward(dy, u, w, None, "silu", None, dx, dw, None, ws, need)
+            lirpa.lirpa_embed_backward(tokens, dy, 1.0, None, dtable, ws, need)
+            lirpa.lirpa_logprob_forward(logits, 1.0, None, None, lse, entropy, 4, top, top_tokens,
+                                        ws, need)
+
+        run.held = u, dt, z, dy, Bm, Cm, A, w, tokens, kept, logits, seq  # scan has their addresses
+        return run, out
+
+    jobs, graphs, want = [job(*s) for s in sizes], [], []
+    for run, out in jobs:
+        run()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in out])
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run()
+    for turn in (0, 1, 1, 0, 1, 0):
+        for t in jobs[turn][1]:
+            t.zero_()
+        graphs[turn].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(jobs[turn][1], want[turn])), turn
