@@ -336,6 +336,14 @@ __global__ __launch_bounds__(256) void k_scan_local(Scan<T> a, int groups) {
   put_deltas(a, at, chunk, group, sum, sh);
 }
 
+// 2^x h, where 2^x by itself may be no float: over a chunk a state that is 0 stays 0 and a small one
+// small, whatever an A over 0 makes of a state of 1.  Past 2^+-600 nothing is left to tell apart.
+__device__ __forceinline__ float decayed(float h, float x) {
+  x = __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -600.f), 600.f);
+  const float whole = floorf(x);
+  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(x - whole) * h, (int)whole);
+}
+
 // The states that enter the chunks, in the place of what the chunks add: that of chunk c + 1 stands
 // at c.  BACK: from the last chunk on; what enters chunk c from behind stands at c + 1.
 template <typename T, int LANES, bool BACK>
@@ -364,7 +372,7 @@ __global__ __launch_bounds__(256) void k_scan_link(Scan<T> a) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         // what a chunk without a link holds was never written
-        const float left = whole ? __builtin_amdgcn_exp2f(sum[j] * A2[k]) * h[k] : 0.f;
+        const float left = whole ? decayed(h[k], sum[j] * A2[k]) : 0.f;
         h[k] = goes_on ? left + add[j][k] : 0.f;
       }
       if (goes_on) store_padded<LANES>(a.local, c, a.n, col, lane, h);

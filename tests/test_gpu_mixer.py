@@ -416,6 +416,30 @@ def test_scan_in_parts(B):
     check(state[0], last[0][0], last[0][1] + 1e-37, "state")
 
 
+def test_scan_states_that_grow(B):
+    """An A over 0 whose growth over a chunk is no float: what it meets is 0, or that small."""
+    rows, n, N = 1200, 3, 2  # chunks of 32 rows
+    g = gen_of(12)
+    A = torch.tensor([[1.0, -1.0], [0.97, 0.5], [1.02, -0.1]], device="cuda")
+    u, dy = torch.zeros(2, rows, n, device="cuda").unbind()
+    dt = torch.full((rows, n), 2.8, device="cuda") + rand(g, rows, n, scale=0.05)
+    Bm, Cm = (rand(g, rows, N) for _ in range(2))
+    u[31] = 1e-30  # sequence 0 has 70 rows, sequence 1 all others but the last 3
+    u[-3:] = 1.0
+    dy[:40] = rand(g, 40, n, scale=1e-30)
+    dy[80:90] = 1.0
+    dy[-3:] = 1.0
+    seq = (torch.arange(rows, device="cuda") >= 70).to(torch.int32)
+    seq[-3:] = 2
+    want, _ = plain_scan(u, dt, Bm, Cm, None, A, None, None, runs_of(seq), dy=dy)
+    op = B.SelectiveScan(A)
+    y, kept = op.forward(u, dt, Bm, Cm, None, seq, keep=True)
+    within(y, want["y"], torch.float32, "y")
+    grads = op.backward(dy, kept)
+    for k in ("du", "ddt", "dB", "dC", "dA"):
+        within(grads[k], want[k], torch.float32, k)
+
+
 def test_scan_ends_of_softplus(B):
     """Steps from nothing to huge, and decays that leave nothing."""
     x = torch.tensor([-100.0, -60, -20, -1, 0, 1, 20, 88, 1000, 3e4], device="cuda")
