@@ -409,9 +409,11 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
 /* The gradient of the logits from those of logp and entropy (float [rows], either may be NULL) and
  * the lse and entropy (NULL where dentropy is) that the forward call returned:
  *     dl_j = scale (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)).
- * p comes from lse, whose rounding (2^-24 of its magnitude) is a relative error of it.  dlogp is
- * not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer of
- * logits. */
+ * p comes from lse, whose rounding (2^-24 of its magnitude) is a relative error of it, up to a
+ * magnitude of 256; past that the row's sums are taken again, at some 1.9 times the time.  An lse
+ * that is not the row's own (that of all logits, for a part of the columns) stands as it is given.
+ * dlogp is not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer
+ * of logits. */
 int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                            float scale, const int64_t* tokens, const float* lse,
                            const float* entropy, const float* dlogp, const float* dentropy,

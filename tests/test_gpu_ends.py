@@ -372,6 +372,99 @@ def test_logprob_backward(B, dtype, rows, n, pad, shift, which):
         assert torch.equal(logits, got) and not torch.equal(keep, got)
 
 
+def far_rows(g, n, dtype):
+    """Rows whose lse's rounding is no small part of log p: a shared offset, the ends of the type's
+    range in all places; and some that are not so."""
+    x = torch.randn(8, n, generator=g, device="cuda") * 2
+    x[1] += 3000.0
+    x[2] -= 5000.0
+    x[3] = torch.finfo(dtype).min
+    x[4] = torch.finfo(dtype).min
+    x[4, n // 2] = 1.0
+    x[5] = torch.finfo(dtype).max
+    x[6] += 300.0
+    x[6, ::3] = -INF
+    x[7] *= 1e4
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("n", [7, 2100, 70001])
+@pytest.mark.parametrize("scale", [1.0, 1.2])
+def test_logprob_backward_of_far_rows(B, dtype, n, scale):
+    """As good as near 0: the definition takes differences to the largest logit first."""
+    g = gen_of(n)
+    logits = far_rows(g, n, dtype)
+    tokens = torch.randint(0, n, (8,), generator=g, device="cuda")
+    tokens[4], tokens[7] = n // 2, -1
+    f = B.LogProbs(scale).forward(logits, tokens)
+    dlogp, dent = torch.randn(2, 8, generator=g, device="cuda")
+    s = torch.tensor(scale).double().item()
+    x = logits.double() * s
+    most = x.amax(1, keepdim=True)
+    d = x - most
+    log_total = torch.log(torch.exp(d).sum(1, keepdim=True))
+    lse, log_p = most + log_total, d - log_total
+    p = torch.exp(log_p)
+    gd, h = (tokens >= 0).double()[:, None] * dlogp.double()[:, None], dent.double()[:, None]
+    slope = torch.where(p > 0, log_p + f.entropy.double()[:, None], 0.0)
+    hit = torch.zeros_like(p).scatter_(1, tokens.clamp(0, n - 1)[:, None], 1.0)
+    want = s * (gd * hit - p * (gd + h * slope))
+    got = B.LogProbs(scale).backward(logits, tokens, f.lse, f.entropy, dlogp, dent)
+    # log p: the sum (as in compare), its logarithm, the difference and its product; where it is
+    # taken from lse, |lse| <= 256, the roundings of that and of the logit too
+    size = torch.where(p > 0, d, 0.0).abs()
+    span = torch.where(torch.isinf(d), 0.0, d).amin(1, keepdim=True).abs().clamp(max=200)
+    off = (n / 256 + 64 + 8 * span) * E + 4 * E * log_total.abs() + 3 * E * size
+    near0 = 4 * E * (lse.abs() + most.abs() + torch.where(p > 0, x, 0.0).abs())
+    off = off + torch.where(lse.abs() <= 260, near0, 0.0)
+    part = p * (gd.abs() + h.abs() * slope.abs())
+    tol = s * (part * (off + 3 * E * torch.where(p > 0, log_p, 0.0).abs() + 10 * E)
+               + p * h.abs() * (off + 2 * E * slope.abs()) + 4 * E * gd.abs() * hit)
+    # a p under 2^-126 is nothing; it meets at most 5 + 5 * 100
+    tol = tol + (UNIT[dtype] + E) * want.abs() + TINY[dtype] + 1e-35
+    bad = torch.isinf(logits).any(1) & (most[:, 0] == INF)  # 1e4 times the numbers, in f16
+    assert torch.isnan(got[bad]).all()
+    check(got[~bad], want[~bad], tol[~bad], "dlogits")
+    B.LogProbs(scale).backward(logits, tokens, f.lse, f.entropy, dlogp, dent, out=logits)
+    assert torch.equal(torch.nan_to_num(logits), torch.nan_to_num(got))
+
+
+def test_logprob_backward_where_products_are_no_floats(B):
+    """Logits whose product with scale is infinite: the largest takes all."""
+    x = torch.tensor([[1e9, 3e9, -2e9], [-1e9, -3e9, -2e9]], device="cuda")
+    scale, a = 1e30, torch.tensor([0.5, -2.0], device="cuda")
+    f = B.LogProbs(scale).forward(x, torch.tensor([0, 1], device="cuda"))
+    assert f.lse.tolist() == [INF, -INF] and f.entropy.tolist() == [0, 0]
+    got = B.LogProbs(scale).backward(x, torch.tensor([0, 1], device="cuda"), f.lse, dlogp=a)
+    v = (a * scale).tolist()
+    want = torch.tensor([[v[0], -v[0], 0], [-v[1], v[1], 0]], device="cuda")
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("offset", [0.0, 1000.0, -4000.0])
+def test_logprob_backward_of_a_part_of_the_vocabulary(B, offset):
+    """With the lse of all logits a part of their columns gets that part of the gradient."""
+    g = gen_of(int(abs(offset)))
+    x = torch.randn(5, 9000, generator=g, device="cuda") * 2 + offset
+    t = torch.tensor([3, 8999, 4500, -1, 0], device="cuda")
+    f = B.LogProbs().forward(x, t)
+    a, b = torch.randn(2, 5, generator=g, device="cuda")
+    want = B.LogProbs().backward(x, t, f.lse, f.entropy, a, b)
+    for part in (slice(0, 4500), slice(4500, 9000)):
+        mine = torch.where((t >= part.start) & (t < part.stop), t - part.start, -1)
+        # the token's own share is the call's that has it; -p dlogp is every part's
+        got = B.LogProbs().backward(x[:, part], mine, f.lse, f.entropy, None, b)
+        both = B.LogProbs().backward(x, t, f.lse, f.entropy, None, b)
+        p = torch.exp(x[:, part].double() - f.lse.double()[:, None])
+        # lse's rounding and forward's error, in log p and thereby in p (log p + H)
+        off = 4 * E * (f.lse.double().abs() + 200)[:, None]
+        tol = 2 * off * b.double().abs()[:, None] * p * (
+            1 + (torch.log(p) + f.entropy.double()[:, None]).abs())
+        check(got, both[:, part].double(), tol + 1e-37, "part")
+    assert torch.isfinite(want).all()
+
+
 def test_logprob_gradient_by_differences(B):
     """In 64 bits by the definition: the loss sum(a logp + b H)."""
     g = gen_of(11)
