@@ -63,9 +63,9 @@ struct Scan {
 constexpr int kGoesOn = 1, kWhole = 2;
 
 // log(1 + e^x) and, for its slope, v = e^-|x|.  The logarithm instruction is right to a unit in the
-// last place, next to 1 too; what 1 + v loses of v is added again, where it counts (a small v), as it
-// is.  Together at most 3.3 x 2^-24 of log(1 + v), for 2^22 values of v in each of eight octaves down
-// to 2^-40.  (A series for the inverse hyperbolic tangent took 8 instructions more.)
+// last place, next to 1 too; what 1 + v loses of v is added again, where it counts (a small v), as
+// it is.  Together at most 3.3 x 2^-24 of log(1 + v), for 2^22 values of v in each of eight octaves
+// down to 2^-40.  (A series for the inverse hyperbolic tangent took 8 instructions more.)
 __device__ __forceinline__ float softplus(float x, float& v) {
   v = __builtin_amdgcn_exp2f(fabsf(x) * -1.44269504f);
   const float w = 1.f + v;
