@@ -364,19 +364,30 @@ __global__ __launch_bounds__(256) void k_scan_link(Scan<T> a) {
       load_padded<LANES>(a.local, c, a.n, col, lane, add[j]);
       sum[j] = load_global<float>(a.deltas + (int64_t)c * a.n + col);
     }
+    auto follow = [&](auto grows) {
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (i0 + j + 1 >= a.chunks) break;
-      const int c = BACK ? a.chunks - 1 - (i0 + j) : i0 + j;
-      const bool goes_on = link[j] & kGoesOn, whole = link[j] & kWhole;
+      for (int j = 0; j < kAhead; ++j) {
+        if (i0 + j + 1 >= a.chunks) break;
+        const int c = BACK ? a.chunks - 1 - (i0 + j) : i0 + j;
+        const bool goes_on = link[j] & kGoesOn, whole = link[j] & kWhole;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // what a chunk without a link holds was never written
-        const float left = whole ? decayed(h[k], sum[j] * A2[k]) : 0.f;
-        h[k] = goes_on ? left + add[j][k] : 0.f;
+        for (int k = 0; k < 4; ++k) {
+          // what a chunk without a link holds was never written
+          const float x = sum[j] * A2[k];
+          const float left = !whole        ? 0.f
+                             : grows.value ? decayed(h[k], x)
+                                           : __builtin_amdgcn_exp2f(x) * h[k];
+          h[k] = goes_on ? left + add[j][k] : 0.f;
+        }
+        if (goes_on) store_padded<LANES>(a.local, c, a.n, col, lane, h);
       }
-      if (goes_on) store_padded<LANES>(a.local, c, a.n, col, lane, h);
-    }
+    };
+    // Without an A over 0 nothing grows.  8192 x 4096: 8.9 us; taking `decayed` for all 11.9, asking
+    // before the first loads 11.1.
+    if (A[0] > 0.f || A[1] > 0.f || A[2] > 0.f || A[3] > 0.f)
+      follow(std::true_type{});
+    else
+      follow(std::false_type{});
   }
 }
 
