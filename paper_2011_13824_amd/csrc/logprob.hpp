@@ -21,7 +21,7 @@
 //
 // Bound by bytes and nearly as much by the vector units (9 instructions and an exponential of two a
 // logit).  4096 rows of 128000 bf16 logits: 187 us for 1.05 GB (5.6 TB/s, vector units 87 % busy),
-// the gradient 405 us for 2.1 GB (5.2 TB/s, 79 %).  One row of 128000 with 20 alternatives: 10 + 8
+// the gradient 405 us for 2.1 GB (5.2 TB/s, 68 %).  One row of 128000 with 20 alternatives: 10 + 8
 // us, latency.
 #pragma once
 
