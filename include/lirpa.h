@@ -481,9 +481,9 @@ int lirpa_scan_forward(const lirpa_scan* scan, const float* state, float* state_
 int lirpa_scan_step(const lirpa_scan* scan, const float* state, float* state_out, void* y,
                     int64_t ldy, hipStream_t stream);
 
-/* Gradients from what was kept, for the same inputs: du, ddt, dz (NULL without z) [rows][n], dB, dC
- * [rows][states] of dtype; dA [n][states], dD, dbias [n] of float, each NULL where it is not
- * wanted. */
+/* Gradients from what was kept, for the same inputs and slots (what was padding has no states in
+ * kept): du, ddt, dz (NULL without z) [rows][n], dB, dC [rows][states] of dtype; dA [n][states], dD,
+ * dbias [n] of float, each NULL where it is not wanted. */
 int lirpa_scan_backward(const lirpa_scan* scan, const void* dy, int64_t lddy, const void* kept,
                         void* du, int64_t lddu, void* ddt, int64_t ldddt, void* dz, int64_t lddz,
                         void* dB, int64_t lddB, void* dC, int64_t lddC, float* dA, float* dD,

@@ -288,10 +288,11 @@ class CausalConv:
 
 
 class KeptScan:
-    """What SelectiveScan.forward kept for its backward pass: the inputs, and states of the walk."""
+    """What SelectiveScan.forward kept for its backward pass: the inputs, states of the walk, and the
+    number of slots, on which depends what is padding."""
 
-    def __init__(self, u, dt, B, C, z, seq, states):
-        self.inputs, self.seq, self.states = (u, dt, B, C, z), seq, states
+    def __init__(self, u, dt, B, C, z, seq, states, slots=lirpa.ANY_SLOT):
+        self.inputs, self.seq, self.states, self.slots = (u, dt, B, C, z), seq, states, slots
 
 
 class SelectiveScan:
@@ -304,8 +305,8 @@ class SelectiveScan:
     def __init__(self, A, D=None, bias=None):
         self.A, self.D, self.bias = A, D, bias
 
-    def _inputs(self, u, dt, B, C, z, seq):
-        return lirpa.lirpa_scan_inputs(u, dt, B, C, z, self.A, self.D, self.bias, seq)
+    def _inputs(self, u, dt, B, C, z, seq, slots=lirpa.ANY_SLOT):
+        return lirpa.lirpa_scan_inputs(u, dt, B, C, z, self.A, self.D, self.bias, seq, slots)
 
     def forward(self, u, dt, B, C, z=None, seq=None, state=None, state_out=None, keep=False):
         """y; with ``keep`` (y, KeptScan), for sequences that begin with states of 0."""
@@ -319,7 +320,7 @@ class SelectiveScan:
         kept = _bytes(lirpa.lirpa_scan_kept_bytes(*size), u.device) if keep else None
         need = lirpa.lirpa_scan_workspace_bytes(*size, 0)
         lirpa.lirpa_scan_forward(scan, state, state_out, y, kept, _bytes(need, u.device), need)
-        return (y, KeptScan(u, dt, B, C, z, seq, kept)) if keep else y
+        return (y, KeptScan(u, dt, B, C, z, seq, kept, scan.kept_slots)) if keep else y
 
     def step(self, u, dt, B, C, z=None, state=None, seq=None, state_out=None):
         """One row of every sequence: row t is that of slot seq[t], of slot t without seq."""
@@ -333,7 +334,7 @@ class SelectiveScan:
         """The gradients of what the forward pass took: du, ddt, dB, dC, dA, and dz, dD, dbias where
         there are z, D and bias."""
         u, dt, B, C, z = kept.inputs
-        scan = self._inputs(u, dt, B, C, z, kept.seq)
+        scan = self._inputs(u, dt, B, C, z, kept.seq, kept.slots)
         like = {"du": u, "ddt": dt, "dz": z, "dB": B, "dC": C, "dA": self.A, "dD": self.D,
                 "dbias": self.bias}
         grads = {k: torch.empty_like(t) for k, t in like.items() if t is not None}

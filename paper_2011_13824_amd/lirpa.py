@@ -615,14 +615,21 @@ def _state(t, rest, dtype, what):
     return shape[0], _dev(t, dtype, what)
 
 
-def _slots(state, state_out, rest, dtype):
-    """(slots, pointers of state and state_out) of [slots, *rest] tensors."""
+def _slots(state, state_out, rest, dtype, without=ANY_SLOT):
+    """(slots, pointers of state and state_out) of [slots, *rest] tensors; `without`: the slots where
+    neither is given."""
     n_in, p_in = _state(state, rest, dtype, "state")
     n_out, p_out = _state(state_out, rest, dtype, "state_out")
     if n_in is not None and n_out is not None and n_in != n_out:
         raise ValueError(f"state has {n_in} slots, state_out {n_out}")
     slots = n_out if n_in is None else n_in
-    return ANY_SLOT if slots is None else slots, p_in, p_out
+    return without if slots is None else slots, p_in, p_out
+
+
+def _slot_count(slots):
+    if not 1 <= slots <= ANY_SLOT:
+        raise ValueError(f"slots must be 1 to 2^31 - 1, got {slots}")
+    return slots
 
 
 def _conv(call, x, w, bias, act, seq, state, state_out, y, stream):
@@ -666,7 +673,8 @@ def lirpa_conv_backward(dy, x, w, bias, act, seq, dx, dw, dbias, ws, ws_bytes, s
 
 
 def lirpa_scan_inputs(u, dt, B, C, z, A, D, bias, seq, slots=ANY_SLOT):
-    """The lirpa_scan of device tensors, which have to outlive the calls that take it."""
+    """The lirpa_scan of device tensors, which have to outlive the calls that take it.  ``slots``
+    holds for calls without states: rows of a number from there on are padding."""
     rows, n = _2d(u, "u")
     states = _2d(A, "A")[1]
     kind, f32 = _dtype(u, "u"), torch.float32
@@ -678,7 +686,7 @@ def lirpa_scan_inputs(u, dt, B, C, z, A, D, bias, seq, slots=ANY_SLOT):
     pC, ldC = _matrix(C, rows, states, kind, "C")
     return lirpa_scan(DTYPES[kind], rows, n, states, pu, pdt, pz, pB, pC, ldu, lddt, ldz, ldB, ldC,
                       _vector(A, n * states, f32, "A"), _vector(D, n, f32, "D"),
-                      _vector(bias, n, f32, "bias"), _seq(seq, rows), slots)
+                      _vector(bias, n, f32, "bias"), _seq(seq, rows), _slot_count(slots))
 
 
 def lirpa_scan_workspace_bytes(rows, n, states, backward) -> int:
@@ -700,36 +708,51 @@ def _kept_states(kept, scan):
     return _dev(kept, None, "kept")
 
 
+def _with_slots(scan, slots):
+    """The scan with other slots: a caller's struct stays as it is."""
+    if slots != scan.slots:
+        scan = lirpa_scan.from_buffer_copy(scan)
+        scan.slots = slots
+    return ctypes.byref(scan)
+
+
 def lirpa_scan_forward(scan, state, state_out, y, kept, ws, ws_bytes, stream=None):
-    """``scan`` is what lirpa_scan_inputs returned; its slots become those of the states."""
+    """``scan`` is what lirpa_scan_inputs returned.  The slots are those of the states, or the scan's
+    without any; ``kept`` is of these, and the scan notes them (kept_slots) for its backward pass."""
     rows, n, states, dt = _of_scan(scan)
     st = _here(stream, state, state_out, y, kept, ws)
-    scan.slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32)
+    slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32, scan.slots)
     _check(load().lirpa_scan_forward(
-        ctypes.byref(scan), s_in, s_out, *_matrix(y, rows, n, dt, "y"), _kept_states(kept, scan),
-        _dev(ws, None, "ws"), int(ws_bytes), st))
+        _with_slots(scan, slots), s_in, s_out, *_matrix(y, rows, n, dt, "y"),
+        _kept_states(kept, scan), _dev(ws, None, "ws"), int(ws_bytes), st))
+    if kept is not None:
+        scan.kept_slots = slots
 
 
 def lirpa_scan_step(scan, state, state_out, y, stream=None):
     rows, n, states, dt = _of_scan(scan)
     st = _here(stream, state, state_out, y)
-    scan.slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32)
-    _check(load().lirpa_scan_step(ctypes.byref(scan), s_in, s_out, *_matrix(y, rows, n, dt, "y"),
-                                  st))
+    slots, s_in, s_out = _slots(state, state_out, (n, states), torch.float32, scan.slots)
+    _check(load().lirpa_scan_step(_with_slots(scan, slots), s_in, s_out,
+                                  *_matrix(y, rows, n, dt, "y"), st))
 
 
 def lirpa_scan_backward(scan, dy, kept, du, ddt, dz, dB, dC, dA, dD, dbias, ws, ws_bytes,
-                        stream=None):
+                        stream=None, slots=None):
+    """``slots``: those that ``kept`` is of; by default those of the scan's last call that kept, or
+    the scan's own."""
     rows, n, states, dt = _of_scan(scan)
     f32 = torch.float32
     st = _here(stream, dy, kept, du, ddt, dz, dB, dC, dA, dD, dbias, ws)
+    if slots is None:
+        slots = getattr(scan, "kept_slots", scan.slots)
     _check(load().lirpa_scan_backward(
-        ctypes.byref(scan), *_matrix(dy, rows, n, dt, "dy"), _kept_states(kept, scan),
-        *_matrix(du, rows, n, dt, "du"), *_matrix(ddt, rows, n, dt, "ddt"),
-        *_matrix(dz, rows, n, dt, "dz"), *_matrix(dB, rows, states, dt, "dB"),
-        *_matrix(dC, rows, states, dt, "dC"), _vector(dA, n * states, f32, "dA"),
-        _vector(dD, n, f32, "dD"), _vector(dbias, n, f32, "dbias"), _dev(ws, None, "ws"),
-        int(ws_bytes), st))
+        _with_slots(scan, _slot_count(slots)), *_matrix(dy, rows, n, dt, "dy"),
+        _kept_states(kept, scan), *_matrix(du, rows, n, dt, "du"),
+        *_matrix(ddt, rows, n, dt, "ddt"), *_matrix(dz, rows, n, dt, "dz"),
+        *_matrix(dB, rows, states, dt, "dB"), *_matrix(dC, rows, states, dt, "dC"),
+        _vector(dA, n * states, f32, "dA"), _vector(dD, n, f32, "dD"),
+        _vector(dbias, n, f32, "dbias"), _dev(ws, None, "ws"), int(ws_bytes), st))
 
 
 class Network:

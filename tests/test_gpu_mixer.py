@@ -639,3 +639,70 @@ def test_binding_checks(B):
         conv.forward(s["x"].clone().requires_grad_())
     with pytest.warns(UserWarning, match="autograd"):
         op.forward(s["u"].clone().requires_grad_(), *pass_on(s)[1:])
+
+
+# ---------------------------------------------------------------------------------------------
+# Gradients where the last sequences have no slot
+# ---------------------------------------------------------------------------------------------
+def slotless(g, rows, *tensors):
+    """(seq, slots, runs, rows of sequences with a slot): the last sequences have none, and hold NaN
+    in the given tensors."""
+    seq = layout(g, rows, "ragged")
+    slots = int(seq.max()) - 2
+    runs = runs_of(seq, slots)
+    assert 0 < len(runs) < len(runs_of(seq))
+    inside = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    for a, r, _ in runs:
+        inside[a:a + r] = True
+    for t in tensors:
+        t[~inside] = float("nan")
+    return seq, slots, runs, inside
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,N", [(450, 37, 16), (450, 70, 5), (130, 20, 40), (1500, 33, 16)])
+def test_scan_gradient_of_rows_without_a_slot(B, lirpa, dtype, rows, n, N):
+    """What was padding in the forward pass is so in the backward pass, whatever came between."""
+    g = gen_of(rows + N)
+    s = scan_inputs(g, rows, n, N, dtype)
+    dy = rand(g, rows, n, dtype=dtype)
+    seq, slots, runs, inside = slotless(g, rows, dy, *pass_on(s))
+    want, last = plain_scan(**s, runs=runs, dy=dy)
+    op = B.SelectiveScan(s["A"], s["D"], s["bias"])
+    out = torch.zeros(slots, n, N, device="cuda")
+    y, kept = op.forward(*pass_on(s), seq, state_out=out, keep=True)
+    within(y, want["y"], dtype, "y")
+    for _, _, i in runs:
+        check(out[i], last[i][0], last[i][1] + E * last[i][0].abs() + 1e-37, f"state {i}")
+    assert kept.slots == slots
+    grads = op.backward(dy, kept)
+    for k, v in grads.items():
+        within(v, want[k], torch.float32 if k in ("dA", "dD", "dbias") else dtype, k)
+    for k in ("du", "ddt", "dz", "dB", "dC"):
+        assert (grads[k][~inside] == 0).all(), k
+
+    # the library's calls on one lirpa_scan: a call without kept leaves the gradient's slots alone
+    scan = lirpa.lirpa_scan_inputs(*pass_on(s), s["A"], s["D"], s["bias"], seq)
+    size = (rows, n, N)
+    states = torch.empty(lirpa.lirpa_scan_kept_bytes(*size), dtype=torch.uint8, device="cuda")
+    need = max(lirpa.lirpa_scan_workspace_bytes(*size, back) for back in (0, 1))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    y2 = torch.empty_like(y)
+    lirpa.lirpa_scan_forward(scan, None, out, y2, states, ws, need)
+    assert torch.equal(y2, y)
+    many = torch.zeros(slots + 9, n, N, device="cuda")
+    lirpa.lirpa_scan_forward(scan, None, many, torch.empty_like(y), None, ws, need)
+    lirpa.lirpa_scan_step(scan, many, None, torch.empty_like(y))
+    assert scan.slots == lirpa.ANY_SLOT
+    order = ("du", "ddt", "dz", "dB", "dC", "dA", "dD", "dbias")
+    for more in ({}, {"slots": slots}):
+        again = {k: torch.empty_like(grads[k]) for k in order}
+        lirpa.lirpa_scan_backward(scan, dy, states, *again.values(), ws, need, **more)
+        assert all(torch.equal(again[k], grads[k]) for k in order)
+
+    # without states the scan's own slots hold
+    scan = lirpa.lirpa_scan_inputs(*pass_on(s), s["A"], s["D"], s["bias"], seq, slots)
+    lirpa.lirpa_scan_forward(scan, None, None, y2.fill_(7.0), states, ws, need)
+    assert torch.equal(y2, y)
+    with pytest.raises(ValueError, match="slots"):
+        lirpa.lirpa_scan_backward(scan, dy, states, *again.values(), ws, need, slots=1 << 31)
