@@ -433,7 +433,8 @@ int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, i
  *   Slots that no row names are not touched.  A slot is named by one sequence of a call; if it is
  *   named by more, its state is one of theirs, or parts of several.
  * - *_step takes one row of every sequence: row t is that of slot seq[t] (slot t without seq).
- * - The backward passes are those of sequences that begin with states of 0.
+ * - The backward passes are those of sequences that begin with states of 0; their slots are those of
+ *   the forward pass, where it wrote states.
  * ============================================================================================= */
 typedef enum { LIRPA_CONV_LINEAR = 0, LIRPA_CONV_SILU = 1 } lirpa_conv_act;
 

@@ -274,8 +274,10 @@ class CausalConv:
         lirpa.lirpa_conv_step(x, self.w, self.bias, self.act, seq, state, state_out, y)
         return y
 
-    def backward(self, dy, x, seq=None):
-        """{"dx", "dw", "dbias"} (dbias where there is a bias), for sequences without a state."""
+    def backward(self, dy, x, seq=None, slots=lirpa.ANY_SLOT):
+        """{"dx", "dw", "dbias"} (dbias where there is a bias), for sequences without a state.  Where
+        the forward pass had a state_out, ``slots`` is the number of its slots: rows of a number from
+        there on were padding."""
         lirpa._2d(x, "x")
         dx = torch.empty_like(x)
         grads = {"dx": dx, "dw": torch.empty_like(self.w)}
@@ -283,7 +285,7 @@ class CausalConv:
             grads["dbias"] = torch.empty_like(self.bias)
         need = lirpa.lirpa_conv_workspace_bytes(*x.shape, self.w.shape[0])
         lirpa.lirpa_conv_backward(dy, x, self.w, self.bias, self.act, seq, dx, grads["dw"],
-                                  grads.get("dbias"), _bytes(need, x.device), need)
+                                  grads.get("dbias"), _bytes(need, x.device), need, slots=slots)
         return grads
 
 

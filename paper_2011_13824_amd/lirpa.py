@@ -658,7 +658,9 @@ def lirpa_conv_workspace_bytes(rows, n, taps) -> int:
     return int(load().lirpa_conv_workspace_bytes(int(rows), int(n), int(taps)))
 
 
-def lirpa_conv_backward(dy, x, w, bias, act, seq, dx, dw, dbias, ws, ws_bytes, stream=None):
+def lirpa_conv_backward(dy, x, w, bias, act, seq, dx, dw, dbias, ws, ws_bytes, stream=None,
+                        slots=ANY_SLOT):
+    """``slots``: those of the forward pass, the number that its states had."""
     rows, n = _2d(x, "x")
     taps = _2d(w, "w")[0]
     dt = _dtype(x, "x")
@@ -668,8 +670,9 @@ def lirpa_conv_backward(dy, x, w, bias, act, seq, dx, dw, dbias, ws, ws_bytes, s
     _check(load().lirpa_conv_backward(
         DTYPES[dt], rows, n, taps, *_matrix(dy, rows, n, dt, "dy"), *_matrix(x, rows, n, dt, "x"),
         _vector(w, taps * n, dt, "w"), _vector(bias, n, dt, "bias"), CONV_ACTS[act],
-        _seq(seq, rows), ANY_SLOT, *_matrix(dx, rows, n, dt, "dx"), _vector(dw, taps * n, dt, "dw"),
-        _vector(dbias, n, dt, "dbias"), _dev(ws, None, "ws"), int(ws_bytes), st))
+        _seq(seq, rows), _slot_count(slots), *_matrix(dx, rows, n, dt, "dx"),
+        _vector(dw, taps * n, dt, "dw"), _vector(dbias, n, dt, "dbias"), _dev(ws, None, "ws"),
+        int(ws_bytes), st))
 
 
 def lirpa_scan_inputs(u, dt, B, C, z, A, D, bias, seq, slots=ANY_SLOT):

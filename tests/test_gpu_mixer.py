@@ -706,3 +706,23 @@ def test_scan_gradient_of_rows_without_a_slot(B, lirpa, dtype, rows, n, N):
     assert torch.equal(y2, y)
     with pytest.raises(ValueError, match="slots"):
         lirpa.lirpa_scan_backward(scan, dy, states, *again.values(), ws, need, slots=1 << 31)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,taps", [(450, 37, 4), (130, 20, 8), (1500, 130, 3)])
+def test_conv_gradient_of_rows_without_a_slot(B, dtype, rows, n, taps):
+    g = gen_of(rows + taps)
+    x, dy = (rand(g, rows, n, dtype=dtype) for _ in range(2))
+    w, b = rand(g, taps, n, dtype=dtype), rand(g, 1, n, dtype=dtype)[0]
+    seq, slots, runs, inside = slotless(g, rows, x, dy)
+    op = B.CausalConv(w, b)
+    want, _ = plain_conv(x, w, b, "silu", runs, dy=dy)
+    out = torch.zeros(slots, taps - 1, n, dtype=dtype, device="cuda")
+    within(op.forward(x, seq, state_out=out), want["y"], dtype, "y")
+    grads = op.backward(dy, x, seq, slots)
+    for k, v in grads.items():
+        within(v, want[k], dtype, k)
+    assert (grads["dx"][~inside] == 0).all()
+    for bad in (0, -1, 1 << 31, (1 << 32) + 3):
+        with pytest.raises(ValueError, match="slots"):
+            op.backward(dy, x, seq, bad)
