@@ -411,8 +411,9 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
  *     dl_j = scale (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)).
  * p comes from lse, whose rounding (2^-24 of its magnitude) is a relative error of it, up to a
  * magnitude of 256; past that the row's sums are taken again, at some 1.9 times the time.  An lse
- * that is not the row's own (that of all logits, for a part of the columns) stands as it is given.
- * dlogp is not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer
+ * that is not the row's own (that of all logits, for a part of the columns) stands as it is given,
+ * but for one past 256 that its own rounding does not tell from the row's: within 5/8 of the distance
+ * of two floats there, p is taken from the row's sums.  dlogp is not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer
  * of logits. */
 int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                            float scale, const int64_t* tokens, const float* lse,

@@ -422,11 +422,14 @@ __global__ __launch_bounds__(256) void k_logprob_back(LogProbBack<T> a) {
     if (threadIdx.x == 0) row_most = s.most, row_total = s.total;
     __syncthreads();
     const float most = row_most, total = row_total;
-    // the row's own log S, where lse is its lse but for rounding; else what the given one says
+    // the row's own log S, where lse is a rounding of its lse; else what the given one says
     float log_total = logf(total);
-    const float own = fmaf(most, a.scale, log_total);
-    if (!(own == lse || fabsf(own - lse) <= 0x1p-22f * fabsf(lse)))
-      log_total = fmaf(-most, a.scale, lse);
+    const float own = fmaf(most, a.scale, log_total), given = fmaf(-most, a.scale, lse);
+    // Half the distance of floats at lse, and a quarter more for log S in another order of its sum:
+    // an lse of more than the row's logits (of all columns, where these are a part) that is nearer
+    // than that cannot be told from the row's own.
+    const float half_step = __uint_as_float(__float_as_uint(lse) & 0x7f800000u) * 0x1p-24f;
+    if (!(own == lse || fabsf(given - log_total) < 1.25f * half_step)) log_total = given;
     const bool empty = total == 0.f && own == lse;  // no logit over -inf: nothing to move
     walk<T>(l, 0, a.n, [&](const float(&v)[8], int col) {
       float d[8];

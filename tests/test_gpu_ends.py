@@ -607,3 +607,35 @@ def test_binding_checks(B):
         B.Embedding(x).backward(t, x, base=x.half())
     with pytest.raises(ValueError, match="contiguous"):
         B.LogProbs().backward(x, t, torch.zeros(1, device="cuda").expand(4), dlogp=x[:, 0])
+
+
+@pytest.mark.parametrize("offset", [300.0, -270.0, 4000.0, -5000.0, 65536.0, 1e6, -1e6])
+def test_logprob_backward_of_a_part_that_holds_most(B, offset):
+    """The lse of all logits stands in a part that holds nearly all of them too: where it differs from
+    the part's own by a few steps of 32 bits, p is off by no more than lse's rounding explains."""
+    n = 3000
+    step = 2.0 ** (math.frexp(offset)[1] - 24)  # the distance of floats there
+    shares = torch.tensor([0.3, 0.8, 1.0, 1.5, 2.0, 3.0, 3.9, 6.0], device="cuda") * step
+    rows = len(shares)
+    g = gen_of(int(abs(offset)))
+    x = torch.randn(rows, 2 * n, generator=g, device="cuda") * 2
+    mass = torch.logsumexp(x[:, :n], 1) - torch.logsumexp(x[:, n:], 1)
+    x[:, n:] += (mass + torch.log(torch.expm1(shares)))[:, None]  # log(1 + the rest) is the share
+    x += offset
+    t = torch.randint(0, n, (rows,), generator=g, device="cuda")
+    f = B.LogProbs().forward(x, t)
+    assert (f.lse.abs() > 256).all()
+    total = torch.zeros(rows, dtype=torch.float64, device="cuda")
+    for part in (slice(0, n), slice(n, 2 * n)):
+        l = x[:, part]
+        got = -B.LogProbs().backward(l, t, f.lse, dlogp=torch.ones(rows, device="cuda")).double()
+        hit = torch.zeros_like(got).scatter_(1, t[:, None], 1.0)
+        p = torch.exp(l.double() - f.lse.double()[:, None])
+        d = l.double() - l.double().amax(1, keepdim=True)
+        # 5/8 of a step where p is from the part's own sum; that sum's order, its logarithm, the
+        # differences and their exponential
+        off = math.expm1(0.625 * step) + (n / 256 + 64 + 4 * d.abs()) * E
+        check(got + hit, p, p * off + 2 * E * hit + 1e-37, f"part from {part.start}")
+        total += (got + hit).sum(1)
+    # both parts: lse's own rounding, and the first part's 5/8 of a step
+    assert ((total - 1).abs() <= math.expm1(1.2 * step) + (n / 256 + 200) * E).all()
