@@ -413,8 +413,9 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
  * magnitude of 256; past that the row's sums are taken again, at some 1.9 times the time.  An lse
  * that is not the row's own (that of all logits, for a part of the columns) stands as it is given,
  * but for one past 256 that its own rounding does not tell from the row's: within 5/8 of the distance
- * of two floats there, p is taken from the row's sums.  dlogp is not read for padding.  A row of -inf alone takes no gradient.  dlogits may be the buffer
- * of logits. */
+ * of two floats there, p is taken from the row's sums.  dlogp is not read for padding, and a token
+ * that lies outside a part is padding there: the part then lacks its -scale dlogp p.  A row of -inf
+ * alone takes no gradient.  dlogits may be the buffer of logits. */
 int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                            float scale, const int64_t* tokens, const float* lse,
                            const float* entropy, const float* dlogp, const float* dentropy,

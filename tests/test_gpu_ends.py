@@ -639,3 +639,35 @@ def test_logprob_backward_of_a_part_that_holds_most(B, offset):
         total += (got + hit).sum(1)
     # both parts: lse's own rounding, and the first part's 5/8 of a step
     assert ((total - 1).abs() <= math.expm1(1.2 * step) + (n / 256 + 200) * E).all()
+
+
+@pytest.mark.parametrize("offset", [0.0, 1000.0, -4000.0])
+@pytest.mark.parametrize("which", ["logp", "entropy", "both"])
+def test_logprob_backward_of_halves_of_the_vocabulary(B, offset, which):
+    """With the lse and entropy of all logits, against 64 bits.  A token of the other half is padding,
+    whose dlogp is not read."""
+    n = 9001
+    g = gen_of(int(abs(offset)) + 1)
+    x = torch.randn(6, n, generator=g, device="cuda") * 2 + offset
+    t = torch.tensor([3, n - 1, 4500, -1, 0, 4499], device="cuda")
+    f = B.LogProbs().forward(x, t)
+    a, b = torch.randn(2, 6, generator=g, device="cuda")
+    a, b = a if which != "entropy" else None, b if which != "logp" else None
+    for part in (slice(0, 4500), slice(4500, n)):
+        l = x[:, part]
+        mine = torch.where((t >= part.start) & (t < part.stop), t - part.start, -1)
+        dlogp = None if a is None else torch.where(mine >= 0, a, float("nan"))
+        got = B.LogProbs().backward(l, mine, f.lse, f.entropy, dlogp, b)
+        log_p = l.double() - f.lse.double()[:, None]
+        p = torch.exp(log_p)
+        gd = torch.where(mine >= 0, 0.0 if a is None else a.double(), 0.0)[:, None]
+        h = torch.zeros_like(gd) if b is None else b.double()[:, None]
+        slope = log_p + f.entropy.double()[:, None]
+        hit = torch.zeros_like(p).scatter_(1, mine.clamp(min=0)[:, None], 1.0)
+        want = gd * hit - p * (gd + h * slope)
+        # log p: near 0 from a logit and lse, far from it from differences to the largest logit
+        size = l.double().abs() + f.lse.double().abs()[:, None] if offset == 0 else log_p.abs() + 20
+        off = 4 * E * size + 4 * E
+        tol = p * (gd.abs() + h.abs() * slope.abs()) * (off + 3 * E * log_p.abs() + 10 * E) \
+            + p * h.abs() * (off + 2 * E * slope.abs()) + 4 * E * gd.abs() * hit
+        check(got, want, tol + E * want.abs() + 1e-37, f"part from {part.start}")
