@@ -54,18 +54,24 @@ int64_t pieces(int n, int wide) { return (n + wide - 1) / wide; }
 // 32), 37 with 2^19 (of 8); 4099 x 1001 f16: strips of 5 14 us, of 8 16.
 constexpr int64_t kConvThreads = (int64_t)1 << 18;
 constexpr int kConvLeast = 4, kConvBackLeast = 8;  // a strip of the gradient writes a part of dw
+constexpr int kConvMost = 8;                       // times what is on its way: the longest strip
 int conv_strip(int64_t rows, int n, int wide, int ahead, int more, int least) {
   int strip = 0;
-  for (int m : {2, 3, 4, 5, 6, 8}) {
+  for (int m : {2, 3, 4, 5, 6, kConvMost}) {
     strip = m * ahead - more;
     if (strip >= least && (rows + strip - 1) / strip * pieces(n, wide) <= kConvThreads) break;
   }
   return strip;
 }
 
-// For any type and up to `rows` rows: it does not fall as rows grow.
+// For any type and up to `rows` rows: it does not fall as rows grow.  There are as many strips as the
+// least rows a strip or the threads allow, those of the fewest pieces a row, or what the longest
+// strips leave.
 size_t conv_bytes(int64_t rows, int n, int taps) {
-  const int64_t strips = (rows + kConvBackLeast - 1) / kConvBackLeast;
+  const int longest = kConvMost * kConvAhead - 2 * (taps - 1);
+  const int64_t allowed = std::min((rows + kConvBackLeast - 1) / kConvBackLeast,
+                                   kConvThreads / pieces(n, kConvBackWide<bf16>));
+  const int64_t strips = std::max(allowed, (rows + longest - 1) / longest);
   return std::max<size_t>(256, (size_t)strips * (taps + 1) * n * sizeof(float));
 }
 

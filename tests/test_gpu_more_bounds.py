@@ -252,3 +252,22 @@ def test_two_graphs_share_a_workspace(lirpa):
         graphs[turn].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(jobs[turn][1], want[turn])), turn
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ids)
+@pytest.mark.parametrize("rows,n,taps", [(9001, 4100, 4), (6000, 8200, 8), (20011, 1030, 1),
+                                         (2600, 4097, 3)])
+def test_convolution_of_many_rows(lirpa, dtype, rows, n, taps):
+    """Around the sizes from which strips grow no longer: the workspace holds their parts."""
+    f = Frame(dtype, rows + taps)
+    x, dy = f.input(rows, n), f.input(rows, n)
+    w, b = f.input(taps, n), f.input(1, n)[0]
+    need = lirpa.lirpa_conv_workspace_bytes(rows, n, taps)
+    ws = f.output(1, need, dtype=torch.uint8)[0]
+    dx, dw, db = f.output(rows, n), f.output(taps, n), f.output(1, n)[0]
+    lirpa.lirpa_conv_backward(dy, x, w, b, "linear", None, dx, dw, db, ws, need)
+    f.check("convolution")
+    # bias gradient: a sum of `rows` values, rounded to the type
+    want, size = dy.double().sum(0), dy.double().abs().sum(0)
+    unit = torch.finfo(dtype).eps / 2
+    assert ((db.double() - want).abs() <= (rows + 4) * 2.0 ** -24 * size + unit * want.abs()).all()

@@ -151,3 +151,15 @@ def test_binding_refuses():
         s.forward(x, x, x[:, :2], x[:, :2])
     with pytest.raises(TypeError, match="float32, bfloat16 or float16"):
         s.forward(x.double(), x, x[:, :2], x[:, :2])
+
+
+def test_conv_workspace_is_what_a_call_writes(L):
+    """Many rows are cut into strips of 32 - 2 (taps - 1) rows, each with a part of dw and dbias: no
+    room for more, while few rows may be cut into strips of 8."""
+    for n in (4096, 5000, 1 << 20):
+        for taps in range(1, 9):
+            longest = 32 - 2 * (taps - 1)
+            for rows in (1 << 18, (1 << 20) + 7, 1 << 30):
+                want = -(-rows // longest) * (taps + 1) * n * 4
+                assert L.lirpa_conv_workspace_bytes(rows, n, taps) == want
+    assert L.lirpa_conv_workspace_bytes(800, 64, 4) == 100 * 5 * 64 * 4
