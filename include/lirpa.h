@@ -372,7 +372,9 @@ int lirpa_ffn_backward(const lirpa_ffn* ffn, int64_t rows, const void* dout, int
 /* =============================================================================================
  * The ends of a language model: tokens into rows, rows of logits into log probabilities
  *
- * Conventions as for the feed-forward block.  Tokens are int64; one outside [0, vocab) (-1, say) is
+ * Conventions as for the feed-forward block, but that rows of any alignment and length are read
+ * where they are: no call copies them, and those without `ws` need no workspace.  LIRPA_EUNSUPPORTED
+ * where a launch would pass 2^32 threads.  Tokens are int64; one outside [0, vocab) (-1, say) is
  * padding wherever tokens are read.
  * ============================================================================================= */
 
@@ -383,7 +385,7 @@ int lirpa_embed_forward(int dtype, int64_t rows, int n, int vocab, const int64_t
 
 /* The table's gradient: dtable_v = base_v + scale * (sum of dout over the positions of token v, in
  * their order, in 32 bits).  base [vocab][n] may be NULL (zeros) or dtable itself: then only rows
- * that a token names are read and written.  EUNSUPPORTED where a launch would pass 2^32 threads. */
+ * that a token names are read and written. */
 size_t lirpa_embed_workspace_bytes(int64_t rows, int n); /* 0 for invalid arguments */
 int lirpa_embed_backward(int dtype, int64_t rows, int n, int vocab, const int64_t* tokens,
                          const void* dout, int64_t lddo, float scale, const void* base, int64_t ldb,
@@ -399,7 +401,8 @@ int lirpa_embed_backward(int dtype, int64_t rows, int n, int vocab, const int64_
  * of -inf is a token that cannot come: it is no alternative, and places that are left over hold
  * token -1 and log probability -inf.  A row of -inf alone has lse and logp -inf and entropy 0.  A
  * row with a NaN or +inf has NaN everywhere (but for padding's logp) and alternatives -1.  logp,
- * entropy and top_logp are taken from the differences to the row's largest logit, not from lse. */
+ * entropy and top_logp are taken from the differences to the row's largest logit, not from lse (a
+ * difference that is no float counts as -inf). */
 size_t lirpa_logprob_workspace_bytes(int64_t rows, int n, int top); /* 0 for invalid arguments */
 int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                           float scale, const int64_t* tokens, float* logp, float* lse,
@@ -424,7 +427,7 @@ int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, i
 /* =============================================================================================
  * What mixes the rows of a sequence: a short causal convolution and a selective state space scan
  *
- * Conventions as for the feed-forward block, and:
+ * Conventions as for the ends of a language model, and:
  * - Sequences lie behind each other in the rows.  seq (int32 [rows], on the device) names the
  *   sequence of every row, and the slot of its state; rows of one sequence are neighbours, so a
  *   sequence begins and ends where the number changes.  seq = NULL: all rows are sequence 0.  A
@@ -441,8 +444,7 @@ int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, i
 typedef enum { LIRPA_CONV_LINEAR = 0, LIRPA_CONV_SILU = 1 } lirpa_conv_act;
 
 /* y_t = act(bias + sum_{k < taps} w_k x_{t - taps + 1 + k}) for every column; w [taps][n], bias [n]
- * or NULL, taps 1 to 8.  state [slots][taps - 1][n] of dtype: the last inputs, oldest first.
- * EUNSUPPORTED where a launch would pass 2^32 threads. */
+ * or NULL, taps 1 to 8.  state [slots][taps - 1][n] of dtype: the last inputs, oldest first. */
 int lirpa_conv_forward(int dtype, int64_t rows, int n, int taps, const void* x, int64_t ldx,
                        const void* w, const void* bias, int act, const int32_t* seq, int slots,
                        const void* state, void* state_out, void* y, int64_t ldy,
