@@ -275,9 +275,10 @@ class CausalConv:
         return y
 
     def backward(self, dy, x, seq=None, slots=lirpa.ANY_SLOT):
-        """{"dx", "dw", "dbias"} (dbias where there is a bias), for sequences without a state.  Where
-        the forward pass had a state_out, ``slots`` is the number of its slots: rows of a number from
-        there on were padding."""
+        """{"dx", "dw", "dbias"} (dbias where there is a bias) for the x and parameters of the forward
+        pass, which kept nothing, and sequences without a state.  Where the forward pass had a
+        state_out, ``slots`` is the number of its slots: rows of a number from there on were
+        padding."""
         lirpa._2d(x, "x")
         dx = torch.empty_like(x)
         grads = {"dx": dx, "dw": torch.empty_like(self.w)}
@@ -291,7 +292,11 @@ class CausalConv:
 
 class KeptScan:
     """What SelectiveScan.forward kept for its backward pass: the inputs, states of the walk, and the
-    number of slots, on which depends what is padding."""
+    number of slots, on which depends what is padding.
+
+    The inputs are held, not copied: the backward pass reads u, dt, B, C, z, seq and the scan's
+    parameters again, as they then are.  Nothing notices a write to them between the passes; the
+    gradients would be of neither."""
 
     def __init__(self, u, dt, B, C, z, seq, states, slots=lirpa.ANY_SLOT):
         self.inputs, self.seq, self.states, self.slots = (u, dt, B, C, z), seq, states, slots
