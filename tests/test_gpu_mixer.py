@@ -726,3 +726,31 @@ def test_conv_gradient_of_rows_without_a_slot(B, dtype, rows, n, taps):
     for bad in (0, -1, 1 << 31, (1 << 32) + 3):
         with pytest.raises(ValueError, match="slots"):
             op.backward(dy, x, seq, bad)
+
+
+def test_scan_gradient_past_2_31_values(B):
+    """Inputs, gradients, kept states and parts of dB and dC of more than 2^31 values each, the last
+    rows a sequence of their own, the others zeros."""
+    rows, n, N = 540000, 4096, 32
+    dtype = torch.bfloat16
+    g = gen_of(3)
+    tail = scan_inputs(g, 64, n, N, dtype)
+    dy_tail = rand(g, 64, n, dtype=dtype)
+    whole = {k: torch.zeros(rows, t.shape[1], dtype=dtype, device="cuda")
+             for k, t in {**tail, "dy": dy_tail}.items() if k in ("u", "dt", "z", "Bm", "Cm", "dy")}
+    for k, t in whole.items():
+        t[-64:] = dy_tail if k == "dy" else tail[k]
+    seq = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    seq[-64:] = 1
+    op = B.SelectiveScan(tail["A"], tail["D"], tail["bias"])
+    y, kept = op.forward(*pass_on(whole), seq, keep=True)
+    assert kept.states.numel() > 1 << 33 and not y[:-64].any()
+    del y
+    grads = op.backward(whole["dy"], kept)
+    want, _ = plain_scan(**tail, runs=[(0, 64, 0)], dy=dy_tail)
+    for k, v in grads.items():
+        if k in ("dA", "dD", "dbias"):
+            within(v, want[k], torch.float32, k)
+        else:
+            within(v[-64:], want[k], dtype, k)
+            assert not v[:-64].any(), k
