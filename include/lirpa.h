@@ -373,9 +373,9 @@ int lirpa_ffn_backward(const lirpa_ffn* ffn, int64_t rows, const void* dout, int
  * The ends of a language model: tokens into rows, rows of logits into log probabilities
  *
  * Conventions as for the feed-forward block, but that rows of any alignment and length are read
- * where they are: no call copies them, and those without `ws` need no workspace.  LIRPA_EUNSUPPORTED
- * where a launch would pass 2^32 threads.  Tokens are int64; one outside [0, vocab) (-1, say) is
- * padding wherever tokens are read.
+ * where they are: no call copies them, and those without `ws` need no workspace.
+ * LIRPA_EUNSUPPORTED where a launch would pass 2^32 threads.  Tokens are int64; one outside [0,
+ * vocab) (-1, say) is padding wherever tokens are read.
  * ============================================================================================= */
 
 /* out = scale * table[token], a row of 0 for padding.  table is [vocab][n], vocab up to 2^20. */
@@ -413,12 +413,13 @@ int lirpa_logprob_forward(int dtype, int64_t rows, int n, const void* logits, in
  * the lse and entropy (NULL where dentropy is) that the forward call returned:
  *     dl_j = scale (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)).
  * p comes from lse, whose rounding (2^-24 of its magnitude) is a relative error of it, up to a
- * magnitude of 256; past that the row's sums are taken again, at some 1.9 times the time.  An lse
- * that is not the row's own (that of all logits, for a part of the columns) stands as it is given,
- * but for one past 256 that its own rounding does not tell from the row's: within 5/8 of the distance
- * of two floats there, p is taken from the row's sums.  dlogp is not read for padding, and a token
- * that lies outside a part is padding there: the part then lacks its -scale dlogp p.  A row of -inf
- * alone takes no gradient.  dlogits may be the buffer of logits. */
+ * magnitude of 256; past that the row's sums are taken again, by one block a row: 1.8 times the
+ * time for thousands of rows, 3 to 9 times for up to 500.  An lse that is not the row's own (that
+ * of all logits, for a part of the columns) stands as it is given, but for one past 256 that its
+ * own rounding does not tell from the row's: within 5/8 of the distance of two floats there, p is
+ * taken from the row's sums.  dlogp is not read for padding, and a token that lies outside a part
+ * is padding there: the part then lacks its -scale dlogp p.  A row of -inf alone takes no
+ * gradient.  dlogits may be the buffer of logits. */
 int lirpa_logprob_backward(int dtype, int64_t rows, int n, const void* logits, int64_t ldl,
                            float scale, const int64_t* tokens, const float* lse,
                            const float* entropy, const float* dlogp, const float* dentropy,
@@ -487,8 +488,8 @@ int lirpa_scan_step(const lirpa_scan* scan, const float* state, float* state_out
                     int64_t ldy, hipStream_t stream);
 
 /* Gradients from what was kept, for the same inputs and slots (what was padding has no states in
- * kept): du, ddt, dz (NULL without z) [rows][n], dB, dC [rows][states] of dtype; dA [n][states], dD,
- * dbias [n] of float, each NULL where it is not wanted. */
+ * kept): du, ddt, dz (NULL without z) [rows][n], dB, dC [rows][states] of dtype; dA [n][states],
+ * dD, dbias [n] of float, each NULL where it is not wanted. */
 int lirpa_scan_backward(const lirpa_scan* scan, const void* dy, int64_t lddy, const void* kept,
                         void* du, int64_t lddu, void* ddt, int64_t ldddt, void* dz, int64_t lddz,
                         void* dB, int64_t lddB, void* dC, int64_t lddC, float* dA, float* dD,

@@ -14,10 +14,12 @@
 // inputs reach, and adds a strip's part of dw and dbias in registers; the strips' parts are joined
 // in order by k_sum_parts.
 //
-// 4 taps with silu: 8192 x 4096 bf16 33 us for 147 MB (4.4 TB/s, vector units 75 % busy); 4099 x
-// 1001 f16 12 us forward, 22 + 5 backward, of which 64 rows take 4 and 9 + 2: the latency of a few
-// loads in a row.  With 8 columns a thread the gradient's registers left two waves a SIMD (34 us
-// for 24); with 8 rows ahead instead of 4 the forward pass took 52 us for 33.
+// 4 taps with silu: 8192 x 4096 bf16 33 us for 147 MB (4.4 TB/s, vector units 74 % busy), backward
+// 55 + 8 us between events (201 MB read and written, and 26 MB of parts of dw and dbias twice; with
+// 8 taps 105 + 15, of strips of 18 rows for 26); 4099 x 1001 f16 12 us forward, 22 + 5 backward, of
+// which 64 rows take 4 and 9 + 2: the latency of a few loads in a row.  With 8 columns a thread the
+// gradient's registers left two waves a SIMD (34 us for 24); with 8 rows ahead instead of 4 the
+// forward pass took 52 us for 33.
 #pragma once
 
 #include "sequences.hpp"

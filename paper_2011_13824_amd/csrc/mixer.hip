@@ -134,10 +134,10 @@ int64_t scan_groups(int n, int states) {
 }
 
 // Rows are cut into chunks until there are kScanBlocks blocks, or kMostChunks chunks: their states
-// are linked one after the other.  16 states, bf16, first walk, link and real walk, us: 8192 x 4096
-// 131 + 10 + 244 with 512 blocks, 115 + 14 + 183 with 1024, 105 + 11 + 178 with 2048; 512 x 1024
-// with chunks of 16 rows 8 + 9 + 11, of 64 11 + 6 + 18, of 256 29 + 6 + 51; 8192 x 256 with 64
-// chunks 18 + 15 + 29, with 512 14 + 97 + 19.
+// are linked one after the other.  16 states, bf16, first walk, link and real walk, us (between
+// events, which add some 2 to each): 8192 x 4096 129 + 7 + 243 with 512 blocks, 114 + 8 + 185 with
+// 1024, 106 + 11 + 181 with 2048; 512 x 1024 with chunks of 16 rows 8 + 9 + 11, of 64 11 + 6 + 18, of
+// 256 28 + 6 + 50; 8192 x 256 with 64 chunks 17 + 15 + 29, with 512 14 + 93 + 21.
 constexpr int kScanBlocks = 2048, kMostChunks = 64;
 int64_t scan_most_chunks(int n, int states) {
   const int64_t groups = scan_groups(n, states);
